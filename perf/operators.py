@@ -339,7 +339,7 @@ def _own_attn(st):
     if not train:
         return {"o": plan.forward(*args, key_lengths=st["lengths"], workspace=st["workspace"])}
     o, saved = plan.forward(*args, key_lengths=st["lengths"], workspace=st["workspace"], save=True)
-    dq, dk, dv, dlam = plan.backward(st["do"], *args, o, saved, key_lengths=st["lengths"],
+    dq, dk, dv, dlam = plan.backward(st["do"], *args, saved, key_lengths=st["lengths"],
                                      workspace=st["workspace"])
     return {"o": o, "dq": dq, "dk": dk, "dv": dv, "dlam": dlam}
 
