@@ -333,6 +333,105 @@ fftsplit_status_t fftsplit_direct_conv2d(fftsplit_plan_t plan, const float* x, c
 fftsplit_status_t fftsplit_maxpool2x2(const float* x, float* y, int n, int c, int h, int w,
                                       hipStream_t stream);
 
+/* ---------------------------------------------------------------------
+ * Operators of the attention block that follows a convolution backbone:
+ * layer norm, rotary positions over several axes, differential attention.
+ * They are not part of the paper's method.  The conventions above hold,
+ * except that tensors may also be bf16 and that attention and the rotation
+ * take strides where they say so.
+ * ------------------------------------------------------------------- */
+
+typedef enum {
+    FFTSPLIT_F32 = 0,
+    FFTSPLIT_BF16 = 1
+} fftsplit_dtype_t;
+
+/* Differential attention.  Every head holds two softmax maps over the same
+ * values; for sequence b, query row i and query head h with key head
+ * g = h / (heads_q / heads_k),
+ *   o[b][i][h] = sum_j (P1[j] - lam[h] P2[j]) v[b][j][g],
+ *   Pm[j] = softmax_j(scale <q[b][i][h][m], k[b][j][g][m]>)  over the visible j.
+ * Key j is visible to row i if j < key_lengths[b] and, with causal set, if
+ * j <= i + key_lengths[b] - queries (the last row sees every key).  A row
+ * that sees no key gives o = 0 and contributes to no gradient.  What lies in
+ * k and v from row key_lengths[b] on is not read.
+ * Scores, the softmax statistics and all sums are fp32; with bf16 tensors the
+ * terms of the softmax (and the score gradients) are rounded to bf16 as
+ * operands of the matrix products. */
+typedef struct {
+    int batch;            /* sequences */
+    int queries, keys;    /* query rows; room for keys (each sequence may fill less) */
+    int heads_q, heads_k; /* heads_k divides heads_q */
+    int dim;              /* width of one map's queries and keys, at most 128 */
+    int dim_v;            /* width of the values, at most 256 */
+    int dtype;            /* fftsplit_dtype_t of q, k, v, o and their gradients */
+    int causal;           /* 0 or 1 */
+    float scale;          /* factor of the scores; 0: 1 / sqrt(dim) */
+} fftsplit_attention_problem_t;
+
+typedef struct fftsplit_attention_plan_s* fftsplit_attention_plan_t;   /* opaque, host-side */
+
+typedef struct {
+    size_t forward_workspace_bytes, backward_workspace_bytes;
+    size_t lse_bytes;     /* of the statistics saved for the backward pass */
+    /* Kernel choice: head widths the tiles are padded to, and how many
+     * workgroups share the keys of a tile of few rows (0: the kernel for
+     * many rows, whose workgroups each go over all keys). */
+    int tile_dim, tile_dim_v, key_splits;
+} fftsplit_attention_info_t;
+
+/* Input tensors (device).  Strides are in elements, of the dimensions
+ *   q [batch][queries][heads_q][2][dim], k [batch][keys][heads_k][2][dim]:
+ *     batch, token, head, map;
+ *   v [batch][keys][heads_k][dim_v]: batch, token, head;
+ * the last dimension is dense and no stride is negative.  q, k and v may be
+ * slices of one tensor.  Pointers need only their type's alignment; where
+ * pointers, strides and widths allow 16-byte accesses those are used.
+ *   lam: one value for all heads or one per query head (lam_count 1 or
+ *     heads_q), of type lam_dtype;
+ *   key_lengths: [batch], or NULL: every sequence has `keys` keys.  Values
+ *     outside [0, keys] are taken as the nearest of the two. */
+typedef struct {
+    const void *q, *k, *v, *lam;
+    const int* key_lengths;
+    long long q_stride[4], k_stride[4], v_stride[3];
+    int lam_dtype, lam_count;
+} fftsplit_attention_inputs_t;
+
+/* Validate `prob` and create a plan for `device`, as fftsplit_plan does; the
+ * _for_arch form makes one that can be queried but not run. */
+fftsplit_status_t fftsplit_attention_plan(const fftsplit_attention_problem_t* prob, int device,
+                                          fftsplit_attention_plan_t* out);
+fftsplit_status_t fftsplit_attention_plan_for_arch(const fftsplit_attention_problem_t* prob, const char* arch,
+                                                   fftsplit_attention_plan_t* out);
+fftsplit_status_t fftsplit_attention_plan_info(fftsplit_attention_plan_t plan, fftsplit_attention_info_t* out /* host */);
+void fftsplit_attention_plan_destroy(fftsplit_attention_plan_t plan);   /* NULL is ignored */
+
+/* o (device) [batch][queries][heads_q][dim_v], dense, 16-byte aligned.
+ * For a backward pass also o1 and o2 (like o: the maps' own outputs) and lse
+ * (device, info.lse_bytes: fp32 [batch][heads_q][2][queries], log2 of the sum
+ * of exp2 of the scaled scores); all NULL otherwise.  Outputs must not
+ * overlap the inputs or the workspace (of info.forward_workspace_bytes; NULL
+ * allowed if that is 0).  The result does not depend on what runs beside it:
+ * no atomics are used. */
+fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_plan_t plan, const fftsplit_attention_inputs_t* in /* host */,
+                                             void* o, void* o1, void* o2, float* lse, void* workspace, size_t workspace_bytes,
+                                             hipStream_t stream);
+
+/* Gradients of fftsplit_attention_forward's inputs from that of o.
+ *   dout (device): [batch][queries][heads_q][dim_v], strides batch, token,
+ *     head in elements, last dimension dense;
+ *   o1, o2, lse: as the forward pass left them;
+ *   dq, dk, dv (device): dense, laid out as q, k and v are declared above;
+ *     gradients of keys that no query sees (those past key_lengths among
+ *     them) are zero; a key head's sums over its query heads;
+ *   dlam (device): like lam (type and count; one value sums over heads). */
+fftsplit_status_t fftsplit_attention_backward(fftsplit_attention_plan_t plan, const fftsplit_attention_inputs_t* in /* host */,
+                                              const void* dout, const long long dout_stride[3], const void* o1,
+                                              const void* o2, const float* lse, void* dq, void* dk, void* dv,
+                                              void* dlam, void* workspace, size_t workspace_bytes,
+                                              hipStream_t stream);
+
 /* Benchmark hook (host, per calling thread): until called again with
  * NULL, NULL, every later fftsplit_transform_weights / fftsplit_conv2d /
  * stage call made by this thread records `start` (if non-NULL) when its

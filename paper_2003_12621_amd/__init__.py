@@ -439,3 +439,9 @@ def bin_coords(L: int):
     coords.append(((0, 0), (h2, 0)))
     coords.append(((0, h2), (h2, h2)))
     return coords
+
+
+from . import attention as _attention  # noqa: E402
+from .attention import DiffAttention  # noqa: E402,F401
+
+_SIGNATURES.update(_attention.SIGNATURES)

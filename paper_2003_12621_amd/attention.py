@@ -1,0 +1,198 @@
+"""Operators of the attention block over a convolution's feature map.
+
+    import paper_2003_12621_amd as fs
+    plan = fs.DiffAttention(n, tokens, tokens, heads, heads, dim, dim_v, dtype=torch.bfloat16)
+    o = plan.forward(q, k, v, lam)
+
+Argument marshalling only, as in the rest of the binding: the computation runs
+in the HIP kernels behind fftsplit.h.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import paper_2003_12621_amd as _fs
+
+F32, BF16 = 0, 1
+
+
+class AttentionProblem(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("batch", "queries", "keys", "heads_q", "heads_k", "dim", "dim_v", "dtype",
+                                            "causal")] + [("scale", ctypes.c_float)]
+
+
+class AttentionInfo(ctypes.Structure):
+    _fields_ = [("forward_workspace_bytes", ctypes.c_size_t), ("backward_workspace_bytes", ctypes.c_size_t),
+                ("lse_bytes", ctypes.c_size_t), ("tile_dim", ctypes.c_int), ("tile_dim_v", ctypes.c_int),
+                ("key_splits", ctypes.c_int)]
+
+
+class AttentionInputs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("lam", ctypes.c_void_p),
+                ("key_lengths", ctypes.c_void_p), ("q_stride", ctypes.c_longlong * 4),
+                ("k_stride", ctypes.c_longlong * 4), ("v_stride", ctypes.c_longlong * 3), ("lam_dtype", ctypes.c_int),
+                ("lam_count", ctypes.c_int)]
+
+
+_P, _SZ = ctypes.c_void_p, ctypes.c_size_t
+SIGNATURES = {
+    "fftsplit_attention_plan": (ctypes.c_int, [ctypes.POINTER(AttentionProblem), ctypes.c_int, ctypes.POINTER(_P)]),
+    "fftsplit_attention_plan_for_arch": (ctypes.c_int, [ctypes.POINTER(AttentionProblem), ctypes.c_char_p,
+                                                        ctypes.POINTER(_P)]),
+    "fftsplit_attention_plan_info": (ctypes.c_int, [_P, ctypes.POINTER(AttentionInfo)]),
+    "fftsplit_attention_plan_destroy": (None, [_P]),
+    "fftsplit_attention_forward": (ctypes.c_int, [_P, ctypes.POINTER(AttentionInputs), _P, _P, _P, _P, _P, _SZ, _P]),
+    "fftsplit_attention_backward": (ctypes.c_int, [_P, ctypes.POINTER(AttentionInputs), _P,
+                                                   ctypes.POINTER(ctypes.c_longlong), _P, _P, _P, _P, _P, _P, _P, _P,
+                                                   _SZ, _P]),
+}
+
+
+def _type_code(dtype) -> int:
+    torch = _fs._torch()
+    if dtype == torch.float32:
+        return F32
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
+
+
+def _strided(t, name, dtype, shape, device):
+    """Pointer of a tensor of the given shape whose last dimension is dense."""
+    if not isinstance(t, _fs._torch().Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    return t.data_ptr()
+
+
+def _dense(t, name, dtype, numel, device):
+    """Pointer of a dense tensor of `numel` elements (any shape)."""
+    p = _fs._dev_tensor(t, name, dtype, numel)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return p
+
+
+class DiffAttention:
+    """Differential attention of `batch` sequences: `queries` query rows over
+    room for `keys` keys, `heads_q` query heads sharing `heads_k` key heads,
+    widths `dim` (one map's queries and keys) and `dim_v` (values).  See
+    fftsplit.h for the formula, masks and limits."""
+
+    def __init__(self, batch, queries, keys, heads_q, heads_k, dim, dim_v, dtype=None, causal=False, scale=None,
+                 device=None, arch: Optional[str] = None):
+        torch = _fs._torch()
+        self.dtype = torch.float32 if dtype is None else dtype
+        if scale is not None and not scale > 0:
+            raise ValueError("scale must be positive")
+        self.prob = AttentionProblem(batch, queries, keys, heads_q, heads_k, dim, dim_v, _type_code(self.dtype),
+                                     int(bool(causal)), 0.0 if scale is None else float(scale))
+        handle = ctypes.c_void_p()
+        if arch is not None:
+            _fs._check(_fs.lib().fftsplit_attention_plan_for_arch(ctypes.byref(self.prob), arch.encode(),
+                                                                  ctypes.byref(handle)),
+                       "fftsplit_attention_plan_for_arch")
+            self.device = None
+        else:
+            dev = torch.device("cuda", torch.cuda.current_device() if device is None else int(device))
+            _fs._check(_fs.lib().fftsplit_attention_plan(ctypes.byref(self.prob), dev.index, ctypes.byref(handle)),
+                       "fftsplit_attention_plan")
+            self.device = dev
+        self._h = handle
+        self.info = AttentionInfo()
+        _fs._check(_fs.lib().fftsplit_attention_plan_info(self._h, ctypes.byref(self.info)),
+                   "fftsplit_attention_plan_info")
+        self.q_shape = (batch, queries, heads_q, 2, dim)
+        self.k_shape = (batch, keys, heads_k, 2, dim)
+        self.v_shape = (batch, keys, heads_k, dim_v)
+        self.out_shape = (batch, queries, heads_q, dim_v)
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value and _fs._lib is not None:
+            _fs._lib.fftsplit_attention_plan_destroy(h)
+            self._h = None
+
+    def new_workspace(self, backward=False):
+        """Scratch for forward, or for forward and backward.  One workspace
+        serves one call at a time."""
+        need = self.info.forward_workspace_bytes
+        if backward:
+            need = max(need, self.info.backward_workspace_bytes)
+        return _fs._torch().empty(need, dtype=_fs._torch().uint8, device=self.device)
+
+    def _inputs(self, q, k, v, lam, key_lengths):
+        torch, dev = _fs._torch(), self.device
+        x = AttentionInputs()
+        x.q = _strided(q, "q", self.dtype, self.q_shape, dev)
+        x.k = _strided(k, "k", self.dtype, self.k_shape, dev)
+        x.v = _strided(v, "v", self.dtype, self.v_shape, dev)
+        x.q_stride[:] = q.stride()[:4]
+        x.k_stride[:] = k.stride()[:4]
+        x.v_stride[:] = v.stride()[:3]
+        if not isinstance(lam, torch.Tensor) or lam.numel() not in (1, self.prob.heads_q):
+            raise ValueError(f"lam must be a tensor of 1 or {self.prob.heads_q} elements")
+        x.lam = _dense(lam, "lam", None, None, dev)
+        x.lam_dtype = _type_code(lam.dtype)
+        x.lam_count = lam.numel()
+        if key_lengths is not None:
+            x.key_lengths = _dense(key_lengths, "key_lengths", torch.int32, self.prob.batch, dev)
+        return x
+
+    def _workspace(self, ws, need):
+        torch = _fs._torch()
+        if ws is None:
+            if need == 0:
+                return None, 0
+            ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return _dense(ws, "workspace", None, None, self.device), ws.numel() * ws.element_size()
+
+    def forward(self, q, k, v, lam, key_lengths=None, out=None, workspace=None, save=False):
+        """o [batch, queries, heads_q, dim_v]; with save=True (o, saved), where
+        `saved` is what backward needs beside the inputs and o."""
+        torch = _fs._torch()
+        x = self._inputs(q, k, v, lam, key_lengths)
+        numel = _fs._prod(self.out_shape)
+        o = torch.empty(self.out_shape, dtype=self.dtype, device=self.device) if out is None else out
+        op = _dense(o, "out", self.dtype, numel, self.device)
+        saved = None
+        sp = (None, None, None)
+        if save:
+            saved = (torch.empty_like(o), torch.empty_like(o),
+                     torch.empty(self.info.lse_bytes // 4, dtype=torch.float32, device=self.device))
+            sp = tuple(t.data_ptr() for t in saved)
+        ws, nbytes = self._workspace(workspace, self.info.forward_workspace_bytes)
+        _fs._check(_fs.lib().fftsplit_attention_forward(self._h, ctypes.byref(x), op, *sp, ws, nbytes,
+                                                        _fs._stream_handle(self.device)),
+                   "fftsplit_attention_forward")
+        return (o, saved) if save else o
+
+    def backward(self, dout, q, k, v, lam, saved, key_lengths=None, workspace=None):
+        """(dq, dk, dv, dlam) from the gradient of o; `saved` as
+        forward(save=True) returned it."""
+        torch, dev = _fs._torch(), self.device
+        x = self._inputs(q, k, v, lam, key_lengths)
+        gp = _strided(dout, "dout", self.dtype, self.out_shape, dev)
+        gs = (ctypes.c_longlong * 3)(*dout.stride()[:3])
+        numel = _fs._prod(self.out_shape)
+        o1 = _dense(saved[0], "saved[0]", self.dtype, numel, dev)
+        o2 = _dense(saved[1], "saved[1]", self.dtype, numel, dev)
+        lse = _dense(saved[2], "saved[2]", torch.float32, self.info.lse_bytes // 4, dev)
+        dq = torch.empty(self.q_shape, dtype=self.dtype, device=dev)
+        dk = torch.empty(self.k_shape, dtype=self.dtype, device=dev)
+        dv = torch.empty(self.v_shape, dtype=self.dtype, device=dev)
+        dlam = torch.empty_like(lam)
+        ws, nbytes = self._workspace(workspace, self.info.backward_workspace_bytes)
+        _fs._check(_fs.lib().fftsplit_attention_backward(self._h, ctypes.byref(x), gp, gs, o1, o2, lse, dq.data_ptr(),
+                                                         dk.data_ptr(), dv.data_ptr(), dlam.data_ptr(), ws, nbytes,
+                                                         _fs._stream_handle(dev)),
+                   "fftsplit_attention_backward")
+        return dq, dk, dv, dlam

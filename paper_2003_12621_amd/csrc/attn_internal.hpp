@@ -1,0 +1,68 @@
+// Declarations shared by the attention entry points and kernels.
+#pragma once
+
+#include "fftsplit_internal.hpp"
+
+struct fftsplit_attention_plan_s {
+    fftsplit_attention_problem_t prob;
+    int device;              // HIP ordinal, or -1 for an architecture-only plan
+    float scale;             // of the products, before the softmax
+    int shape;               // index into kAttnShapes: the kernels' padded head widths
+    int splits;              // workgroups that share the keys of one tile of few rows; 0: the tiled kernel runs
+    size_t forward_ws, backward_ws;
+};
+
+namespace fftsplit {
+
+// Head widths (of a map's queries and keys, of the values) the kernels are
+// compiled for; a plan takes the first pair that holds its own.
+struct AttnShape {
+    int d, dv;
+};
+constexpr AttnShape kAttnShapes[] = {{32, 64}, {64, 128}, {128, 256}};
+constexpr int kAttnShapeCount = 3;
+
+// Query rows a workgroup of the tiled kernel takes (4 waves of 32).
+constexpr int kAttnRows = 128;
+// Query rows, packed over the heads that share a key head, of the kernel for few rows.
+constexpr int kAttnFewRows = 32;
+
+// What the attention kernels get.  Strides are in elements.
+struct AttnArgs {
+    const void *q, *k, *v, *lam;
+    const int* lengths;              // keys of each sequence, or null: all sk
+    int n, sq, sk, hq, hk, d, dv;
+    int causal;
+    float scale_log2;                // scale * log2(e)
+    float scale;
+    int lam_f32, lam_step;           // lam is fp32; 0 if one lam serves all heads
+    long long qb, qt, qh, qm;        // batch, token, head, map
+    long long kb, kt, kh, km;
+    long long vb, vt, vh;
+    int q_wide, k_wide, v_wide;      // 16-byte accesses allowed
+    void* o;                         // [n][sq][hq][dv]
+    void *o1, *o2;                   // the maps' own outputs, same layout, or null
+    float* lse;                      // [n][hq][2][sq]: log2 of the sum of exp2, or null
+    int o_wide;
+    // few rows
+    int splits;
+    float* part;                     // [tile row][split][2][dv]
+    float* part_stats;               // [tile row][split][4]: max and sum of both maps
+    // backward
+    const void* dout;
+    long long gb, gt, gh;            // batch, token, head strides of dout
+    int g_wide;
+    float* delta;                    // [n][hq][2][sq]
+    float* dlam_part;                // [hq][parts]
+    int parts;
+    void *dq, *dk, *dv_out, *dlam;
+};
+
+hipError_t launch_attn_forward(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s,
+                               const LaunchEvents& ev);
+hipError_t launch_attn_backward(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s,
+                                const LaunchEvents& ev);
+// Rows of one head that a workgroup of the backward's first kernel reduces.
+constexpr int kAttnDeltaRows = 64;
+
+}  // namespace fftsplit

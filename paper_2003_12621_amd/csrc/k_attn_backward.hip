@@ -1,0 +1,457 @@
+// Differential attention, backward.
+//
+// With P1, P2 the two maps (recomputed from the saved log sums), t = dO v^T and
+// D1 = <dO, o1>, D2 = <dO, o2> per row:
+//     dv = (P1 - lam P2)^T dO,   dlam = - sum D2,
+//     dS1 = P1 (t - D1),   dS2 = lam P2 (D2 - t),
+//     dqm = scale dSm km,   dkm = scale dSm^T qm.
+// t and the value product are shared by both maps.  The key side (dk, dv) and
+// the query side (dq) are two kernels that each own their outputs and
+// recompute the scores, rather than one that would add to dq with atomics:
+// results do not depend on the order of workgroups.
+#include "attn_common.hpp"
+
+namespace fftsplit {
+
+namespace {
+
+constexpr int kDeltaLanes = 16;   // lanes that share a row
+
+// Sum over the 16 lanes of a row group, the same in all of them.
+__device__ __forceinline__ float row_group_sum(float x) {
+#pragma unroll
+    for (int m = 1; m < kDeltaLanes; m *= 2) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool wide) {
+    if (wide && left >= 8) {
+        T e[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 16 / int(sizeof(T)))
+            *reinterpret_cast<uint4*>(e + j) = *reinterpret_cast<const uint4*>(p + j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = float(e[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = j < left ? float(p[j]) : 0.f;
+    }
+}
+
+}  // namespace
+
+// D1 and D2 of kAttnDeltaRows rows of one head, and their share of dlam.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
+    __shared__ float sums[256 / kDeltaLanes];
+    const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
+    const int h = blockIdx.x % a.hq, c = blockIdx.x / a.hq % chunks, b = blockIdx.x / a.hq / chunks;
+    const int l = threadIdx.x % kDeltaLanes, group = threadIdx.x / kDeltaLanes;
+    const bool wide = a.g_wide && a.dv % 8 == 0;
+    float total = 0.f;
+    for (int i = group; i < kAttnDeltaRows; i += 256 / kDeltaLanes) {
+        const int row = c * kAttnDeltaRows + i;
+        if (row >= a.sq) break;      // (the same in all lanes of the group)
+        const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
+        const T* o1 = static_cast<const T*>(a.o1) + at;
+        const T* o2 = static_cast<const T*>(a.o2) + at;
+        const T* g = static_cast<const T*>(a.dout) + b * a.gb + row * a.gt + h * a.gh;
+        float s1 = 0.f, s2 = 0.f;
+        for (int col = l * 8; col < a.dv; col += kDeltaLanes * 8) {
+            float x[8], y[8], z[8];
+            load8(x, g + col, a.dv - col, wide);
+            load8(y, o1 + col, a.dv - col, wide);
+            load8(z, o2 + col, a.dv - col, wide);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s1 = fmaf(x[j], y[j], s1);
+                s2 = fmaf(x[j], z[j], s2);
+            }
+        }
+        s1 = row_group_sum(s1);
+        s2 = row_group_sum(s2);
+        total += s2;
+        if (l == 0) {
+            float* delta = a.delta + (size_t(b) * a.hq + h) * 2 * a.sq + row;
+            delta[0] = s1;
+            delta[a.sq] = s2;
+        }
+    }
+    if (l == 0) sums[group] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float t = 0.f;
+        for (int i = 0; i < 256 / kDeltaLanes; ++i) t += sums[i];
+        a.dlam_part[size_t(h) * a.parts + b * chunks + c] = -t;
+    }
+}
+
+// dlam from its parts, in a fixed order: one workgroup a head, or one for all
+// heads together.
+__global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
+    __shared__ float sums[256];
+    const int heads = a.lam_step ? 1 : a.hq;
+    const float* part = a.dlam_part + size_t(blockIdx.x) * a.parts;
+    float t = 0.f;
+    for (long long i = threadIdx.x; i < (long long)heads * a.parts; i += 256) t += part[i];
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    for (int m = 128; m > 0; m /= 2) {
+        if (int(threadIdx.x) < m) sums[threadIdx.x] += sums[threadIdx.x + m];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        if (a.lam_f32)
+            static_cast<float*>(a.dlam)[blockIdx.x] = sums[0];
+        else
+            static_cast<__bf16*>(a.dlam)[blockIdx.x] = __bf16(sums[0]);
+    }
+}
+
+namespace {
+
+template <typename T, int D, int DV>
+struct KeySideShape {
+    static constexpr int kRows = 32;                                   // queries per stage
+    static constexpr int kQueryBytes = TileShape<T, D>::bytes(kRows);
+    static constexpr int kGradBytes = TileShape<T, DV>::bytes(kRows);
+    static constexpr int kStatBytes = 4 * kRows * 4;
+    static constexpr int kBufferBytes = 2 * kQueryBytes + kGradBytes + kStatBytes;
+    static constexpr int kLds = 2 * kBufferBytes;
+};
+constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
+
+// Sixteen values of an array in LDS in the order of an accumulator's rows.
+__device__ __forceinline__ floatx16 rows_of(const float* x, int hi) {
+    floatx16 y;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const float4 v = *reinterpret_cast<const float4*>(x + acc_row(4 * g, hi));
+        y[4 * g] = v.x;
+        y[4 * g + 1] = v.y;
+        y[4 * g + 2] = v.z;
+        y[4 * g + 3] = v.w;
+    }
+    return y;
+}
+
+// A transposed accumulator [columns of the row][rows = lanes] to a dense row in memory.
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int cols, bool wide, float scale, int hi) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            store4(p, 32 * d + acc_row(4 * g, hi), cols, wide, acc[d][4 * g] * scale, acc[d][4 * g + 1] * scale,
+                   acc[d][4 * g + 2] * scale, acc[d][4 * g + 3] * scale);
+}
+
+}  // namespace
+
+// Key side: one workgroup takes 128 keys of one key head, 32 a wave, and goes
+// over the queries of all heads that share it.  Each wave keeps its rows of
+// k1, k2 and v as operands and dk1, dk2, dv as accumulators in registers.
+template <typename T, int D, int DV, bool DK, bool DVAL>
+__global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
+    using Shape = KeySideShape<T, D, DV>;
+    constexpr int kRows = Shape::kRows;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+    const int tiles = (a.sk + kKeySideKeys - 1) / kKeySideKeys;
+    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
+    const int tile = id % tiles, hkv = id / tiles % a.hk, b = id / tiles / a.hk;
+    const int group = a.hq / a.hk;
+    const int length = attn_length(a, b), offset = length - a.sq;
+    const int first = tile * kKeySideKeys, wave_first = first + wave * 32, key = wave_first + (lane & 31);
+    const bool exists = key < length;
+    // rows from which on this lane's key is visible (none: beyond all rows)
+    const int from = !exists ? 0x7fffffff : (a.causal ? key - offset : 0);
+    // every row from here on sees all of the wave's keys
+    const int all_from = wave_first + 31 >= length ? 0x7fffffff : (a.causal ? wave_first + 31 - offset : 0);
+
+    Operand<T> k1[D / 16], k2[D / 16], v[DV / 16];
+    {
+        const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
+        load_row_operands<T, D>(k1, p, a.d, exists, a.k_wide, lane);
+        load_row_operands<T, D>(k2, p + a.km, a.d, exists, a.k_wide, lane);
+        if constexpr (DK)
+            load_row_operands<T, DV>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
+                                     a.dv, exists, a.v_wide, lane);
+    }
+    floatx16 dk1[DK ? D / 32 : 1], dk2[DK ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
+#pragma unroll
+    for (auto& x : dk1) x = zero16();
+#pragma unroll
+    for (auto& x : dk2) x = zero16();
+#pragma unroll
+    for (auto& x : dval) x = zero16();
+
+    // row tiles that see any of the workgroup's keys
+    const int row_tiles = (a.sq + kRows - 1) / kRows;
+    const int tile0 = !a.causal ? 0 : max(0, first - offset) / kRows;
+    const int per_head = first >= length ? 0 : max(0, row_tiles - tile0);
+    const int steps = per_head * group;
+
+    Stage<T, D, kRows, 256> g1, g2;
+    Stage<T, DV, kRows, 256> gg;
+    float stat = 0.f;
+    auto fetch = [&](int step) {
+        const int h = hkv * group + step / per_head, row0 = (tile0 + step % per_head) * kRows;
+        const int left = a.sq - row0;
+        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
+        g1.load(RowBlock<T>{q, a.qt, left, a.d, bool(a.q_wide)}, tid);
+        g2.load(RowBlock<T>{q + a.qm, a.qt, left, a.d, bool(a.q_wide)}, tid);
+        gg.load(RowBlock<T>{static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left,
+                            a.dv, bool(a.g_wide)},
+                tid);
+        if (tid < 4 * kRows) {
+            // lse of both maps, then delta of both; rows beyond the last have no terms
+            const int i = tid % kRows, which = tid / kRows;
+            const float* from_mem = (which < 2 ? a.lse : a.delta) + ((size_t(b) * a.hq + h) * 2 + which % 2) * a.sq;
+            stat = i < left ? from_mem[row0 + i] : (which < 2 ? kInf : 0.f);
+        }
+    };
+    if (steps > 0) fetch(0);
+    for (int step = 0; step < steps; ++step) {
+        char* buffer = lds + (step & 1) * Shape::kBufferBytes;
+        T* t1 = reinterpret_cast<T*>(buffer);
+        T* t2 = reinterpret_cast<T*>(buffer + Shape::kQueryBytes);
+        T* tg = reinterpret_cast<T*>(buffer + 2 * Shape::kQueryBytes);
+        float* ts = reinterpret_cast<float*>(buffer + 2 * Shape::kQueryBytes + Shape::kGradBytes);
+        g1.store(t1, tid);
+        g2.store(t2, tid);
+        gg.store(tg, tid);
+        if (tid < 4 * kRows) ts[tid] = stat;
+        __syncthreads();
+        if (step + 1 < steps) fetch(step + 1);
+        const int row0 = (tile0 + step % per_head) * kRows;
+        const float lam = attn_lambda(a, hkv * group + step / per_head);
+
+        floatx16 p1 = zero16(), p2 = zero16();
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            mma(p1, read_row<T, D>(t1, 0, s, lane), k1[s]);
+            mma(p2, read_row<T, D>(t2, 0, s, lane), k2[s]);
+        }
+        {
+            const floatx16 l1 = rows_of(ts, hi), l2 = rows_of(ts + kRows, hi);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -l1[r]));
+                p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -l2[r]));
+            }
+        }
+        if (row0 < all_from) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (row0 + acc_row(r, hi) < from) p1[r] = p2[r] = 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p2[r] *= lam;
+        if constexpr (DVAL) {
+            floatx16 w;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) w[r] = p1[r] - p2[r];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Operand<T> x = acc_operand<T>(w, s);
+#pragma unroll
+                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(tg, 0, 32 * d, s, lane), x);
+            }
+        }
+        if constexpr (DK) {
+            floatx16 t = zero16();
+#pragma unroll
+            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(tg, 0, s, lane), v[s]);
+            {
+                const floatx16 d1 = rows_of(ts + 2 * kRows, hi), d2 = rows_of(ts + 3 * kRows, hi);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p1[r] *= t[r] - d1[r];
+                    p2[r] *= d2[r] - t[r];
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    mma(dk1[d], read_column<T, D>(t1, 0, 32 * d, s, lane), x1);
+                    mma(dk2[d], read_column<T, D>(t2, 0, 32 * d, s, lane), x2);
+                }
+            }
+        }
+    }
+    if (key >= a.sk) return;
+    if constexpr (DK) {
+        T* dk = static_cast<T*>(a.dk) + ((size_t(b) * a.sk + key) * a.hk + hkv) * 2 * a.d;
+        const bool whole = a.d % 4 == 0;
+        store_row(dk, dk1, a.d, whole, a.scale, hi);
+        store_row(dk + a.d, dk2, a.d, whole, a.scale, hi);
+    }
+    if constexpr (DVAL)
+        store_row(static_cast<T*>(a.dv_out) + ((size_t(b) * a.sk + key) * a.hk + hkv) * a.dv, dval, a.dv, a.o_wide, 1.f,
+                  hi);
+}
+
+namespace {
+template <typename T, int D, int DV>
+struct QuerySideShape {
+    static constexpr int kKeys = 32;
+    static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
+    static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
+    static constexpr int kLds = 2 * kBufferBytes;
+};
+}  // namespace
+
+// Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
+// goes over the keys, as the forward kernel does.
+template <typename T, int D, int DV>
+__global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
+    using Shape = QuerySideShape<T, D, DV>;
+    constexpr int kKeys = Shape::kKeys;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+    const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
+    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
+    const int tile = tiles - 1 - id % tiles;
+    const int h = id / tiles % a.hq, b = id / tiles / a.hq;
+    const int hkv = h / (a.hq / a.hk);
+    const int length = attn_length(a, b);
+    const int first = tile * kAttnRows + wave * 32, row = first + (lane & 31);
+    const int last = attn_last_key(a, row, length);
+    const int first_last = attn_last_key(a, first, length);
+    const int wave_end = attn_last_key(a, min(first + 31, a.sq - 1), length) + 1;
+    const int end = attn_last_key(a, min(tile * kAttnRows + kAttnRows, a.sq) - 1, length) + 1;
+    const float lam = attn_lambda(a, h);
+
+    const T* kp = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
+    const T* vp = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
+    const bool valid = row < a.sq;
+    Operand<T> q1[D / 16], q2[D / 16], g[DV / 16];
+    {
+        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh;
+        load_row_operands<T, D>(q1, q, a.d, valid, a.q_wide, lane);
+        load_row_operands<T, D>(q2, q + a.qm, a.d, valid, a.q_wide, lane);
+        load_row_operands<T, DV>(g, static_cast<const T*>(a.dout) + b * a.gb + (long long)row * a.gt + h * a.gh, a.dv,
+                                 valid, a.g_wide, lane);
+    }
+    const size_t at = (size_t(b) * a.hq + h) * 2 * a.sq + row;
+    const float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
+    const float d1 = valid ? a.delta[at] : 0.f, d2 = valid ? a.delta[at + a.sq] : 0.f;
+    floatx16 dq1[D / 32], dq2[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) dq1[d] = dq2[d] = zero16();
+
+    Stage<T, D, kKeys, 256> g1, g2;
+    Stage<T, DV, kKeys, 256> gv;
+    auto fetch = [&](int key) {
+        const int left = end - key;
+        g1.load(RowBlock<T>{kp + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
+        g2.load(RowBlock<T>{kp + a.km + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
+        gv.load(RowBlock<T>{vp + (long long)key * a.vt, a.vt, left, a.dv, bool(a.v_wide)}, tid);
+    };
+    if (end > 0) fetch(0);
+    for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
+        char* buffer = lds + (i & 1) * Shape::kBufferBytes;
+        T* t1 = reinterpret_cast<T*>(buffer);
+        T* t2 = reinterpret_cast<T*>(buffer + Shape::kKeyBytes);
+        T* tv = reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes);
+        g1.store(t1, tid);
+        g2.store(t2, tid);
+        gv.store(tv, tid);
+        __syncthreads();
+        if (key + kKeys < end) fetch(key + kKeys);
+        if (key >= wave_end) continue;
+        floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            mma(p1, read_row<T, D>(t1, 0, s, lane), q1[s]);
+            mma(p2, read_row<T, D>(t2, 0, s, lane), q2[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(tv, 0, s, lane), g[s]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
+            p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2)) * lam;
+        }
+        if (key + 31 > first_last) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (key + acc_row(r, hi) > last) p1[r] = p2[r] = 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            p1[r] *= t[r] - d1;
+            p2[r] *= d2 - t[r];
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                mma(dq1[d], read_column<T, D>(t1, 0, 32 * d, s, lane), x1);
+                mma(dq2[d], read_column<T, D>(t2, 0, 32 * d, s, lane), x2);
+            }
+        }
+    }
+    if (!valid) return;
+    T* dq = static_cast<T*>(a.dq) + ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
+    const bool whole = a.d % 4 == 0;
+    store_row(dq, dq1, a.d, whole, a.scale, hi);
+    store_row(dq + a.d, dq2, a.d, whole, a.scale, hi);
+}
+
+namespace {
+
+template <typename T, int D, int DV, bool DK, bool DVAL>
+hipError_t launch_key_side(const AttnArgs& a, hipStream_t s) {
+    using Shape = KeySideShape<T, D, DV>;
+    const long long blocks = (long long)a.n * a.hk * ((a.sk + kKeySideKeys - 1) / kKeySideKeys);
+    if (hipError_t e = allow_dynamic_lds(attn_key_side_kernel<T, D, DV, DK, DVAL>, Shape::kLds)) return e;
+    return launch_kernel(attn_key_side_kernel<T, D, DV, DK, DVAL>, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s,
+                         nullptr, nullptr, a);
+}
+
+template <typename T, int D, int DV>
+hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
+    const long long rows = (long long)a.n * a.hq * chunks;
+    if (hipError_t e = launch_kernel(attn_delta_kernel<T>, dim3(unsigned(rows)), dim3(256), 0, s, ev.start, nullptr, a))
+        return e;
+    if (hipError_t e = launch_kernel(attn_dlam_kernel, dim3(a.lam_step ? a.hq : 1), dim3(256), 0, s, nullptr, nullptr, a))
+        return e;
+    // fp32 operands and accumulators of both gradients at the largest widths
+    // would not fit the 512 registers of a lane: there dk and dv are two passes
+    if constexpr (sizeof(T) * D >= 512) {
+        if (hipError_t e = launch_key_side<T, D, DV, true, false>(a, s)) return e;
+        if (hipError_t e = launch_key_side<T, D, DV, false, true>(a, s)) return e;
+    } else {
+        if (hipError_t e = launch_key_side<T, D, DV, true, true>(a, s)) return e;
+    }
+    using Shape = QuerySideShape<T, D, DV>;
+    const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnRows - 1) / kAttnRows);
+    if (hipError_t e = allow_dynamic_lds(attn_query_side_kernel<T, D, DV>, Shape::kLds)) return e;
+    return launch_kernel(attn_query_side_kernel<T, D, DV>, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr,
+                         ev.stop, a);
+}
+
+template <typename T>
+hipError_t launch_typed(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    switch (p.shape) {
+        case 0: return launch_shaped<T, 32, 64>(a, s, ev);
+        case 1: return launch_shaped<T, 64, 128>(a, s, ev);
+        default: return launch_shaped<T, 128, 256>(a, s, ev);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attn_backward(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s,
+                                const LaunchEvents& ev) {
+    return p.prob.dtype == FFTSPLIT_BF16 ? launch_typed<__bf16>(p, a, s, ev) : launch_typed<float>(p, a, s, ev);
+}
+
+}  // namespace fftsplit
