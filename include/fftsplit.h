@@ -432,6 +432,65 @@ fftsplit_status_t fftsplit_attention_backward(fftsplit_attention_plan_t plan, co
                                               void* dlam, void* workspace, size_t workspace_bytes,
                                               hipStream_t stream);
 
+/* Layer norm over the channels of each position of each image or sequence:
+ *   y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(var + eps),
+ * statistics in fp32 (the mean first, then the squared deviations from it). */
+enum {
+    FFTSPLIT_CHANNELS_LAST = 0,    /* [batch][positions][channels]: tokens */
+    FFTSPLIT_CHANNELS_FIRST = 1    /* [batch][channels][positions]: a feature map */
+};
+typedef struct {
+    int batch, positions, channels;   /* channels at most 8192, with x channels first 2048 */
+    int x_dtype, y_dtype;             /* fftsplit_dtype_t; both the same, or fp32 to bf16 */
+    int x_layout, y_layout;           /* both the same, or a feature map to tokens */
+    float eps;
+} fftsplit_layer_norm_t;
+
+/* x (device, x_dtype, x_layout) -> y (device, y_dtype, y_layout); weight and
+ * bias (device, fp32 [channels]) or NULL (1 and 0); mean and rstd (device,
+ * fp32 [batch][positions], for the backward pass) or both NULL.  Runs on the
+ * current device. */
+fftsplit_status_t fftsplit_layer_norm(const fftsplit_layer_norm_t* desc /* host */, const void* x, const float* weight,
+                                      const float* bias, void* y, float* mean, float* rstd, hipStream_t stream);
+
+/* Gradients: dy (like y), x, mean, rstd, weight as in the forward pass ->
+ * dx (like x), dweight and dbias (device, fp32 [channels]; sums over all
+ * positions in a fixed order).  workspace: device, of the bytes that
+ * fftsplit_layer_norm_workspace gives. */
+fftsplit_status_t fftsplit_layer_norm_workspace(const fftsplit_layer_norm_t* desc /* host */, size_t* bytes /* host */);
+fftsplit_status_t fftsplit_layer_norm_backward(const fftsplit_layer_norm_t* desc /* host */, const void* dy,
+                                               const void* x, const float* mean, const float* rstd,
+                                               const float* weight, void* dx, float* dweight, float* dbias,
+                                               void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Rotary positions over several axes (row and column of an image's tokens,
+ * and time).  The first sections[0] pairs of a head's elements follow the
+ * token's first coordinate, the next sections[1] its second, and so on: pair
+ * i = (a, b) at coordinate p becomes
+ *   (a cos t - b sin t, b cos t + a sin t),  t = p * freqs[i]
+ * (inverse: -t, which is also the gradient).  With r pairs in all, pair i is
+ * elements (i, i + r), or (2 i, 2 i + 1) where interleaved; elements from 2 r
+ * on are passed on.  The angle's whole turns are taken off in 64 bits. */
+#define FFTSPLIT_ROTARY_MAX_AXES 4
+typedef struct {
+    int batch, tokens, dim;        /* dim: elements of a head, at most 1024 */
+    int heads0, heads1;            /* heads of the two tensors; heads1 0: only the first */
+    int dtype;                     /* fftsplit_dtype_t */
+    int axes;                      /* 1 to FFTSPLIT_ROTARY_MAX_AXES */
+    int sections[FFTSPLIT_ROTARY_MAX_AXES];   /* pairs of each axis */
+    int positions_per_batch;       /* positions are [batch][tokens][axes], else [tokens][axes] */
+    int inverse, interleaved;
+} fftsplit_rotary_t;
+
+/* positions (device, int), freqs (device, fp32, one per pair).  x0 -> y0 and,
+ * with heads1, x1 -> y1 (device): strides of batch, token and head in
+ * elements, last dimension dense.  y may be x (in place, with equal strides)
+ * and must not overlap it otherwise.  Runs on the current device. */
+fftsplit_status_t fftsplit_rotary(const fftsplit_rotary_t* desc /* host */, const int* positions, const float* freqs,
+                                  const void* x0, const long long x0_stride[3], void* y0, const long long y0_stride[3],
+                                  const void* x1, const long long x1_stride[3], void* y1, const long long y1_stride[3],
+                                  hipStream_t stream);
+
 /* Benchmark hook (host, per calling thread): until called again with
  * NULL, NULL, every later fftsplit_transform_weights / fftsplit_conv2d /
  * stage call made by this thread records `start` (if non-NULL) when its

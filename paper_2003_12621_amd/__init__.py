@@ -442,6 +442,6 @@ def bin_coords(L: int):
 
 
 from . import attention as _attention  # noqa: E402
-from .attention import DiffAttention  # noqa: E402,F401
+from .attention import DiffAttention, layer_norm, layer_norm_backward, rotary  # noqa: E402,F401
 
 _SIGNATURES.update(_attention.SIGNATURES)

@@ -15,6 +15,8 @@ from typing import Optional
 import paper_2003_12621_amd as _fs
 
 F32, BF16 = 0, 1
+CHANNELS_LAST, CHANNELS_FIRST = 0, 1
+ROTARY_MAX_AXES = 4
 
 
 class AttentionProblem(ctypes.Structure):
@@ -35,7 +37,19 @@ class AttentionInputs(ctypes.Structure):
                 ("lam_count", ctypes.c_int)]
 
 
+class LayerNorm(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("batch", "positions", "channels", "x_dtype", "y_dtype", "x_layout",
+                                            "y_layout")] + [("eps", ctypes.c_float)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int) for f in ("batch", "tokens", "dim", "heads0", "heads1", "dtype", "axes")]
+                + [("sections", ctypes.c_int * ROTARY_MAX_AXES)]
+                + [(f, ctypes.c_int) for f in ("positions_per_batch", "inverse", "interleaved")])
+
+
 _P, _SZ = ctypes.c_void_p, ctypes.c_size_t
+_STRIDES = ctypes.POINTER(ctypes.c_longlong)
 SIGNATURES = {
     "fftsplit_attention_plan": (ctypes.c_int, [ctypes.POINTER(AttentionProblem), ctypes.c_int, ctypes.POINTER(_P)]),
     "fftsplit_attention_plan_for_arch": (ctypes.c_int, [ctypes.POINTER(AttentionProblem), ctypes.c_char_p,
@@ -46,6 +60,12 @@ SIGNATURES = {
     "fftsplit_attention_backward": (ctypes.c_int, [_P, ctypes.POINTER(AttentionInputs), _P,
                                                    ctypes.POINTER(ctypes.c_longlong), _P, _P, _P, _P, _P, _P, _P, _P,
                                                    _SZ, _P]),
+    "fftsplit_layer_norm": (ctypes.c_int, [ctypes.POINTER(LayerNorm), _P, _P, _P, _P, _P, _P, _P]),
+    "fftsplit_layer_norm_workspace": (ctypes.c_int, [ctypes.POINTER(LayerNorm), ctypes.POINTER(_SZ)]),
+    "fftsplit_layer_norm_backward": (ctypes.c_int, [ctypes.POINTER(LayerNorm), _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                                    _SZ, _P]),
+    "fftsplit_rotary": (ctypes.c_int, [ctypes.POINTER(Rotary), _P, _P, _P, _STRIDES, _P, _STRIDES, _P, _STRIDES, _P,
+                                       _STRIDES, _P]),
 }
 
 
@@ -196,3 +216,148 @@ class DiffAttention:
                                                          _fs._stream_handle(dev)),
                    "fftsplit_attention_backward")
         return dq, dk, dv, dlam
+
+
+_LAYOUTS = {"last": CHANNELS_LAST, "first": CHANNELS_FIRST}
+
+
+def _device_of(t, name):
+    if not isinstance(t, _fs._torch().Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
+    return t.device
+
+
+def _launch(device, name, *args):
+    """Calls an entry point that runs on the current device on `device`'s
+    current stream."""
+    torch = _fs._torch()
+    fn = getattr(_fs.lib(), name)
+    if torch.cuda.current_device() == device.index:
+        _fs._check(fn(*args, _fs._stream_handle(device)), name)
+    else:
+        with torch.cuda.device(device):
+            _fs._check(fn(*args, _fs._stream_handle(device)), name)
+
+
+def _norm_desc(x, layout, out_layout, out_dtype, eps):
+    out_layout = layout if out_layout is None else out_layout
+    if layout not in _LAYOUTS or out_layout not in _LAYOUTS:
+        raise ValueError("layout must be 'last' or 'first'")
+    if x.dim() < 2:
+        raise ValueError("layer_norm needs at least two dimensions")
+    if layout == "first":
+        n, c, s = x.shape[0], x.shape[1], _fs._prod(x.shape[2:])
+        shape = tuple(x.shape) if out_layout == "first" else (n, s, c)
+    else:
+        n, s, c = 1, _fs._prod(x.shape[:-1]), x.shape[-1]
+        shape = tuple(x.shape)
+    return LayerNorm(n, s, c, _type_code(x.dtype), _type_code(out_dtype), _LAYOUTS[layout], _LAYOUTS[out_layout],
+                     eps), shape
+
+
+def _param(t, name, c, device):
+    return None if t is None else _dense(t, name, _fs._torch().float32, c, device)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, layout="last", out_layout=None, out_dtype=None, out=None,
+               return_stats=False):
+    """Layer norm over the channels: of tokens [..., channels] (layout "last")
+    or of feature maps [n, channels, ...] ("first").  out_layout="last" turns
+    a feature map into tokens [n, positions, channels], out_dtype an fp32 one
+    into bf16.  return_stats=True also returns mean and rstd (fp32, one per
+    position) for layer_norm_backward."""
+    torch, dev = _fs._torch(), _device_of(x, "x")
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    desc, shape = _norm_desc(x, layout, out_layout, out_dtype, eps)
+    xp = _dense(x, "x", None, None, dev)
+    wp, bp = _param(weight, "weight", desc.channels, dev), _param(bias, "bias", desc.channels, dev)
+    y = torch.empty(shape, dtype=out_dtype, device=dev) if out is None else out
+    yp = _dense(y, "out", out_dtype, _fs._prod(shape), dev)
+    mean = rstd = None
+    if return_stats:
+        mean, rstd = torch.empty((2, desc.batch * desc.positions), dtype=torch.float32, device=dev)
+    _launch(dev, "fftsplit_layer_norm", ctypes.byref(desc), xp, wp, bp, yp,
+            mean.data_ptr() if return_stats else None, rstd.data_ptr() if return_stats else None)
+    return (y, mean, rstd) if return_stats else y
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, layout="last", out_layout=None, workspace=None):
+    """(dx, dweight, dbias) from the gradient of layer_norm's output; the
+    parameters' gradients are fp32."""
+    torch, dev = _fs._torch(), _device_of(x, "x")
+    _device_of(dy, "dy")
+    desc, shape = _norm_desc(x, layout, out_layout, dy.dtype, 0.0)
+    rows = desc.batch * desc.positions
+    gp = _dense(dy, "dy", dy.dtype, _fs._prod(shape), dev)
+    xp = _dense(x, "x", None, None, dev)
+    mp, rp = _dense(mean, "mean", torch.float32, rows, dev), _dense(rstd, "rstd", torch.float32, rows, dev)
+    wp = _param(weight, "weight", desc.channels, dev)
+    need = ctypes.c_size_t()
+    _fs._check(_fs.lib().fftsplit_layer_norm_workspace(ctypes.byref(desc), ctypes.byref(need)),
+               "fftsplit_layer_norm_workspace")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if workspace is None else workspace
+    dx = torch.empty_like(x)
+    dweight, dbias = torch.empty((2, desc.channels), dtype=torch.float32, device=dev)
+    _launch(dev, "fftsplit_layer_norm_backward", ctypes.byref(desc), gp, xp, mp, rp, wp, dx.data_ptr(),
+            dweight.data_ptr(), dbias.data_ptr(), _dense(ws, "workspace", None, None, dev),
+            ws.numel() * ws.element_size())
+    return dx, dweight, dbias
+
+
+def _heads_view(t, name):
+    """[batch, tokens, heads, dim] strides of a [batch, tokens, ..., dim] tensor."""
+    if t.dim() < 4:
+        raise ValueError(f"{name} must be [batch, tokens, heads, dim], heads possibly in several dimensions")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    heads, stride = 1, 0
+    for size, st in zip(reversed(t.shape[2:-1]), reversed(t.stride()[2:-1])):
+        if size == 1:
+            continue
+        if heads == 1:
+            stride = st
+        elif st != stride * heads:
+            raise ValueError(f"{name}: its head dimensions do not form one")
+        heads *= size
+    return heads, (ctypes.c_longlong * 3)(t.stride(0), t.stride(1), stride)
+
+
+def rotary(x, positions, freqs, sections, other=None, interleaved=False, inverse=False, out=None, out_other=None):
+    """Turns the pairs of every head of x [batch, tokens, heads, dim] (heads
+    possibly in several dimensions) by its token's positions times freqs;
+    `sections` counts the pairs of each axis of `positions` ([tokens, axes] or
+    [batch, tokens, axes], int32).  `other` is turned in the same launch (the
+    keys beside the queries); then both results are returned.  out=x works in
+    place; inverse=True gives the gradient."""
+    torch, dev = _fs._torch(), _device_of(x, "x")
+    if other is None and out_other is not None:
+        raise ValueError("out_other given without other")
+    n, s, d = x.shape[0], x.shape[1], x.shape[-1]
+    sections = tuple(int(p) for p in sections)
+    axes = len(sections)
+    if not 1 <= axes <= ROTARY_MAX_AXES:
+        raise ValueError(f"sections must name 1 to {ROTARY_MAX_AXES} axes")
+    per_batch = positions.dim() == 3
+    if tuple(positions.shape) != ((n, s, axes) if per_batch else (s, axes)):
+        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected [{s}, {axes}] or [{n}, {s}, {axes}]")
+    pp = _dense(positions, "positions", torch.int32, None, dev)
+    fp = _dense(freqs, "freqs", torch.float32, sum(sections), dev)
+    ptrs, outs, heads = [], [], [0, 0]
+    for i, (t, o, name) in enumerate(((x, out, "x"), (other, out_other, "other"))):
+        if t is None:
+            ptrs += [None] * 4
+            continue
+        if t.dim() < 4 or t.shape[0] != n or t.shape[1] != s or t.shape[-1] != d:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{n}, {s}, heads, {d}]")
+        o = torch.empty(t.shape, dtype=t.dtype, device=dev) if o is None else o
+        xp = _strided(t, name, x.dtype, tuple(t.shape), dev)
+        yp = _strided(o, f"output of {name}", x.dtype, tuple(t.shape), dev)
+        heads[i], xs = _heads_view(t, name)
+        _, ys = _heads_view(o, f"output of {name}")
+        ptrs += [xp, xs, yp, ys]
+        outs.append(o)
+    desc = Rotary(n, s, d, heads[0], heads[1], _type_code(x.dtype), axes,
+                  (ctypes.c_int * ROTARY_MAX_AXES)(*sections), int(per_batch), int(bool(inverse)),
+                  int(bool(interleaved)))
+    _launch(dev, "fftsplit_rotary", ctypes.byref(desc), pp, fp, *ptrs)
+    return outs[0] if other is None else tuple(outs)

@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libfftsplit.so")
 
 SOURCES = ["plan.cpp", "api.cpp", "k_weights.hip", "k_forward.hip", "k_contract.hip", "k_contract_split.hip", "k_inverse.hip", "k_pool.hip",
            "k_direct.hip", "k_oaa.hip", "noalloc.hip", "k_probe.hip", "attention.cpp", "k_attn_forward.hip",
-           "k_attn_backward.hip"]
+           "k_attn_backward.hip", "block_ops.cpp", "k_norm.hip", "k_rotary.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
