@@ -384,7 +384,8 @@ typedef struct {
  *   q [batch][queries][heads_q][2][dim], k [batch][keys][heads_k][2][dim]:
  *     batch, token, head, map;
  *   v [batch][keys][heads_k][dim_v]: batch, token, head;
- * the last dimension is dense and no stride is negative.  q, k and v may be
+ * the last dimension is dense, no stride is negative and those of tokens are at
+ * most 2^22.  q, k and v may be
  * slices of one tensor.  Pointers need only their type's alignment; where
  * pointers, strides and widths allow 16-byte accesses those are used.
  *   lam: one value for all heads or one per query head (lam_count 1 or

@@ -34,6 +34,9 @@ fftsplit_status_t check_strides(const int* dims, const long long* strides, int n
         if (strides[i] < 0) return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(name) + " has a negative stride");
         if (dims[i] > 1 && size_t(strides[i]) > (size_t(1) << 58) / size_t(dims[i]))
             return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(name) + " has a stride out of range");
+        // (a tile's rows are addressed with 32-bit offsets from its first)
+        if (i == 1 && dims[i] > 1 && strides[i] > kAttnMaxTokenStride)
+            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, std::string(name) + ": token strides above 2^22 elements");
     }
     return FFTSPLIT_SUCCESS;
 }
@@ -157,9 +160,8 @@ fftsplit_status_t check_inputs(fftsplit_attention_plan_t plan, const fftsplit_at
     a.vb = in->v_stride[0];
     a.vt = in->v_stride[1];
     a.vh = in->v_stride[2];
-    a.q_wide = wide(in->q, in->q_stride, 4, p.dim, es);
-    a.k_wide = wide(in->k, in->k_stride, 4, p.dim, es);
-    a.v_wide = wide(in->v, in->v_stride, 3, p.dim_v, es);
+    a.wide = wide(in->q, in->q_stride, 4, p.dim, es) && wide(in->k, in->k_stride, 4, p.dim, es) &&
+             wide(in->v, in->v_stride, 3, p.dim_v, es);
     a.o_wide = p.dim_v % 4 == 0;
     spans.add(in->q, extent(qd, in->q_stride, 4, p.dim, es), "q");
     spans.add(in->k, extent(kd, in->k_stride, 4, p.dim, es), "k");
@@ -281,7 +283,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.gb = dout_stride[0];
         a.gt = dout_stride[1];
         a.gh = dout_stride[2];
-        a.g_wide = wide(dout, dout_stride, 3, p.dim_v, es);
+        a.wide = a.wide && wide(dout, dout_stride, 3, p.dim_v, es);
         a.parts = delta_parts(p);
         a.delta = static_cast<float*>(workspace);
         a.dlam_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + round256(lse_bytes(p)));

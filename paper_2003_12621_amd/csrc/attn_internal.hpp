@@ -27,6 +27,10 @@ constexpr int kAttnRows = 128;
 // Query rows, packed over the heads that share a key head, of the kernel for few rows.
 constexpr int kAttnFewRows = 32;
 
+// Tiles hold at most 64 rows of 4-byte elements: their byte offsets stay below
+// 2^31.
+constexpr long long kAttnMaxTokenStride = 1 << 22;
+
 // What the attention kernels get.  Strides are in elements.
 struct AttnArgs {
     const void *q, *k, *v, *lam;
@@ -39,7 +43,7 @@ struct AttnArgs {
     long long qb, qt, qh, qm;        // batch, token, head, map
     long long kb, kt, kh, km;
     long long vb, vt, vh;
-    int q_wide, k_wide, v_wide;      // 16-byte accesses allowed
+    int wide;                        // 16-byte accesses of all input rows allowed
     void* o;                         // [n][sq][hq][dv]
     void *o1, *o2;                   // the maps' own outputs, same layout, or null
     float* lse;                      // [n][hq][2][sq]: log2 of the sum of exp2, or null
@@ -51,7 +55,6 @@ struct AttnArgs {
     // backward
     const void* dout;
     long long gb, gt, gh;            // batch, token, head strides of dout
-    int g_wide;
     float* delta;                    // [n][hq][2][sq]
     float* dlam_part;                // [hq][parts]
     int parts;

@@ -136,82 +136,98 @@ __device__ __forceinline__ Operand<T> read_column(const T* tile, int row0, int c
     return o;
 }
 
-// A block of rows in memory: row r at base + r * stride (elements).  Elements
-// in rows from `rows` on and columns from `cols` on read as zero and are not
-// touched in memory.  `wide`: base, stride and cols allow 16-byte accesses.
-template <typename T>
-struct RowBlock {
-    const T* base;
-    long long stride;
-    int rows, cols;
-    bool wide;
-};
-
-// ROWS rows of W elements on their way from memory to a tile in LDS, spread
-// over THREADS threads: chunk i of thread t is chunk t + i * THREADS in row order.
-template <typename T, int W, int ROWS, int THREADS>
+// Rows in memory on their way to a tile of ROWS rows of W elements in LDS,
+// spread over THREADS threads: chunk i of thread t is chunk t + i THREADS in row
+// order.  Loads go through a buffer descriptor of the rows that exist, so rows
+// beyond them read as zero and are not touched; so do columns from `cols` on.
+// WIDE: base, stride and cols allow 16-byte accesses, else single elements.
+template <typename T, int W, int ROWS, int THREADS, bool WIDE>
 struct Stage {
     using Shape = TileShape<T, W>;
     static constexpr int kChunks = ROWS * Shape::kRowChunks;
     static constexpr int kPer = (kChunks + THREADS - 1) / THREADS;
+    static constexpr bool kWhole = kChunks % THREADS == 0;
     uint4 r[kPer];
 
-    __device__ __forceinline__ void load(const RowBlock<T>& b, int t) {
+    // Byte offsets of a thread's chunks from the tile's first row, the same
+    // for all tiles of a tensor.
+    struct Map {
+        unsigned off[kPer];
+        int cols, col;
+        __device__ __forceinline__ Map(long long stride, int cols_, int t) : cols(cols_) {
+            col = t % Shape::kRowChunks * Shape::kChunk;    // (THREADS is a multiple of kRowChunks)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int c = t + i * THREADS, row = c / Shape::kRowChunks;
+                off[i] = (kWhole || c < kChunks) && col < cols ? unsigned((row * stride + col) * int(sizeof(T))) : kOutOfRange;
+            }
+        }
+    };
+
+    // `rows` (possibly none or more than ROWS) rows exist from `base` on.
+    __device__ __forceinline__ void load(const Map& m, const T* base, long long stride, int rows) {
+        const int n = min(rows, ROWS);
+        const BufRsrc rsrc = make_rsrc(base, n > 0 ? unsigned(((n - 1) * stride + m.cols) * int(sizeof(T))) : 0u);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int c = t + i * THREADS, row = c / Shape::kRowChunks, col = c % Shape::kRowChunks * Shape::kChunk;
-            r[i] = make_uint4(0, 0, 0, 0);
-            if ((kChunks % THREADS == 0 || c < kChunks) && row < b.rows && col < b.cols) {
-                const T* p = b.base + (long long)row * b.stride + col;
-                if (b.wide) {
-                    r[i] = *reinterpret_cast<const uint4*>(p);
-                } else {
-                    T e[Shape::kChunk];
+            if constexpr (WIDE) {
+                r[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, m.off[i], 0, 0));
+            } else {
+                T e[Shape::kChunk];
 #pragma unroll
-                    for (int j = 0; j < Shape::kChunk; ++j) e[j] = col + j < b.cols ? p[j] : T(0.f);
-                    __builtin_memcpy(&r[i], e, 16);
+                for (int j = 0; j < Shape::kChunk; ++j) {
+                    const unsigned o = m.col + j < m.cols && m.off[i] != kOutOfRange ? m.off[i] + j * unsigned(sizeof(T))
+                                                                                    : kOutOfRange;
+                    if constexpr (sizeof(T) == 4)
+                        e[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, o, 0, 0));
+                    else
+                        e[j] = __builtin_bit_cast(__bf16, __builtin_amdgcn_raw_buffer_load_b16(rsrc, o, 0, 0));
                 }
+                __builtin_memcpy(&r[i], e, 16);
             }
         }
     }
     __device__ __forceinline__ void store(T* tile, int t) const {
+        T* p = tile + t / Shape::kRowChunks * Shape::kStride + t % Shape::kRowChunks * Shape::kChunk;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int c = t + i * THREADS, row = c / Shape::kRowChunks, col = c % Shape::kRowChunks * Shape::kChunk;
-            if (kChunks % THREADS == 0 || c < kChunks) *reinterpret_cast<uint4*>(tile + row * Shape::kStride + col) = r[i];
-        }
+        for (int i = 0; i < kPer; ++i)
+            if (kWhole || t + i * THREADS < kChunks)
+                *reinterpret_cast<uint4*>(p + i * (THREADS / Shape::kRowChunks) * Shape::kStride) = r[i];
     }
 };
 
 // The operand steps of one row of `cols` elements that lane % 32 holds, from
 // memory (p may be anything where `valid` is false).
-template <typename T, int W>
-__device__ __forceinline__ void load_row_operands(Operand<T> (&o)[W / 16], const T* p, int cols, bool valid, bool wide,
-                                                  int lane) {
+template <typename T, int W, bool WIDE>
+__device__ __forceinline__ void load_row_operands(Operand<T> (&o)[W / 16], const T* p, int cols, bool valid, int lane) {
 #pragma unroll
     for (int s = 0; s < W / 16; ++s) {
         const int col = 16 * s + 8 * (lane >> 5);
         T e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = T(0.f);
-        if (valid && wide) {
+        if (valid) {
+            if constexpr (WIDE) {
 #pragma unroll
-            for (int j = 0; j < 8; j += 16 / int(sizeof(T)))
-                if (col + j < cols) *reinterpret_cast<uint4*>(e + j) = *reinterpret_cast<const uint4*>(p + col + j);
-        } else if (valid) {
+                for (int j = 0; j < 8; j += 16 / int(sizeof(T)))
+                    if (col + j < cols) *reinterpret_cast<uint4*>(e + j) = *reinterpret_cast<const uint4*>(p + col + j);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + j < cols) e[j] = p[col + j];
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < cols) e[j] = p[col + j];
+            }
         }
         __builtin_memcpy(&o[s].v, e, sizeof(e));
     }
 }
 
-// Four consecutive elements of an output row, elements from `cols` on left out.
+// Four consecutive elements of an output row, elements from `cols` on left out
+// (`wide`: cols is a multiple of 4).
 template <typename T>
 __device__ __forceinline__ void store4(T* p, int col, int cols, bool wide, float a, float b, float c, float d) {
     const float v[4] = {a, b, c, d};
-    if (wide && col + 4 <= cols) {
+    if (wide) {
+        if (col >= cols) return;
         if constexpr (sizeof(T) == 4)
             *reinterpret_cast<float4*>(p + col) = make_float4(a, b, c, d);
         else

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
     const int h = blockIdx.x % a.hq, c = blockIdx.x / a.hq % chunks, b = blockIdx.x / a.hq / chunks;
     const int l = threadIdx.x % kDeltaLanes, group = threadIdx.x / kDeltaLanes;
-    const bool wide = a.g_wide && a.dv % 8 == 0;
+    const bool wide = a.wide && a.dv % 8 == 0;
     float total = 0.f;
     for (int i = group; i < kAttnDeltaRows; i += 256 / kDeltaLanes) {
         const int row = c * kAttnDeltaRows + i;
@@ -152,7 +152,7 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 // Key side: one workgroup takes 128 keys of one key head, 32 a wave, and goes
 // over the queries of all heads that share it.  Each wave keeps its rows of
 // k1, k2 and v as operands and dk1, dk2, dv as accumulators in registers.
-template <typename T, int D, int DV, bool DK, bool DVAL>
+template <typename T, int D, int DV, bool WIDE, bool DK, bool DVAL>
 __global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
     using Shape = KeySideShape<T, D, DV>;
     constexpr int kRows = Shape::kRows;
@@ -173,11 +173,11 @@ __global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
     Operand<T> k1[D / 16], k2[D / 16], v[DV / 16];
     {
         const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
-        load_row_operands<T, D>(k1, p, a.d, exists, a.k_wide, lane);
-        load_row_operands<T, D>(k2, p + a.km, a.d, exists, a.k_wide, lane);
+        load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
+        load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
         if constexpr (DK)
-            load_row_operands<T, DV>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
-                                     a.dv, exists, a.v_wide, lane);
+            load_row_operands<T, DV, WIDE>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
+                                     a.dv, exists, lane);
     }
     floatx16 dk1[DK ? D / 32 : 1], dk2[DK ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
 #pragma unroll
@@ -193,18 +193,20 @@ __global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
     const int per_head = first >= length ? 0 : max(0, row_tiles - tile0);
     const int steps = per_head * group;
 
-    Stage<T, D, kRows, 256> g1, g2;
-    Stage<T, DV, kRows, 256> gg;
+    using QueryStage = Stage<T, D, kRows, 256, WIDE>;
+    using GradStage = Stage<T, DV, kRows, 256, WIDE>;
+    const typename QueryStage::Map query_map(a.qt, a.d, tid);
+    const typename GradStage::Map grad_map(a.gt, a.dv, tid);
+    QueryStage g1, g2;
+    GradStage gg;
     float stat = 0.f;
     auto fetch = [&](int step) {
         const int h = hkv * group + step / per_head, row0 = (tile0 + step % per_head) * kRows;
         const int left = a.sq - row0;
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
-        g1.load(RowBlock<T>{q, a.qt, left, a.d, bool(a.q_wide)}, tid);
-        g2.load(RowBlock<T>{q + a.qm, a.qt, left, a.d, bool(a.q_wide)}, tid);
-        gg.load(RowBlock<T>{static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left,
-                            a.dv, bool(a.g_wide)},
-                tid);
+        g1.load(query_map, q, a.qt, left);
+        g2.load(query_map, q + a.qm, a.qt, left);
+        gg.load(grad_map, static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left);
         if (tid < 4 * kRows) {
             // lse of both maps, then delta of both; rows beyond the last have no terms
             const int i = tid % kRows, which = tid / kRows;
@@ -307,7 +309,7 @@ struct QuerySideShape {
 
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does.
-template <typename T, int D, int DV>
+template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
     constexpr int kKeys = Shape::kKeys;
@@ -332,10 +334,10 @@ __global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
     Operand<T> q1[D / 16], q2[D / 16], g[DV / 16];
     {
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh;
-        load_row_operands<T, D>(q1, q, a.d, valid, a.q_wide, lane);
-        load_row_operands<T, D>(q2, q + a.qm, a.d, valid, a.q_wide, lane);
-        load_row_operands<T, DV>(g, static_cast<const T*>(a.dout) + b * a.gb + (long long)row * a.gt + h * a.gh, a.dv,
-                                 valid, a.g_wide, lane);
+        load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
+        load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
+        load_row_operands<T, DV, WIDE>(g, static_cast<const T*>(a.dout) + b * a.gb + (long long)row * a.gt + h * a.gh, a.dv,
+                                 valid, lane);
     }
     const size_t at = (size_t(b) * a.hq + h) * 2 * a.sq + row;
     const float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
@@ -344,13 +346,16 @@ __global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) dq1[d] = dq2[d] = zero16();
 
-    Stage<T, D, kKeys, 256> g1, g2;
-    Stage<T, DV, kKeys, 256> gv;
+    using KeyStage = Stage<T, D, kKeys, 256, WIDE>;
+    using ValueStage = Stage<T, DV, kKeys, 256, WIDE>;
+    const typename KeyStage::Map key_map(a.kt, a.d, tid);
+    const typename ValueStage::Map value_map(a.vt, a.dv, tid);
+    KeyStage g1, g2;
+    ValueStage gv;
     auto fetch = [&](int key) {
-        const int left = end - key;
-        g1.load(RowBlock<T>{kp + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
-        g2.load(RowBlock<T>{kp + a.km + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
-        gv.load(RowBlock<T>{vp + (long long)key * a.vt, a.vt, left, a.dv, bool(a.v_wide)}, tid);
+        g1.load(key_map, kp + (long long)key * a.kt, a.kt, end - key);
+        g2.load(key_map, kp + a.km + (long long)key * a.kt, a.kt, end - key);
+        gv.load(value_map, vp + (long long)key * a.vt, a.vt, end - key);
     };
     if (end > 0) fetch(0);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
@@ -410,8 +415,9 @@ template <typename T, int D, int DV, bool DK, bool DVAL>
 hipError_t launch_key_side(const AttnArgs& a, hipStream_t s) {
     using Shape = KeySideShape<T, D, DV>;
     const long long blocks = (long long)a.n * a.hk * ((a.sk + kKeySideKeys - 1) / kKeySideKeys);
-    if (hipError_t e = allow_dynamic_lds(attn_key_side_kernel<T, D, DV, DK, DVAL>, Shape::kLds)) return e;
-    return launch_kernel(attn_key_side_kernel<T, D, DV, DK, DVAL>, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s,
+    auto kernel = a.wide ? attn_key_side_kernel<T, D, DV, true, DK, DVAL> : attn_key_side_kernel<T, D, DV, false, DK, DVAL>;
+    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s,
                          nullptr, nullptr, a);
 }
 
@@ -433,8 +439,9 @@ hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& e
     }
     using Shape = QuerySideShape<T, D, DV>;
     const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnRows - 1) / kAttnRows);
-    if (hipError_t e = allow_dynamic_lds(attn_query_side_kernel<T, D, DV>, Shape::kLds)) return e;
-    return launch_kernel(attn_query_side_kernel<T, D, DV>, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr,
+    auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true> : attn_query_side_kernel<T, D, DV, false>;
+    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr,
                          ev.stop, a);
 }
 

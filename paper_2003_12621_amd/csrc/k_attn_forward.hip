@@ -1,9 +1,9 @@
 // Differential attention, forward: o = (softmax(q1 k1^T) - lam softmax(q2 k2^T)) v.
 //
-// Both maps are taken in one pass over the keys with a running maximum and sum
-// each, and an output accumulator each: the two softmax denominators are known
-// only at the end, where the accumulators are joined.  With values as wide as
-// both maps together that costs what a second pass over the keys for the
+// Each map is taken in one pass over the keys with a running maximum and sum
+// and an output accumulator of its own: the two softmax denominators are known
+// only at the end, where the outputs are joined.  With values as wide as both
+// maps together that costs what a second pass over the keys for the
 // denominators would (4 d + 4 dv operations per query and key, or 8 d + 2 dv).
 #include "attn_common.hpp"
 
@@ -58,52 +58,37 @@ __device__ __forceinline__ void mask_scores(floatx16& s, int key0, int last, int
         if (key0 + acc_row(r, hi) > last) s[r] = -kInf;
 }
 
+// A wave takes one map of RB x 32 query rows: half the waves of a workgroup
+// work on the first map and half on the second of the same rows, and the two
+// outputs are joined through LDS at the end.  A wave with both maps of 32 rows
+// reads a third more operands from LDS per product (each key operand serves
+// one product instead of two), and at 256-wide values its two accumulators
+// alone would take 256 registers.
 template <typename T, int D, int DV>
 struct ForwardShape {
-    static constexpr int kKeys = D * sizeof(T) >= 128 * 2 ? 32 : 64;   // keys per stage
-    static constexpr int kBlocks = D * sizeof(T) >= 128 * 2 ? 1 : 2;   // workgroups per compute unit aimed at
+    static constexpr int kRowBlocks = DV <= 128 ? 2 : 1;
+    static constexpr int kWaves = kAttnRows / 32 / kRowBlocks * 2;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kKeys = sizeof(T) * DV <= 512 ? 64 : 32;         // keys per stage
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;         // workgroups per compute unit aimed at
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
-    static constexpr int kLds = 2 * kBufferBytes;
+    static constexpr int kJoinBytes = kAttnRows * DV * 4;
+    static constexpr int kLds = 2 * kBufferBytes > kJoinBytes ? 2 * kBufferBytes : kJoinBytes;
 };
-
-// The joined output of the lane's query, and for a backward pass each map's own.
-template <typename T, int DT>
-__device__ __forceinline__ void store_output(const AttnArgs& a, const floatx16 (&o1)[DT], const floatx16 (&o2)[DT],
-                                             float inv1, float inv2, float lam, size_t row, int hi) {
-    T* out = static_cast<T*>(a.o) + row * a.dv;
-    T* out1 = a.o1 ? static_cast<T*>(a.o1) + row * a.dv : nullptr;
-    T* out2 = a.o1 ? static_cast<T*>(a.o2) + row * a.dv : nullptr;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * d + acc_row(4 * g, hi);
-            float x[4], y[4], z[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[j] = o2[d][4 * g + j] * inv2;
-                x[j] = o1[d][4 * g + j] * inv1;
-                y[j] = x[j] - lam * z[j];
-            }
-            store4(out, col, a.dv, a.o_wide, y[0], y[1], y[2], y[3]);
-            if (out1) {
-                store4(out1, col, a.dv, a.o_wide, x[0], x[1], x[2], x[3]);
-                store4(out2, col, a.dv, a.o_wide, z[0], z[1], z[2], z[3]);
-            }
-        }
-}
 
 }  // namespace
 
-// One workgroup: 128 query rows of one head, 32 a wave; the keys pass through
-// LDS in double-buffered stages that all four waves read.
-template <typename T, int D, int DV>
-__global__ __launch_bounds__(256, (ForwardShape<T, D, DV>::kBlocks)) void attn_forward_kernel(AttnArgs a) {
+// One workgroup: 128 query rows of one head; the keys pass through LDS in
+// double-buffered stages that all waves read.
+template <typename T, int D, int DV, bool WIDE>
+__global__ __launch_bounds__((ForwardShape<T, D, DV>::kThreads), (ForwardShape<T, D, DV>::kBlocks)) void
+attn_forward_kernel(AttnArgs a) {
     using Shape = ForwardShape<T, D, DV>;
-    constexpr int kKeys = Shape::kKeys, DT = DV / 32;
+    constexpr int kKeys = Shape::kKeys, DT = DV / 32, RB = Shape::kRowBlocks;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, group = wave >> 1;
     const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     const int tile = tiles - 1 - id % tiles;           // under a causal mask the longest first
@@ -111,42 +96,48 @@ __global__ __launch_bounds__(256, (ForwardShape<T, D, DV>::kBlocks)) void attn_f
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
 
-    const int first = tile * kAttnRows + wave * 32, row = first + (lane & 31);
-    const int last = attn_last_key(a, row, length);                  // this lane's query
-    const int first_last = attn_last_key(a, first, length);          // the wave's first and last query
-    const int wave_end = attn_last_key(a, min(first + 31, a.sq - 1), length) + 1;
+    const int first = tile * kAttnRows + group * (32 * RB), row = first + (lane & 31);
+    const int first_last = attn_last_key(a, first, length);          // last key of the wave's first row
+    const int wave_end = attn_last_key(a, min(first + 32 * RB, a.sq) - 1, length) + 1;
     const int end = attn_last_key(a, min(tile * kAttnRows + kAttnRows, a.sq) - 1, length) + 1;
 
     const T* k1 = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
     const T* v = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
 
-    Operand<T> q1[D / 16], q2[D / 16];
-    {
-        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh;
-        load_row_operands<T, D>(q1, q, a.d, row < a.sq, a.q_wide, lane);
-        load_row_operands<T, D>(q2, q + a.qm, a.d, row < a.sq, a.q_wide, lane);
-    }
-    floatx16 o1[DT], o2[DT];
+    Operand<T> q[RB][D / 16];
+    floatx16 o[RB][DT];
+    RowState st[RB];
+    int last[RB];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o1[d] = o2[d] = zero16();
-    RowState s1{-kInf, 0.f}, s2{-kInf, 0.f};
+    for (int r = 0; r < RB; ++r) {
+        const int i = row + 32 * r;
+        load_row_operands<T, D, WIDE>(q[r],
+                                      static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + h * a.qh + map * a.qm,
+                                      a.d, i < a.sq, lane);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[r][d] = zero16();
+        st[r] = RowState{-kInf, 0.f};
+        last[r] = attn_last_key(a, i, length);
+    }
 
-    Stage<T, D, kKeys, 256> g1, g2;
-    Stage<T, DV, kKeys, 256> gv;
+    using KeyStage = Stage<T, D, kKeys, Shape::kThreads, WIDE>;
+    using ValueStage = Stage<T, DV, kKeys, Shape::kThreads, WIDE>;
+    const typename KeyStage::Map key_map(a.kt, a.d, tid);
+    const typename ValueStage::Map value_map(a.vt, a.dv, tid);
+    KeyStage g1, g2;
+    ValueStage gv;
     auto fetch = [&](int key) {
-        const int left = end - key;
-        g1.load(RowBlock<T>{k1 + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
-        g2.load(RowBlock<T>{k1 + a.km + (long long)key * a.kt, a.kt, left, a.d, bool(a.k_wide)}, tid);
-        gv.load(RowBlock<T>{v + (long long)key * a.vt, a.vt, left, a.dv, bool(a.v_wide)}, tid);
+        g1.load(key_map, k1 + (long long)key * a.kt, a.kt, end - key);
+        g2.load(key_map, k1 + a.km + (long long)key * a.kt, a.kt, end - key);
+        gv.load(value_map, v + (long long)key * a.vt, a.vt, end - key);
     };
-    auto buffer = [&](int i) { return lds + (i & 1) * Shape::kBufferBytes; };
     if (end > 0) fetch(0);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
-        T* t1 = reinterpret_cast<T*>(buffer(i));
-        T* t2 = reinterpret_cast<T*>(buffer(i) + Shape::kKeyBytes);
-        T* tv = reinterpret_cast<T*>(buffer(i) + 2 * Shape::kKeyBytes);
-        g1.store(t1, tid);
-        g2.store(t2, tid);
+        char* buffer = lds + (i & 1) * Shape::kBufferBytes;
+        T* tk = reinterpret_cast<T*>(buffer + map * Shape::kKeyBytes);
+        T* tv = reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes);
+        g1.store(reinterpret_cast<T*>(buffer), tid);
+        g2.store(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), tid);
         gv.store(tv, tid);
         // (the buffer's readers of two stages ago passed the last barrier)
         __syncthreads();
@@ -155,42 +146,76 @@ __global__ __launch_bounds__(256, (ForwardShape<T, D, DV>::kBlocks)) void attn_f
         for (int sub = 0; sub < kKeys; sub += 32) {
             const int key0 = key + sub;
             if (key0 >= wave_end) break;
-            floatx16 c1 = zero16(), c2 = zero16();
+            floatx16 c[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) c[r] = zero16();
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                mma(c1, read_row<T, D>(t1, sub, s, lane), q1[s]);
-                mma(c2, read_row<T, D>(t2, sub, s, lane), q2[s]);
+                const Operand<T> x = read_row<T, D>(tk, sub, s, lane);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) mma(c[r], x, q[r][s]);
             }
-            if (key0 + 31 > first_last) {
-                mask_scores(c1, key0, last, hi);
-                mask_scores(c2, key0, last, hi);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                if (key0 + 31 > first_last) mask_scores(c[r], key0, last[r], hi);
+                softmax_step(c[r], st[r], o[r], a.scale_log2);
             }
-            softmax_step(c1, s1, o1, a.scale_log2);
-            softmax_step(c2, s2, o2, a.scale_log2);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const Operand<T> p1 = acc_operand<T>(c1, s), p2 = acc_operand<T>(c2, s);
+                Operand<T> p[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) p[r] = acc_operand<T>(c[r], s);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const Operand<T> x = read_column<T, DV>(tv, sub, 32 * d, s, lane);
-                    mma(o1[d], x, p1);
-                    mma(o2[d], x, p2);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) mma(o[r][d], x, p[r]);
                 }
             }
         }
     }
 
-    const float2 h1 = both_halves(s1.l), h2 = both_halves(s2.l);
-    const float l1 = h1.x + h1.y, l2 = h2.x + h2.y;
-    if (row >= a.sq) return;
-    // (m stays -inf where no key is visible: such a row is zero)
-    const bool none = last < 0;
-    store_output<T, DT>(a, o1, o2, none ? 0.f : 1.f / l1, none ? 0.f : 1.f / l2, attn_lambda(a, h),
-                        (size_t(b) * a.sq + row) * a.hq + h, hi);
-    if (a.lse && hi == 0) {
-        float* lse = a.lse + (size_t(b) * a.hq + h) * 2 * a.sq + row;
-        lse[0] = none ? 0.f : s1.m + log2f(l1);
-        lse[a.sq] = none ? 0.f : s2.m + log2f(l2);
+    // each map's own output, then the second map's scaled by lam to the waves of the first
+    const float lam = attn_lambda(a, h);
+    float4* join = reinterpret_cast<float4*>(lds) + group * (RB * DT * 4 * 64) + lane;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int i = row + 32 * r;
+        const float2 halves = both_halves(st[r].l);
+        const float l = halves.x + halves.y;
+        const bool none = last[r] < 0;                 // no key is visible: the row is zero
+        const float inv = none ? 0.f : 1.f / l;
+        const size_t at = ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
+        T* own = a.o1 && i < a.sq ? static_cast<T*>(map ? a.o2 : a.o1) + at : nullptr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[r][d][4 * g + j] *= inv;
+                const float4 y = make_float4(o[r][d][4 * g], o[r][d][4 * g + 1], o[r][d][4 * g + 2], o[r][d][4 * g + 3]);
+                if (own) store4(own, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, y.x, y.y, y.z, y.w);
+                if (map) join[((r * DT + d) * 4 + g) * 64] = make_float4(y.x * lam, y.y * lam, y.z * lam, y.w * lam);
+            }
+        if (a.lse && hi == 0 && i < a.sq)
+            a.lse[((size_t(b) * a.hq + h) * 2 + map) * a.sq + i] = none ? 0.f : st[r].m + log2f(l);
+    }
+    __syncthreads();
+    if (map) return;
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int i = row + 32 * r;
+        if (i >= a.sq) break;
+        T* out = static_cast<T*>(a.o) + ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 z = join[((r * DT + d) * 4 + g) * 64];
+                store4(out, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, o[r][d][4 * g] - z.x, o[r][d][4 * g + 1] - z.y,
+                       o[r][d][4 * g + 2] - z.z, o[r][d][4 * g + 3] - z.w);
+            }
     }
 }
 
@@ -199,8 +224,9 @@ template <typename T, int D, int DV>
 hipError_t launch_tiled(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
     using Shape = ForwardShape<T, D, DV>;
     const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnRows - 1) / kAttnRows);
-    if (hipError_t e = allow_dynamic_lds(attn_forward_kernel<T, D, DV>, Shape::kLds)) return e;
-    return launch_kernel(attn_forward_kernel<T, D, DV>, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, ev.start,
+    auto kernel = a.wide ? attn_forward_kernel<T, D, DV, true> : attn_forward_kernel<T, D, DV, false>;
+    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(Shape::kThreads), Shape::kLds, s, ev.start,
                          ev.stop, a);
 }
 
