@@ -69,7 +69,7 @@ struct ForwardShape {
     static constexpr int kRowBlocks = DV <= 128 ? 2 : 1;
     static constexpr int kWaves = kAttnRows / 32 / kRowBlocks * 2;
     static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kKeys = sizeof(T) * DV <= 512 ? 64 : 32;         // keys per stage
+    static constexpr int kKeys = sizeof(T) * DV <= 128 ? 64 : 32;         // keys per stage
     static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;         // workgroups per compute unit aimed at
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
