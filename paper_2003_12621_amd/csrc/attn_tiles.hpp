@@ -86,28 +86,40 @@ __device__ __forceinline__ float to_float(T x) {
     return float(x);
 }
 
-// An LDS tile of rows of W elements.  Rows are padded by 16 bytes (bf16) or
-// 8 elements (fp32): reads of 16 bytes at one column of 16 rows then fall into
-// different banks, and so do the column reads of read_column.
+// An LDS tile: rows of W elements in 16-byte chunks, without padding (copies
+// from memory fill 1024 consecutive bytes a wave).  Chunk c of row r lies in
+// place c ^ swizzle(r) of its row, so that 16 lanes that read one chunk of 16
+// rows, or two neighbouring chunks of 4 consecutive rows, use all banks alike:
+// of the rows that start in the same bank, 8 in a row differ in the swizzle, and
+// consecutive ones in more than its last bit.  Period: 16 rows.
 template <typename T, int W>
 struct TileShape {
-    static constexpr int kStride = W + 8;
-    static constexpr int kChunk = 16 / sizeof(T);          // elements per 16 bytes
+    static constexpr int kChunk = 16 / sizeof(T);          // elements
     static constexpr int kRowChunks = W / kChunk;
-    static constexpr int bytes(int rows) { return rows * kStride * int(sizeof(T)); }
+    static constexpr int bytes(int rows) { return rows * W * int(sizeof(T)); }
+    static __device__ __forceinline__ int swizzle(int row) {
+        if constexpr (kRowChunks == 4) return (row >> 2) & 3;
+        if constexpr (kRowChunks == 8) return ((row >> 1) & 3) << 1 | ((row >> 3) & 1);
+        return (row & 7) << 1 | ((row >> 3) & 1);
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * W + (chunk ^ swizzle(row)) * kChunk; }
 };
 
 // Operand whose row (or column) lane % 32 is a row of the tile, contracted
 // along the row: elements 16 s + 8 (lane / 32) + e of row row0 + lane % 32.
+// (row0 and col0 below are multiples of 32.)
 template <typename T, int W>
 __device__ __forceinline__ Operand<T> read_row(const T* tile, int row0, int s, int lane) {
-    const T* p = tile + (row0 + (lane & 31)) * TileShape<T, W>::kStride + 16 * s + 8 * (lane >> 5);
+    using Shape = TileShape<T, W>;
+    tile += row0 * W;
+    const int row = lane & 31, chunk = (16 * s + 8 * (lane >> 5)) / Shape::kChunk;
     Operand<T> o;
     if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        const float4 a = *reinterpret_cast<const float4*>(tile + Shape::at(row, chunk));
+        const float4 b = *reinterpret_cast<const float4*>(tile + Shape::at(row, chunk + 1));
         o.v = floatx8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     } else {
-        o.v = *reinterpret_cast<const bf16x8*>(p);
+        o.v = *reinterpret_cast<const bf16x8*>(tile + Shape::at(row, chunk));
     }
     return o;
 }
@@ -119,80 +131,106 @@ __device__ __forceinline__ Operand<T> read_row(const T* tile, int row0, int s, i
 // the 16 gives the address of 4 columns of row i / 4 and gets column i.
 template <typename T, int W>
 __device__ __forceinline__ Operand<T> read_column(const T* tile, int row0, int col0, int s, int lane) {
-    constexpr int kStride = TileShape<T, W>::kStride;
+    using Shape = TileShape<T, W>;
+    tile += (row0 + 16 * s) * W;
     Operand<T> o;
     if constexpr (sizeof(T) == 4) {
-        const T* p = tile + (row0 + 16 * s + 4 * (lane >> 5)) * kStride + col0 + (lane & 31);
+        const int chunk = (col0 + (lane & 31)) / 4, row = 4 * (lane >> 5);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o.v[e] = p[(8 * (e >> 2) + (e & 3)) * kStride];
+        for (int e = 0; e < 8; ++e) o.v[e] = tile[Shape::at(row + 8 * (e >> 2) + (e & 3), chunk) + (lane & 3)];
     } else {
-        const T* p = tile + (row0 + 16 * s + 4 * (lane >> 5) + ((lane >> 2) & 3)) * kStride + col0 +
-                     16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3);
+        const int chunk = col0 / 8 + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), part = 4 * (lane & 1);
         typedef __attribute__((address_space(3))) bf16x4* LdsQuad;
-        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(p));
-        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(p + 8 * kStride));
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(tile + Shape::at(row, chunk) + part));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(tile + Shape::at(row + 8, chunk) + part));
         o.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     return o;
 }
 
-// Rows in memory on their way to a tile of ROWS rows of W elements in LDS,
-// spread over THREADS threads: chunk i of thread t is chunk t + i THREADS in row
-// order.  Loads go through a buffer descriptor of the rows that exist, so rows
-// beyond them read as zero and are not touched; so do columns from `cols` on.
-// WIDE: base, stride and cols allow 16-byte accesses, else single elements.
+// 16 bytes a lane from a buffer straight into LDS: lane l fills LDS bytes
+// [lds + 16 l, lds + 16 l + 16), with zeros where its offset is out of range.
+// Inline assembly because for the builtin the compiler waits for every
+// outstanding load before each LDS read; copies_done waits before the barrier
+// that publishes a tile.  The wait states cover a descriptor that a vector
+// instruction wrote just before and the M0 write.
+__device__ __forceinline__ void copy16(u32x4 rsrc, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(lds)
+                 : "memory", "m0");
+}
+// All copies that this thread's wave has started are complete, in all waves.
+__device__ __forceinline__ void copies_done() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// Copies rows from memory into a tile of ROWS rows of W elements, spread over
+// THREADS threads: chunk place i of thread t is place t + i THREADS in row
+// order.  Memory is read through a descriptor of the rows that exist, so rows
+// beyond them become zero and are not touched; so do columns from `cols` on.
+// WIDE: base, stride and cols allow 16-byte accesses, and the copy goes straight
+// into LDS; else elements pass through registers one by one.
 template <typename T, int W, int ROWS, int THREADS, bool WIDE>
-struct Stage {
+struct RowCopy {
     using Shape = TileShape<T, W>;
     static constexpr int kChunks = ROWS * Shape::kRowChunks;
     static constexpr int kPer = (kChunks + THREADS - 1) / THREADS;
     static constexpr bool kWhole = kChunks % THREADS == 0;
-    uint4 r[kPer];
+    static_assert(kChunks % 64 == 0, "whole waves");
 
-    // Byte offsets of a thread's chunks from the tile's first row, the same
-    // for all tiles of a tensor.
-    struct Map {
-        unsigned off[kPer];
-        int cols, col;
-        __device__ __forceinline__ Map(long long stride, int cols_, int t) : cols(cols_) {
-            col = t % Shape::kRowChunks * Shape::kChunk;    // (THREADS is a multiple of kRowChunks)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int c = t + i * THREADS, row = c / Shape::kRowChunks;
-                off[i] = (kWhole || c < kChunks) && col < cols ? unsigned((row * stride + col) * int(sizeof(T))) : kOutOfRange;
-            }
-        }
-    };
+    // Byte offsets of a thread's chunks from the tile's first row in memory, the
+    // same for all tiles of a tensor.
+    unsigned off[kPer];
+    int cols;
 
-    // `rows` (possibly none or more than ROWS) rows exist from `base` on.
-    __device__ __forceinline__ void load(const Map& m, const T* base, long long stride, int rows) {
-        const int n = min(rows, ROWS);
-        const BufRsrc rsrc = make_rsrc(base, n > 0 ? unsigned(((n - 1) * stride + m.cols) * int(sizeof(T))) : 0u);
+    __device__ __forceinline__ RowCopy(long long stride, int cols_, int t) : cols(cols_) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            if constexpr (WIDE) {
-                r[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, m.off[i], 0, 0));
-            } else {
+            const int row = (t + i * THREADS) / Shape::kRowChunks;
+            const int col = ((t % Shape::kRowChunks) ^ Shape::swizzle(row)) * Shape::kChunk;
+            off[i] = col < cols ? unsigned((row * stride + col) * int(sizeof(T))) : kOutOfRange;
+        }
+    }
+
+    // Starts the copy of `rows` (possibly none or more than ROWS) rows from `base` on.
+    __device__ __forceinline__ void start(T* tile, const T* base, long long stride, int rows, int t) const {
+        const int n = min(rows, ROWS);
+        const unsigned bytes = n > 0 ? unsigned(((n - 1) * stride + cols) * int(sizeof(T))) : 0u;
+        const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        if constexpr (WIDE) {
+            const uint64_t p = reinterpret_cast<uintptr_t>(base);
+            u32x4 rsrc;
+            rsrc[0] = __builtin_amdgcn_readfirstlane(unsigned(p));
+            rsrc[1] = __builtin_amdgcn_readfirstlane(unsigned(p >> 32) & 0xffffu);
+            rsrc[2] = __builtin_amdgcn_readfirstlane(bytes);
+            rsrc[3] = 0x00020000u;
+            const unsigned lds = unsigned(reinterpret_cast<uintptr_t>(tile)) + wave * 1024;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (kWhole || wave * 64 + i * THREADS < kChunks)
+                    copy16(rsrc, off[i], __builtin_amdgcn_readfirstlane(lds + i * THREADS * 16));
+        } else {
+            const BufRsrc rsrc = make_rsrc(base, bytes);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (!(kWhole || wave * 64 + i * THREADS < kChunks)) continue;
+                const int row = (t + i * THREADS) / Shape::kRowChunks;
+                const int col = ((t % Shape::kRowChunks) ^ Shape::swizzle(row)) * Shape::kChunk;
                 T e[Shape::kChunk];
 #pragma unroll
                 for (int j = 0; j < Shape::kChunk; ++j) {
-                    const unsigned o = m.col + j < m.cols && m.off[i] != kOutOfRange ? m.off[i] + j * unsigned(sizeof(T))
-                                                                                    : kOutOfRange;
+                    const unsigned o = col + j < cols ? off[i] + j * unsigned(sizeof(T)) : kOutOfRange;
                     if constexpr (sizeof(T) == 4)
                         e[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, o, 0, 0));
                     else
                         e[j] = __builtin_bit_cast(__bf16, __builtin_amdgcn_raw_buffer_load_b16(rsrc, o, 0, 0));
                 }
-                __builtin_memcpy(&r[i], e, 16);
+                uint4 u;
+                __builtin_memcpy(&u, e, 16);
+                *reinterpret_cast<uint4*>(tile + (t + i * THREADS) * Shape::kChunk) = u;
             }
         }
-    }
-    __device__ __forceinline__ void store(T* tile, int t) const {
-        T* p = tile + t / Shape::kRowChunks * Shape::kStride + t % Shape::kRowChunks * Shape::kChunk;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (kWhole || t + i * THREADS < kChunks)
-                *reinterpret_cast<uint4*>(p + i * (THREADS / Shape::kRowChunks) * Shape::kStride) = r[i];
     }
 };
 

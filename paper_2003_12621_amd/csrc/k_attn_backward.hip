@@ -153,7 +153,7 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 // over the queries of all heads that share it.  Each wave keeps its rows of
 // k1, k2 and v as operands and dk1, dk2, dv as accumulators in registers.
 template <typename T, int D, int DV, bool WIDE, bool DK, bool DVAL>
-__global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key_side_kernel(AttnArgs a) {
     using Shape = KeySideShape<T, D, DV>;
     constexpr int kRows = Shape::kRows;
     extern __shared__ __align__(16) char lds[];
@@ -193,20 +193,19 @@ __global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
     const int per_head = first >= length ? 0 : max(0, row_tiles - tile0);
     const int steps = per_head * group;
 
-    using QueryStage = Stage<T, D, kRows, 256, WIDE>;
-    using GradStage = Stage<T, DV, kRows, 256, WIDE>;
-    const typename QueryStage::Map query_map(a.qt, a.d, tid);
-    const typename GradStage::Map grad_map(a.gt, a.dv, tid);
-    QueryStage g1, g2;
-    GradStage gg;
+    using QueryCopy = RowCopy<T, D, kRows, 256, WIDE>;
+    using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
+    const QueryCopy query_copy(a.qt, a.d, tid);
+    const GradCopy grad_copy(a.gt, a.dv, tid);
     float stat = 0.f;
-    auto fetch = [&](int step) {
+    auto fetch = [&](int step, char* buffer) {
         const int h = hkv * group + step / per_head, row0 = (tile0 + step % per_head) * kRows;
         const int left = a.sq - row0;
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
-        g1.load(query_map, q, a.qt, left);
-        g2.load(query_map, q + a.qm, a.qt, left);
-        gg.load(grad_map, static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left);
+        query_copy.start(reinterpret_cast<T*>(buffer), q, a.qt, left, tid);
+        query_copy.start(reinterpret_cast<T*>(buffer + Shape::kQueryBytes), q + a.qm, a.qt, left, tid);
+        grad_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kQueryBytes),
+                        static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
         if (tid < 4 * kRows) {
             // lse of both maps, then delta of both; rows beyond the last have no terms
             const int i = tid % kRows, which = tid / kRows;
@@ -214,19 +213,16 @@ __global__ __launch_bounds__(256, 1) void attn_key_side_kernel(AttnArgs a) {
             stat = i < left ? from_mem[row0 + i] : (which < 2 ? kInf : 0.f);
         }
     };
-    if (steps > 0) fetch(0);
+    if (steps > 0) fetch(0, lds);
     for (int step = 0; step < steps; ++step) {
         char* buffer = lds + (step & 1) * Shape::kBufferBytes;
-        T* t1 = reinterpret_cast<T*>(buffer);
-        T* t2 = reinterpret_cast<T*>(buffer + Shape::kQueryBytes);
-        T* tg = reinterpret_cast<T*>(buffer + 2 * Shape::kQueryBytes);
+        const T* t1 = reinterpret_cast<const T*>(buffer);
+        const T* t2 = reinterpret_cast<const T*>(buffer + Shape::kQueryBytes);
+        const T* tg = reinterpret_cast<const T*>(buffer + 2 * Shape::kQueryBytes);
         float* ts = reinterpret_cast<float*>(buffer + 2 * Shape::kQueryBytes + Shape::kGradBytes);
-        g1.store(t1, tid);
-        g2.store(t2, tid);
-        gg.store(tg, tid);
         if (tid < 4 * kRows) ts[tid] = stat;
-        __syncthreads();
-        if (step + 1 < steps) fetch(step + 1);
+        copies_done();
+        if (step + 1 < steps) fetch(step + 1, lds + ((step + 1) & 1) * Shape::kBufferBytes);
         const int row0 = (tile0 + step % per_head) * kRows;
         const float lam = attn_lambda(a, hkv * group + step / per_head);
 
@@ -310,7 +306,7 @@ struct QuerySideShape {
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does.
 template <typename T, int D, int DV, bool WIDE>
-__global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
     constexpr int kKeys = Shape::kKeys;
     extern __shared__ __align__(16) char lds[];
@@ -346,28 +342,25 @@ __global__ __launch_bounds__(256, 1) void attn_query_side_kernel(AttnArgs a) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) dq1[d] = dq2[d] = zero16();
 
-    using KeyStage = Stage<T, D, kKeys, 256, WIDE>;
-    using ValueStage = Stage<T, DV, kKeys, 256, WIDE>;
-    const typename KeyStage::Map key_map(a.kt, a.d, tid);
-    const typename ValueStage::Map value_map(a.vt, a.dv, tid);
-    KeyStage g1, g2;
-    ValueStage gv;
-    auto fetch = [&](int key) {
-        g1.load(key_map, kp + (long long)key * a.kt, a.kt, end - key);
-        g2.load(key_map, kp + a.km + (long long)key * a.kt, a.kt, end - key);
-        gv.load(value_map, vp + (long long)key * a.vt, a.vt, end - key);
+    using KeyCopy = RowCopy<T, D, kKeys, 256, WIDE>;
+    using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
+    const KeyCopy key_copy(a.kt, a.d, tid);
+    const ValueCopy value_copy(a.vt, a.dv, tid);
+    auto fetch = [&](int key, char* buffer) {
+        key_copy.start(reinterpret_cast<T*>(buffer), kp + (long long)key * a.kt, a.kt, end - key, tid);
+        key_copy.start(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), kp + a.km + (long long)key * a.kt, a.kt, end - key,
+                       tid);
+        value_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes), vp + (long long)key * a.vt, a.vt, end - key,
+                         tid);
     };
-    if (end > 0) fetch(0);
+    if (end > 0) fetch(0, lds);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
-        char* buffer = lds + (i & 1) * Shape::kBufferBytes;
-        T* t1 = reinterpret_cast<T*>(buffer);
-        T* t2 = reinterpret_cast<T*>(buffer + Shape::kKeyBytes);
-        T* tv = reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes);
-        g1.store(t1, tid);
-        g2.store(t2, tid);
-        gv.store(tv, tid);
-        __syncthreads();
-        if (key + kKeys < end) fetch(key + kKeys);
+        const char* buffer = lds + (i & 1) * Shape::kBufferBytes;
+        const T* t1 = reinterpret_cast<const T*>(buffer);
+        const T* t2 = reinterpret_cast<const T*>(buffer + Shape::kKeyBytes);
+        const T* tv = reinterpret_cast<const T*>(buffer + 2 * Shape::kKeyBytes);
+        copies_done();
+        if (key + kKeys < end) fetch(key + kKeys, lds + ((i + 1) & 1) * Shape::kBufferBytes);
         if (key >= wave_end) continue;
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll

@@ -120,28 +120,25 @@ attn_forward_kernel(AttnArgs a) {
         last[r] = attn_last_key(a, i, length);
     }
 
-    using KeyStage = Stage<T, D, kKeys, Shape::kThreads, WIDE>;
-    using ValueStage = Stage<T, DV, kKeys, Shape::kThreads, WIDE>;
-    const typename KeyStage::Map key_map(a.kt, a.d, tid);
-    const typename ValueStage::Map value_map(a.vt, a.dv, tid);
-    KeyStage g1, g2;
-    ValueStage gv;
-    auto fetch = [&](int key) {
-        g1.load(key_map, k1 + (long long)key * a.kt, a.kt, end - key);
-        g2.load(key_map, k1 + a.km + (long long)key * a.kt, a.kt, end - key);
-        gv.load(value_map, v + (long long)key * a.vt, a.vt, end - key);
+    using KeyCopy = RowCopy<T, D, kKeys, Shape::kThreads, WIDE>;
+    using ValueCopy = RowCopy<T, DV, kKeys, Shape::kThreads, WIDE>;
+    const KeyCopy key_copy(a.kt, a.d, tid);
+    const ValueCopy value_copy(a.vt, a.dv, tid);
+    auto fetch = [&](int key, char* buffer) {
+        key_copy.start(reinterpret_cast<T*>(buffer), k1 + (long long)key * a.kt, a.kt, end - key, tid);
+        key_copy.start(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), k1 + a.km + (long long)key * a.kt, a.kt, end - key,
+                       tid);
+        value_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes), v + (long long)key * a.vt, a.vt, end - key,
+                         tid);
     };
-    if (end > 0) fetch(0);
+    if (end > 0) fetch(0, lds);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
-        char* buffer = lds + (i & 1) * Shape::kBufferBytes;
-        T* tk = reinterpret_cast<T*>(buffer + map * Shape::kKeyBytes);
-        T* tv = reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes);
-        g1.store(reinterpret_cast<T*>(buffer), tid);
-        g2.store(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), tid);
-        gv.store(tv, tid);
-        // (the buffer's readers of two stages ago passed the last barrier)
-        __syncthreads();
-        if (key + kKeys < end) fetch(key + kKeys);
+        const char* buffer = lds + (i & 1) * Shape::kBufferBytes;
+        const T* tk = reinterpret_cast<const T*>(buffer + map * Shape::kKeyBytes);
+        const T* tv = reinterpret_cast<const T*>(buffer + 2 * Shape::kKeyBytes);
+        // this stage is there, and all waves are done with the other buffer
+        copies_done();
+        if (key + kKeys < end) fetch(key + kKeys, lds + ((i + 1) & 1) * Shape::kBufferBytes);
 #pragma unroll
         for (int sub = 0; sub < kKeys; sub += 32) {
             const int key0 = key + sub;
