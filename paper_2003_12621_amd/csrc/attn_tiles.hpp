@@ -102,24 +102,48 @@ struct TileShape {
         if constexpr (kRowChunks == 8) return ((row >> 1) & 3) << 1 | ((row >> 3) & 1);
         return (row & 7) << 1 | ((row >> 3) & 1);
     }
-    static __device__ __forceinline__ int at(int row, int chunk) { return row * W + (chunk ^ swizzle(row)) * kChunk; }
+    static __device__ __forceinline__ unsigned at(int row, int chunk) {
+        return unsigned(row * kRowChunks + (chunk ^ swizzle(row))) * 16;
+    }
 };
+
+// LDS is addressed by byte offset.  Tiles start at multiples of 1024, so what a
+// step changes of a lane's address is an exclusive or with a constant (its
+// chunk) and a constant distance (its row): one register a lane and tile, from
+// the two functions below, serves all of a tile's reads.
+typedef __attribute__((address_space(3))) const char* LdsBytes;
+template <typename V>
+__device__ __forceinline__ V lds_at(unsigned address, int distance) {
+    return *reinterpret_cast<__attribute__((address_space(3))) const V*>(LdsBytes(address) + distance);
+}
+// A lane's part of the address of read_row ...
+template <typename T, int W>
+__device__ __forceinline__ unsigned row_lane(int lane) {
+    return TileShape<T, W>::at(lane & 31, 8 * (lane >> 5) / TileShape<T, W>::kChunk);
+}
+// ... and of read_column.
+template <typename T, int W>
+__device__ __forceinline__ unsigned column_lane(int lane) {
+    using Shape = TileShape<T, W>;
+    if constexpr (sizeof(T) == 4) return Shape::at(4 * (lane >> 5), (lane & 31) / 4) + (lane & 3) * 4;
+    return Shape::at(4 * (lane >> 5) + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + (lane & 1) * 8;
+}
 
 // Operand whose row (or column) lane % 32 is a row of the tile, contracted
 // along the row: elements 16 s + 8 (lane / 32) + e of row row0 + lane % 32.
-// (row0 and col0 below are multiples of 32.)
+// `at`: the tile's address plus row_lane.  (row0 and col0 below are multiples
+// of 32.)
 template <typename T, int W>
-__device__ __forceinline__ Operand<T> read_row(const T* tile, int row0, int s, int lane) {
+__device__ __forceinline__ Operand<T> read_row(unsigned at, int row0, int s) {
     using Shape = TileShape<T, W>;
-    tile += row0 * W;
-    const int row = lane & 31, chunk = (16 * s + 8 * (lane >> 5)) / Shape::kChunk;
+    const int distance = row0 * Shape::kRowChunks * 16;
+    const unsigned chunk = 16 * s / Shape::kChunk;
     Operand<T> o;
     if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4*>(tile + Shape::at(row, chunk));
-        const float4 b = *reinterpret_cast<const float4*>(tile + Shape::at(row, chunk + 1));
-        o.v = floatx8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const floatx4 a = lds_at<floatx4>(at ^ (chunk * 16), distance), b = lds_at<floatx4>(at ^ ((chunk + 1) * 16), distance);
+        o.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-        o.v = *reinterpret_cast<const bf16x8*>(tile + Shape::at(row, chunk));
+        o.v = lds_at<bf16x8>(at ^ (chunk * 16), distance);
     }
     return o;
 }
@@ -127,23 +151,30 @@ __device__ __forceinline__ Operand<T> read_row(const T* tile, int row0, int s, i
 // Operand whose row lane % 32 is column col0 + lane % 32 of the tile,
 // contracted along the tile's rows in the order of an accumulator's registers:
 // element e stands for row row0 + 16 s + 8 (e / 4) + 4 (lane / 32) + e % 4.
+// `at`: the tile's address plus column_lane.
 // bf16: a transposing read takes 4 rows of 16 columns per 16 lanes; lane i of
 // the 16 gives the address of 4 columns of row i / 4 and gets column i.
 template <typename T, int W>
-__device__ __forceinline__ Operand<T> read_column(const T* tile, int row0, int col0, int s, int lane) {
+__device__ __forceinline__ Operand<T> read_column(unsigned at, int row0, int col0, int s) {
     using Shape = TileShape<T, W>;
-    tile += (row0 + 16 * s) * W;
+    constexpr int kRowBytes = Shape::kRowChunks * 16;
+    // what 8 rows further changes of the swizzle
+    constexpr unsigned kEight = Shape::kRowChunks == 4 ? 2 : 1;
+    const int distance = (row0 + 16 * s) * kRowBytes;
+    at ^= unsigned(col0 / Shape::kChunk) * 16;
     Operand<T> o;
     if constexpr (sizeof(T) == 4) {
-        const int chunk = (col0 + (lane & 31)) / 4, row = 4 * (lane >> 5);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o.v[e] = tile[Shape::at(row + 8 * (e >> 2) + (e & 3), chunk) + (lane & 3)];
+        for (int e = 0; e < 8; ++e) {
+            const int j = e & 3, far = e >> 2;
+            const unsigned turned = (Shape::kRowChunks == 8 ? 2 * (j >> 1) : 2 * j) ^ (far * kEight);
+            o.v[e] = lds_at<float>(at ^ (turned * 16), distance + (8 * far + j) * kRowBytes);
+        }
     } else {
-        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3);
-        const int chunk = col0 / 8 + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), part = 4 * (lane & 1);
         typedef __attribute__((address_space(3))) bf16x4* LdsQuad;
-        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(tile + Shape::at(row, chunk) + part));
-        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(tile + Shape::at(row + 8, chunk) + part));
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(LdsBytes(at) + distance));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+            (LdsQuad)(LdsBytes(at ^ (kEight * 16)) + distance + 8 * kRowBytes));
         o.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     return o;
@@ -167,7 +198,7 @@ __device__ __forceinline__ void copies_done() {
 
 // Copies rows from memory into a tile of ROWS rows of W elements, spread over
 // THREADS threads: chunk place i of thread t is place t + i THREADS in row
-// order.  Memory is read through a descriptor of the rows that exist, so rows
+// order.  Tiles are given by their LDS address.  Memory is read through a descriptor of the rows that exist, so rows
 // beyond them become zero and are not touched; so do columns from `cols` on.
 // WIDE: base, stride and cols allow 16-byte accesses, and the copy goes straight
 // into LDS; else elements pass through registers one by one.
@@ -194,7 +225,7 @@ struct RowCopy {
     }
 
     // Starts the copy of `rows` (possibly none or more than ROWS) rows from `base` on.
-    __device__ __forceinline__ void start(T* tile, const T* base, long long stride, int rows, int t) const {
+    __device__ __forceinline__ void start(unsigned tile, const T* base, long long stride, int rows, int t) const {
         const int n = min(rows, ROWS);
         const unsigned bytes = n > 0 ? unsigned(((n - 1) * stride + cols) * int(sizeof(T))) : 0u;
         const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -205,7 +236,7 @@ struct RowCopy {
             rsrc[1] = __builtin_amdgcn_readfirstlane(unsigned(p >> 32) & 0xffffu);
             rsrc[2] = __builtin_amdgcn_readfirstlane(bytes);
             rsrc[3] = 0x00020000u;
-            const unsigned lds = unsigned(reinterpret_cast<uintptr_t>(tile)) + wave * 1024;
+            const unsigned lds = tile + wave * 1024;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
                 if (kWhole || wave * 64 + i * THREADS < kChunks)
@@ -228,7 +259,8 @@ struct RowCopy {
                 }
                 uint4 u;
                 __builtin_memcpy(&u, e, 16);
-                *reinterpret_cast<uint4*>(tile + (t + i * THREADS) * Shape::kChunk) = u;
+                *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(
+                    (__attribute__((address_space(3))) char*)(tile + (t + i * THREADS) * 16)) = __builtin_bit_cast(u32x4, u);
             }
         }
     }

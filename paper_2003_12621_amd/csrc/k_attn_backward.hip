@@ -111,29 +111,27 @@ __global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
 
 namespace {
 
+constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
+
 template <typename T, int D, int DV>
 struct KeySideShape {
     static constexpr int kRows = 32;                                   // queries per stage
     static constexpr int kQueryBytes = TileShape<T, D>::bytes(kRows);
     static constexpr int kGradBytes = TileShape<T, DV>::bytes(kRows);
-    static constexpr int kStatBytes = 4 * kRows * 4;
+    static constexpr int kStatBytes = 1024;                            // 4 values a row; tiles start at multiples of 1024
     static constexpr int kBufferBytes = 2 * kQueryBytes + kGradBytes + kStatBytes;
-    static constexpr int kLds = 2 * kBufferBytes;
+    // The workgroup's keys stay in LDS where two workgroups a compute unit are
+    // aimed at: as operands in registers they would not leave room for that.
+    static constexpr bool kKeysInLds = sizeof(T) * DV <= 256;
+    static constexpr int kBlocks = kKeysInLds ? 2 : 1;
+    static constexpr int kKeyBytes = kKeysInLds ? TileShape<T, D>::bytes(kKeySideKeys) : 0;
+    static constexpr int kLds = 2 * kBufferBytes + 2 * kKeyBytes;
 };
-constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
 
-// Sixteen values of an array in LDS in the order of an accumulator's rows.
-__device__ __forceinline__ floatx16 rows_of(const float* x, int hi) {
-    floatx16 y;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const float4 v = *reinterpret_cast<const float4*>(x + acc_row(4 * g, hi));
-        y[4 * g] = v.x;
-        y[4 * g + 1] = v.y;
-        y[4 * g + 2] = v.z;
-        y[4 * g + 3] = v.w;
-    }
-    return y;
+// Four values of an array in LDS that belong to rows 4 g .. 4 g + 3 of a lane's
+// accumulator registers.
+__device__ __forceinline__ float4 rows_of(const float* x, int g, int hi) {
+    return *reinterpret_cast<const float4*>(x + acc_row(4 * g, hi));
 }
 
 // A transposed accumulator [columns of the row][rows = lanes] to a dense row in memory.
@@ -153,7 +151,7 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 // over the queries of all heads that share it.  Each wave keeps its rows of
 // k1, k2 and v as operands and dk1, dk2, dv as accumulators in registers.
 template <typename T, int D, int DV, bool WIDE, bool DK, bool DVAL>
-__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key_side_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_key_side_kernel(AttnArgs a) {
     using Shape = KeySideShape<T, D, DV>;
     constexpr int kRows = Shape::kRows;
     extern __shared__ __align__(16) char lds[];
@@ -170,11 +168,23 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key
     // every row from here on sees all of the wave's keys
     const int all_from = wave_first + 31 >= length ? 0x7fffffff : (a.causal ? wave_first + 31 - offset : 0);
 
-    Operand<T> k1[D / 16], k2[D / 16], v[DV / 16];
+    constexpr bool kKeysInLds = Shape::kKeysInLds;
+    const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
+    Operand<T> k1[kKeysInLds ? 1 : D / 16], k2[kKeysInLds ? 1 : D / 16], v[DV / 16];
+    unsigned key1 = 0;      // LDS address of this lane's key
     {
-        const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
-        load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
-        load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
+        if constexpr (kKeysInLds) {
+            const unsigned tile1 = base + 2 * Shape::kBufferBytes;
+            const RowCopy<T, D, kKeySideKeys, 256, WIDE> key_copy(a.kt, a.d, tid);
+            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)first * a.kt + hkv * a.kh;
+            key_copy.start(tile1, p, a.kt, length - first, tid);
+            key_copy.start(tile1 + Shape::kKeyBytes, p + a.km, a.kt, length - first, tid);
+            key1 = tile1 + row_lane<T, D>(lane) + wave * TileShape<T, D>::bytes(32);
+        } else {
+            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
+            load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
+            load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
+        }
         if constexpr (DK)
             load_row_operands<T, DV, WIDE>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
                                      a.dv, exists, lane);
@@ -197,14 +207,16 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key
     using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
     const QueryCopy query_copy(a.qt, a.d, tid);
     const GradCopy grad_copy(a.gt, a.dv, tid);
+    const unsigned query_row = row_lane<T, D>(lane), query_column = column_lane<T, D>(lane);
+    const unsigned grad_row = row_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
+    const unsigned grad_column = column_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
     float stat = 0.f;
-    auto fetch = [&](int step, char* buffer) {
-        const int h = hkv * group + step / per_head, row0 = (tile0 + step % per_head) * kRows;
+    auto fetch = [&](int h, int row0, unsigned buffer) {
         const int left = a.sq - row0;
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
-        query_copy.start(reinterpret_cast<T*>(buffer), q, a.qt, left, tid);
-        query_copy.start(reinterpret_cast<T*>(buffer + Shape::kQueryBytes), q + a.qm, a.qt, left, tid);
-        grad_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kQueryBytes),
+        query_copy.start(buffer, q, a.qt, left, tid);
+        query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
+        grad_copy.start(buffer + 2 * Shape::kQueryBytes,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
         if (tid < 4 * kRows) {
             // lse of both maps, then delta of both; rows beyond the last have no terms
@@ -213,40 +225,51 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key
             stat = i < left ? from_mem[row0 + i] : (which < 2 ? kInf : 0.f);
         }
     };
-    if (steps > 0) fetch(0, lds);
+    int h = hkv * group, row0 = tile0 * kRows;
+    if (steps > 0) fetch(h, row0, base);
     for (int step = 0; step < steps; ++step) {
-        char* buffer = lds + (step & 1) * Shape::kBufferBytes;
-        const T* t1 = reinterpret_cast<const T*>(buffer);
-        const T* t2 = reinterpret_cast<const T*>(buffer + Shape::kQueryBytes);
-        const T* tg = reinterpret_cast<const T*>(buffer + 2 * Shape::kQueryBytes);
-        float* ts = reinterpret_cast<float*>(buffer + 2 * Shape::kQueryBytes + Shape::kGradBytes);
+        const unsigned buffer = base + (step & 1) * Shape::kBufferBytes;
+        const unsigned r1 = buffer + query_row, c1 = buffer + query_column;
+        const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
+        const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
+        float* ts = reinterpret_cast<float*>(lds + (step & 1) * Shape::kBufferBytes + 2 * Shape::kQueryBytes + Shape::kGradBytes);
         if (tid < 4 * kRows) ts[tid] = stat;
         copies_done();
-        if (step + 1 < steps) fetch(step + 1, lds + ((step + 1) & 1) * Shape::kBufferBytes);
-        const int row0 = (tile0 + step % per_head) * kRows;
-        const float lam = attn_lambda(a, hkv * group + step / per_head);
+        const int this_row0 = row0;
+        const float lam = attn_lambda(a, h);
+        row0 += kRows;
+        if (row0 >= a.sq) {
+            row0 = tile0 * kRows;
+            ++h;
+        }
+        if (step + 1 < steps) fetch(h, row0, base + ((step + 1) & 1) * Shape::kBufferBytes);
 
         floatx16 p1 = zero16(), p2 = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            mma(p1, read_row<T, D>(t1, 0, s, lane), k1[s]);
-            mma(p2, read_row<T, D>(t2, 0, s, lane), k2[s]);
-        }
-        {
-            const floatx16 l1 = rows_of(ts, hi), l2 = rows_of(ts + kRows, hi);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -l1[r]));
-                p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -l2[r]));
+            if constexpr (kKeysInLds) {
+                mma(p1, read_row<T, D>(r1, 0, s), read_row<T, D>(key1, 0, s));
+                mma(p2, read_row<T, D>(r2, 0, s), read_row<T, D>(key1 + Shape::kKeyBytes, 0, s));
+            } else {
+                mma(p1, read_row<T, D>(r1, 0, s), k1[s]);
+                mma(p2, read_row<T, D>(r2, 0, s), k2[s]);
             }
         }
-        if (row0 < all_from) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 l1 = rows_of(ts, g, hi), l2 = rows_of(ts + kRows, g, hi);
+            const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
+                p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j])) * lam;
+            }
+        }
+        if (this_row0 < all_from) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                if (row0 + acc_row(r, hi) < from) p1[r] = p2[r] = 0.f;
+                if (this_row0 + acc_row(r, hi) < from) p1[r] = p2[r] = 0.f;
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p2[r] *= lam;
         if constexpr (DVAL) {
             floatx16 w;
 #pragma unroll
@@ -255,19 +278,21 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key
             for (int s = 0; s < 2; ++s) {
                 const Operand<T> x = acc_operand<T>(w, s);
 #pragma unroll
-                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(tg, 0, 32 * d, s, lane), x);
+                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(cg, 0, 32 * d, s), x);
             }
         }
         if constexpr (DK) {
             floatx16 t = zero16();
 #pragma unroll
-            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(tg, 0, s, lane), v[s]);
-            {
-                const floatx16 d1 = rows_of(ts + 2 * kRows, hi), d2 = rows_of(ts + 3 * kRows, hi);
+            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rg, 0, s), v[s]);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p1[r] *= t[r] - d1[r];
-                    p2[r] *= d2[r] - t[r];
+            for (int g = 0; g < 4; ++g) {
+                const float4 u1 = rows_of(ts + 2 * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
+                const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    p1[4 * g + j] *= t[4 * g + j] - d1[j];
+                    p2[4 * g + j] *= d2[j] - t[4 * g + j];
                 }
             }
 #pragma unroll
@@ -275,8 +300,8 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_key
                 const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d) {
-                    mma(dk1[d], read_column<T, D>(t1, 0, 32 * d, s, lane), x1);
-                    mma(dk2[d], read_column<T, D>(t2, 0, 32 * d, s, lane), x2);
+                    mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
+                    mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
                 }
             }
         }
@@ -346,30 +371,32 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
     using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
     const KeyCopy key_copy(a.kt, a.d, tid);
     const ValueCopy value_copy(a.vt, a.dv, tid);
-    auto fetch = [&](int key, char* buffer) {
-        key_copy.start(reinterpret_cast<T*>(buffer), kp + (long long)key * a.kt, a.kt, end - key, tid);
-        key_copy.start(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), kp + a.km + (long long)key * a.kt, a.kt, end - key,
+    const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
+    const unsigned key_row = row_lane<T, D>(lane), key_column = column_lane<T, D>(lane);
+    const unsigned value_row = row_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
+    auto fetch = [&](int key, unsigned buffer) {
+        key_copy.start(buffer, kp + (long long)key * a.kt, a.kt, end - key, tid);
+        key_copy.start(buffer + Shape::kKeyBytes, kp + a.km + (long long)key * a.kt, a.kt, end - key,
                        tid);
-        value_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes), vp + (long long)key * a.vt, a.vt, end - key,
+        value_copy.start(buffer + 2 * Shape::kKeyBytes, vp + (long long)key * a.vt, a.vt, end - key,
                          tid);
     };
-    if (end > 0) fetch(0, lds);
+    if (end > 0) fetch(0, base);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
-        const char* buffer = lds + (i & 1) * Shape::kBufferBytes;
-        const T* t1 = reinterpret_cast<const T*>(buffer);
-        const T* t2 = reinterpret_cast<const T*>(buffer + Shape::kKeyBytes);
-        const T* tv = reinterpret_cast<const T*>(buffer + 2 * Shape::kKeyBytes);
+        const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
+        const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
+        const unsigned r2 = r1 + Shape::kKeyBytes, c2 = c1 + Shape::kKeyBytes, rv = buffer + value_row;
         copies_done();
-        if (key + kKeys < end) fetch(key + kKeys, lds + ((i + 1) & 1) * Shape::kBufferBytes);
+        if (key + kKeys < end) fetch(key + kKeys, base + ((i + 1) & 1) * Shape::kBufferBytes);
         if (key >= wave_end) continue;
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            mma(p1, read_row<T, D>(t1, 0, s, lane), q1[s]);
-            mma(p2, read_row<T, D>(t2, 0, s, lane), q2[s]);
+            mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
+            mma(p2, read_row<T, D>(r2, 0, s), q2[s]);
         }
 #pragma unroll
-        for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(tv, 0, s, lane), g[s]);
+        for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rv, 0, s), g[s]);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
@@ -390,8 +417,8 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
             const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
-                mma(dq1[d], read_column<T, D>(t1, 0, 32 * d, s, lane), x1);
-                mma(dq2[d], read_column<T, D>(t2, 0, 32 * d, s, lane), x2);
+                mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
+                mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
             }
         }
     }

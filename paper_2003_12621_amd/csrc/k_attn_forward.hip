@@ -124,21 +124,23 @@ attn_forward_kernel(AttnArgs a) {
     using ValueCopy = RowCopy<T, DV, kKeys, Shape::kThreads, WIDE>;
     const KeyCopy key_copy(a.kt, a.d, tid);
     const ValueCopy value_copy(a.vt, a.dv, tid);
-    auto fetch = [&](int key, char* buffer) {
-        key_copy.start(reinterpret_cast<T*>(buffer), k1 + (long long)key * a.kt, a.kt, end - key, tid);
-        key_copy.start(reinterpret_cast<T*>(buffer + Shape::kKeyBytes), k1 + a.km + (long long)key * a.kt, a.kt, end - key,
+    const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
+    const unsigned key_lane = row_lane<T, D>(lane) + map * Shape::kKeyBytes;
+    const unsigned value_lane = column_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
+    auto fetch = [&](int key, unsigned buffer) {
+        key_copy.start(buffer, k1 + (long long)key * a.kt, a.kt, end - key, tid);
+        key_copy.start(buffer + Shape::kKeyBytes, k1 + a.km + (long long)key * a.kt, a.kt, end - key,
                        tid);
-        value_copy.start(reinterpret_cast<T*>(buffer + 2 * Shape::kKeyBytes), v + (long long)key * a.vt, a.vt, end - key,
+        value_copy.start(buffer + 2 * Shape::kKeyBytes, v + (long long)key * a.vt, a.vt, end - key,
                          tid);
     };
-    if (end > 0) fetch(0, lds);
+    if (end > 0) fetch(0, base);
     for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
-        const char* buffer = lds + (i & 1) * Shape::kBufferBytes;
-        const T* tk = reinterpret_cast<const T*>(buffer + map * Shape::kKeyBytes);
-        const T* tv = reinterpret_cast<const T*>(buffer + 2 * Shape::kKeyBytes);
+        const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
+        const unsigned tk = buffer + key_lane, tv = buffer + value_lane;
         // this stage is there, and all waves are done with the other buffer
         copies_done();
-        if (key + kKeys < end) fetch(key + kKeys, lds + ((i + 1) & 1) * Shape::kBufferBytes);
+        if (key + kKeys < end) fetch(key + kKeys, base + ((i + 1) & 1) * Shape::kBufferBytes);
 #pragma unroll
         for (int sub = 0; sub < kKeys; sub += 32) {
             const int key0 = key + sub;
@@ -148,7 +150,7 @@ attn_forward_kernel(AttnArgs a) {
             for (int r = 0; r < RB; ++r) c[r] = zero16();
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                const Operand<T> x = read_row<T, D>(tk, sub, s, lane);
+                const Operand<T> x = read_row<T, D>(tk, sub, s);
 #pragma unroll
                 for (int r = 0; r < RB; ++r) mma(c[r], x, q[r][s]);
             }
@@ -164,7 +166,7 @@ attn_forward_kernel(AttnArgs a) {
                 for (int r = 0; r < RB; ++r) p[r] = acc_operand<T>(c[r], s);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const Operand<T> x = read_column<T, DV>(tv, sub, 32 * d, s, lane);
+                    const Operand<T> x = read_column<T, DV>(tv, sub, 32 * d, s);
 #pragma unroll
                     for (int r = 0; r < RB; ++r) mma(o[r][d], x, p[r]);
                 }
