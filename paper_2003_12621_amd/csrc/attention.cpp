@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <string>
@@ -54,6 +55,19 @@ size_t output_bytes(const fftsplit_attention_problem_t& p) {
 }
 size_t lse_bytes(const fftsplit_attention_problem_t& p) { return size_t(p.batch) * p.heads_q * 2 * p.queries * 4; }
 
+// How many workgroups share the keys of a tile of the kernel for few rows, or
+// 0 for the kernel that takes 128 rows of one head.
+int choose_splits(const fftsplit_attention_problem_t& p) {
+    const long long rows = (long long)(p.heads_q / p.heads_k) * p.queries;
+    if (const char* e = std::getenv("FFTSPLIT_ATTENTION_SPLITS")) return std::atoi(e);
+    if (rows > kAttnFewRows) return 0;
+    const long long tiles = (long long)p.batch * p.heads_k * ((rows + kAttnFewRows - 1) / kAttnFewRows);
+    long long splits = 512 / tiles, most = (p.keys + 255) / 256;
+    if (splits > most) splits = most;
+    if (splits > 64) splits = 64;
+    return splits < 1 ? 1 : int(splits);
+}
+
 int delta_parts(const fftsplit_attention_problem_t& p) {
     return p.batch * ((p.queries + kAttnDeltaRows - 1) / kAttnDeltaRows);
 }
@@ -96,8 +110,9 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->device = device;
     plan->scale = p.scale > 0.f ? p.scale : float(1.0 / std::sqrt(double(p.dim)));
     plan->shape = shape;
-    plan->splits = 0;
-    plan->forward_ws = 0;
+    plan->splits = choose_splits(p);
+    const size_t parts = size_t(rows) * plan->splits;
+    plan->forward_ws = plan->splits ? round256(parts * 2 * kAttnShapes[shape].dv * 4) + round256(parts * 4 * 4) : 0;
     plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * delta_parts(p) * 4);
     *out = plan;
     return FFTSPLIT_SUCCESS;
@@ -235,6 +250,13 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_
         a.o1 = o1;
         a.o2 = o2;
         a.lse = lse;
+        a.splits = plan->splits;
+        if (plan->splits) {
+            const size_t parts = size_t(a.n) * a.hq * a.sq * plan->splits;
+            a.part = static_cast<float*>(workspace);
+            a.part_stats = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                                    round256(parts * 2 * kAttnShapes[plan->shape].dv * 4));
+        }
         DeviceGuard g(plan->device);
         if (!g.ok()) return fail(FFTSPLIT_ERROR_DEVICE, "cannot select the plan's device");
         return launched_ok(launch_attn_forward(*plan, a, stream, timing_events()), "attention launch");

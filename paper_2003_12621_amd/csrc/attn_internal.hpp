@@ -50,8 +50,8 @@ struct AttnArgs {
     int o_wide;
     // few rows
     int splits;
-    float* part;                     // [tile row][split][2][dv]
-    float* part_stats;               // [tile row][split][4]: max and sum of both maps
+    float* part;                     // [batch][key head][packed row][split][2][padded dv]
+    float* part_stats;               // [batch][key head][packed row][split][4]: maximum and sum of both maps
     // backward
     const void* dout;
     long long gb, gt, gh;            // batch, token, head strides of dout

@@ -196,6 +196,15 @@ __device__ __forceinline__ void copies_done() {
     __syncthreads();
 }
 
+// As above for a tile that only this wave copies and reads: all but the last
+// `later` copies it has started are complete.
+template <int LATER>
+__device__ __forceinline__ void own_copies_done() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
+}
+// This wave's reads of LDS are complete, so that it may copy over what they read.
+__device__ __forceinline__ void own_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Copies rows from memory into a tile of ROWS rows of W elements, spread over
 // THREADS threads: chunk place i of thread t is place t + i THREADS in row
 // order.  Tiles are given by their LDS address.  Memory is read through a descriptor of the rows that exist, so rows
@@ -208,6 +217,7 @@ struct RowCopy {
     static constexpr int kChunks = ROWS * Shape::kRowChunks;
     static constexpr int kPer = (kChunks + THREADS - 1) / THREADS;
     static constexpr bool kWhole = kChunks % THREADS == 0;
+    static constexpr int kCopies = WIDE ? kPer : 0;       // memory operations in flight after start
     static_assert(kChunks % 64 == 0, "whole waves");
 
     // Byte offsets of a thread's chunks from the tile's first row in memory, the
@@ -225,6 +235,7 @@ struct RowCopy {
     }
 
     // Starts the copy of `rows` (possibly none or more than ROWS) rows from `base` on.
+    // (t: the thread's place among the THREADS)
     __device__ __forceinline__ void start(unsigned tile, const T* base, long long stride, int rows, int t) const {
         const int n = min(rows, ROWS);
         const unsigned bytes = n > 0 ? unsigned(((n - 1) * stride + cols) * int(sizeof(T))) : 0u;

@@ -218,6 +218,231 @@ attn_forward_kernel(AttnArgs a) {
     }
 }
 
+// ---- few rows: single tokens over a long cache ----
+//
+// Bound by reading k and v once.  The rows of all heads that share a key head
+// are packed into tiles of 32, and the keys of a tile are shared by several
+// workgroups, whose partial results a second kernel joins.  Within a
+// workgroup every wave goes over key blocks of its own, copied into LDS of its
+// own, so nothing waits at a barrier; the waves are joined at the end.  The
+// matrix instructions have time to spare, so the terms of the softmax enter as
+// two bf16 numbers (the rounded term and what that left out).
+
+namespace {
+
+template <typename T, int D, int DV>
+struct FewShape {
+    static constexpr int kKeys = 32;
+    static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
+    static constexpr int kStageBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
+    // the next stage on its way while one is worked on, in at most 128 KB
+    static constexpr int kBuffers = kStageBytes <= 32768 ? 2 : 1;
+    static constexpr int kWaves = kStageBytes <= 16384 ? 4 : 2;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kJoinBytes = 2 * (DV / 32) * 16 * 64 * 4;      // a wave's outputs
+    static constexpr int kStatBytes = kWaves * 2 * 2 * 32 * 4;
+    static constexpr int kTileBytes = kBuffers * kStageBytes > kJoinBytes ? kBuffers * kStageBytes : kJoinBytes;
+    static constexpr int kLds = kWaves * kTileBytes + kStatBytes;
+};
+
+// The rounding error of an operand's elements, as an operand.
+__device__ __forceinline__ Operand<__bf16> rest_operand(const floatx16& c, const Operand<__bf16>& rounded, int s) {
+    floatx16 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = c[8 * s + e] - float(rounded.v[e]);
+    return acc_operand<__bf16>(r, 0);
+}
+
+}  // namespace
+
+template <typename T, int D, int DV, bool WIDE>
+__global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_kernel(AttnArgs a) {
+    using Shape = FewShape<T, D, DV>;
+    constexpr int kWaves = Shape::kWaves, DT = DV / 32;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = a.hq / a.hk, rows = group * a.sq, tiles = (rows + kAttnFewRows - 1) / kAttnFewRows;
+    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
+    // (the tiles of one key head and share of the keys next to one another)
+    const int tile = id % tiles, split = id / tiles % a.splits, hkv = id / tiles / a.splits % a.hk;
+    const int b = id / tiles / a.splits / a.hk;
+    const int length = attn_length(a, b);
+    const int packed = tile * kAttnFewRows + (lane & 31);
+    const bool valid = packed < rows;
+    const int head = hkv * group + (valid ? packed / a.sq : 0), i = valid ? packed % a.sq : 0;
+    const int last = valid ? attn_last_key(a, i, length) : -1;
+    // this workgroup's keys: a whole number of blocks for each wave
+    constexpr int kStep = Shape::kKeys * kWaves;
+    const int share = ((length + a.splits - 1) / a.splits + kStep - 1) / kStep * kStep;
+    const int begin = min(split * (long long)share, (long long)length), end = min(begin + share, length);
+
+    const T* k1 = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
+    const T* v = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
+    Operand<T> q1[D / 16], q2[D / 16];
+    {
+        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + head * a.qh;
+        load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
+        load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
+    }
+    floatx16 o1[DT], o2[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o1[d] = o2[d] = zero16();
+    RowState s1{-kInf, 0.f}, s2{-kInf, 0.f};
+
+    using KeyCopy = RowCopy<T, D, Shape::kKeys, 64, WIDE>;
+    using ValueCopy = RowCopy<T, DV, Shape::kKeys, 64, WIDE>;
+    const KeyCopy key_copy(a.kt, a.d, lane);
+    const ValueCopy value_copy(a.vt, a.dv, lane);
+    constexpr int kCopies = 2 * KeyCopy::kCopies + ValueCopy::kCopies;
+    const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds)) + wave * Shape::kTileBytes;
+    const unsigned key_lane = row_lane<T, D>(lane), value_lane = column_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
+    auto fetch = [&](int key, unsigned buffer) {
+        key_copy.start(buffer, k1 + (long long)key * a.kt, a.kt, end - key, lane);
+        key_copy.start(buffer + Shape::kKeyBytes, k1 + a.km + (long long)key * a.kt, a.kt, end - key, lane);
+        value_copy.start(buffer + 2 * Shape::kKeyBytes, v + (long long)key * a.vt, a.vt, end - key, lane);
+    };
+    int key = begin + wave * Shape::kKeys;
+    if (Shape::kBuffers == 2 && key < end) fetch(key, base);
+    for (int n = 0; key < end; ++n, key += kStep) {
+        unsigned buffer = base;
+        own_reads_done();
+        if constexpr (Shape::kBuffers == 2) {
+            buffer += (n & 1) * Shape::kStageBytes;
+            if (key + kStep < end) {
+                fetch(key + kStep, base + ((n + 1) & 1) * Shape::kStageBytes);
+                own_copies_done<kCopies>();
+            } else {
+                own_copies_done<0>();
+            }
+        } else {
+            fetch(key, buffer);
+            own_copies_done<0>();
+        }
+        const unsigned r1 = buffer + key_lane, r2 = r1 + Shape::kKeyBytes, tv = buffer + value_lane;
+        floatx16 c1 = zero16(), c2 = zero16();
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            mma(c1, read_row<T, D>(r1, 0, s), q1[s]);
+            mma(c2, read_row<T, D>(r2, 0, s), q2[s]);
+        }
+        mask_scores(c1, key, last, hi);
+        mask_scores(c2, key, last, hi);
+        softmax_step(c1, s1, o1, a.scale_log2);
+        softmax_step(c2, s2, o2, a.scale_log2);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const Operand<T> p1 = acc_operand<T>(c1, s), p2 = acc_operand<T>(c2, s);
+            Operand<T> e1, e2;
+            if constexpr (sizeof(T) == 2) {
+                e1 = rest_operand(c1, p1, s);
+                e2 = rest_operand(c2, p2, s);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const Operand<T> x = read_column<T, DV>(tv, 0, 32 * d, s);
+                mma(o1[d], x, p1);
+                mma(o2[d], x, p2);
+                if constexpr (sizeof(T) == 2) {
+                    mma(o1[d], x, e1);
+                    mma(o2[d], x, e2);
+                }
+            }
+        }
+    }
+
+    // join the waves: outputs relative to the largest maximum, added up through LDS
+    float* stats = reinterpret_cast<float*>(lds + kWaves * Shape::kTileBytes);   // [wave][map][max, sum][32]
+    const float2 h1 = both_halves(s1.l), h2 = both_halves(s2.l);
+    if (hi == 0) {
+        float* x = stats + wave * 128 + lane;
+        x[0] = s1.m;
+        x[32] = h1.x + h1.y;
+        x[64] = s2.m;
+        x[96] = h2.x + h2.y;
+    }
+    __syncthreads();
+    float top[2] = {-kInf, -kInf}, sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top[m] = fmaxf(top[m], stats[w * 128 + m * 64 + (lane & 31)]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = stats[w * 128 + m * 64 + (lane & 31)];
+            sum[m] += mw == -kInf ? 0.f : exp2_fast(mw - top[m]) * stats[w * 128 + m * 64 + 32 + (lane & 31)];
+        }
+    }
+    const float f1 = s1.m == -kInf ? 0.f : exp2_fast(s1.m - top[0]), f2 = s2.m == -kInf ? 0.f : exp2_fast(s2.m - top[1]);
+    {
+        float4* own = reinterpret_cast<float4*>(lds + wave * Shape::kTileBytes) + lane;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                own[(d * 4 + g) * 64] = make_float4(o1[d][4 * g] * f1, o1[d][4 * g + 1] * f1, o1[d][4 * g + 2] * f1,
+                                                    o1[d][4 * g + 3] * f1);
+                own[((DT + d) * 4 + g) * 64] = make_float4(o2[d][4 * g] * f2, o2[d][4 * g + 1] * f2, o2[d][4 * g + 2] * f2,
+                                                           o2[d][4 * g + 3] * f2);
+            }
+    }
+    __syncthreads();
+    if (!valid) return;
+    const size_t at = ((size_t(b) * a.hk + hkv) * rows + packed) * a.splits + split;
+    if (wave == 0 && hi == 0)
+        *reinterpret_cast<float4*>(a.part_stats + at * 4) = make_float4(top[0], sum[0], top[1], sum[1]);
+    for (int e = wave; e < 2 * DT * 4; e += kWaves) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float4 x = reinterpret_cast<const float4*>(lds + w * Shape::kTileBytes)[e * 64 + lane];
+            t = make_float4(t.x + x.x, t.y + x.y, t.z + x.z, t.w + x.w);
+        }
+        const int m = e / (DT * 4), d = e / 4 % DT, g = e % 4;
+        *reinterpret_cast<float4*>(a.part + (at * 2 + m) * DV + 32 * d + acc_row(4 * g, hi)) = t;
+    }
+}
+
+// Joins the workgroups that shared a row's keys: 128 threads a row, 64 a map, 4
+// columns each.
+template <typename T, int DV>
+__global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
+    __shared__ float4 second[64];
+    const int map = threadIdx.x >> 6, col = 4 * (threadIdx.x & 63);
+    const int group = a.hq / a.hk, rows = group * a.sq;
+    const int packed = blockIdx.x % rows, kv = blockIdx.x / rows, b = kv / a.hk, h = kv % a.hk * group + packed / a.sq;
+    const int i = packed % a.sq;
+    const float4* stats = reinterpret_cast<const float4*>(a.part_stats) + size_t(blockIdx.x) * a.splits;
+    float top = -kInf;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, map ? stats[s].z : stats[s].x);
+    float sum = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < a.splits; ++s) {
+        const float4 st = stats[s];
+        const float m = map ? st.z : st.x, l = map ? st.w : st.y;
+        if (m == -kInf) continue;
+        const float f = exp2_fast(m - top);
+        sum = fmaf(l, f, sum);
+        if (col < DV) {
+            const float4 x = *reinterpret_cast<const float4*>(a.part + ((size_t(blockIdx.x) * a.splits + s) * 2 + map) * DV + col);
+            y = make_float4(fmaf(x.x, f, y.x), fmaf(x.y, f, y.y), fmaf(x.z, f, y.z), fmaf(x.w, f, y.w));
+        }
+    }
+    const bool none = attn_last_key(a, i, attn_length(a, b)) < 0;
+    const float inv = none ? 0.f : 1.f / sum;
+    y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+    const size_t at = ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
+    if (a.o1) store4(static_cast<T*>(map ? a.o2 : a.o1) + at, col, a.dv, a.o_wide, y.x, y.y, y.z, y.w);
+    if (a.lse && col == 0)
+        a.lse[((size_t(b) * a.hq + h) * 2 + map) * a.sq + i] = none ? 0.f : top + log2f(sum);
+    if (map) second[threadIdx.x & 63] = y;
+    __syncthreads();
+    if (map) return;
+    const float4 z = second[threadIdx.x];
+    const float lam = attn_lambda(a, h);
+    store4(static_cast<T*>(a.o) + at, col, a.dv, a.o_wide, y.x - lam * z.x, y.y - lam * z.y, y.z - lam * z.z,
+           y.w - lam * z.w);
+}
+
 namespace {
 template <typename T, int D, int DV>
 hipError_t launch_tiled(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
@@ -229,12 +454,31 @@ hipError_t launch_tiled(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev
                          ev.stop, a);
 }
 
+template <typename T, int D, int DV>
+hipError_t launch_few_rows(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    using Shape = FewShape<T, D, DV>;
+    const long long rows = (long long)(a.hq / a.hk) * a.sq, heads = (long long)a.n * a.hk;
+    const long long blocks = heads * ((rows + kAttnFewRows - 1) / kAttnFewRows) * a.splits;
+    auto kernel = a.wide ? attn_few_rows_kernel<T, D, DV, true> : attn_few_rows_kernel<T, D, DV, false>;
+    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
+    if (hipError_t e = launch_kernel(kernel, dim3(unsigned(blocks)), dim3(Shape::kThreads), Shape::kLds, s, ev.start,
+                                     nullptr, a))
+        return e;
+    return launch_kernel(attn_few_rows_join_kernel<T, DV>, dim3(unsigned(heads * rows)), dim3(128), 0, s, nullptr, ev.stop,
+                         a);
+}
+
+template <typename T, int D, int DV>
+hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    return a.splits ? launch_few_rows<T, D, DV>(a, s, ev) : launch_tiled<T, D, DV>(a, s, ev);
+}
+
 template <typename T>
 hipError_t launch_typed(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
     switch (p.shape) {
-        case 0: return launch_tiled<T, 32, 64>(a, s, ev);
-        case 1: return launch_tiled<T, 64, 128>(a, s, ev);
-        default: return launch_tiled<T, 128, 256>(a, s, ev);
+        case 0: return launch_shaped<T, 32, 64>(a, s, ev);
+        case 1: return launch_shaped<T, 64, 128>(a, s, ev);
+        default: return launch_shaped<T, 128, 256>(a, s, ev);
     }
 }
 }  // namespace
