@@ -2,7 +2,6 @@
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
-#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <string>
@@ -57,15 +56,26 @@ size_t lse_bytes(const fftsplit_attention_problem_t& p) { return size_t(p.batch)
 
 // How many workgroups share the keys of a tile of the kernel for few rows, or
 // 0 for the kernel that takes 128 rows of one head.
+//
+// A workgroup of either works on 128 x 32 or 32 x 128 scores of each map a step.
+// The kernel for few rows pays a second launch but can use the whole chip for a
+// handful of rows: one workgroup a compute unit, with 256 keys at least.
+// Measured in us, without / with: 1 token over 8192 keys, 4 key heads 277 / 25;
+// 64 rows over 1024 keys, 32 heads 40 / 21; 128 rows over 4096 keys, 4 heads
+// 135 / 22; 200 rows over 200 keys, 16 heads 15 / 17.
 int choose_splits(const fftsplit_attention_problem_t& p) {
-    const long long rows = (long long)(p.heads_q / p.heads_k) * p.queries;
-    if (const char* e = std::getenv("FFTSPLIT_ATTENTION_SPLITS")) return std::atoi(e);
-    if (rows > kAttnFewRows) return 0;
-    const long long tiles = (long long)p.batch * p.heads_k * ((rows + kAttnFewRows - 1) / kAttnFewRows);
-    long long splits = 512 / tiles, most = (p.keys + 255) / 256;
-    if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
-    return splits < 1 ? 1 : int(splits);
+    const long long group = p.heads_q / p.heads_k, heads = (long long)p.batch * p.heads_k;
+    const long long tiled = heads * group * ((p.queries + kAttnRows - 1) / kAttnRows);
+    const long long few = heads * ((group * p.queries + kAttnFewRows - 1) / kAttnFewRows);
+    if (tiled > 256) return 0;
+    long long splits = 256 / few, most = (p.keys + 255LL) / 256;
+    splits = splits > most ? most : splits;
+    splits = splits > 32 ? 32 : splits;
+    splits = splits < 1 ? 1 : splits;
+    // times in us, of steps and of launches
+    const double tiled_time = 3 + 1.05 * ((p.keys + 31) / 32);
+    const double few_time = 8 + 1.5 * double((few * splits + 255) / 256) * double((p.keys + 128 * splits - 1) / (128 * splits));
+    return few_time < tiled_time ? int(splits) : 0;
 }
 
 int delta_parts(const fftsplit_attention_problem_t& p) {

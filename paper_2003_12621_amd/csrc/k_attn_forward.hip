@@ -233,14 +233,18 @@ namespace {
 template <typename T, int D, int DV>
 struct FewShape {
     static constexpr int kKeys = 32;
+    // Maps a wave takes: both, or one where the outputs of both would take 256
+    // registers (the two waves of a block then each copy its values).
+    static constexpr int kMaps = DV <= 128 ? 2 : 1;
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
-    static constexpr int kStageBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
+    static constexpr int kStageBytes = kMaps * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
     // the next stage on its way while one is worked on, in at most 128 KB
-    static constexpr int kBuffers = kStageBytes <= 32768 ? 2 : 1;
-    static constexpr int kWaves = kStageBytes <= 16384 ? 4 : 2;
+    static constexpr int kBuffers = kStageBytes <= 16384 || kMaps == 2 ? 2 : 1;
+    static constexpr int kWaves = kStageBytes <= (kMaps == 2 ? 16384 : 24576) ? 4 : 2;
+    static constexpr int kKeyWaves = kWaves * kMaps / 2;                // key blocks worked on at a time
     static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kJoinBytes = 2 * (DV / 32) * 16 * 64 * 4;      // a wave's outputs
-    static constexpr int kStatBytes = kWaves * 2 * 2 * 32 * 4;
+    static constexpr int kJoinBytes = kMaps * (DV / 32) * 16 * 64 * 4;  // a wave's outputs
+    static constexpr int kStatBytes = kKeyWaves * 2 * 2 * 32 * 4;
     static constexpr int kTileBytes = kBuffers * kStageBytes > kJoinBytes ? kBuffers * kStageBytes : kJoinBytes;
     static constexpr int kLds = kWaves * kTileBytes + kStatBytes;
 };
@@ -258,9 +262,10 @@ __device__ __forceinline__ Operand<__bf16> rest_operand(const floatx16& c, const
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_kernel(AttnArgs a) {
     using Shape = FewShape<T, D, DV>;
-    constexpr int kWaves = Shape::kWaves, DT = DV / 32;
+    constexpr int kWaves = Shape::kWaves, kKeyWaves = Shape::kKeyWaves, MAPS = Shape::kMaps, DT = DV / 32;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int key_wave = MAPS == 2 ? wave : wave >> 1, map0 = MAPS == 2 ? 0 : wave & 1;
     const int group = a.hq / a.hk, rows = group * a.sq, tiles = (rows + kAttnFewRows - 1) / kAttnFewRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     // (the tiles of one key head and share of the keys next to one another)
@@ -272,36 +277,39 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
     const int head = hkv * group + (valid ? packed / a.sq : 0), i = valid ? packed % a.sq : 0;
     const int last = valid ? attn_last_key(a, i, length) : -1;
     // this workgroup's keys: a whole number of blocks for each wave
-    constexpr int kStep = Shape::kKeys * kWaves;
+    constexpr int kStep = Shape::kKeys * kKeyWaves;
     const int share = ((length + a.splits - 1) / a.splits + kStep - 1) / kStep * kStep;
-    const int begin = min(split * (long long)share, (long long)length), end = min(begin + share, length);
+    const int begin = int(min(split * (long long)share, (long long)length)), end = min(begin + share, length);
 
-    const T* k1 = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
+    const T* k = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh + map0 * a.km;
     const T* v = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
-    Operand<T> q1[D / 16], q2[D / 16];
-    {
-        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + head * a.qh;
-        load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
-        load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
-    }
-    floatx16 o1[DT], o2[DT];
+    Operand<T> q[MAPS][D / 16];
+    floatx16 o[MAPS][DT];
+    RowState st[MAPS];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o1[d] = o2[d] = zero16();
-    RowState s1{-kInf, 0.f}, s2{-kInf, 0.f};
+    for (int m = 0; m < MAPS; ++m) {
+        load_row_operands<T, D, WIDE>(
+            q[m], static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + head * a.qh + (map0 + m) * a.qm, a.d, valid,
+            lane);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[m][d] = zero16();
+        st[m] = RowState{-kInf, 0.f};
+    }
 
     using KeyCopy = RowCopy<T, D, Shape::kKeys, 64, WIDE>;
     using ValueCopy = RowCopy<T, DV, Shape::kKeys, 64, WIDE>;
     const KeyCopy key_copy(a.kt, a.d, lane);
     const ValueCopy value_copy(a.vt, a.dv, lane);
-    constexpr int kCopies = 2 * KeyCopy::kCopies + ValueCopy::kCopies;
+    constexpr int kCopies = MAPS * KeyCopy::kCopies + ValueCopy::kCopies;
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds)) + wave * Shape::kTileBytes;
-    const unsigned key_lane = row_lane<T, D>(lane), value_lane = column_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
+    const unsigned key_lane = row_lane<T, D>(lane), value_lane = column_lane<T, DV>(lane) + MAPS * Shape::kKeyBytes;
     auto fetch = [&](int key, unsigned buffer) {
-        key_copy.start(buffer, k1 + (long long)key * a.kt, a.kt, end - key, lane);
-        key_copy.start(buffer + Shape::kKeyBytes, k1 + a.km + (long long)key * a.kt, a.kt, end - key, lane);
-        value_copy.start(buffer + 2 * Shape::kKeyBytes, v + (long long)key * a.vt, a.vt, end - key, lane);
+#pragma unroll
+        for (int m = 0; m < MAPS; ++m)
+            key_copy.start(buffer + m * Shape::kKeyBytes, k + m * a.km + (long long)key * a.kt, a.kt, end - key, lane);
+        value_copy.start(buffer + MAPS * Shape::kKeyBytes, v + (long long)key * a.vt, a.vt, end - key, lane);
     };
-    int key = begin + wave * Shape::kKeys;
+    int key = begin + key_wave * Shape::kKeys;
     if (Shape::kBuffers == 2 && key < end) fetch(key, base);
     for (int n = 0; key < end; ++n, key += kStep) {
         unsigned buffer = base;
@@ -318,72 +326,73 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
             fetch(key, buffer);
             own_copies_done<0>();
         }
-        const unsigned r1 = buffer + key_lane, r2 = r1 + Shape::kKeyBytes, tv = buffer + value_lane;
-        floatx16 c1 = zero16(), c2 = zero16();
+        const unsigned tk = buffer + key_lane, tv = buffer + value_lane;
+        floatx16 c[MAPS];
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            mma(c1, read_row<T, D>(r1, 0, s), q1[s]);
-            mma(c2, read_row<T, D>(r2, 0, s), q2[s]);
+        for (int m = 0; m < MAPS; ++m) c[m] = zero16();
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int m = 0; m < MAPS; ++m) mma(c[m], read_row<T, D>(tk + m * Shape::kKeyBytes, 0, s), q[m][s]);
+#pragma unroll
+        for (int m = 0; m < MAPS; ++m) {
+            mask_scores(c[m], key, last, hi);
+            softmax_step(c[m], st[m], o[m], a.scale_log2);
         }
-        mask_scores(c1, key, last, hi);
-        mask_scores(c2, key, last, hi);
-        softmax_step(c1, s1, o1, a.scale_log2);
-        softmax_step(c2, s2, o2, a.scale_log2);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const Operand<T> p1 = acc_operand<T>(c1, s), p2 = acc_operand<T>(c2, s);
-            Operand<T> e1, e2;
-            if constexpr (sizeof(T) == 2) {
-                e1 = rest_operand(c1, p1, s);
-                e2 = rest_operand(c2, p2, s);
+            Operand<T> p[MAPS], e[MAPS];
+#pragma unroll
+            for (int m = 0; m < MAPS; ++m) {
+                p[m] = acc_operand<T>(c[m], s);
+                if constexpr (sizeof(T) == 2) e[m] = rest_operand(c[m], p[m], s);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const Operand<T> x = read_column<T, DV>(tv, 0, 32 * d, s);
-                mma(o1[d], x, p1);
-                mma(o2[d], x, p2);
-                if constexpr (sizeof(T) == 2) {
-                    mma(o1[d], x, e1);
-                    mma(o2[d], x, e2);
+#pragma unroll
+                for (int m = 0; m < MAPS; ++m) {
+                    mma(o[m][d], x, p[m]);
+                    if constexpr (sizeof(T) == 2) mma(o[m][d], x, e[m]);
                 }
             }
         }
     }
 
     // join the waves: outputs relative to the largest maximum, added up through LDS
-    float* stats = reinterpret_cast<float*>(lds + kWaves * Shape::kTileBytes);   // [wave][map][max, sum][32]
-    const float2 h1 = both_halves(s1.l), h2 = both_halves(s2.l);
-    if (hi == 0) {
-        float* x = stats + wave * 128 + lane;
-        x[0] = s1.m;
-        x[32] = h1.x + h1.y;
-        x[64] = s2.m;
-        x[96] = h2.x + h2.y;
+    float* stats = reinterpret_cast<float*>(lds + kWaves * Shape::kTileBytes);   // [key wave][map][maximum, sum][32]
+#pragma unroll
+    for (int m = 0; m < MAPS; ++m) {
+        const float2 halves = both_halves(st[m].l);
+        if (hi == 0) {
+            float* x = stats + (key_wave * 2 + map0 + m) * 64 + lane;
+            x[0] = st[m].m;
+            x[32] = halves.x + halves.y;
+        }
     }
     __syncthreads();
     float top[2] = {-kInf, -kInf}, sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
+        const float* x = stats + m * 64 + (lane & 31);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top[m] = fmaxf(top[m], stats[w * 128 + m * 64 + (lane & 31)]);
+        for (int w = 0; w < kKeyWaves; ++w) top[m] = fmaxf(top[m], x[w * 128]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = stats[w * 128 + m * 64 + (lane & 31)];
-            sum[m] += mw == -kInf ? 0.f : exp2_fast(mw - top[m]) * stats[w * 128 + m * 64 + 32 + (lane & 31)];
-        }
+        for (int w = 0; w < kKeyWaves; ++w)
+            sum[m] += x[w * 128] == -kInf ? 0.f : exp2_fast(x[w * 128] - top[m]) * x[w * 128 + 32];
     }
-    const float f1 = s1.m == -kInf ? 0.f : exp2_fast(s1.m - top[0]), f2 = s2.m == -kInf ? 0.f : exp2_fast(s2.m - top[1]);
     {
         float4* own = reinterpret_cast<float4*>(lds + wave * Shape::kTileBytes) + lane;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int m = 0; m < MAPS; ++m) {
+            const float f = st[m].m == -kInf ? 0.f : exp2_fast(st[m].m - (map0 + m ? top[1] : top[0]));
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                own[(d * 4 + g) * 64] = make_float4(o1[d][4 * g] * f1, o1[d][4 * g + 1] * f1, o1[d][4 * g + 2] * f1,
-                                                    o1[d][4 * g + 3] * f1);
-                own[((DT + d) * 4 + g) * 64] = make_float4(o2[d][4 * g] * f2, o2[d][4 * g + 1] * f2, o2[d][4 * g + 2] * f2,
-                                                           o2[d][4 * g + 3] * f2);
-            }
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    own[((m * DT + d) * 4 + g) * 64] = make_float4(o[m][d][4 * g] * f, o[m][d][4 * g + 1] * f,
+                                                                   o[m][d][4 * g + 2] * f, o[m][d][4 * g + 3] * f);
+        }
     }
     __syncthreads();
     if (!valid) return;
@@ -391,13 +400,14 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
     if (wave == 0 && hi == 0)
         *reinterpret_cast<float4*>(a.part_stats + at * 4) = make_float4(top[0], sum[0], top[1], sum[1]);
     for (int e = wave; e < 2 * DT * 4; e += kWaves) {
+        const int m = e / (DT * 4), d = e / 4 % DT, g = e % 4;
         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float4 x = reinterpret_cast<const float4*>(lds + w * Shape::kTileBytes)[e * 64 + lane];
+        for (int w = 0; w < kKeyWaves; ++w) {
+            const char* from = lds + (MAPS == 2 ? w : 2 * w + m) * Shape::kTileBytes;
+            const float4 x = reinterpret_cast<const float4*>(from)[(MAPS == 2 ? e : e % (DT * 4)) * 64 + lane];
             t = make_float4(t.x + x.x, t.y + x.y, t.z + x.z, t.w + x.w);
         }
-        const int m = e / (DT * 4), d = e / 4 % DT, g = e % 4;
         *reinterpret_cast<float4*>(a.part + (at * 2 + m) * DV + 32 * d + acc_row(4 * g, hi)) = t;
     }
 }
