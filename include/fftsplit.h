@@ -441,7 +441,7 @@ enum {
     FFTSPLIT_CHANNELS_FIRST = 1    /* [batch][channels][positions]: a feature map */
 };
 typedef struct {
-    int batch, positions, channels;   /* channels at most 8192, with x channels first 2048 */
+    int batch, positions, channels;   /* at most 8192 channels; with x channels first 2048, and 2^22 positions */
     int x_dtype, y_dtype;             /* fftsplit_dtype_t; both the same, or fp32 to bf16 */
     int x_layout, y_layout;           /* both the same, or a feature map to tokens */
     float eps;

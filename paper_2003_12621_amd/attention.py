@@ -10,6 +10,7 @@ in the HIP kernels behind fftsplit.h.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional
 
 import paper_2003_12621_amd as _fs
@@ -239,20 +240,26 @@ def _launch(device, name, *args):
             _fs._check(fn(*args, _fs._stream_handle(device)), name)
 
 
-def _norm_desc(x, layout, out_layout, out_dtype, eps):
+@functools.lru_cache(maxsize=256)
+def _norm_desc(shape, dtype, layout, out_layout, out_dtype, eps):
+    """The description of a call, the output's shape and the bytes of the
+    backward pass's workspace, which depend on shapes and types alone."""
     out_layout = layout if out_layout is None else out_layout
     if layout not in _LAYOUTS or out_layout not in _LAYOUTS:
         raise ValueError("layout must be 'last' or 'first'")
-    if x.dim() < 2:
+    if len(shape) < 2:
         raise ValueError("layer_norm needs at least two dimensions")
     if layout == "first":
-        n, c, s = x.shape[0], x.shape[1], _fs._prod(x.shape[2:])
-        shape = tuple(x.shape) if out_layout == "first" else (n, s, c)
+        n, c, s = shape[0], shape[1], _fs._prod(shape[2:])
+        out_shape = tuple(shape) if out_layout == "first" else (n, s, c)
     else:
-        n, s, c = 1, _fs._prod(x.shape[:-1]), x.shape[-1]
-        shape = tuple(x.shape)
-    return LayerNorm(n, s, c, _type_code(x.dtype), _type_code(out_dtype), _LAYOUTS[layout], _LAYOUTS[out_layout],
-                     eps), shape
+        n, s, c = 1, _fs._prod(shape[:-1]), shape[-1]
+        out_shape = tuple(shape)
+    desc = LayerNorm(n, s, c, _type_code(dtype), _type_code(out_dtype), _LAYOUTS[layout], _LAYOUTS[out_layout], eps)
+    need = ctypes.c_size_t()
+    _fs._check(_fs.lib().fftsplit_layer_norm_workspace(ctypes.byref(desc), ctypes.byref(need)),
+               "fftsplit_layer_norm_workspace")
+    return desc, out_shape, _fs._prod(out_shape), need.value
 
 
 def _param(t, name, c, device):
@@ -268,11 +275,11 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, layout="last", out_layout=No
     position) for layer_norm_backward."""
     torch, dev = _fs._torch(), _device_of(x, "x")
     out_dtype = x.dtype if out_dtype is None else out_dtype
-    desc, shape = _norm_desc(x, layout, out_layout, out_dtype, eps)
+    desc, shape, numel, _ = _norm_desc(x.shape, x.dtype, layout, out_layout, out_dtype, eps)
     xp = _dense(x, "x", None, None, dev)
     wp, bp = _param(weight, "weight", desc.channels, dev), _param(bias, "bias", desc.channels, dev)
     y = torch.empty(shape, dtype=out_dtype, device=dev) if out is None else out
-    yp = _dense(y, "out", out_dtype, _fs._prod(shape), dev)
+    yp = _dense(y, "out", out_dtype, numel, dev)
     mean = rstd = None
     if return_stats:
         mean, rstd = torch.empty((2, desc.batch * desc.positions), dtype=torch.float32, device=dev)
@@ -286,16 +293,13 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, layout="last", out_layou
     parameters' gradients are fp32."""
     torch, dev = _fs._torch(), _device_of(x, "x")
     _device_of(dy, "dy")
-    desc, shape = _norm_desc(x, layout, out_layout, dy.dtype, 0.0)
+    desc, _, numel, need = _norm_desc(x.shape, x.dtype, layout, out_layout, dy.dtype, 0.0)
     rows = desc.batch * desc.positions
-    gp = _dense(dy, "dy", dy.dtype, _fs._prod(shape), dev)
+    gp = _dense(dy, "dy", dy.dtype, numel, dev)
     xp = _dense(x, "x", None, None, dev)
     mp, rp = _dense(mean, "mean", torch.float32, rows, dev), _dense(rstd, "rstd", torch.float32, rows, dev)
     wp = _param(weight, "weight", desc.channels, dev)
-    need = ctypes.c_size_t()
-    _fs._check(_fs.lib().fftsplit_layer_norm_workspace(ctypes.byref(desc), ctypes.byref(need)),
-               "fftsplit_layer_norm_workspace")
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if workspace is None else workspace
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
     dx = torch.empty_like(x)
     dweight, dbias = torch.empty((2, desc.channels), dtype=torch.float32, device=dev)
     _launch(dev, "fftsplit_layer_norm_backward", ctypes.byref(desc), gp, xp, mp, rp, wp, dx.data_ptr(),
@@ -304,14 +308,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, layout="last", out_layou
     return dx, dweight, dbias
 
 
-def _heads_view(t, name):
+def _heads_view(shape, strides, name):
     """[batch, tokens, heads, dim] strides of a [batch, tokens, ..., dim] tensor."""
-    if t.dim() < 4:
-        raise ValueError(f"{name} must be [batch, tokens, heads, dim], heads possibly in several dimensions")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if shape[-1] > 1 and strides[-1] != 1:
         raise ValueError(f"{name} must be dense in its last dimension")
     heads, stride = 1, 0
-    for size, st in zip(reversed(t.shape[2:-1]), reversed(t.stride()[2:-1])):
+    for size, st in zip(reversed(shape[2:-1]), reversed(strides[2:-1])):
         if size == 1:
             continue
         if heads == 1:
@@ -319,7 +321,33 @@ def _heads_view(t, name):
         elif st != stride * heads:
             raise ValueError(f"{name}: its head dimensions do not form one")
         heads *= size
-    return heads, (ctypes.c_longlong * 3)(t.stride(0), t.stride(1), stride)
+    return heads, (ctypes.c_longlong * 3)(strides[0], strides[1], stride)
+
+
+@functools.lru_cache(maxsize=256)
+def _rotary_desc(shape, other_shape, strides, dtype, pos_shape, sections, interleaved, inverse):
+    """The description and strides of a call, which depend on shapes alone.
+    `strides`: of x, its output, other, its output (None without other)."""
+    if len(shape) < 4:
+        raise ValueError("x must be [batch, tokens, heads, dim], heads possibly in several dimensions")
+    n, s, d = shape[0], shape[1], shape[-1]
+    axes = len(sections)
+    if not 1 <= axes <= ROTARY_MAX_AXES:
+        raise ValueError(f"sections must name 1 to {ROTARY_MAX_AXES} axes")
+    if pos_shape not in ((s, axes), (n, s, axes)):
+        raise ValueError(f"positions has shape {pos_shape}, expected [{s}, {axes}] or [{n}, {s}, {axes}]")
+    if other_shape is not None and (len(other_shape) < 4 or other_shape[:2] != (n, s) or other_shape[-1] != d):
+        raise ValueError(f"other has shape {tuple(other_shape)}, expected [{n}, {s}, heads, {d}]")
+    heads, views = [0, 0], []
+    for i, st in enumerate(strides):
+        name = ("x", "output of x", "other", "output of other")[i]
+        if st is None:
+            views.append(None)
+            continue
+        heads[i // 2], view = _heads_view(other_shape if i >= 2 else shape, st, name)
+        views.append(view)
+    return Rotary(n, s, d, heads[0], heads[1], _type_code(dtype), axes, (ctypes.c_int * ROTARY_MAX_AXES)(*sections),
+                  int(len(pos_shape) == 3), int(inverse), int(interleaved)), views
 
 
 def rotary(x, positions, freqs, sections, other=None, interleaved=False, inverse=False, out=None, out_other=None):
@@ -332,32 +360,22 @@ def rotary(x, positions, freqs, sections, other=None, interleaved=False, inverse
     torch, dev = _fs._torch(), _device_of(x, "x")
     if other is None and out_other is not None:
         raise ValueError("out_other given without other")
-    n, s, d = x.shape[0], x.shape[1], x.shape[-1]
-    sections = tuple(int(p) for p in sections)
-    axes = len(sections)
-    if not 1 <= axes <= ROTARY_MAX_AXES:
-        raise ValueError(f"sections must name 1 to {ROTARY_MAX_AXES} axes")
-    per_batch = positions.dim() == 3
-    if tuple(positions.shape) != ((n, s, axes) if per_batch else (s, axes)):
-        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected [{s}, {axes}] or [{n}, {s}, {axes}]")
+    sections = tuple(sections)
+    out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
+    tensors = [(x, "x", x), (out, "output of x", x)]
+    strides = (x.stride(), out.stride(), None, None)
+    if other is not None:
+        _device_of(other, "other")
+        out_other = torch.empty(other.shape, dtype=other.dtype, device=dev) if out_other is None else out_other
+        tensors += [(other, "other", other), (out_other, "output of other", other)]
+        strides = strides[:2] + (other.stride(), out_other.stride())
+    for t, name, like in tensors:
+        if t.dtype != x.dtype or t.device != dev or t.shape != like.shape:
+            raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(like.shape)} on {dev}")
+    desc, v = _rotary_desc(x.shape, None if other is None else other.shape, strides, x.dtype, tuple(positions.shape),
+                           sections, bool(interleaved), bool(inverse))
     pp = _dense(positions, "positions", torch.int32, None, dev)
     fp = _dense(freqs, "freqs", torch.float32, sum(sections), dev)
-    ptrs, outs, heads = [], [], [0, 0]
-    for i, (t, o, name) in enumerate(((x, out, "x"), (other, out_other, "other"))):
-        if t is None:
-            ptrs += [None] * 4
-            continue
-        if t.dim() < 4 or t.shape[0] != n or t.shape[1] != s or t.shape[-1] != d:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{n}, {s}, heads, {d}]")
-        o = torch.empty(t.shape, dtype=t.dtype, device=dev) if o is None else o
-        xp = _strided(t, name, x.dtype, tuple(t.shape), dev)
-        yp = _strided(o, f"output of {name}", x.dtype, tuple(t.shape), dev)
-        heads[i], xs = _heads_view(t, name)
-        _, ys = _heads_view(o, f"output of {name}")
-        ptrs += [xp, xs, yp, ys]
-        outs.append(o)
-    desc = Rotary(n, s, d, heads[0], heads[1], _type_code(x.dtype), axes,
-                  (ctypes.c_int * ROTARY_MAX_AXES)(*sections), int(per_batch), int(bool(inverse)),
-                  int(bool(interleaved)))
-    _launch(dev, "fftsplit_rotary", ctypes.byref(desc), pp, fp, *ptrs)
-    return outs[0] if other is None else tuple(outs)
+    _launch(dev, "fftsplit_rotary", ctypes.byref(desc), pp, fp, x.data_ptr(), v[0], out.data_ptr(), v[1],
+            None if other is None else other.data_ptr(), v[2], None if other is None else out_other.data_ptr(), v[3])
+    return out if other is None else (out, out_other)

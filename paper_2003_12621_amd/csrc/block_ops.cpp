@@ -30,6 +30,8 @@ fftsplit_status_t check_norm(const fftsplit_layer_norm_t* d, NormArgs& a) {
         return fail(FFTSPLIT_ERROR_INVALID_VALUE, "layer norm: eps must be finite and not negative");
     if ((long long)d->batch * d->positions > 0x7fffffffLL)
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: batch * positions must be below 2^31");
+    if (first && d->positions > (1 << 22))
+        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: at most 2^22 positions of a feature map");
     a.n = d->batch;
     a.s = d->positions;
     a.c = d->channels;
@@ -44,8 +46,13 @@ fftsplit_status_t check_norm(const fftsplit_layer_norm_t* d, NormArgs& a) {
 
 size_t elements(const NormArgs& a) { return size_t(a.n) * a.s * a.c; }
 size_t part_bytes(const NormArgs& a) { return size_t(a.blocks) * 2 * a.c * 4; }
-// Rows of whole 16-byte pieces of 8 elements, or groups of 4 positions.
-bool norm_wide(const NormArgs& a) { return a.x_first ? a.s % 4 == 0 : a.c % 8 == 0; }
+// Whether rows are whole 16-byte pieces of 8 elements (channels last), or four
+// positions can be accessed at once (channels first; of fp32 tensors always).
+// A map's bf16 output beside an fp32 input is written in fours, too.
+bool norm_wide(const NormArgs& a) {
+    if (a.x_first) return a.s % 4 == 0 || (a.x_type == FFTSPLIT_F32 && (a.y_type == FFTSPLIT_F32 || !a.y_first));
+    return a.c % 8 == 0 && aligned16(a.weight) && aligned16(a.bias);
+}
 
 }  // namespace
 

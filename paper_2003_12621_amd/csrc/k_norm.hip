@@ -34,6 +34,17 @@ __device__ __forceinline__ void store_n(T* p, const float (&y)[N]) {
     *reinterpret_cast<Vec<T, N>*>(p) = u;
 }
 
+// N values of a parameter, `or_else` where there is none.
+template <int N>
+__device__ __forceinline__ void load_param(float (&y)[N], const float* p, int c, float or_else) {
+    if (p) {
+        load_n<float, N>(y, p + c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[j] = or_else;
+    }
+}
+
 // Sum over the G lanes (or, G = 256, threads of the workgroup) of a row, the same in all.
 template <int G>
 __device__ __forceinline__ float row_sum(float x, float* lds) {
@@ -91,12 +102,10 @@ __global__ __launch_bounds__(256) void norm_last_forward_kernel(NormArgs a) {
         const int c = (i * G + l) * N;
         if (c >= a.c) continue;
         float w[N], b[N], o[N];
+        load_param<N>(w, a.weight, c, 1.f);
+        load_param<N>(b, a.bias, c, 0.f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            w[j] = a.weight ? a.weight[c + j] : 1.f;
-            b[j] = a.bias ? a.bias[c + j] : 0.f;
-            o[j] = fmaf(v[i][j] * rstd, w[j], b[j]);
-        }
+        for (int j = 0; j < N; ++j) o[j] = fmaf(v[i][j] * rstd, w[j], b[j]);
         store_n<TY, N>(y + c, o);
     }
     if (a.mean && l == 0) {
@@ -129,12 +138,14 @@ __global__ __launch_bounds__(256) void norm_last_backward_kernel(NormArgs a) {
             if (c >= a.c) continue;
             load_n<TX, N>(v[i], x + c);
             load_n<TY, N>(u[i], g + c);
+            float w[N];
+            load_param<N>(w, a.weight, c, 1.f);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 v[i][j] = (v[i][j] - mean) * rstd;
                 db[i][j] += u[i][j];
                 dw[i][j] = fmaf(u[i][j], v[i][j], dw[i][j]);
-                u[i][j] *= a.weight ? a.weight[c + j] : 1.f;
+                u[i][j] *= w[j];
                 s1 += u[i][j];
                 s2 = fmaf(u[i][j], v[i][j], s2);
             }
@@ -223,6 +234,61 @@ struct FirstShape {
     }
 };
 
+// VP consecutive positions of the channels of a thread: channel i of NH at
+// base + i * step, of which those below `channels` exist, and of the positions
+// `count`; all others are zero.  `base` is the same for the workgroup, `off` (in
+// elements) the lane's, so that an access needs no 64-bit lane address.  fp32
+// rows need no alignment: 16-byte accesses to memory ask for 4.
+template <typename T, int VP>
+struct alignas(sizeof(T) == 4 ? 4 : sizeof(T) * VP) Positions {
+    T v[VP];
+};
+template <typename T, int VP, int NH>
+__device__ __forceinline__ void load_positions(float (&y)[NH][VP], const T* base, size_t step, unsigned off, int count,
+                                               int channels) {
+#pragma unroll
+    for (int i = 0; i < NH; ++i)
+#pragma unroll
+        for (int j = 0; j < VP; ++j) y[i][j] = 0.f;
+    if (count == VP) {
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
+            if (i < channels) {
+                const char* p = reinterpret_cast<const char*>(base + i * step) + off * unsigned(sizeof(T));
+                const Positions<T, VP> u = *reinterpret_cast<const Positions<T, VP>*>(p);
+#pragma unroll
+                for (int j = 0; j < VP; ++j) y[i][j] = float(u.v[j]);
+            }
+    } else if (count > 0) {      // the last positions of a row
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
+#pragma unroll
+            for (int j = 0; j < VP; ++j)
+                if (i < channels && j < count) y[i][j] = float((base + i * step)[off + j]);
+    }
+}
+template <typename T, int VP, int NH>
+__device__ __forceinline__ void store_positions(T* base, size_t step, unsigned off, const float (&y)[NH][VP], int count,
+                                                int channels) {
+    if (count == VP) {
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
+            if (i < channels) {
+                Positions<T, VP> u;
+#pragma unroll
+                for (int j = 0; j < VP; ++j) u.v[j] = T(y[i][j]);
+                char* p = reinterpret_cast<char*>(base + i * step) + off * unsigned(sizeof(T));
+                *reinterpret_cast<Positions<T, VP>*>(p) = u;
+            }
+    } else if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
+#pragma unroll
+            for (int j = 0; j < VP; ++j)
+                if (i < channels && j < count) (base + i * step)[off + j] = T(y[i][j]);
+    }
+}
+
 }  // namespace
 
 template <typename TX, typename TY, int NT, int LP, int VP, int NH, bool SWAP>
@@ -232,22 +298,15 @@ __global__ __launch_bounds__(NT) void norm_first_forward_kernel(NormArgs a) {
     const int lp = threadIdx.x % LP, cr = threadIdx.x / LP;
     const int tiles = (a.s + Shape::kPos - 1) / Shape::kPos;
     const int b = blockIdx.x / tiles, pos0 = blockIdx.x % tiles * Shape::kPos, pos = pos0 + lp * VP;
-    const bool in = pos < a.s;      // (VP > 1 only where it divides s)
-    const TX* x = static_cast<const TX*>(a.x) + (size_t)b * a.c * a.s + pos;
+    const int count = max(0, min(VP, a.s - pos));       // positions of this thread that exist
+    const size_t at = (size_t)b * a.c * a.s + pos0, step = (size_t)Shape::kRows * a.s;
+    const unsigned off = unsigned(cr * a.s + lp * VP);
+    const int channels = (a.c - cr + Shape::kRows - 1) / Shape::kRows;   // of this thread's that exist
     float v[NH][VP];
     float sum[1][VP];
+    load_positions<TX, VP, NH>(v, static_cast<const TX*>(a.x) + at, step, off, count, channels);
 #pragma unroll
     for (int p = 0; p < VP; ++p) sum[0][p] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NH; ++i) {
-        const int c = cr + i * Shape::kRows;
-        if (in && c < a.c) {
-            load_n<TX, VP>(v[i], x + (size_t)c * a.s);
-        } else {
-#pragma unroll
-            for (int p = 0; p < VP; ++p) v[i][p] = 0.f;
-        }
-    }
 #pragma unroll
     for (int i = 0; i < NH; ++i)
 #pragma unroll
@@ -270,12 +329,13 @@ __global__ __launch_bounds__(NT) void norm_first_forward_kernel(NormArgs a) {
     column_sum<NT, LP, VP, 1>(sum, lds);
 #pragma unroll
     for (int p = 0; p < VP; ++p) rstd[p] = 1.f / sqrtf(sum[0][p] / float(a.c) + a.eps);
-    if (a.mean && cr == 0 && in)
+    if (a.mean && cr == 0)
 #pragma unroll
-        for (int p = 0; p < VP; ++p) {
-            a.mean[(size_t)b * a.s + pos + p] = mean[p];
-            a.rstd[(size_t)b * a.s + pos + p] = rstd[p];
-        }
+        for (int p = 0; p < VP; ++p)
+            if (p < count) {
+                a.mean[(size_t)b * a.s + pos + p] = mean[p];
+                a.rstd[(size_t)b * a.s + pos + p] = rstd[p];
+            }
 #pragma unroll
     for (int i = 0; i < NH; ++i) {
         const int c = cr + i * Shape::kRows;
@@ -284,15 +344,10 @@ __global__ __launch_bounds__(NT) void norm_first_forward_kernel(NormArgs a) {
         for (int p = 0; p < VP; ++p) v[i][p] = fmaf(v[i][p] * rstd[p], w, bias);
     }
     if constexpr (!SWAP) {
-        TY* y = static_cast<TY*>(a.y) + (size_t)b * a.c * a.s + pos;
-#pragma unroll
-        for (int i = 0; i < NH; ++i) {
-            const int c = cr + i * Shape::kRows;
-            if (in && c < a.c) store_n<TY, VP>(y + (size_t)c * a.s, v[i]);
-        }
+        store_positions<TY, VP, NH>(static_cast<TY*>(a.y) + at, step, off, v, count, channels);
     } else {
         TY* y = static_cast<TY*>(a.y) + ((size_t)b * a.s + pos0) * a.c;
-        const int count = min(Shape::kPos, a.s - pos0);
+        const int positions = min(Shape::kPos, a.s - pos0);
 #pragma unroll
         for (int i0 = 0; i0 < NH; i0 += Shape::kSteps) {
             const int c0 = i0 * Shape::kRows;
@@ -305,7 +360,7 @@ __global__ __launch_bounds__(NT) void norm_first_forward_kernel(NormArgs a) {
                         lds[(lp * VP + p) * Shape::kPitch + i * Shape::kRows + cr] = v[i0 + i < NH ? i0 + i : 0][p];
             __syncthreads();
             const int width = min(Shape::kSwap, a.c - c0);
-            for (int e = threadIdx.x; e < count * Shape::kSwap; e += NT) {
+            for (int e = threadIdx.x; e < positions * Shape::kSwap; e += NT) {
                 const int p = e / Shape::kSwap, c = e % Shape::kSwap;
                 if (c < width) y[(size_t)p * a.c + c0 + c] = TY(lds[p * Shape::kPitch + c]);
             }
@@ -320,63 +375,65 @@ __global__ __launch_bounds__(NT) void norm_first_backward_kernel(NormArgs a) {
     extern __shared__ float lds[];
     const int lp = threadIdx.x % LP, cr = threadIdx.x / LP;
     const int tiles = (a.s + Shape::kPos - 1) / Shape::kPos;
+    const size_t step = (size_t)Shape::kRows * a.s;
+    const unsigned off = unsigned(cr * a.s + lp * VP);
     const float inv_c = 1.f / float(a.c);
+    const int channels = (a.c - cr + Shape::kRows - 1) / Shape::kRows;
     float dw[NH], db[NH];
 #pragma unroll
     for (int i = 0; i < NH; ++i) dw[i] = db[i] = 0.f;
     for (long long tile = blockIdx.x; tile < (long long)a.n * tiles; tile += gridDim.x) {
         const int b = int(tile / tiles), pos0 = int(tile % tiles) * Shape::kPos, pos = pos0 + lp * VP;
-        const bool in = pos < a.s;
-        const size_t at = (size_t)b * a.c * a.s + pos;
+        const int count = max(0, min(VP, a.s - pos));
+        const size_t at = (size_t)b * a.c * a.s + pos0;
         float v[NH][VP], u[NH][VP];
         float mean[VP], rstd[VP], sum[2][VP];
 #pragma unroll
         for (int p = 0; p < VP; ++p) {
-            mean[p] = in ? a.mean[(size_t)b * a.s + pos + p] : 0.f;
-            rstd[p] = in ? a.rstd[(size_t)b * a.s + pos + p] : 0.f;
+            mean[p] = p < count ? a.mean[(size_t)b * a.s + pos + p] : 0.f;
+            rstd[p] = p < count ? a.rstd[(size_t)b * a.s + pos + p] : 0.f;
             sum[0][p] = sum[1][p] = 0.f;
         }
+        load_positions<TX, VP, NH>(v, static_cast<const TX*>(a.x) + at, step, off, count, channels);
+        if constexpr (!SWAP) {
+            load_positions<TY, VP, NH>(u, static_cast<const TY*>(a.dy) + at, step, off, count, channels);
+        } else {
 #pragma unroll
-        for (int i = 0; i < NH; ++i) {
-            const int c = cr + i * Shape::kRows;
-            const bool have = in && c < a.c;
-            if (have) load_n<TX, VP>(v[i], static_cast<const TX*>(a.x) + at + (size_t)c * a.s);
-            if constexpr (!SWAP)
-                if (have) load_n<TY, VP>(u[i], static_cast<const TY*>(a.dy) + at + (size_t)c * a.s);
-            if (!have)
+            for (int i = 0; i < NH; ++i)
 #pragma unroll
-                for (int p = 0; p < VP; ++p) v[i][p] = u[i][p] = 0.f;
+                for (int p = 0; p < VP; ++p) u[i][p] = 0.f;
         }
         if constexpr (SWAP) {
             const TY* g = static_cast<const TY*>(a.dy) + ((size_t)b * a.s + pos0) * a.c;
-            const int count = min(Shape::kPos, a.s - pos0);
+            const int positions = min(Shape::kPos, a.s - pos0);
 #pragma unroll
             for (int i0 = 0; i0 < NH; i0 += Shape::kSteps) {
                 const int c0 = i0 * Shape::kRows;
                 if (c0 >= a.c) break;
                 const int width = min(Shape::kSwap, a.c - c0);
                 __syncthreads();
-                for (int e = threadIdx.x; e < count * Shape::kSwap; e += NT) {
+                for (int e = threadIdx.x; e < positions * Shape::kSwap; e += NT) {
                     const int p = e / Shape::kSwap, c = e % Shape::kSwap;
                     if (c < width) lds[p * Shape::kPitch + c] = float(g[(size_t)p * a.c + c0 + c]);
                 }
                 __syncthreads();
 #pragma unroll
                 for (int i = 0; i < Shape::kSteps; ++i)
-                    if (i0 + i < NH && in && c0 + i * Shape::kRows + cr < a.c)
+                    if (i0 + i < NH && c0 + i * Shape::kRows + cr < a.c)
 #pragma unroll
                         for (int p = 0; p < VP; ++p)
-                            u[i0 + i < NH ? i0 + i : 0][p] = lds[(lp * VP + p) * Shape::kPitch + i * Shape::kRows + cr];
+                            u[i0 + i < NH ? i0 + i : 0][p] =
+                                p < count ? lds[(lp * VP + p) * Shape::kPitch + i * Shape::kRows + cr] : 0.f;
             }
             __syncthreads();
         }
+        // (positions and channels that do not exist have rstd or dy zero: no terms)
 #pragma unroll
         for (int i = 0; i < NH; ++i) {
             const int c = cr + i * Shape::kRows;
             const float w = a.weight && c < a.c ? a.weight[c] : 1.f;
 #pragma unroll
             for (int p = 0; p < VP; ++p) {
-                if (!(in && c < a.c)) continue;
                 v[i][p] = (v[i][p] - mean[p]) * rstd[p];
                 db[i] += u[i][p];
                 dw[i] = fmaf(u[i][p], v[i][p], dw[i]);
@@ -387,14 +444,11 @@ __global__ __launch_bounds__(NT) void norm_first_backward_kernel(NormArgs a) {
         }
         column_sum<NT, LP, VP, 2>(sum, lds);
 #pragma unroll
-        for (int i = 0; i < NH; ++i) {
-            const int c = cr + i * Shape::kRows;
-            if (!(in && c < a.c)) continue;
-            float o[VP];
+        for (int i = 0; i < NH; ++i)
 #pragma unroll
-            for (int p = 0; p < VP; ++p) o[p] = rstd[p] * (u[i][p] - sum[0][p] * inv_c - v[i][p] * (sum[1][p] * inv_c));
-            store_n<TX, VP>(static_cast<TX*>(a.dx) + at + (size_t)c * a.s, o);
-        }
+            for (int p = 0; p < VP; ++p)
+                u[i][p] = rstd[p] * (u[i][p] - sum[0][p] * inv_c - v[i][p] * (sum[1][p] * inv_c));
+        store_positions<TX, VP, NH>(static_cast<TX*>(a.dx) + at, step, off, u, count, channels);
     }
 #pragma unroll
     for (int i = 0; i < NH; ++i) {
@@ -417,8 +471,10 @@ __global__ __launch_bounds__(1024) void norm_gradient_sum_kernel(NormArgs a) {
     __shared__ float lds[16][64];
     const int i = blockIdx.x * 64 + threadIdx.x % 64, part = threadIdx.x / 64;
     float t = 0.f;
-    if (i < 2 * a.c)
+    if (i < 2 * a.c) {
+#pragma unroll 8
         for (int b = part; b < a.blocks; b += 16) t += a.part[(size_t)b * 2 * a.c + i];
+    }
     lds[part][threadIdx.x % 64] = t;
     __syncthreads();
     if (part == 0 && i < 2 * a.c) {
@@ -473,32 +529,47 @@ hipError_t first_backward(const NormArgs& a, hipStream_t s, const LaunchEvents& 
     return launch_kernel(kernel, dim3(a.blocks), dim3(NT), Shape::lds(SWAP), s, ev.start, nullptr, a);
 }
 
-// A thread holds 64 elements forward; 2 x 64 and 2 x 16 sums backward, or half
-// of that where 1024 threads leave it 128 registers.
+// Positions side by side are what memory sees as one piece: 64 (256 bytes of
+// fp32) where there are enough of them for every compute unit, else 16.  A
+// thread holds up to 64 elements forward; 2 x 64 and 2 x 16 sums backward.
 template <typename TX, typename TY, bool SWAP>
 hipError_t first_sized(bool backward, const NormArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    const bool small = (long long)a.n * ((a.s + 63) / 64) < 256;
     if (!backward) {
+        if (a.wide && small) {
+            if (a.c <= 256) return first_forward<TX, TY, 256, 4, 4, 4, SWAP>(a, s, ev);
+            if (a.c <= 512) return first_forward<TX, TY, 512, 4, 4, 4, SWAP>(a, s, ev);
+            if (a.c <= 1024) return first_forward<TX, TY, 1024, 4, 4, 4, SWAP>(a, s, ev);
+            return first_forward<TX, TY, 1024, 4, 4, 8, SWAP>(a, s, ev);
+        }
         if (a.wide) {
+            if (a.c <= 64) return first_forward<TX, TY, 256, 16, 4, 4, SWAP>(a, s, ev);
+            if (a.c <= 128) return first_forward<TX, TY, 256, 16, 4, 8, SWAP>(a, s, ev);
             if (a.c <= 256) return first_forward<TX, TY, 256, 16, 4, 16, SWAP>(a, s, ev);
             if (a.c <= 512) return first_forward<TX, TY, 512, 16, 4, 16, SWAP>(a, s, ev);
-            if (a.c <= 1024) return first_forward<TX, TY, 1024, 16, 4, 16, SWAP>(a, s, ev);
-            return first_forward<TX, TY, 1024, 8, 4, 16, SWAP>(a, s, ev);
+            if (a.c <= 1024) return first_forward<TX, TY, 1024, 8, 4, 8, SWAP>(a, s, ev);
+            return first_forward<TX, TY, 1024, 4, 4, 8, SWAP>(a, s, ev);
         }
-        if (a.c <= 256) return first_forward<TX, TY, 256, 64, 1, 64, SWAP>(a, s, ev);
-        if (a.c <= 512) return first_forward<TX, TY, 512, 64, 1, 64, SWAP>(a, s, ev);
-        if (a.c <= 1024) return first_forward<TX, TY, 1024, 64, 1, 64, SWAP>(a, s, ev);
-        return first_forward<TX, TY, 1024, 32, 1, 64, SWAP>(a, s, ev);
-    }
-    if (a.wide) {
+    } else if (a.wide) {
+        if (a.c <= 64) return first_backward<TX, TY, 256, 16, 4, 4, SWAP>(a, s, ev);
+        if (a.c <= 128) return first_backward<TX, TY, 256, 16, 4, 8, SWAP>(a, s, ev);
         if (a.c <= 256) return first_backward<TX, TY, 256, 16, 4, 16, SWAP>(a, s, ev);
-        if (a.c <= 512) return first_backward<TX, TY, 512, 16, 4, 16, SWAP>(a, s, ev);
-        if (a.c <= 1024) return first_backward<TX, TY, 1024, 8, 4, 8, SWAP>(a, s, ev);
-        return first_backward<TX, TY, 1024, 4, 4, 8, SWAP>(a, s, ev);
+        if (a.c <= 512) return first_backward<TX, TY, 512, 8, 4, 8, SWAP>(a, s, ev);
+        if (a.c <= 1024) return first_backward<TX, TY, 512, 4, 4, 8, SWAP>(a, s, ev);
+        return first_backward<TX, TY, 512, 4, 4, 16, SWAP>(a, s, ev);
     }
-    if (a.c <= 256) return first_backward<TX, TY, 1024, 64, 1, 16, SWAP>(a, s, ev);
-    if (a.c <= 512) return first_backward<TX, TY, 1024, 32, 1, 16, SWAP>(a, s, ev);
-    if (a.c <= 1024) return first_backward<TX, TY, 1024, 16, 1, 16, SWAP>(a, s, ev);
-    return first_backward<TX, TY, 1024, 8, 1, 16, SWAP>(a, s, ev);
+    // rows with bf16 elements and a length that 4 does not divide
+    if constexpr (sizeof(TX) == 2 || (sizeof(TY) == 2 && !SWAP)) {
+        if (!backward) {
+            if (a.c <= 128) return first_forward<TX, TY, 512, 64, 1, 16, SWAP>(a, s, ev);
+            if (a.c <= 512) return first_forward<TX, TY, 1024, 32, 1, 16, SWAP>(a, s, ev);
+            return first_forward<TX, TY, 1024, 8, 1, 16, SWAP>(a, s, ev);
+        }
+        if (a.c <= 128) return first_backward<TX, TY, 512, 64, 1, 16, SWAP>(a, s, ev);
+        if (a.c <= 512) return first_backward<TX, TY, 512, 16, 1, 16, SWAP>(a, s, ev);
+        return first_backward<TX, TY, 512, 8, 1, 32, SWAP>(a, s, ev);
+    }
+    return hipErrorInvalidValue;      // (not reached: rows of fp32 alone are always wide)
 }
 
 template <typename TX, typename TY>
