@@ -70,8 +70,18 @@ SIGNATURES = {
 }
 
 
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        _torch_module = _fs._torch()
+    return _torch_module
+
+
 def _type_code(dtype) -> int:
-    torch = _fs._torch()
+    torch = _torch()
     if dtype == torch.float32:
         return F32
     if dtype == torch.bfloat16:
@@ -79,15 +89,24 @@ def _type_code(dtype) -> int:
     raise TypeError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
 
 
-def _strided(t, name, dtype, shape, device):
-    """Pointer of a tensor of the given shape whose last dimension is dense."""
-    if not isinstance(t, _fs._torch().Tensor) or not t.is_cuda:
+def _stream(device) -> int:
+    """Handle of the device's current stream."""
+    return _torch()._C._cuda_getCurrentRawStream(device.index)
+
+
+def _tensor(t, name, dtype, device):
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
-    if t.dtype != dtype:
+    if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if tuple(t.shape) != shape:
+
+
+def _strided(t, name, dtype, shape, device):
+    """Pointer of a tensor of the given shape whose last dimension is dense."""
+    _tensor(t, name, dtype, device)
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     if shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must be dense in its last dimension")
@@ -96,10 +115,12 @@ def _strided(t, name, dtype, shape, device):
 
 def _dense(t, name, dtype, numel, device):
     """Pointer of a dense tensor of `numel` elements (any shape)."""
-    p = _fs._dev_tensor(t, name, dtype, numel)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    return p
+    _tensor(t, name, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    return t.data_ptr()
 
 
 class DiffAttention:
@@ -110,7 +131,7 @@ class DiffAttention:
 
     def __init__(self, batch, queries, keys, heads_q, heads_k, dim, dim_v, dtype=None, causal=False, scale=None,
                  device=None, arch: Optional[str] = None):
-        torch = _fs._torch()
+        torch = _torch()
         self.dtype = torch.float32 if dtype is None else dtype
         if scale is not None and not scale > 0:
             raise ValueError("scale must be positive")
@@ -135,6 +156,7 @@ class DiffAttention:
         self.k_shape = (batch, keys, heads_k, 2, dim)
         self.v_shape = (batch, keys, heads_k, dim_v)
         self.out_shape = (batch, queries, heads_q, dim_v)
+        self._layouts = {}
 
     def __del__(self):
         h = getattr(self, "_h", None)
@@ -148,28 +170,40 @@ class DiffAttention:
         need = self.info.forward_workspace_bytes
         if backward:
             need = max(need, self.info.backward_workspace_bytes)
-        return _fs._torch().empty(need, dtype=_fs._torch().uint8, device=self.device)
+        return _torch().empty(need, dtype=_torch().uint8, device=self.device)
+
+    def _layout(self, q, k, v, lam):
+        """AttentionInputs for these strides, without pointers: the same for
+        all calls with tensors laid out alike."""
+        key = (q.stride(), k.stride(), v.stride(), lam.dtype, lam.numel())
+        x = self._layouts.get(key)
+        if x is None:
+            if lam.numel() not in (1, self.prob.heads_q):
+                raise ValueError(f"lam must have 1 or {self.prob.heads_q} elements, has {lam.numel()}")
+            x = AttentionInputs()
+            x.q_stride[:] = q.stride()[:4]
+            x.k_stride[:] = k.stride()[:4]
+            x.v_stride[:] = v.stride()[:3]
+            x.lam_dtype, x.lam_count = _type_code(lam.dtype), lam.numel()
+            if len(self._layouts) >= 64:
+                self._layouts.clear()
+            self._layouts[key] = x
+        return AttentionInputs.from_buffer_copy(x)
 
     def _inputs(self, q, k, v, lam, key_lengths):
-        torch, dev = _fs._torch(), self.device
-        x = AttentionInputs()
-        x.q = _strided(q, "q", self.dtype, self.q_shape, dev)
-        x.k = _strided(k, "k", self.dtype, self.k_shape, dev)
-        x.v = _strided(v, "v", self.dtype, self.v_shape, dev)
-        x.q_stride[:] = q.stride()[:4]
-        x.k_stride[:] = k.stride()[:4]
-        x.v_stride[:] = v.stride()[:3]
-        if not isinstance(lam, torch.Tensor) or lam.numel() not in (1, self.prob.heads_q):
-            raise ValueError(f"lam must be a tensor of 1 or {self.prob.heads_q} elements")
-        x.lam = _dense(lam, "lam", None, None, dev)
-        x.lam_dtype = _type_code(lam.dtype)
-        x.lam_count = lam.numel()
+        dev = self.device
+        qp = _strided(q, "q", self.dtype, self.q_shape, dev)
+        kp = _strided(k, "k", self.dtype, self.k_shape, dev)
+        vp = _strided(v, "v", self.dtype, self.v_shape, dev)
+        lp = _dense(lam, "lam", None, None, dev)
+        x = self._layout(q, k, v, lam)
+        x.q, x.k, x.v, x.lam = qp, kp, vp, lp
         if key_lengths is not None:
-            x.key_lengths = _dense(key_lengths, "key_lengths", torch.int32, self.prob.batch, dev)
+            x.key_lengths = _dense(key_lengths, "key_lengths", _torch().int32, self.prob.batch, dev)
         return x
 
     def _workspace(self, ws, need):
-        torch = _fs._torch()
+        torch = _torch()
         if ws is None:
             if need == 0:
                 return None, 0
@@ -179,7 +213,7 @@ class DiffAttention:
     def forward(self, q, k, v, lam, key_lengths=None, out=None, workspace=None, save=False):
         """o [batch, queries, heads_q, dim_v]; with save=True (o, saved), where
         `saved` is what backward needs beside the inputs and o."""
-        torch = _fs._torch()
+        torch = _torch()
         x = self._inputs(q, k, v, lam, key_lengths)
         numel = _fs._prod(self.out_shape)
         o = torch.empty(self.out_shape, dtype=self.dtype, device=self.device) if out is None else out
@@ -192,14 +226,14 @@ class DiffAttention:
             sp = tuple(t.data_ptr() for t in saved)
         ws, nbytes = self._workspace(workspace, self.info.forward_workspace_bytes)
         _fs._check(_fs.lib().fftsplit_attention_forward(self._h, ctypes.byref(x), op, *sp, ws, nbytes,
-                                                        _fs._stream_handle(self.device)),
+                                                        _stream(self.device)),
                    "fftsplit_attention_forward")
         return (o, saved) if save else o
 
     def backward(self, dout, q, k, v, lam, saved, key_lengths=None, workspace=None):
         """(dq, dk, dv, dlam) from the gradient of o; `saved` as
         forward(save=True) returned it."""
-        torch, dev = _fs._torch(), self.device
+        torch, dev = _torch(), self.device
         x = self._inputs(q, k, v, lam, key_lengths)
         gp = _strided(dout, "dout", self.dtype, self.out_shape, dev)
         gs = (ctypes.c_longlong * 3)(*dout.stride()[:3])
@@ -214,7 +248,7 @@ class DiffAttention:
         ws, nbytes = self._workspace(workspace, self.info.backward_workspace_bytes)
         _fs._check(_fs.lib().fftsplit_attention_backward(self._h, ctypes.byref(x), gp, gs, o1, o2, lse, dq.data_ptr(),
                                                          dk.data_ptr(), dv.data_ptr(), dlam.data_ptr(), ws, nbytes,
-                                                         _fs._stream_handle(dev)),
+                                                         _stream(dev)),
                    "fftsplit_attention_backward")
         return dq, dk, dv, dlam
 
@@ -223,7 +257,7 @@ _LAYOUTS = {"last": CHANNELS_LAST, "first": CHANNELS_FIRST}
 
 
 def _device_of(t, name):
-    if not isinstance(t, _fs._torch().Tensor) or not t.is_cuda:
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
     return t.device
 
@@ -231,13 +265,15 @@ def _device_of(t, name):
 def _launch(device, name, *args):
     """Calls an entry point that runs on the current device on `device`'s
     current stream."""
-    torch = _fs._torch()
+    torch = _torch()
     fn = getattr(_fs.lib(), name)
-    if torch.cuda.current_device() == device.index:
-        _fs._check(fn(*args, _fs._stream_handle(device)), name)
+    if torch._C._cuda_getDevice() == device.index:
+        status = fn(*args, _stream(device))
     else:
         with torch.cuda.device(device):
-            _fs._check(fn(*args, _fs._stream_handle(device)), name)
+            status = fn(*args, _stream(device))
+    if status != _fs.SUCCESS:
+        _fs._check(status, name)
 
 
 @functools.lru_cache(maxsize=256)
@@ -263,7 +299,7 @@ def _norm_desc(shape, dtype, layout, out_layout, out_dtype, eps):
 
 
 def _param(t, name, c, device):
-    return None if t is None else _dense(t, name, _fs._torch().float32, c, device)
+    return None if t is None else _dense(t, name, _torch().float32, c, device)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, layout="last", out_layout=None, out_dtype=None, out=None,
@@ -273,7 +309,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, layout="last", out_layout=No
     a feature map into tokens [n, positions, channels], out_dtype an fp32 one
     into bf16.  return_stats=True also returns mean and rstd (fp32, one per
     position) for layer_norm_backward."""
-    torch, dev = _fs._torch(), _device_of(x, "x")
+    torch, dev = _torch(), _device_of(x, "x")
     out_dtype = x.dtype if out_dtype is None else out_dtype
     desc, shape, numel, _ = _norm_desc(x.shape, x.dtype, layout, out_layout, out_dtype, eps)
     xp = _dense(x, "x", None, None, dev)
@@ -291,7 +327,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, layout="last", out_layout=No
 def layer_norm_backward(dy, x, mean, rstd, weight=None, layout="last", out_layout=None, workspace=None):
     """(dx, dweight, dbias) from the gradient of layer_norm's output; the
     parameters' gradients are fp32."""
-    torch, dev = _fs._torch(), _device_of(x, "x")
+    torch, dev = _torch(), _device_of(x, "x")
     _device_of(dy, "dy")
     desc, _, numel, need = _norm_desc(x.shape, x.dtype, layout, out_layout, dy.dtype, 0.0)
     rows = desc.batch * desc.positions
@@ -322,6 +358,11 @@ def _heads_view(shape, strides, name):
             raise ValueError(f"{name}: its head dimensions do not form one")
         heads *= size
     return heads, (ctypes.c_longlong * 3)(strides[0], strides[1], stride)
+
+
+def _like(t, name, shaped, typed):
+    if t.dtype != typed.dtype or t.device != typed.device or t.shape != shaped.shape:
+        raise ValueError(f"{name} must be a {typed.dtype} tensor of shape {tuple(shaped.shape)} on {typed.device}")
 
 
 @functools.lru_cache(maxsize=256)
@@ -357,22 +398,20 @@ def rotary(x, positions, freqs, sections, other=None, interleaved=False, inverse
     [batch, tokens, axes], int32).  `other` is turned in the same launch (the
     keys beside the queries); then both results are returned.  out=x works in
     place; inverse=True gives the gradient."""
-    torch, dev = _fs._torch(), _device_of(x, "x")
+    torch, dev = _torch(), _device_of(x, "x")
     if other is None and out_other is not None:
         raise ValueError("out_other given without other")
     sections = tuple(sections)
     out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
-    tensors = [(x, "x", x), (out, "output of x", x)]
+    _like(out, "output of x", x, x)
     strides = (x.stride(), out.stride(), None, None)
     if other is not None:
         _device_of(other, "other")
         out_other = torch.empty(other.shape, dtype=other.dtype, device=dev) if out_other is None else out_other
-        tensors += [(other, "other", other), (out_other, "output of other", other)]
+        _like(other, "other", other, x)
+        _like(out_other, "output of other", other, x)
         strides = strides[:2] + (other.stride(), out_other.stride())
-    for t, name, like in tensors:
-        if t.dtype != x.dtype or t.device != dev or t.shape != like.shape:
-            raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(like.shape)} on {dev}")
-    desc, v = _rotary_desc(x.shape, None if other is None else other.shape, strides, x.dtype, tuple(positions.shape),
+    desc, v = _rotary_desc(x.shape, None if other is None else other.shape, strides, x.dtype, positions.shape,
                            sections, bool(interleaved), bool(inverse))
     pp = _dense(positions, "positions", torch.int32, None, dev)
     fp = _dense(freqs, "freqs", torch.float32, sum(sections), dev)
