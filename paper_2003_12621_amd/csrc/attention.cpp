@@ -78,6 +78,24 @@ int choose_splits(const fftsplit_attention_problem_t& p) {
     return few_time < tiled_time ? int(splits) : 0;
 }
 
+// Workgroups that share the steps of a tile of 128 keys or rows in the backward
+// pass: as many as fill the chip, of at least 8 steps each (bf16; an fp32 step
+// takes four times as long).  Their parts are added up by another launch.
+int choose_backward_splits(const fftsplit_attention_problem_t& p, int shape, long long tiles, long long steps) {
+    const bool two = kAttnShapes[shape].dv * type_bytes(p.dtype) <= 256;     // workgroups a compute unit
+    const long long least = p.dtype == FFTSPLIT_F32 ? 2 : 8;
+    long long splits = (two ? 512 : 256) / tiles;
+    if (splits > steps / least) splits = steps / least;
+    if (splits > 8) splits = 8;
+    return splits < 1 ? 1 : int(splits);
+}
+size_t key_part_bytes(const fftsplit_attention_problem_t& p, int splits) {
+    return splits > 1 ? round256(size_t(splits) * p.batch * p.keys * p.heads_k * (2 * p.dim + p.dim_v) * 4) : 0;
+}
+size_t query_part_bytes(const fftsplit_attention_problem_t& p, int splits) {
+    return splits > 1 ? round256(size_t(splits) * p.batch * p.queries * p.heads_q * 2 * p.dim * 4) : 0;
+}
+
 int delta_parts(const fftsplit_attention_problem_t& p) {
     return p.batch * ((p.queries + kAttnDeltaRows - 1) / kAttnDeltaRows);
 }
@@ -123,7 +141,14 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->splits = choose_splits(p);
     const size_t parts = size_t(rows) * plan->splits;
     plan->forward_ws = plan->splits ? round256(parts * 2 * kAttnShapes[shape].dv * 4) + round256(parts * 4 * 4) : 0;
-    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * delta_parts(p) * 4);
+    const long long group = p.heads_q / p.heads_k;
+    plan->key_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_k * ((p.keys + 127LL) / 128),
+                                              group * ((p.queries + 31LL) / 32));
+    plan->query_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_q * ((p.queries + 127LL) / 128),
+                                                (p.keys + 31LL) / 32);
+    const size_t shared = key_part_bytes(p, plan->key_splits), other = query_part_bytes(p, plan->query_splits);
+    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * delta_parts(p) * 4) +
+                        (shared > other ? shared : other);
     *out = plan;
     return FFTSPLIT_SUCCESS;
 }
@@ -319,6 +344,10 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.parts = delta_parts(p);
         a.delta = static_cast<float*>(workspace);
         a.dlam_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + round256(lse_bytes(p)));
+        // (the two kernels' parts in turn)
+        a.key_splits = plan->key_splits;
+        a.query_splits = plan->query_splits;
+        a.key_part = a.query_part = a.dlam_part + round256(size_t(p.heads_q) * a.parts * 4) / 4;
         a.dq = dq;
         a.dk = dk;
         a.dv_out = dv;

@@ -9,6 +9,9 @@ struct fftsplit_attention_plan_s {
     float scale;             // of the products, before the softmax
     int shape;               // index into kAttnShapes: the kernels' padded head widths
     int splits;              // workgroups that share the keys of one tile of few rows; 0: the tiled kernel runs
+    // Workgroups that share the rows of a tile of keys, and the keys of a tile
+    // of rows, in the backward pass (1: each goes over all).
+    int key_splits, query_splits;
     size_t forward_ws, backward_ws;
 };
 
@@ -58,6 +61,9 @@ struct AttnArgs {
     float* delta;                    // [n][hq][2][sq]
     float* dlam_part;                // [hq][parts]
     int parts;
+    int key_splits, query_splits;
+    float* key_part;                 // [split][n][sk][hk][2 d + dv]
+    float* query_part;               // [split][n][sq][hq][2][d]
     void *dq, *dk, *dv_out, *dlam;
 };
 

@@ -147,18 +147,28 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 
 }  // namespace
 
+// What a launch of either kernel below computes.
+constexpr int kFirst = 1, kSecond = 2, kBoth = 3;    // the gradients of a map's keys or queries
+constexpr int kValues = 4;                           // dv
+constexpr int kAll = 7;
+
 // Key side: one workgroup takes 128 keys of one key head, 32 a wave, and goes
-// over the queries of all heads that share it.  Each wave keeps its rows of
-// k1, k2 and v as operands and dk1, dk2, dv as accumulators in registers.
-template <typename T, int D, int DV, bool WIDE, bool DK, bool DVAL>
+// over the queries of all heads that share it (or over its share of them).
+// Each wave keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as
+// accumulators in registers.
+template <typename T, int D, int DV, bool WIDE, int DO>
 __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_key_side_kernel(AttnArgs a) {
     using Shape = KeySideShape<T, D, DV>;
     constexpr int kRows = Shape::kRows;
+    constexpr bool DK = (DO & kBoth) != 0, DVAL = (DO & kValues) != 0;
+    constexpr bool M1 = DVAL || (DO & kFirst), M2 = DVAL || (DO & kSecond);      // maps whose scores are needed
+    constexpr bool DK1 = DO & kFirst, DK2 = DO & kSecond;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
     const int tiles = (a.sk + kKeySideKeys - 1) / kKeySideKeys;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int tile = id % tiles, hkv = id / tiles % a.hk, b = id / tiles / a.hk;
+    const int tile = id % tiles, split = id / tiles % a.key_splits, hkv = id / tiles / a.key_splits % a.hk;
+    const int b = id / tiles / a.key_splits / a.hk;
     const int group = a.hq / a.hk;
     const int length = attn_length(a, b), offset = length - a.sq;
     const int first = tile * kKeySideKeys, wave_first = first + wave * 32, key = wave_first + (lane & 31);
@@ -170,7 +180,7 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
 
     constexpr bool kKeysInLds = Shape::kKeysInLds;
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
-    Operand<T> k1[kKeysInLds ? 1 : D / 16], k2[kKeysInLds ? 1 : D / 16], v[DV / 16];
+    Operand<T> k1[kKeysInLds || !M1 ? 1 : D / 16], k2[kKeysInLds || !M2 ? 1 : D / 16], v[DK ? DV / 16 : 1];
     unsigned key1 = 0;      // LDS address of this lane's key
     {
         if constexpr (kKeysInLds) {
@@ -182,14 +192,14 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
             key1 = tile1 + row_lane<T, D>(lane) + wave * TileShape<T, D>::bytes(32);
         } else {
             const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
-            load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
-            load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
+            if constexpr (M1) load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
+            if constexpr (M2) load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
         }
         if constexpr (DK)
             load_row_operands<T, DV, WIDE>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
                                      a.dv, exists, lane);
     }
-    floatx16 dk1[DK ? D / 32 : 1], dk2[DK ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
+    floatx16 dk1[DK1 ? D / 32 : 1], dk2[DK2 ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
 #pragma unroll
     for (auto& x : dk1) x = zero16();
 #pragma unroll
@@ -201,7 +211,9 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
     const int row_tiles = (a.sq + kRows - 1) / kRows;
     const int tile0 = !a.causal ? 0 : max(0, first - offset) / kRows;
     const int per_head = first >= length ? 0 : max(0, row_tiles - tile0);
-    const int steps = per_head * group;
+    // this workgroup's share of the steps
+    const long long steps = (long long)per_head * group;
+    const int begin = int(steps * split / a.key_splits), end = int(steps * (split + 1) / a.key_splits);
 
     using QueryCopy = RowCopy<T, D, kRows, 256, WIDE>;
     using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
@@ -225,14 +237,15 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
             stat = i < left ? from_mem[row0 + i] : (which < 2 ? kInf : 0.f);
         }
     };
-    int h = hkv * group, row0 = tile0 * kRows;
-    if (steps > 0) fetch(h, row0, base);
-    for (int step = 0; step < steps; ++step) {
-        const unsigned buffer = base + (step & 1) * Shape::kBufferBytes;
+    int h = hkv * group + (begin < end ? begin / per_head : 0);
+    int row0 = (tile0 + (begin < end ? begin % per_head : 0)) * kRows;
+    if (begin < end) fetch(h, row0, base);
+    for (int step = begin; step < end; ++step) {
+        const unsigned parity = (step - begin) & 1, buffer = base + parity * Shape::kBufferBytes;
         const unsigned r1 = buffer + query_row, c1 = buffer + query_column;
         const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
         const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
-        float* ts = reinterpret_cast<float*>(lds + (step & 1) * Shape::kBufferBytes + 2 * Shape::kQueryBytes + Shape::kGradBytes);
+        float* ts = reinterpret_cast<float*>(lds + parity * Shape::kBufferBytes + 2 * Shape::kQueryBytes + Shape::kGradBytes);
         if (tid < 4 * kRows) ts[tid] = stat;
         copies_done();
         const int this_row0 = row0;
@@ -242,18 +255,15 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
             row0 = tile0 * kRows;
             ++h;
         }
-        if (step + 1 < steps) fetch(h, row0, base + ((step + 1) & 1) * Shape::kBufferBytes);
+        if (step + 1 < end) fetch(h, row0, base + (parity ^ 1) * Shape::kBufferBytes);
 
         floatx16 p1 = zero16(), p2 = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            if constexpr (kKeysInLds) {
-                mma(p1, read_row<T, D>(r1, 0, s), read_row<T, D>(key1, 0, s));
-                mma(p2, read_row<T, D>(r2, 0, s), read_row<T, D>(key1 + Shape::kKeyBytes, 0, s));
-            } else {
-                mma(p1, read_row<T, D>(r1, 0, s), k1[s]);
-                mma(p2, read_row<T, D>(r2, 0, s), k2[s]);
-            }
+            if constexpr (M1) mma(p1, read_row<T, D>(r1, 0, s), kKeysInLds ? read_row<T, D>(key1, 0, s) : k1[kKeysInLds ? 0 : s]);
+            if constexpr (M2)
+                mma(p2, read_row<T, D>(r2, 0, s),
+                    kKeysInLds ? read_row<T, D>(key1 + Shape::kKeyBytes, 0, s) : k2[kKeysInLds ? 0 : s]);
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -261,8 +271,8 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
             const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
-                p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j])) * lam;
+                if constexpr (M1) p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
+                if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j])) * lam;
             }
         }
         if (this_row0 < all_from) {
@@ -291,8 +301,8 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
                 const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    p1[4 * g + j] *= t[4 * g + j] - d1[j];
-                    p2[4 * g + j] *= d2[j] - t[4 * g + j];
+                    if constexpr (DK1) p1[4 * g + j] *= t[4 * g + j] - d1[j];
+                    if constexpr (DK2) p2[4 * g + j] *= d2[j] - t[4 * g + j];
                 }
             }
 #pragma unroll
@@ -300,22 +310,27 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
                 const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d) {
-                    mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
-                    mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
+                    if constexpr (DK1) mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
+                    if constexpr (DK2) mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
                 }
             }
         }
     }
     if (key >= a.sk) return;
-    if constexpr (DK) {
-        T* dk = static_cast<T*>(a.dk) + ((size_t(b) * a.sk + key) * a.hk + hkv) * 2 * a.d;
-        const bool whole = a.d % 4 == 0;
-        store_row(dk, dk1, a.d, whole, a.scale, hi);
-        store_row(dk + a.d, dk2, a.d, whole, a.scale, hi);
+    const size_t at = (size_t(b) * a.sk + key) * a.hk + hkv;
+    const bool whole = a.d % 4 == 0;
+    if (a.key_splits > 1) {
+        // [split][key][dk1, dk2, dv], unscaled
+        float* part = a.key_part + (size_t(split) * a.n * a.sk * a.hk + at) * (2 * a.d + a.dv);
+        if constexpr (DK1) store_row(part, dk1, a.d, whole && a.o_wide, 1.f, hi);
+        if constexpr (DK2) store_row(part + a.d, dk2, a.d, whole && a.o_wide, 1.f, hi);
+        if constexpr (DVAL) store_row(part + 2 * a.d, dval, a.dv, whole && a.o_wide, 1.f, hi);
+        return;
     }
-    if constexpr (DVAL)
-        store_row(static_cast<T*>(a.dv_out) + ((size_t(b) * a.sk + key) * a.hk + hkv) * a.dv, dval, a.dv, a.o_wide, 1.f,
-                  hi);
+    T* dk = static_cast<T*>(a.dk) + at * 2 * a.d;
+    if constexpr (DK1) store_row(dk, dk1, a.d, whole, a.scale, hi);
+    if constexpr (DK2) store_row(dk + a.d, dk2, a.d, whole, a.scale, hi);
+    if constexpr (DVAL) store_row(static_cast<T*>(a.dv_out) + at * a.dv, dval, a.dv, a.o_wide, 1.f, hi);
 }
 
 namespace {
@@ -330,42 +345,49 @@ struct QuerySideShape {
 
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does.
-template <typename T, int D, int DV, bool WIDE>
+template <typename T, int D, int DV, bool WIDE, int DO>
 __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
     constexpr int kKeys = Shape::kKeys;
+    constexpr bool M1 = DO & kFirst, M2 = DO & kSecond;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
     const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int tile = tiles - 1 - id % tiles;
-    const int h = id / tiles % a.hq, b = id / tiles / a.hq;
+    const int tile = tiles - 1 - id % tiles, split = id / tiles % a.query_splits;
+    const int h = id / tiles / a.query_splits % a.hq, b = id / tiles / a.query_splits / a.hq;
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
     const int first = tile * kAttnRows + wave * 32, row = first + (lane & 31);
     const int last = attn_last_key(a, row, length);
     const int first_last = attn_last_key(a, first, length);
     const int wave_end = attn_last_key(a, min(first + 31, a.sq - 1), length) + 1;
-    const int end = attn_last_key(a, min(tile * kAttnRows + kAttnRows, a.sq) - 1, length) + 1;
+    const int seen = attn_last_key(a, min(tile * kAttnRows + kAttnRows, a.sq) - 1, length) + 1;
+    // this workgroup's share of the stages
+    const long long stages = (seen + kKeys - 1) / kKeys;
+    const int begin = int(stages * split / a.query_splits) * kKeys;
+    const int end = min(seen, int(stages * (split + 1) / a.query_splits) * kKeys);
     const float lam = attn_lambda(a, h);
 
     const T* kp = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
     const T* vp = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
     const bool valid = row < a.sq;
-    Operand<T> q1[D / 16], q2[D / 16], g[DV / 16];
+    Operand<T> q1[M1 ? D / 16 : 1], q2[M2 ? D / 16 : 1], g[DV / 16];
     {
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh;
-        load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
-        load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
+        if constexpr (M1) load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
+        if constexpr (M2) load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
         load_row_operands<T, DV, WIDE>(g, static_cast<const T*>(a.dout) + b * a.gb + (long long)row * a.gt + h * a.gh, a.dv,
                                  valid, lane);
     }
     const size_t at = (size_t(b) * a.hq + h) * 2 * a.sq + row;
     const float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
     const float d1 = valid ? a.delta[at] : 0.f, d2 = valid ? a.delta[at + a.sq] : 0.f;
-    floatx16 dq1[D / 32], dq2[D / 32];
+    floatx16 dq1[M1 ? D / 32 : 1], dq2[M2 ? D / 32 : 1];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) dq1[d] = dq2[d] = zero16();
+    for (auto& x : dq1) x = zero16();
+#pragma unroll
+    for (auto& x : dq2) x = zero16();
 
     using KeyCopy = RowCopy<T, D, kKeys, 256, WIDE>;
     using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
@@ -375,14 +397,15 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
     const unsigned key_row = row_lane<T, D>(lane), key_column = column_lane<T, D>(lane);
     const unsigned value_row = row_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
     auto fetch = [&](int key, unsigned buffer) {
-        key_copy.start(buffer, kp + (long long)key * a.kt, a.kt, end - key, tid);
-        key_copy.start(buffer + Shape::kKeyBytes, kp + a.km + (long long)key * a.kt, a.kt, end - key,
+        if constexpr (M1) key_copy.start(buffer, kp + (long long)key * a.kt, a.kt, end - key, tid);
+        if constexpr (M2)
+            key_copy.start(buffer + Shape::kKeyBytes, kp + a.km + (long long)key * a.kt, a.kt, end - key,
                        tid);
         value_copy.start(buffer + 2 * Shape::kKeyBytes, vp + (long long)key * a.vt, a.vt, end - key,
                          tid);
     };
-    if (end > 0) fetch(0, base);
-    for (int i = 0, key = 0; key < end; ++i, key += kKeys) {
+    if (begin < end) fetch(begin, base);
+    for (int i = 0, key = begin; key < end; ++i, key += kKeys) {
         const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
         const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
         const unsigned r2 = r1 + Shape::kKeyBytes, c2 = c1 + Shape::kKeyBytes, rv = buffer + value_row;
@@ -392,15 +415,15 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
-            mma(p2, read_row<T, D>(r2, 0, s), q2[s]);
+            if constexpr (M1) mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
+            if constexpr (M2) mma(p2, read_row<T, D>(r2, 0, s), q2[s]);
         }
 #pragma unroll
         for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rv, 0, s), g[s]);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
-            p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2)) * lam;
+            if constexpr (M1) p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
+            if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2)) * lam;
         }
         if (key + 31 > first_last) {
 #pragma unroll
@@ -409,36 +432,76 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            p1[r] *= t[r] - d1;
-            p2[r] *= d2 - t[r];
+            if constexpr (M1) p1[r] *= t[r] - d1;
+            if constexpr (M2) p2[r] *= d2 - t[r];
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
-                mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
-                mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
+                if constexpr (M1) mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
+                if constexpr (M2) mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
             }
         }
     }
     if (!valid) return;
-    T* dq = static_cast<T*>(a.dq) + ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
+    const size_t out = ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
     const bool whole = a.d % 4 == 0;
-    store_row(dq, dq1, a.d, whole, a.scale, hi);
-    store_row(dq + a.d, dq2, a.d, whole, a.scale, hi);
+    if (a.query_splits > 1) {
+        float* part = a.query_part + size_t(split) * a.n * a.sq * a.hq * 2 * a.d + out;
+        if constexpr (M1) store_row(part, dq1, a.d, whole, 1.f, hi);
+        if constexpr (M2) store_row(part + a.d, dq2, a.d, whole, 1.f, hi);
+        return;
+    }
+    T* dq = static_cast<T*>(a.dq) + out;
+    if constexpr (M1) store_row(dq, dq1, a.d, whole, a.scale, hi);
+    if constexpr (M2) store_row(dq + a.d, dq2, a.d, whole, a.scale, hi);
+}
+
+// Adds up the parts of workgroups that shared the steps, in their order:
+// rows of `width` values, of which the first `scaled` go to `a0` (times scale),
+// the rest to `a1`.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_parts_kernel(const float* part, int splits, long long rows, int width, int scaled,
+                                                         float scale, T* a0, T* a1) {
+    const long long n = rows * width;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        float t = 0.f;
+        for (int s = 0; s < splits; ++s) t += part[s * n + i];
+        const long long row = i / width;
+        const int col = int(i - row * width);
+        if (col < scaled)
+            a0[row * scaled + col] = T(t * scale);
+        else
+            a1[row * (width - scaled) + col - scaled] = T(t);
+    }
 }
 
 namespace {
 
-template <typename T, int D, int DV, bool DK, bool DVAL>
+template <typename T, int D, int DV, int DO>
 hipError_t launch_key_side(const AttnArgs& a, hipStream_t s) {
     using Shape = KeySideShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hk * ((a.sk + kKeySideKeys - 1) / kKeySideKeys);
-    auto kernel = a.wide ? attn_key_side_kernel<T, D, DV, true, DK, DVAL> : attn_key_side_kernel<T, D, DV, false, DK, DVAL>;
+    const long long blocks = (long long)a.n * a.hk * a.key_splits * ((a.sk + kKeySideKeys - 1) / kKeySideKeys);
+    auto kernel = a.wide ? attn_key_side_kernel<T, D, DV, true, DO> : attn_key_side_kernel<T, D, DV, false, DO>;
     if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s,
-                         nullptr, nullptr, a);
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, nullptr, a);
+}
+template <typename T, int D, int DV, int DO>
+hipError_t launch_query_side(const AttnArgs& a, hipStream_t s, hipEvent_t stop) {
+    using Shape = QuerySideShape<T, D, DV>;
+    const long long blocks = (long long)a.n * a.hq * a.query_splits * ((a.sq + kAttnRows - 1) / kAttnRows);
+    auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true, DO> : attn_query_side_kernel<T, D, DV, false, DO>;
+    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, stop, a);
+}
+template <typename T>
+hipError_t launch_parts(const float* part, int splits, long long rows, int width, int scaled, float scale, void* a0, void* a1,
+                        hipStream_t s, hipEvent_t stop) {
+    const long long blocks = (rows * width + 255) / 256;
+    return launch_kernel(attn_parts_kernel<T>, dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, nullptr, stop,
+                         part, splits, rows, width, scaled, scale, static_cast<T*>(a0), static_cast<T*>(a1));
 }
 
 template <typename T, int D, int DV>
@@ -449,20 +512,34 @@ hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& e
         return e;
     if (hipError_t e = launch_kernel(attn_dlam_kernel, dim3(a.lam_step ? a.hq : 1), dim3(256), 0, s, nullptr, nullptr, a))
         return e;
-    // fp32 operands and accumulators of both gradients at the largest widths
-    // would not fit the 512 registers of a lane: there dk and dv are two passes
-    if constexpr (sizeof(T) * D >= 512) {
-        if (hipError_t e = launch_key_side<T, D, DV, true, false>(a, s)) return e;
-        if (hipError_t e = launch_key_side<T, D, DV, false, true>(a, s)) return e;
+    // At the largest widths the operands and accumulators of all gradients do
+    // not fit a lane's registers: there they are computed one after another.
+    constexpr bool kApart = sizeof(T) * D >= 512;
+    if constexpr (kApart) {
+        if (hipError_t e = launch_key_side<T, D, DV, kFirst>(a, s)) return e;
+        if (hipError_t e = launch_key_side<T, D, DV, kSecond>(a, s)) return e;
+        if (hipError_t e = launch_key_side<T, D, DV, kValues>(a, s)) return e;
+    } else if constexpr (sizeof(T) * D >= 256 && sizeof(T) == 2) {
+        if (hipError_t e = launch_key_side<T, D, DV, kBoth>(a, s)) return e;
+        if (hipError_t e = launch_key_side<T, D, DV, kValues>(a, s)) return e;
     } else {
-        if (hipError_t e = launch_key_side<T, D, DV, true, true>(a, s)) return e;
+        if (hipError_t e = launch_key_side<T, D, DV, kAll>(a, s)) return e;
     }
-    using Shape = QuerySideShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnRows - 1) / kAttnRows);
-    auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true> : attn_query_side_kernel<T, D, DV, false>;
-    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr,
-                         ev.stop, a);
+    if (a.key_splits > 1)
+        if (hipError_t e = launch_parts<T>(a.key_part, a.key_splits, (long long)a.n * a.sk * a.hk, 2 * a.d + a.dv, 2 * a.d,
+                                           a.scale, a.dk, a.dv_out, s, nullptr))
+            return e;
+    hipEvent_t last = a.query_splits > 1 ? nullptr : ev.stop;
+    if constexpr (kApart) {
+        if (hipError_t e = launch_query_side<T, D, DV, kFirst>(a, s, nullptr)) return e;
+        if (hipError_t e = launch_query_side<T, D, DV, kSecond>(a, s, last)) return e;
+    } else {
+        if (hipError_t e = launch_query_side<T, D, DV, kBoth>(a, s, last)) return e;
+    }
+    if (a.query_splits > 1)
+        return launch_parts<T>(a.query_part, a.query_splits, (long long)a.n * a.sq * a.hq, 2 * a.d, 2 * a.d, a.scale, a.dq,
+                               nullptr, s, ev.stop);
+    return hipSuccess;
 }
 
 template <typename T>
