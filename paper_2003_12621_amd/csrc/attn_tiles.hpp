@@ -302,6 +302,15 @@ __device__ __forceinline__ void load_row_operands(Operand<T> (&o)[W / 16], const
     }
 }
 
+// Makes the compiler wait here for the memory that an operand comes from.  It
+// does not know of the copies in flight, and a wait of its own inside a loop
+// for an operand loaded before it would be one for all of them.
+template <typename T, int N>
+__device__ __forceinline__ void settle(Operand<T> (&o)[N]) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) asm volatile("" : "+v"(o[s].v));
+}
+
 // Four consecutive elements of an output row, elements from `cols` on left out
 // (`wide`: cols is a multiple of 4).
 template <typename T>

@@ -118,7 +118,7 @@ struct KeySideShape {
     static constexpr int kRows = 32;                                   // queries per stage
     static constexpr int kQueryBytes = TileShape<T, D>::bytes(kRows);
     static constexpr int kGradBytes = TileShape<T, DV>::bytes(kRows);
-    static constexpr int kStatBytes = 1024;                            // 4 values a row; tiles start at multiples of 1024
+    static constexpr int kStatBytes = 1024;                            // 4 values a row, lam; tiles start at multiples of 1024
     static constexpr int kBufferBytes = 2 * kQueryBytes + kGradBytes + kStatBytes;
     // The workgroup's keys stay in LDS where two workgroups a compute unit are
     // aimed at: as operands in registers they would not leave room for that.
@@ -199,6 +199,9 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
             load_row_operands<T, DV, WIDE>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
                                      a.dv, exists, lane);
     }
+    if constexpr (!kKeysInLds && M1) settle(k1);
+    if constexpr (!kKeysInLds && M2) settle(k2);
+    if constexpr (DK) settle(v);
     floatx16 dk1[DK1 ? D / 32 : 1], dk2[DK2 ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
 #pragma unroll
     for (auto& x : dk1) x = zero16();
@@ -230,11 +233,15 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
         query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
         grad_copy.start(buffer + 2 * Shape::kQueryBytes,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
-        if (tid < 4 * kRows) {
-            // lse of both maps, then delta of both; rows beyond the last have no terms
+        if (tid <= 4 * kRows) {
+            // lse of both maps, then delta of both (rows beyond the last have no terms), and lam
             const int i = tid % kRows, which = tid / kRows;
             const float* from_mem = (which < 2 ? a.lse : a.delta) + ((size_t(b) * a.hq + h) * 2 + which % 2) * a.sq;
-            stat = i < left ? from_mem[row0 + i] : (which < 2 ? kInf : 0.f);
+            stat = which < 2 ? kInf : 0.f;
+            if (which == 4)
+                stat = attn_lambda(a, h);
+            else if (i < left)
+                stat = from_mem[row0 + i];
         }
     };
     int h = hkv * group + (begin < end ? begin / per_head : 0);
@@ -246,10 +253,9 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
         const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
         const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
         float* ts = reinterpret_cast<float*>(lds + parity * Shape::kBufferBytes + 2 * Shape::kQueryBytes + Shape::kGradBytes);
-        if (tid < 4 * kRows) ts[tid] = stat;
+        if (tid <= 4 * kRows) ts[tid] = stat;
         copies_done();
         const int this_row0 = row0;
-        const float lam = attn_lambda(a, h);
         row0 += kRows;
         if (row0 >= a.sq) {
             row0 = tile0 * kRows;
@@ -257,6 +263,7 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
         }
         if (step + 1 < end) fetch(h, row0, base + (parity ^ 1) * Shape::kBufferBytes);
 
+        const float lam = ts[4 * kRows];
         floatx16 p1 = zero16(), p2 = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
@@ -277,8 +284,11 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
         }
         if (this_row0 < all_from) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (this_row0 + acc_row(r, hi) < from) p1[r] = p2[r] = 0.f;
+            for (int r = 0; r < 16; ++r) {
+                const bool hidden = this_row0 + acc_row(r, hi) < from;
+                p1[r] = hidden ? 0.f : p1[r];
+                p2[r] = hidden ? 0.f : p2[r];
+            }
         }
         if constexpr (DVAL) {
             floatx16 w;
@@ -381,8 +391,12 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
                                  valid, lane);
     }
     const size_t at = (size_t(b) * a.hq + h) * 2 * a.sq + row;
-    const float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
-    const float d1 = valid ? a.delta[at] : 0.f, d2 = valid ? a.delta[at + a.sq] : 0.f;
+    float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
+    float d1 = valid ? a.delta[at] : 0.f, d2 = valid ? a.delta[at + a.sq] : 0.f;
+    asm volatile("" : "+v"(lse1), "+v"(lse2), "+v"(d1), "+v"(d2));
+    if constexpr (M1) settle(q1);
+    if constexpr (M2) settle(q2);
+    settle(g);
     floatx16 dq1[M1 ? D / 32 : 1], dq2[M2 ? D / 32 : 1];
 #pragma unroll
     for (auto& x : dq1) x = zero16();
@@ -427,8 +441,11 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
         }
         if (key + 31 > first_last) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key + acc_row(r, hi) > last) p1[r] = p2[r] = 0.f;
+            for (int r = 0; r < 16; ++r) {
+                const bool hidden = acc_row(r, hi) > last - key;
+                p1[r] = hidden ? 0.f : p1[r];
+                p2[r] = hidden ? 0.f : p2[r];
+            }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {

@@ -54,8 +54,7 @@ __device__ __forceinline__ void softmax_step(floatx16& s, RowState& st, floatx16
 // Hides keys beyond `last` (of the lane's query) in a score tile of keys key0 ...
 __device__ __forceinline__ void mask_scores(floatx16& s, int key0, int last, int hi) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-        if (key0 + acc_row(r, hi) > last) s[r] = -kInf;
+    for (int r = 0; r < 16; ++r) s[r] = acc_row(r, hi) > last - key0 ? -kInf : s[r];
 }
 
 // A wave takes one map of RB x 32 query rows: half the waves of a workgroup
@@ -114,6 +113,7 @@ attn_forward_kernel(AttnArgs a) {
         load_row_operands<T, D, WIDE>(q[r],
                                       static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + h * a.qh + map * a.qm,
                                       a.d, i < a.sq, lane);
+        settle(q[r]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[r][d] = zero16();
         st[r] = RowState{-kInf, 0.f};
@@ -291,6 +291,7 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
         load_row_operands<T, D, WIDE>(
             q[m], static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + head * a.qh + (map0 + m) * a.qm, a.d, valid,
             lane);
+        settle(q[m]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[m][d] = zero16();
         st[m] = RowState{-kInf, 0.f};
