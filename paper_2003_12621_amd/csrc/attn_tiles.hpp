@@ -89,9 +89,9 @@ __device__ __forceinline__ float to_float(T x) {
 // An LDS tile: rows of W elements in 16-byte chunks, without padding (copies
 // from memory fill 1024 consecutive bytes a wave).  Chunk c of row r lies in
 // place c ^ swizzle(r) of its row, so that 16 lanes that read one chunk of 16
-// rows, or two neighbouring chunks of 4 consecutive rows, use all banks alike:
-// of the rows that start in the same bank, 8 in a row differ in the swizzle, and
-// consecutive ones in more than its last bit.  Period: 16 rows.
+// rows, or 32 lanes that read 4 neighbouring chunks of 4 consecutive rows, use
+// all 64 banks alike: of the rows that start in the same bank, all of 16
+// consecutive rows differ in the swizzle, and those of 4 by multiples of 4.
 template <typename T, int W>
 struct TileShape {
     static constexpr int kChunk = 16 / sizeof(T);          // elements
@@ -99,8 +99,8 @@ struct TileShape {
     static constexpr int bytes(int rows) { return rows * W * int(sizeof(T)); }
     static __device__ __forceinline__ int swizzle(int row) {
         if constexpr (kRowChunks == 4) return (row >> 2) & 3;
-        if constexpr (kRowChunks == 8) return ((row >> 1) & 3) << 1 | ((row >> 3) & 1);
-        return (row & 7) << 1 | ((row >> 3) & 1);
+        if constexpr (kRowChunks == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+        return (row & 3) << 2 | ((row >> 2) & 3);
     }
     static __device__ __forceinline__ unsigned at(int row, int chunk) {
         return unsigned(row * kRowChunks + (chunk ^ swizzle(row))) * 16;
@@ -158,8 +158,7 @@ template <typename T, int W>
 __device__ __forceinline__ Operand<T> read_column(unsigned at, int row0, int col0, int s) {
     using Shape = TileShape<T, W>;
     constexpr int kRowBytes = Shape::kRowChunks * 16;
-    // what 8 rows further changes of the swizzle
-    constexpr unsigned kEight = Shape::kRowChunks == 4 ? 2 : 1;
+    constexpr unsigned kEight = 2;      // what 8 rows further changes of the swizzle
     const int distance = (row0 + 16 * s) * kRowBytes;
     at ^= unsigned(col0 / Shape::kChunk) * 16;
     Operand<T> o;
@@ -167,7 +166,7 @@ __device__ __forceinline__ Operand<T> read_column(unsigned at, int row0, int col
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int j = e & 3, far = e >> 2;
-            const unsigned turned = (Shape::kRowChunks == 8 ? 2 * (j >> 1) : 2 * j) ^ (far * kEight);
+            const unsigned turned = (Shape::kRowChunks == 8 ? 4 * (j >> 1) : 4 * j) ^ (far * kEight);
             o.v[e] = lds_at<float>(at ^ (turned * 16), distance + (8 * far + j) * kRowBytes);
         }
     } else {

@@ -21,19 +21,23 @@ constexpr float kMaxSlack = 8.f;
 struct RowState {
     float m, l;     // reference maximum (log2 units), sum of this half's terms
 };
+// Before a row has seen a key: below every score, but finite, so that the terms
+// of hidden keys are zero.
+constexpr float kNoMax = -3e38f;
 
 // Scores of 32 keys become terms exp2(score - m); `acc` is rescaled where the
-// reference maximum moves.  A row that has seen no key keeps m = -inf.
+// reference maximum moves.  (The maximum of three NaNs is one, and stays out of
+// m: a NaN score makes its row NaN through its term.)
 template <int DT>
 __device__ __forceinline__ void softmax_step(floatx16& s, RowState& st, floatx16 (&acc)[DT], float scale_log2) {
-    float top = s[0];
+    float top = vmax(s[0], s[1]);
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    for (int r = 2; r < 16; r += 2) top = vmax3(top, s[r], s[r + 1]);
     const float2 t2 = both_halves(top);
-    top = fmaxf(t2.x, t2.y) * scale_log2;
+    top = vmax(t2.x, t2.y) * scale_log2;
     if (__ballot(top > st.m + kMaxSlack) != 0) {
-        const float m = fmaxf(st.m, top);
-        const float alpha = m == -kInf ? 1.f : exp2_fast(st.m - m);
+        const float m = top > st.m ? top : st.m;
+        const float alpha = exp2_fast(st.m - m);
         st.m = m;
         st.l *= alpha;
 #pragma unroll
@@ -41,11 +45,10 @@ __device__ __forceinline__ void softmax_step(floatx16& s, RowState& st, floatx16
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
     }
-    const float ref = st.m == -kInf ? 0.f : st.m;
     float sum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        s[r] = exp2_fast(fmaf(s[r], scale_log2, -ref));
+        s[r] = exp2_fast(fmaf(s[r], scale_log2, -st.m));
         sum += s[r];
     }
     st.l += sum;
@@ -65,14 +68,15 @@ __device__ __forceinline__ void mask_scores(floatx16& s, int key0, int last, int
 // alone would take 256 registers.
 template <typename T, int D, int DV>
 struct ForwardShape {
-    static constexpr int kRowBlocks = DV <= 128 ? 2 : 1;
-    static constexpr int kWaves = kAttnRows / 32 / kRowBlocks * 2;
+    static constexpr int kRowBlocks = 1;
+    static constexpr int kWaves = 4;
+    static constexpr int kRows = kWaves / 2 * 32 * kRowBlocks;           // of a workgroup
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kKeys = sizeof(T) * DV <= 128 ? 64 : 32;         // keys per stage
-    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;         // workgroups per compute unit aimed at
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 3 : (sizeof(T) * DV <= 512 ? 2 : 1);         // workgroups per compute unit aimed at
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
-    static constexpr int kJoinBytes = kAttnRows * DV * 4;
+    static constexpr int kJoinBytes = kRows * DV * 4;
     static constexpr int kLds = 2 * kBufferBytes > kJoinBytes ? 2 * kBufferBytes : kJoinBytes;
 };
 
@@ -88,17 +92,17 @@ attn_forward_kernel(AttnArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, group = wave >> 1;
-    const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
+    const int tiles = (a.sq + Shape::kRows - 1) / Shape::kRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     const int tile = tiles - 1 - id % tiles;           // under a causal mask the longest first
     const int h = id / tiles % a.hq, b = id / tiles / a.hq;
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
 
-    const int first = tile * kAttnRows + group * (32 * RB), row = first + (lane & 31);
+    const int first = tile * Shape::kRows + group * (32 * RB), row = first + (lane & 31);
     const int first_last = attn_last_key(a, first, length);          // last key of the wave's first row
     const int wave_end = attn_last_key(a, min(first + 32 * RB, a.sq) - 1, length) + 1;
-    const int end = attn_last_key(a, min(tile * kAttnRows + kAttnRows, a.sq) - 1, length) + 1;
+    const int end = attn_last_key(a, min(tile * Shape::kRows + Shape::kRows, a.sq) - 1, length) + 1;
 
     const T* k1 = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
     const T* v = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
@@ -116,7 +120,7 @@ attn_forward_kernel(AttnArgs a) {
         settle(q[r]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[r][d] = zero16();
-        st[r] = RowState{-kInf, 0.f};
+        st[r] = RowState{kNoMax, 0.f};
         last[r] = attn_last_key(a, i, length);
     }
 
@@ -294,7 +298,7 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
         settle(q[m]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[m][d] = zero16();
-        st[m] = RowState{-kInf, 0.f};
+        st[m] = RowState{kNoMax, 0.f};
     }
 
     using KeyCopy = RowCopy<T, D, Shape::kKeys, 64, WIDE>;
@@ -372,7 +376,7 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
         }
     }
     __syncthreads();
-    float top[2] = {-kInf, -kInf}, sum[2] = {0.f, 0.f};
+    float top[2] = {kNoMax, kNoMax}, sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
         const float* x = stats + m * 64 + (lane & 31);
@@ -380,13 +384,13 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
         for (int w = 0; w < kKeyWaves; ++w) top[m] = fmaxf(top[m], x[w * 128]);
 #pragma unroll
         for (int w = 0; w < kKeyWaves; ++w)
-            sum[m] += x[w * 128] == -kInf ? 0.f : exp2_fast(x[w * 128] - top[m]) * x[w * 128 + 32];
+            sum[m] = fmaf(exp2_fast(x[w * 128] - top[m]), x[w * 128 + 32], sum[m]);
     }
     {
         float4* own = reinterpret_cast<float4*>(lds + wave * Shape::kTileBytes) + lane;
 #pragma unroll
         for (int m = 0; m < MAPS; ++m) {
-            const float f = st[m].m == -kInf ? 0.f : exp2_fast(st[m].m - (map0 + m ? top[1] : top[0]));
+            const float f = exp2_fast(st[m].m - (map0 + m ? top[1] : top[0]));
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -423,14 +427,14 @@ __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
     const int packed = blockIdx.x % rows, kv = blockIdx.x / rows, b = kv / a.hk, h = kv % a.hk * group + packed / a.sq;
     const int i = packed % a.sq;
     const float4* stats = reinterpret_cast<const float4*>(a.part_stats) + size_t(blockIdx.x) * a.splits;
-    float top = -kInf;
+    float top = kNoMax;
     for (int s = 0; s < a.splits; ++s) top = fmaxf(top, map ? stats[s].z : stats[s].x);
     float sum = 0.f;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s = 0; s < a.splits; ++s) {
         const float4 st = stats[s];
         const float m = map ? st.z : st.x, l = map ? st.w : st.y;
-        if (m == -kInf) continue;
+        if (m == kNoMax) continue;
         const float f = exp2_fast(m - top);
         sum = fmaf(l, f, sum);
         if (col < DV) {
@@ -458,7 +462,7 @@ namespace {
 template <typename T, int D, int DV>
 hipError_t launch_tiled(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
     using Shape = ForwardShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnRows - 1) / kAttnRows);
+    const long long blocks = (long long)a.n * a.hq * ((a.sq + Shape::kRows - 1) / Shape::kRows);
     auto kernel = a.wide ? attn_forward_kernel<T, D, DV, true> : attn_forward_kernel<T, D, DV, false>;
     if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
     return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(Shape::kThreads), Shape::kLds, s, ev.start,
