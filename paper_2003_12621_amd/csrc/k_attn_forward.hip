@@ -73,7 +73,7 @@ struct ForwardShape {
     static constexpr int kRows = kWaves / 2 * 32 * kRowBlocks;           // of a workgroup
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kKeys = sizeof(T) * DV <= 128 ? 64 : 32;         // keys per stage
-    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 3 : (sizeof(T) * DV <= 512 ? 2 : 1);         // workgroups per compute unit aimed at
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 4 : (sizeof(T) * DV <= 512 ? 2 : 1);         // workgroups per compute unit aimed at
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
     static constexpr int kJoinBytes = kRows * DV * 4;
