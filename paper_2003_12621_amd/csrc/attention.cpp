@@ -116,8 +116,8 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     if (shape < 0) return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "attention: dim at most 128 and dim_v at most 256");
     // Token counts and launch sizes stay below 2^30; element offsets are 64-bit.
     const double rows = double(p.batch) * p.heads_q * p.queries, keys = double(p.batch) * p.heads_q * p.keys;
-    if (p.queries > (1 << 30) || p.keys > (1 << 30) || rows > double(1u << 30) || keys > double(1u << 30))
-        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "attention: batch * heads_q * max(queries, keys) must be at most 2^30");
+    if (p.queries > (1 << 28) || p.keys > (1 << 28) || rows > double(1u << 30) || keys > double(1u << 30))
+        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "attention: at most 2^28 queries and keys, and 2^30 of them over all heads and sequences");
 
     char archbuf[64] = {0};
     if (device >= 0) {
@@ -147,7 +147,7 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->query_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_q * ((p.queries + 127LL) / 128),
                                                 (p.keys + 31LL) / 32);
     const size_t shared = key_part_bytes(p, plan->key_splits), other = query_part_bytes(p, plan->query_splits);
-    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * delta_parts(p) * 4) +
+    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (delta_parts(p) + 1) * 4) +
                         (shared > other ? shared : other);
     *out = plan;
     return FFTSPLIT_SUCCESS;
@@ -347,7 +347,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         // (the two kernels' parts in turn)
         a.key_splits = plan->key_splits;
         a.query_splits = plan->query_splits;
-        a.key_part = a.query_part = a.dlam_part + round256(size_t(p.heads_q) * a.parts * 4) / 4;
+        a.lam32 = a.dlam_part + size_t(p.heads_q) * a.parts;
+        a.key_part = a.query_part = a.dlam_part + round256(size_t(p.heads_q) * (a.parts + 1) * 4) / 4;
         a.dq = dq;
         a.dk = dk;
         a.dv_out = dv;

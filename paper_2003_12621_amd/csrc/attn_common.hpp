@@ -26,6 +26,12 @@ __device__ __forceinline__ float attn_lambda(const AttnArgs& a, int h) {
     return a.lam_f32 ? static_cast<const float*>(a.lam)[i] : float(static_cast<const __bf16*>(a.lam)[i]);
 }
 
+// A value at an address that is the same in all lanes, written before this
+// kernel started: by a scalar load, which the vector loads' count leaves out.
+__device__ __forceinline__ float uniform_load(const float* p) {
+    return *(const __attribute__((address_space(4))) float*)(p);
+}
+
 // 2^x by the hardware instruction (results below 2^-126 become zero: they are
 // terms of a sum whose largest is about 1).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

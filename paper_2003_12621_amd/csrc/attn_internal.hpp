@@ -60,6 +60,7 @@ struct AttnArgs {
     long long gb, gt, gh;            // batch, token, head strides of dout
     float* delta;                    // [n][hq][2][sq]
     float* dlam_part;                // [hq][parts]
+    float* lam32;                    // [hq]: lam in fp32
     int parts;
     int key_splits, query_splits;
     float* key_part;                 // [split][n][sk][hk][2 d + dv]

@@ -189,9 +189,24 @@ __device__ __forceinline__ void copy16(u32x4 rsrc, unsigned off, unsigned lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(lds)
                  : "memory", "m0");
 }
-// All copies that this thread's wave has started are complete, in all waves.
+// The same of 4 bytes a lane.
+__device__ __forceinline__ void copy4(u32x4 rsrc, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(lds)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ u32x4 copy_source(const void* base, unsigned bytes) {
+    const uint64_t p = reinterpret_cast<uintptr_t>(base);
+    u32x4 rsrc;
+    rsrc[0] = __builtin_amdgcn_readfirstlane(unsigned(p));
+    rsrc[1] = __builtin_amdgcn_readfirstlane(unsigned(p >> 32) & 0xffffu);
+    rsrc[2] = __builtin_amdgcn_readfirstlane(bytes);
+    rsrc[3] = 0x00020000u;
+    return rsrc;
+}
+// All but the last LATER copies that each wave has started are complete, in all waves.
+template <int LATER = 0>
 __device__ __forceinline__ void copies_done() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
     __syncthreads();
 }
 
@@ -216,7 +231,9 @@ struct RowCopy {
     static constexpr int kChunks = ROWS * Shape::kRowChunks;
     static constexpr int kPer = (kChunks + THREADS - 1) / THREADS;
     static constexpr bool kWhole = kChunks % THREADS == 0;
-    static constexpr int kCopies = WIDE ? kPer : 0;       // memory operations in flight after start
+    // Memory operations of a wave in flight after start; of every wave, where all
+    // have places.
+    static constexpr int kCopies = WIDE ? kPer : 0;
     static_assert(kChunks % 64 == 0, "whole waves");
 
     // Byte offsets of a thread's chunks from the tile's first row in memory, the
@@ -240,12 +257,7 @@ struct RowCopy {
         const unsigned bytes = n > 0 ? unsigned(((n - 1) * stride + cols) * int(sizeof(T))) : 0u;
         const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
         if constexpr (WIDE) {
-            const uint64_t p = reinterpret_cast<uintptr_t>(base);
-            u32x4 rsrc;
-            rsrc[0] = __builtin_amdgcn_readfirstlane(unsigned(p));
-            rsrc[1] = __builtin_amdgcn_readfirstlane(unsigned(p >> 32) & 0xffffu);
-            rsrc[2] = __builtin_amdgcn_readfirstlane(bytes);
-            rsrc[3] = 0x00020000u;
+            const u32x4 rsrc = copy_source(base, bytes);
             const unsigned lds = tile + wave * 1024;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
@@ -309,6 +321,12 @@ __device__ __forceinline__ void settle(Operand<T> (&o)[N]) {
 #pragma unroll
     for (int s = 0; s < N; ++s) asm volatile("" : "+v"(o[s].v));
 }
+
+// No instruction is moved across this.  Kernels that read their operands in
+// batches, one batch ahead of the products, put it between a batch's reads and
+// the products before it: left to itself the compiler, short of registers, puts
+// every read right before its product and waits for it there.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Four consecutive elements of an output row, elements from `cols` on left out
 // (`wide`: cols is a multiple of 4).

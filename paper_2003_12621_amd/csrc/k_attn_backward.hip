@@ -41,7 +41,7 @@ __device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool 
 
 }  // namespace
 
-// D1 and D2 of kAttnDeltaRows rows of one head, and their share of dlam.
+// D1 and lam D2 of kAttnDeltaRows rows of one head, and their share of dlam.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     __shared__ float sums[256 / kDeltaLanes];
@@ -49,6 +49,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     const int h = blockIdx.x % a.hq, c = blockIdx.x / a.hq % chunks, b = blockIdx.x / a.hq / chunks;
     const int l = threadIdx.x % kDeltaLanes, group = threadIdx.x / kDeltaLanes;
     const bool wide = a.wide && a.dv % 8 == 0;
+    const float lam = attn_lambda(a, h);
     float total = 0.f;
     for (int i = group; i < kAttnDeltaRows; i += 256 / kDeltaLanes) {
         const int row = c * kAttnDeltaRows + i;
@@ -75,12 +76,13 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
         if (l == 0) {
             float* delta = a.delta + (size_t(b) * a.hq + h) * 2 * a.sq + row;
             delta[0] = s1;
-            delta[a.sq] = s2;
+            delta[a.sq] = lam * s2;
         }
     }
     if (l == 0) sums[group] = total;
     __syncthreads();
     if (threadIdx.x == 0) {
+        if (b == 0 && c == 0) a.lam32[h] = lam;
         float t = 0.f;
         for (int i = 0; i < 256 / kDeltaLanes; ++i) t += sums[i];
         a.dlam_part[size_t(h) * a.parts + b * chunks + c] = -t;
@@ -115,17 +117,23 @@ constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
 
 template <typename T, int D, int DV>
 struct KeySideShape {
-    static constexpr int kRows = 32;                                   // queries per stage
+    // queries per stage: 64 where two such stages fit, which halves the steps' fixed cost
+    static constexpr int kRows = 32;
     static constexpr int kQueryBytes = TileShape<T, D>::bytes(kRows);
     static constexpr int kGradBytes = TileShape<T, DV>::bytes(kRows);
-    static constexpr int kStatBytes = 1024;                            // 4 values a row, lam; tiles start at multiples of 1024
+    static constexpr int kStatBytes = 1024;                            // 4 values a row, at most 64 rows; tiles start at multiples of 1024
     static constexpr int kBufferBytes = 2 * kQueryBytes + kGradBytes + kStatBytes;
     // The workgroup's keys stay in LDS where two workgroups a compute unit are
     // aimed at: as operands in registers they would not leave room for that.
     static constexpr bool kKeysInLds = sizeof(T) * DV <= 256;
-    static constexpr int kBlocks = kKeysInLds ? 2 : 1;
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;
+    static constexpr int kAhead = sizeof(T) * DV == 256 ? 0 : 1;
     static constexpr int kKeyBytes = kKeysInLds ? TileShape<T, D>::bytes(kKeySideKeys) : 0;
-    static constexpr int kLds = 2 * kBufferBytes + 2 * kKeyBytes;
+    // Stages in LDS: one worked on, the others on their way.  With one on its way
+    // a step waits for most of the memory's latency.
+    static constexpr int kRoom = (163840 / kBlocks - 2 * kKeyBytes) / kBufferBytes;
+    static constexpr int kStages = kRoom < 4 ? kRoom : 4;
+    static constexpr int kLds = kStages * kBufferBytes + 2 * kKeyBytes;
 };
 
 // Four values of an array in LDS that belong to rows 4 g .. 4 g + 3 of a lane's
@@ -157,14 +165,14 @@ constexpr int kAll = 7;
 // Each wave keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as
 // accumulators in registers.
 template <typename T, int D, int DV, bool WIDE, int DO>
-__global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_key_side_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 2) : 1)) void attn_key_side_kernel(AttnArgs a) {
     using Shape = KeySideShape<T, D, DV>;
     constexpr int kRows = Shape::kRows;
     constexpr bool DK = (DO & kBoth) != 0, DVAL = (DO & kValues) != 0;
     constexpr bool M1 = DVAL || (DO & kFirst), M2 = DVAL || (DO & kSecond);      // maps whose scores are needed
     constexpr bool DK1 = DO & kFirst, DK2 = DO & kSecond;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles = (a.sk + kKeySideKeys - 1) / kKeySideKeys;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     const int tile = id % tiles, split = id / tiles % a.key_splits, hkv = id / tiles / a.key_splits % a.hk;
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
     unsigned key1 = 0;      // LDS address of this lane's key
     {
         if constexpr (kKeysInLds) {
-            const unsigned tile1 = base + 2 * Shape::kBufferBytes;
+            const unsigned tile1 = base + Shape::kStages * Shape::kBufferBytes;
             const RowCopy<T, D, kKeySideKeys, 256, WIDE> key_copy(a.kt, a.d, tid);
             const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)first * a.kt + hkv * a.kh;
             key_copy.start(tile1, p, a.kt, length - first, tid);
@@ -218,110 +226,176 @@ __global__ __launch_bounds__(256, (KeySideShape<T, D, DV>::kBlocks)) void attn_k
     const long long steps = (long long)per_head * group;
     const int begin = int(steps * split / a.key_splits), end = int(steps * (split + 1) / a.key_splits);
 
-    using QueryCopy = RowCopy<T, D, kRows, 256, WIDE>;
+    // (small tiles: the first half of the threads copies q1, the second q2)
+    constexpr bool kHalves = kRows * TileShape<T, D>::kRowChunks < 256;
+    using QueryCopy = RowCopy<T, D, kRows, kHalves ? 128 : 256, WIDE>;
     using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
-    const QueryCopy query_copy(a.qt, a.d, tid);
+    const QueryCopy query_copy(a.qt, a.d, kHalves ? tid & 127 : tid);
     const GradCopy grad_copy(a.gt, a.dv, tid);
     const unsigned query_row = row_lane<T, D>(lane), query_column = column_lane<T, D>(lane);
     const unsigned grad_row = row_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
     const unsigned grad_column = column_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
-    float stat = 0.f;
-    auto fetch = [&](int h, int row0, unsigned buffer) {
-        const int left = a.sq - row0;
+    constexpr int kStages = Shape::kStages;
+    // copies of a wave per stage (the same for all waves)
+    constexpr int kCopies = (kHalves ? 1 : 2) * QueryCopy::kCopies + GradCopy::kCopies + 1;
+    static_assert(QueryCopy::kWhole && GradCopy::kWhole, "waves count their copies alike");
+    // A wave copies 64 of the 4 kRows values of lse of both maps and delta of
+    // both: one of them, or two of 32 rows each (then two waves copy the same).
+    constexpr int kStatRows = kRows == 64 ? 64 : 32;
+    const int stat_row = lane % kStatRows, stat_which = kRows == 64 ? wave : 2 * (wave & 1);
+    const unsigned stat_off = unsigned(stat_row + lane / kStatRows * a.sq) * 4;
+    auto fetch = [&](int h, int row0, bool any, unsigned buffer) {
+        const int left = any ? a.sq - row0 : 0;
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
-        query_copy.start(buffer, q, a.qt, left, tid);
-        query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
+        if constexpr (kHalves) {
+            query_copy.start(buffer + (wave >> 1) * Shape::kQueryBytes, q + (wave >> 1) * a.qm, a.qt, left, tid & 127);
+        } else {
+            query_copy.start(buffer, q, a.qt, left, tid);
+            query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
+        }
         grad_copy.start(buffer + 2 * Shape::kQueryBytes,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
-        if (tid <= 4 * kRows) {
-            // lse of both maps, then delta of both (rows beyond the last have no terms), and lam
-            const int i = tid % kRows, which = tid / kRows;
-            const float* from_mem = (which < 2 ? a.lse : a.delta) + ((size_t(b) * a.hq + h) * 2 + which % 2) * a.sq;
-            stat = which < 2 ? kInf : 0.f;
-            if (which == 4)
-                stat = attn_lambda(a, h);
-            else if (i < left)
-                stat = from_mem[row0 + i];
-        }
+        // Rows beyond the last are zero: their terms are finite, and dO, dP and delta zero.
+        const float* x = (stat_which < 2 ? a.lse : a.delta) + ((size_t(b) * a.hq + h) * 2 + (stat_which & 1)) * a.sq + row0;
+        const int maps = kRows == 64 ? 1 : 2;
+        copy4(copy_source(x, left > 0 ? unsigned(maps * a.sq - row0) * 4 : 0u), stat_row < left ? stat_off : kOutOfRange,
+              __builtin_amdgcn_readfirstlane(buffer + 2 * Shape::kQueryBytes + Shape::kGradBytes + stat_which * kRows * 4));
     };
+    // rows of the steps to come
     int h = hkv * group + (begin < end ? begin / per_head : 0);
     int row0 = (tile0 + (begin < end ? begin % per_head : 0)) * kRows;
-    if (begin < end) fetch(h, row0, base);
+    int next_h = h, next_row0 = row0;
+    unsigned fill = base;                 // the stage to be filled next
+    auto fetch_next = [&](bool any) {
+        fetch(next_h, next_row0, any, fill);
+        next_row0 += kRows;
+        if (next_row0 >= a.sq) {
+            next_row0 = tile0 * kRows;
+            ++next_h;
+        }
+        fill = fill + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : fill + Shape::kBufferBytes;
+    };
+    if (begin < end)
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) fetch_next(begin + i < end);
+    unsigned buffer = base;
     for (int step = begin; step < end; ++step) {
-        const unsigned parity = (step - begin) & 1, buffer = base + parity * Shape::kBufferBytes;
         const unsigned r1 = buffer + query_row, c1 = buffer + query_column;
         const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
         const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
-        float* ts = reinterpret_cast<float*>(lds + parity * Shape::kBufferBytes + 2 * Shape::kQueryBytes + Shape::kGradBytes);
-        if (tid <= 4 * kRows) ts[tid] = stat;
-        copies_done();
-        const int this_row0 = row0;
+        const float* stats = reinterpret_cast<const float*>(lds + (buffer - base) + 2 * Shape::kQueryBytes + Shape::kGradBytes);
+        // this stage is there, and all waves are done with the one before
+        copies_done<(kStages - 2) * kCopies>();
+        // (past the last step, copies of nothing keep the count)
+        fetch_next(step + kStages - 1 < end);
+        buffer = buffer + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : buffer + Shape::kBufferBytes;
+        const int stage_row0 = row0;
+        const float lam = uniform_load(a.lam32 + h);
         row0 += kRows;
         if (row0 >= a.sq) {
             row0 = tile0 * kRows;
             ++h;
         }
-        if (step + 1 < end) fetch(h, row0, base + (parity ^ 1) * Shape::kBufferBytes);
+#pragma unroll 1
+        for (int sub = 0; sub < kRows; sub += 32) {
+            const int block_row0 = stage_row0 + sub;
+            const float* ts = stats + sub;
+            if (sub > 0 && block_row0 >= a.sq) break;
+            // The products after the scores: dv (columns of dO with P1 - lam P2), t
+            // (rows of dO with v) and dk (columns of q with dS), two at a time; their
+            // operands from LDS are read kAhead pairs before they are used.
+            constexpr int N = DV / 32;                                // pairs of each (DV = 2 D)
+            static_assert(DV == 2 * D, "pairs");
+            constexpr int kT = DVAL ? N : 0, kK = kT + (DK ? N : 0), kEnd = kK + (DK ? N : 0), kAhead = Shape::kAhead;
+            Operand<T> ring[kAhead + 1][2];
+            auto read_pair = [&](int pair) {
+                if (pair >= kEnd) return;
+                Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (pair < kT) {
+                        const int i = 2 * pair + e;
+                        o[e] = read_column<T, DV>(cg, sub, 32 * (i % N), i / N);
+                    } else if (pair < kK) {
+                        o[e] = read_row<T, DV>(rg, sub, 2 * (pair - kT) + e);
+                    } else {
+                        const int i = pair - kK;                      // column block i % (D / 32), rows i / (D / 32)
+                        if (e ? DK2 : DK1) o[e] = read_column<T, D>(e ? c2 : c1, sub, 32 * (i % (D / 32)), i / (D / 32));
+                    }
+                }
+            };
 
-        const float lam = ts[4 * kRows];
-        floatx16 p1 = zero16(), p2 = zero16();
+            floatx16 p1 = zero16(), p2 = zero16();
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            if constexpr (M1) mma(p1, read_row<T, D>(r1, 0, s), kKeysInLds ? read_row<T, D>(key1, 0, s) : k1[kKeysInLds ? 0 : s]);
-            if constexpr (M2)
-                mma(p2, read_row<T, D>(r2, 0, s),
-                    kKeysInLds ? read_row<T, D>(key1 + Shape::kKeyBytes, 0, s) : k2[kKeysInLds ? 0 : s]);
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 l1 = rows_of(ts, g, hi), l2 = rows_of(ts + kRows, g, hi);
-            const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (M1) p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
-                if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j])) * lam;
+            for (int s = 0; s < D / 16; ++s) {
+                if constexpr (M1) mma(p1, read_row<T, D>(r1, sub, s), kKeysInLds ? read_row<T, D>(key1, 0, s) : k1[kKeysInLds ? 0 : s]);
+                if constexpr (M2)
+                    mma(p2, read_row<T, D>(r2, sub, s),
+                        kKeysInLds ? read_row<T, D>(key1 + Shape::kKeyBytes, 0, s) : k2[kKeysInLds ? 0 : s]);
             }
-        }
-        if (this_row0 < all_from) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const bool hidden = this_row0 + acc_row(r, hi) < from;
-                p1[r] = hidden ? 0.f : p1[r];
-                p2[r] = hidden ? 0.f : p2[r];
-            }
-        }
-        if constexpr (DVAL) {
-            floatx16 w;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = p1[r] - p2[r];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Operand<T> x = acc_operand<T>(w, s);
-#pragma unroll
-                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(cg, 0, 32 * d, s), x);
-            }
-        }
-        if constexpr (DK) {
-            floatx16 t = zero16();
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rg, 0, s), v[s]);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float4 u1 = rows_of(ts + 2 * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
-                const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+                const float4 l1 = rows_of(ts, g, hi), l2 = rows_of(ts + kRows, g, hi);
+                const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if constexpr (DK1) p1[4 * g + j] *= t[4 * g + j] - d1[j];
-                    if constexpr (DK2) p2[4 * g + j] *= d2[j] - t[4 * g + j];
+                    if constexpr (M1) p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
+                    if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j]));
                 }
             }
+            if (block_row0 < all_from) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
+                for (int r = 0; r < 16; ++r) {
+                    const bool hidden = block_row0 + acc_row(r, hi) < from;
+                    p1[r] = hidden ? 0.f : p1[r];
+                    p2[r] = hidden ? 0.f : p2[r];
+                }
+            }
+            floatx16 t = zero16();
+            Operand<T> w[2], s1[2], s2[2];
+            if constexpr (DVAL) {
+                floatx16 difference;
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d) {
-                    if constexpr (DK1) mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
-                    if constexpr (DK2) mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
+                for (int r = 0; r < 16; ++r) difference[r] = fmaf(-lam, p2[r], p1[r]);
+                w[0] = acc_operand<T>(difference, 0);
+                w[1] = acc_operand<T>(difference, 1);
+            }
+            in_order();
+#pragma unroll
+            for (int pair = 0; pair < kAhead; ++pair) read_pair(pair);
+#pragma unroll
+            for (int pair = 0; pair < kEnd; ++pair) {
+                if (kAhead) in_order();
+                read_pair(pair + kAhead);
+                if (kAhead) in_order();
+                Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
+                if (DK && pair == kK) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const float4 u1 = rows_of(ts + 2 * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
+                        const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (DK1) p1[4 * g + j] *= t[4 * g + j] - d1[j];
+                            if constexpr (DK2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        s1[s] = acc_operand<T>(p1, s);
+                        s2[s] = acc_operand<T>(p2, s);
+                    }
+                }
+                if (pair < kT) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) mma(dval[DVAL ? (2 * pair + e) % N : 0], o[e], w[(2 * pair + e) / N % 2]);
+                } else if (pair < kK) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) mma(t, o[e], v[DK ? 2 * (pair - kT) + e : 0]);
+                } else {
+                    const int i = pair - kK, d = i % (D / 32), s = i / (D / 32) % 2;
+                    if constexpr (DK1) mma(dk1[d], o[0], s1[s]);
+                    if constexpr (DK2) mma(dk2[d], o[1], s2[s]);
                 }
             }
         }
@@ -349,19 +423,21 @@ struct QuerySideShape {
     static constexpr int kKeys = 32;
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
-    static constexpr int kLds = 2 * kBufferBytes;
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;
+    static constexpr int kStages = 2;     // (more were no faster)
+    static constexpr int kLds = kStages * kBufferBytes;
 };
 }  // namespace
 
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does.
 template <typename T, int D, int DV, bool WIDE, int DO>
-__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_query_side_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
     constexpr int kKeys = Shape::kKeys;
     constexpr bool M1 = DO & kFirst, M2 = DO & kSecond;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     const int tile = tiles - 1 - id % tiles, split = id / tiles % a.query_splits;
@@ -403,28 +479,44 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
 #pragma unroll
     for (auto& x : dq2) x = zero16();
 
-    using KeyCopy = RowCopy<T, D, kKeys, 256, WIDE>;
+    // (small tiles: the first half of the threads copies k1, the second k2)
+    constexpr bool kHalves = kKeys * TileShape<T, D>::kRowChunks < 256 && DO == kBoth;
+    using KeyCopy = RowCopy<T, D, kKeys, kHalves ? 128 : 256, WIDE>;
     using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
-    const KeyCopy key_copy(a.kt, a.d, tid);
+    const KeyCopy key_copy(a.kt, a.d, kHalves ? tid & 127 : tid);
     const ValueCopy value_copy(a.vt, a.dv, tid);
+    constexpr int kStages = Shape::kStages;
+    constexpr int kCopies = (kHalves ? 1 : int(M1) + int(M2)) * KeyCopy::kCopies + ValueCopy::kCopies;
+    static_assert(KeyCopy::kWhole && ValueCopy::kWhole, "waves count their copies alike");
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
     const unsigned key_row = row_lane<T, D>(lane), key_column = column_lane<T, D>(lane);
     const unsigned value_row = row_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
-    auto fetch = [&](int key, unsigned buffer) {
-        if constexpr (M1) key_copy.start(buffer, kp + (long long)key * a.kt, a.kt, end - key, tid);
-        if constexpr (M2)
-            key_copy.start(buffer + Shape::kKeyBytes, kp + a.km + (long long)key * a.kt, a.kt, end - key,
-                       tid);
-        value_copy.start(buffer + 2 * Shape::kKeyBytes, vp + (long long)key * a.vt, a.vt, end - key,
-                         tid);
+    unsigned fill = base;                 // the stage to be filled next
+    int fill_key = begin;
+    auto fetch_next = [&] {
+        const int left = end - fill_key;
+        const T* k = kp + (long long)fill_key * a.kt;
+        if constexpr (kHalves) {
+            key_copy.start(fill + (wave >> 1) * Shape::kKeyBytes, k + (wave >> 1) * a.km, a.kt, left, tid & 127);
+        } else {
+            if constexpr (M1) key_copy.start(fill, k, a.kt, left, tid);
+            if constexpr (M2) key_copy.start(fill + Shape::kKeyBytes, k + a.km, a.kt, left, tid);
+        }
+        value_copy.start(fill + 2 * Shape::kKeyBytes, vp + (long long)fill_key * a.vt, a.vt, left, tid);
+        fill_key += kKeys;
+        fill = fill + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : fill + Shape::kBufferBytes;
     };
-    if (begin < end) fetch(begin, base);
-    for (int i = 0, key = begin; key < end; ++i, key += kKeys) {
-        const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
+    if (begin < end)
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) fetch_next();
+    unsigned buffer = base;
+    for (int key = begin; key < end; key += kKeys) {
         const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
         const unsigned r2 = r1 + Shape::kKeyBytes, c2 = c1 + Shape::kKeyBytes, rv = buffer + value_row;
-        copies_done();
-        if (key + kKeys < end) fetch(key + kKeys, base + ((i + 1) & 1) * Shape::kBufferBytes);
+        copies_done<(kStages - 2) * kCopies>();
+        // (past the last key, copies of nothing keep the count)
+        fetch_next();
+        buffer = buffer + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : buffer + Shape::kBufferBytes;
         if (key >= wave_end) continue;
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll
@@ -437,7 +529,7 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             if constexpr (M1) p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
-            if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2)) * lam;
+            if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2));
         }
         if (key + 31 > first_last) {
 #pragma unroll
@@ -450,7 +542,7 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? 2 : 1)) void attn_que
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             if constexpr (M1) p1[r] *= t[r] - d1;
-            if constexpr (M2) p2[r] *= d2 - t[r];
+            if constexpr (M2) p2[r] *= fmaf(-lam, t[r], d2);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
