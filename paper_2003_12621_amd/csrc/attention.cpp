@@ -96,8 +96,9 @@ size_t query_part_bytes(const fftsplit_attention_problem_t& p, int splits) {
     return splits > 1 ? round256(size_t(splits) * p.batch * p.queries * p.heads_q * 2 * p.dim * 4) : 0;
 }
 
-int delta_parts(const fftsplit_attention_problem_t& p) {
-    return p.batch * ((p.queries + kAttnDeltaRows - 1) / kAttnDeltaRows);
+// Parts of dlam of a head: one from each workgroup of the query side.
+int dlam_parts(const fftsplit_attention_problem_t& p, int query_splits) {
+    return p.batch * ((p.queries + kAttnRows - 1) / kAttnRows) * query_splits;
 }
 
 fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, const char* arch,
@@ -147,7 +148,7 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->query_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_q * ((p.queries + 127LL) / 128),
                                                 (p.keys + 31LL) / 32);
     const size_t shared = key_part_bytes(p, plan->key_splits), other = query_part_bytes(p, plan->query_splits);
-    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (delta_parts(p) + 1) * 4) +
+    plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (dlam_parts(p, plan->query_splits) + 1) * 4) +
                         (shared > other ? shared : other);
     *out = plan;
     return FFTSPLIT_SUCCESS;
@@ -341,7 +342,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.gt = dout_stride[1];
         a.gh = dout_stride[2];
         a.wide = a.wide && wide(dout, dout_stride, 3, p.dim_v, es);
-        a.parts = delta_parts(p);
+        a.parts = dlam_parts(p, plan->query_splits);
         a.delta = static_cast<float*>(workspace);
         a.dlam_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + round256(lse_bytes(p)));
         // (the two kernels' parts in turn)

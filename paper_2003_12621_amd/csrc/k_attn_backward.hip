@@ -2,13 +2,14 @@
 //
 // With P1, P2 the two maps (recomputed from the saved log sums), t = dO v^T and
 // D1 = <dO, o1>, D2 = <dO, o2> per row:
-//     dv = (P1 - lam P2)^T dO,   dlam = - sum D2,
+//     dv = (P1 - lam P2)^T dO,   dlam = - sum P2 t,
 //     dS1 = P1 (t - D1),   dS2 = lam P2 (D2 - t),
 //     dqm = scale dSm km,   dkm = scale dSm^T qm.
 // t and the value product are shared by both maps.  The key side (dk, dv) and
 // the query side (dq) are two kernels that each own their outputs and
 // recompute the scores, rather than one that would add to dq with atomics:
-// results do not depend on the order of workgroups.
+// results do not depend on the order of workgroups.  D1 and D2 come from the
+// saved outputs; dlam, a sum in which much cancels, from the terms themselves.
 #include "attn_common.hpp"
 
 namespace fftsplit {
@@ -41,16 +42,15 @@ __device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool 
 
 }  // namespace
 
-// D1 and lam D2 of kAttnDeltaRows rows of one head, and their share of dlam.
+// D1 and lam D2 of kAttnDeltaRows rows of one head.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
-    __shared__ float sums[256 / kDeltaLanes];
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
     const int h = blockIdx.x % a.hq, c = blockIdx.x / a.hq % chunks, b = blockIdx.x / a.hq / chunks;
     const int l = threadIdx.x % kDeltaLanes, group = threadIdx.x / kDeltaLanes;
     const bool wide = a.wide && a.dv % 8 == 0;
     const float lam = attn_lambda(a, h);
-    float total = 0.f;
+    if (b == 0 && c == 0 && threadIdx.x == 0) a.lam32[h] = lam;
     for (int i = group; i < kAttnDeltaRows; i += 256 / kDeltaLanes) {
         const int row = c * kAttnDeltaRows + i;
         if (row >= a.sq) break;      // (the same in all lanes of the group)
@@ -72,20 +72,11 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
         }
         s1 = row_group_sum(s1);
         s2 = row_group_sum(s2);
-        total += s2;
         if (l == 0) {
             float* delta = a.delta + (size_t(b) * a.hq + h) * 2 * a.sq + row;
             delta[0] = s1;
             delta[a.sq] = lam * s2;
         }
-    }
-    if (l == 0) sums[group] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        if (b == 0 && c == 0) a.lam32[h] = lam;
-        float t = 0.f;
-        for (int i = 0; i < 256 / kDeltaLanes; ++i) t += sums[i];
-        a.dlam_part[size_t(h) * a.parts + b * chunks + c] = -t;
     }
 }
 
@@ -509,6 +500,7 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
     if (begin < end)
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) fetch_next();
+    float lam_sum = 0.f;
     unsigned buffer = base;
     for (int key = begin; key < end; key += kKeys) {
         const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
@@ -539,6 +531,10 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
                 p2[r] = hidden ? 0.f : p2[r];
             }
         }
+        if constexpr (M2) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) lam_sum = fmaf(p2[r], t[r], lam_sum);
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             if constexpr (M1) p1[r] *= t[r] - d1;
@@ -553,6 +549,18 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
                 if constexpr (M2) mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
             }
         }
+    }
+    if constexpr (M2) {
+        // this workgroup's part of dlam, in a fixed order
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) lam_sum += __shfl_xor(lam_sum, m, 64);
+        __syncthreads();
+        float* sums = reinterpret_cast<float*>(lds);
+        if (lane == 0) sums[wave] = lam_sum;
+        __syncthreads();
+        if (tid == 0)
+            a.dlam_part[size_t(h) * a.parts + (size_t(b) * tiles + tile) * a.query_splits + split] =
+                -(sums[0] + sums[1] + sums[2] + sums[3]);
     }
     if (!valid) return;
     const size_t out = ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
@@ -598,18 +606,18 @@ hipError_t launch_key_side(const AttnArgs& a, hipStream_t s) {
     return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, nullptr, a);
 }
 template <typename T, int D, int DV, int DO>
-hipError_t launch_query_side(const AttnArgs& a, hipStream_t s, hipEvent_t stop) {
+hipError_t launch_query_side(const AttnArgs& a, hipStream_t s) {
     using Shape = QuerySideShape<T, D, DV>;
     const long long blocks = (long long)a.n * a.hq * a.query_splits * ((a.sq + kAttnRows - 1) / kAttnRows);
     auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true, DO> : attn_query_side_kernel<T, D, DV, false, DO>;
     if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, stop, a);
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, nullptr, a);
 }
 template <typename T>
 hipError_t launch_parts(const float* part, int splits, long long rows, int width, int scaled, float scale, void* a0, void* a1,
-                        hipStream_t s, hipEvent_t stop) {
+                        hipStream_t s) {
     const long long blocks = (rows * width + 255) / 256;
-    return launch_kernel(attn_parts_kernel<T>, dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, nullptr, stop,
+    return launch_kernel(attn_parts_kernel<T>, dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, nullptr, nullptr,
                          part, splits, rows, width, scaled, scale, static_cast<T*>(a0), static_cast<T*>(a1));
 }
 
@@ -618,8 +626,6 @@ hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& e
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
     const long long rows = (long long)a.n * a.hq * chunks;
     if (hipError_t e = launch_kernel(attn_delta_kernel<T>, dim3(unsigned(rows)), dim3(256), 0, s, ev.start, nullptr, a))
-        return e;
-    if (hipError_t e = launch_kernel(attn_dlam_kernel, dim3(a.lam_step ? a.hq : 1), dim3(256), 0, s, nullptr, nullptr, a))
         return e;
     // At the largest widths the operands and accumulators of all gradients do
     // not fit a lane's registers: there they are computed one after another.
@@ -636,19 +642,19 @@ hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& e
     }
     if (a.key_splits > 1)
         if (hipError_t e = launch_parts<T>(a.key_part, a.key_splits, (long long)a.n * a.sk * a.hk, 2 * a.d + a.dv, 2 * a.d,
-                                           a.scale, a.dk, a.dv_out, s, nullptr))
+                                           a.scale, a.dk, a.dv_out, s))
             return e;
-    hipEvent_t last = a.query_splits > 1 ? nullptr : ev.stop;
     if constexpr (kApart) {
-        if (hipError_t e = launch_query_side<T, D, DV, kFirst>(a, s, nullptr)) return e;
-        if (hipError_t e = launch_query_side<T, D, DV, kSecond>(a, s, last)) return e;
+        if (hipError_t e = launch_query_side<T, D, DV, kFirst>(a, s)) return e;
+        if (hipError_t e = launch_query_side<T, D, DV, kSecond>(a, s)) return e;
     } else {
-        if (hipError_t e = launch_query_side<T, D, DV, kBoth>(a, s, last)) return e;
+        if (hipError_t e = launch_query_side<T, D, DV, kBoth>(a, s)) return e;
     }
     if (a.query_splits > 1)
-        return launch_parts<T>(a.query_part, a.query_splits, (long long)a.n * a.sq * a.hq, 2 * a.d, 2 * a.d, a.scale, a.dq,
-                               nullptr, s, ev.stop);
-    return hipSuccess;
+        if (hipError_t e = launch_parts<T>(a.query_part, a.query_splits, (long long)a.n * a.sq * a.hq, 2 * a.d, 2 * a.d,
+                                           a.scale, a.dq, nullptr, s))
+            return e;
+    return launch_kernel(attn_dlam_kernel, dim3(a.lam_step ? a.hq : 1), dim3(256), 0, s, nullptr, ev.stop, a);
 }
 
 template <typename T>
