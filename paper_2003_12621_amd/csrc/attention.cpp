@@ -22,10 +22,10 @@ size_t extent(const int* dims, const long long* strides, int nd, int width, int 
 }
 
 // Whether 16-byte accesses of rows are aligned and whole.
-bool wide(const void* p, const long long* strides, int nd, int width, int bytes) {
+bool wide(const void* p, const int* dims, const long long* strides, int nd, int width, int bytes) {
     const int per = 16 / bytes;
     bool ok = reinterpret_cast<uintptr_t>(p) % 16 == 0 && width % per == 0;
-    for (int i = 0; i < nd; ++i) ok = ok && strides[i] % per == 0;
+    for (int i = 0; i < nd; ++i) ok = ok && (dims[i] == 1 || strides[i] % per == 0);
     return ok;
 }
 
@@ -55,27 +55,33 @@ size_t output_bytes(const fftsplit_attention_problem_t& p) {
 size_t lse_bytes(const fftsplit_attention_problem_t& p) { return size_t(p.batch) * p.heads_q * 2 * p.queries * 4; }
 
 // How many workgroups share the keys of a tile of the kernel for few rows, or
-// 0 for the kernel that takes 128 rows of one head.
+// 0 for the kernel that takes kAttnTiledRows rows of one head.
 //
-// A workgroup of either works on 128 x 32 or 32 x 128 scores of each map a step.
-// The kernel for few rows pays a second launch but can use the whole chip for a
-// handful of rows: one workgroup a compute unit, with 256 keys at least.
-// Measured in us, without / with: 1 token over 8192 keys, 4 key heads 277 / 25;
-// 64 rows over 1024 keys, 32 heads 40 / 21; 128 rows over 4096 keys, 4 heads
-// 135 / 22; 200 rows over 200 keys, 16 heads 15 / 17.
-int choose_splits(const fftsplit_attention_problem_t& p) {
+// The kernel for few rows pays a second launch and reads the keys once for every
+// 32 rows, but uses the whole chip for a handful of rows.  Which is faster, and
+// with how many workgroups, is taken from what a step of either was measured to
+// take (us), the tiled kernel's of 32 keys, the other's of 128; 12 and 3 us are
+// the launches, 0.02 us a workgroup the join.  Measured, tiled / few rows: 128
+// rows x 4096 keys, 4 heads 94 / 22 us; 1024 x 1024, 4 heads 28 / 24; 100 x 100,
+// 8 heads 8 / 12; 784 x 784, 16 heads 25 / 53.
+int choose_splits(const fftsplit_attention_problem_t& p, int shape) {
+    static const double kTiledStep[2][kAttnShapeCount] = {{2.2, 3.3, 6.6}, {0.55, 0.72, 1.0}};      // fp32, bf16
+    static const double kFewStep[2][kAttnShapeCount] = {{3.8, 13.4, 27.0}, {0.75, 1.65, 3.8}};
+    const int type = p.dtype == FFTSPLIT_BF16;
     const long long group = p.heads_q / p.heads_k, heads = (long long)p.batch * p.heads_k;
-    const long long tiled = heads * group * ((p.queries + kAttnRows - 1) / kAttnRows);
+    const long long tiled = heads * group * ((p.queries + kAttnTiledRows - 1) / kAttnTiledRows);
     const long long few = heads * ((group * p.queries + kAttnFewRows - 1) / kAttnFewRows);
-    if (tiled > 256) return 0;
-    long long splits = 256 / few, most = (p.keys + 255LL) / 256;
-    splits = splits > most ? most : splits;
-    splits = splits > 32 ? 32 : splits;
-    splits = splits < 1 ? 1 : splits;
-    // times in us, of steps and of launches
-    const double tiled_time = 3 + 1.05 * ((p.keys + 31) / 32);
-    const double few_time = 8 + 1.5 * double((few * splits + 255) / 256) * double((p.keys + 128 * splits - 1) / (128 * splits));
-    return few_time < tiled_time ? int(splits) : 0;
+    if (tiled > 512 || few > 256) return 0;
+    double best = 3 + kTiledStep[type][shape] * ((p.keys + 31) / 32);
+    int splits = 0;
+    for (int s = 1; s <= 32 && few * s <= 256; s *= 2) {
+        const double t = 12 + kFewStep[type][shape] * ((p.keys + 128LL * s - 1) / (128 * s)) + 0.02 * double(few * s);
+        if (t < best) {
+            best = t;
+            splits = s;
+        }
+    }
+    return splits;
 }
 
 // Workgroups that share the steps of a tile of 128 keys or rows in the backward
@@ -139,7 +145,7 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->device = device;
     plan->scale = p.scale > 0.f ? p.scale : float(1.0 / std::sqrt(double(p.dim)));
     plan->shape = shape;
-    plan->splits = choose_splits(p);
+    plan->splits = choose_splits(p, shape);
     const size_t parts = size_t(rows) * plan->splits;
     plan->forward_ws = plan->splits ? round256(parts * 2 * kAttnShapes[shape].dv * 4) + round256(parts * 4 * 4) : 0;
     const long long group = p.heads_q / p.heads_k;
@@ -150,6 +156,15 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     const size_t shared = key_part_bytes(p, plan->key_splits), other = query_part_bytes(p, plan->query_splits);
     plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (dlam_parts(p, plan->query_splits) + 1) * 4) +
                         (shared > other ? shared : other);
+    // workgroups of the largest launches (a dimension of a grid holds below 2^32 threads)
+    const double heads = double(p.batch) * p.heads_q;
+    const double groups[] = {heads * ((p.queries + 63) / 64), heads * ((p.keys + 127) / 128) * plan->key_splits,
+                             heads * ((p.queries + 127) / 128) * plan->query_splits};
+    for (double g : groups)
+        if (g > double(1 << 22)) {
+            delete plan;
+            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "attention: too many tiles of queries or keys (2^22)");
+        }
     *out = plan;
     return FFTSPLIT_SUCCESS;
 }
@@ -211,8 +226,8 @@ fftsplit_status_t check_inputs(fftsplit_attention_plan_t plan, const fftsplit_at
     a.vb = in->v_stride[0];
     a.vt = in->v_stride[1];
     a.vh = in->v_stride[2];
-    a.wide = wide(in->q, in->q_stride, 4, p.dim, es) && wide(in->k, in->k_stride, 4, p.dim, es) &&
-             wide(in->v, in->v_stride, 3, p.dim_v, es);
+    a.wide = wide(in->q, qd, in->q_stride, 4, p.dim, es) && wide(in->k, kd, in->k_stride, 4, p.dim, es) &&
+             wide(in->v, vd, in->v_stride, 3, p.dim_v, es);
     a.o_wide = p.dim_v % 4 == 0;
     spans.add(in->q, extent(qd, in->q_stride, 4, p.dim, es), "q");
     spans.add(in->k, extent(kd, in->k_stride, 4, p.dim, es), "k");
@@ -341,7 +356,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.gb = dout_stride[0];
         a.gt = dout_stride[1];
         a.gh = dout_stride[2];
-        a.wide = a.wide && wide(dout, dout_stride, 3, p.dim_v, es);
+        a.wide = a.wide && wide(dout, gd, dout_stride, 3, p.dim_v, es);
         a.parts = dlam_parts(p, plan->query_splits);
         a.delta = static_cast<float*>(workspace);
         a.dlam_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + round256(lse_bytes(p)));

@@ -25,7 +25,9 @@ struct AttnShape {
 constexpr AttnShape kAttnShapes[] = {{32, 64}, {64, 128}, {128, 256}};
 constexpr int kAttnShapeCount = 3;
 
-// Query rows a workgroup of the tiled kernel takes (4 waves of 32).
+// Query rows a workgroup of the forward kernel takes (two of 32, each by a wave
+// for either map), and of the backward kernels (4 waves of 32).
+constexpr int kAttnTiledRows = 64;
 constexpr int kAttnRows = 128;
 // Query rows, packed over the heads that share a key head, of the kernel for few rows.
 constexpr int kAttnFewRows = 32;

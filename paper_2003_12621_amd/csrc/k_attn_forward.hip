@@ -60,69 +60,61 @@ __device__ __forceinline__ void mask_scores(floatx16& s, int key0, int last, int
     for (int r = 0; r < 16; ++r) s[r] = acc_row(r, hi) > last - key0 ? -kInf : s[r];
 }
 
-// A wave takes one map of RB x 32 query rows: half the waves of a workgroup
-// work on the first map and half on the second of the same rows, and the two
-// outputs are joined through LDS at the end.  A wave with both maps of 32 rows
-// reads a third more operands from LDS per product (each key operand serves
-// one product instead of two), and at 256-wide values its two accumulators
-// alone would take 256 registers.
+// A wave takes one map of 32 query rows: two waves work on the first map and
+// two on the second of the same rows, and their outputs are joined through LDS
+// at the end.  That leaves a lane 128 registers' worth of state at 128-wide
+// values, so that four workgroups a compute unit hide one another's waits.
+// Measured at 4 x 8 heads of 3136 x 3136 (bf16, 64 / 128 wide): 311 us; with 64
+// rows a wave, which reads half as many operands from LDS, and two workgroups
+// 366 us.
 template <typename T, int D, int DV>
 struct ForwardShape {
-    static constexpr int kRowBlocks = 1;
     static constexpr int kWaves = 4;
-    static constexpr int kRows = kWaves / 2 * 32 * kRowBlocks;           // of a workgroup
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kKeys = sizeof(T) * DV <= 128 ? 64 : 32;         // keys per stage
     static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 4 : (sizeof(T) * DV <= 512 ? 2 : 1);         // workgroups per compute unit aimed at
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
     static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
-    static constexpr int kJoinBytes = kRows * DV * 4;
+    static constexpr int kJoinBytes = kAttnTiledRows * DV * 4;
     static constexpr int kLds = 2 * kBufferBytes > kJoinBytes ? 2 * kBufferBytes : kJoinBytes;
 };
 
 }  // namespace
 
-// One workgroup: 128 query rows of one head; the keys pass through LDS in
+// One workgroup: 64 query rows of one head; the keys pass through LDS in
 // double-buffered stages that all waves read.
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__((ForwardShape<T, D, DV>::kThreads), (ForwardShape<T, D, DV>::kBlocks)) void
 attn_forward_kernel(AttnArgs a) {
     using Shape = ForwardShape<T, D, DV>;
-    constexpr int kKeys = Shape::kKeys, DT = DV / 32, RB = Shape::kRowBlocks;
+    constexpr int kKeys = Shape::kKeys, DT = DV / 32;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, group = wave >> 1;
-    const int tiles = (a.sq + Shape::kRows - 1) / Shape::kRows;
+    const int tiles = (a.sq + kAttnTiledRows - 1) / kAttnTiledRows;
     const int id = xcd_logical_block(blockIdx.x, gridDim.x);
     const int tile = tiles - 1 - id % tiles;           // under a causal mask the longest first
     const int h = id / tiles % a.hq, b = id / tiles / a.hq;
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
 
-    const int first = tile * Shape::kRows + group * (32 * RB), row = first + (lane & 31);
+    const int first = tile * kAttnTiledRows + group * 32, row = first + (lane & 31);
     const int first_last = attn_last_key(a, first, length);          // last key of the wave's first row
-    const int wave_end = attn_last_key(a, min(first + 32 * RB, a.sq) - 1, length) + 1;
-    const int end = attn_last_key(a, min(tile * Shape::kRows + Shape::kRows, a.sq) - 1, length) + 1;
+    const int wave_end = attn_last_key(a, min(first + 32, a.sq) - 1, length) + 1;
+    const int end = attn_last_key(a, min(tile * kAttnTiledRows + kAttnTiledRows, a.sq) - 1, length) + 1;
 
     const T* k1 = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
     const T* v = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
 
-    Operand<T> q[RB][D / 16];
-    floatx16 o[RB][DT];
-    RowState st[RB];
-    int last[RB];
+    Operand<T> q[D / 16];
+    load_row_operands<T, D, WIDE>(
+        q, static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh + map * a.qm, a.d, row < a.sq, lane);
+    settle(q);
+    floatx16 o[DT];
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int i = row + 32 * r;
-        load_row_operands<T, D, WIDE>(q[r],
-                                      static_cast<const T*>(a.q) + b * a.qb + (long long)i * a.qt + h * a.qh + map * a.qm,
-                                      a.d, i < a.sq, lane);
-        settle(q[r]);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[r][d] = zero16();
-        st[r] = RowState{kNoMax, 0.f};
-        last[r] = attn_last_key(a, i, length);
-    }
+    for (int d = 0; d < DT; ++d) o[d] = zero16();
+    RowState st{kNoMax, 0.f};
+    const int last = attn_last_key(a, row, length);
 
     using KeyCopy = RowCopy<T, D, kKeys, Shape::kThreads, WIDE>;
     using ValueCopy = RowCopy<T, DV, kKeys, Shape::kThreads, WIDE>;
@@ -149,77 +141,54 @@ attn_forward_kernel(AttnArgs a) {
         for (int sub = 0; sub < kKeys; sub += 32) {
             const int key0 = key + sub;
             if (key0 >= wave_end) break;
-            floatx16 c[RB];
+            floatx16 c = zero16();
 #pragma unroll
-            for (int r = 0; r < RB; ++r) c[r] = zero16();
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const Operand<T> x = read_row<T, D>(tk, sub, s);
-#pragma unroll
-                for (int r = 0; r < RB; ++r) mma(c[r], x, q[r][s]);
-            }
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                if (key0 + 31 > first_last) mask_scores(c[r], key0, last[r], hi);
-                softmax_step(c[r], st[r], o[r], a.scale_log2);
-            }
+            for (int s = 0; s < D / 16; ++s) mma(c, read_row<T, D>(tk, sub, s), q[s]);
+            if (key0 + 31 > first_last) mask_scores(c, key0, last, hi);
+            softmax_step(c, st, o, a.scale_log2);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                Operand<T> p[RB];
+                const Operand<T> p = acc_operand<T>(c, s);
 #pragma unroll
-                for (int r = 0; r < RB; ++r) p[r] = acc_operand<T>(c[r], s);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const Operand<T> x = read_column<T, DV>(tv, sub, 32 * d, s);
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) mma(o[r][d], x, p[r]);
-                }
+                for (int d = 0; d < DT; ++d) mma(o[d], read_column<T, DV>(tv, sub, 32 * d, s), p);
             }
         }
     }
 
     // each map's own output, then the second map's scaled by lam to the waves of the first
     const float lam = attn_lambda(a, h);
-    float4* join = reinterpret_cast<float4*>(lds) + group * (RB * DT * 4 * 64) + lane;
+    float4* join = reinterpret_cast<float4*>(lds) + group * (DT * 4 * 64) + lane;
+    const float2 halves = both_halves(st.l);
+    const float l = halves.x + halves.y;
+    const bool none = last < 0;                        // no key is visible: the row is zero
+    const float inv = none ? 0.f : 1.f / l;
+    const bool valid = row < a.sq;
+    const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
+    T* own = a.o1 && valid ? static_cast<T*>(map ? a.o2 : a.o1) + at : nullptr;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int i = row + 32 * r;
-        const float2 halves = both_halves(st[r].l);
-        const float l = halves.x + halves.y;
-        const bool none = last[r] < 0;                 // no key is visible: the row is zero
-        const float inv = none ? 0.f : 1.f / l;
-        const size_t at = ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
-        T* own = a.o1 && i < a.sq ? static_cast<T*>(map ? a.o2 : a.o1) + at : nullptr;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int g = 0; g < 4; ++g) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[r][d][4 * g + j] *= inv;
-                const float4 y = make_float4(o[r][d][4 * g], o[r][d][4 * g + 1], o[r][d][4 * g + 2], o[r][d][4 * g + 3]);
-                if (own) store4(own, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, y.x, y.y, y.z, y.w);
-                if (map) join[((r * DT + d) * 4 + g) * 64] = make_float4(y.x * lam, y.y * lam, y.z * lam, y.w * lam);
-            }
-        if (a.lse && hi == 0 && i < a.sq)
-            a.lse[((size_t(b) * a.hq + h) * 2 + map) * a.sq + i] = none ? 0.f : st[r].m + log2f(l);
-    }
+            for (int j = 0; j < 4; ++j) o[d][4 * g + j] *= inv;
+            const float4 y = make_float4(o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]);
+            if (own) store4(own, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, y.x, y.y, y.z, y.w);
+            if (map) join[(d * 4 + g) * 64] = make_float4(y.x * lam, y.y * lam, y.z * lam, y.w * lam);
+        }
+    if (a.lse && hi == 0 && valid)
+        a.lse[((size_t(b) * a.hq + h) * 2 + map) * a.sq + row] = none ? 0.f : st.m + log2f(l);
     __syncthreads();
-    if (map) return;
+    if (map || !valid) return;
+    T* out = static_cast<T*>(a.o) + at;
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int i = row + 32 * r;
-        if (i >= a.sq) break;
-        T* out = static_cast<T*>(a.o) + ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 z = join[((r * DT + d) * 4 + g) * 64];
-                store4(out, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, o[r][d][4 * g] - z.x, o[r][d][4 * g + 1] - z.y,
-                       o[r][d][4 * g + 2] - z.z, o[r][d][4 * g + 3] - z.w);
-            }
-    }
+        for (int g = 0; g < 4; ++g) {
+            const float4 z = join[(d * 4 + g) * 64];
+            store4(out, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, o[d][4 * g] - z.x, o[d][4 * g + 1] - z.y,
+                   o[d][4 * g + 2] - z.z, o[d][4 * g + 3] - z.w);
+        }
 }
 
 // ---- few rows: single tokens over a long cache ----
@@ -462,7 +431,7 @@ namespace {
 template <typename T, int D, int DV>
 hipError_t launch_tiled(const AttnArgs& a, hipStream_t s, const LaunchEvents& ev) {
     using Shape = ForwardShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hq * ((a.sq + Shape::kRows - 1) / Shape::kRows);
+    const long long blocks = (long long)a.n * a.hq * ((a.sq + kAttnTiledRows - 1) / kAttnTiledRows);
     auto kernel = a.wide ? attn_forward_kernel<T, D, DV, true> : attn_forward_kernel<T, D, DV, false>;
     if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
     return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(Shape::kThreads), Shape::kLds, s, ev.start,
