@@ -354,13 +354,14 @@ typedef enum {
  * Key j is visible to row i if j < key_lengths[b] and, with causal set, if
  * j <= i + key_lengths[b] - queries (the last row sees every key).  A row
  * that sees no key gives o = 0 and contributes to no gradient.  What lies in
- * k and v from row key_lengths[b] on is not read.
+ * k and v from row key_lengths[b] on is not read.  What causal hides is: it has
+ * to be finite, as a row takes zero times it.
  * Scores, the softmax statistics and all sums are fp32; with bf16 tensors the
  * terms of the softmax (and the score gradients) are rounded to bf16 as
  * operands of the matrix products. */
 typedef struct {
     int batch;            /* sequences */
-    int queries, keys;    /* query rows; room for keys (each sequence may fill less) */
+    int queries, keys;    /* query rows; room for keys (each sequence may fill less); at most 2^28 */
     int heads_q, heads_k; /* heads_k divides heads_q */
     int dim;              /* width of one map's queries and keys, at most 128 */
     int dim_v;            /* width of the values, at most 256 */
@@ -441,7 +442,10 @@ enum {
     FFTSPLIT_CHANNELS_FIRST = 1    /* [batch][channels][positions]: a feature map */
 };
 typedef struct {
-    int batch, positions, channels;   /* at most 8192 channels; with x channels first 2048, and 2^22 positions */
+    /* At most 8192 channels, with x channels first 2048 and 2^22 positions.
+     * batch * positions: at most 2^25 (2^23 above 1024 channels); with x
+     * channels first batch * ceil(positions / 16) at most 2^21. */
+    int batch, positions, channels;
     int x_dtype, y_dtype;             /* fftsplit_dtype_t; both the same, or fp32 to bf16 */
     int x_layout, y_layout;           /* both the same, or a feature map to tokens */
     float eps;
@@ -474,7 +478,7 @@ fftsplit_status_t fftsplit_layer_norm_backward(const fftsplit_layer_norm_t* desc
  * on are passed on.  The angle's whole turns are taken off in 64 bits. */
 #define FFTSPLIT_ROTARY_MAX_AXES 4
 typedef struct {
-    int batch, tokens, dim;        /* dim: elements of a head, at most 1024 */
+    int batch, tokens, dim;        /* dim: elements of a head, at most 1024; batch * tokens at most 2^26 */
     int heads0, heads1;            /* heads of the two tensors; heads1 0: only the first */
     int dtype;                     /* fftsplit_dtype_t */
     int axes;                      /* 1 to FFTSPLIT_ROTARY_MAX_AXES */

@@ -28,8 +28,10 @@ fftsplit_status_t check_norm(const fftsplit_layer_norm_t* d, NormArgs& a) {
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: at most 8192 channels, 2048 with channels first");
     if (!(d->eps >= 0.f) || !std::isfinite(d->eps))
         return fail(FFTSPLIT_ERROR_INVALID_VALUE, "layer norm: eps must be finite and not negative");
-    if ((long long)d->batch * d->positions > 0x7fffffffLL)
-        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: batch * positions must be below 2^31");
+    // a grid holds below 2^32 threads: 16 positions a workgroup of 1024, or up to 256 threads a position
+    const long long rows = (long long)d->batch * d->positions;
+    if (first ? (long long)d->batch * ((d->positions + 15) / 16) > (1 << 21) : rows * (d->channels > 1024 ? 256 : 64) > 0x7fffffffLL)
+        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: too many positions");
     if (first && d->positions > (1 << 22))
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: at most 2^22 positions of a feature map");
     a.n = d->batch;
@@ -183,7 +185,7 @@ fftsplit_status_t check_rotary_tensor(const fftsplit_rotary_t* d, int which, con
         for (int i = 0; i < 3; ++i) {
             if (st[i] < 0 || (dims[i] > 1 && size_t(st[i]) > (size_t(1) << 58) / size_t(dims[i])))
                 return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(names[t]) + " has a stride out of range");
-            a.wide = a.wide && st[i] % per == 0;
+            a.wide = a.wide && (dims[i] == 1 || st[i] % per == 0);
             (t ? a.ys : a.xs)[which][i] = st[i];
             if (dims[i] > 1 && x == y && xs[i] != ys[i])
                 return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: in place needs equal strides");
@@ -244,8 +246,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_rotary(const fftsplit_rotary_t* d, co
         if (pairs < 1 || 2 * pairs > d->dim)
             return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: the sections must hold 1 to dim / 2 pairs");
         if (d->dim > 1024 || d->heads0 > 65536 || d->heads1 > 65536 ||
-            (long long)d->batch * d->tokens > 0x7fffffffLL)
-            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: dim at most 1024, 65536 heads, 2^31 - 1 tokens");
+            (long long)d->batch * d->tokens > (1 << 26))
+            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: dim at most 1024, 65536 heads, 2^26 tokens");
         if (fftsplit_status_t s = check_device_ptr(positions, "positions", 4)) return s;
         if (fftsplit_status_t s = check_device_ptr(freqs, "freqs", 4)) return s;
         const int es = type_bytes(d->dtype), per = 16 / es;

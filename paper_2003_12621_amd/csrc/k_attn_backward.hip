@@ -565,15 +565,19 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
     if (!valid) return;
     const size_t out = ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
     const bool whole = a.d % 4 == 0;
-    if (a.query_splits > 1) {
-        float* part = a.query_part + size_t(split) * a.n * a.sq * a.hq * 2 * a.d + out;
-        if constexpr (M1) store_row(part, dq1, a.d, whole, 1.f, hi);
-        if constexpr (M2) store_row(part + a.d, dq2, a.d, whole, 1.f, hi);
+    // a part of the sum, unscaled, or the gradient
+    const bool shared = a.query_splits > 1;
+    float* part = a.query_part + (shared ? size_t(split) * a.n * a.sq * a.hq * 2 * a.d + out : 0);
+    const float scale = shared ? 1.f : a.scale;
+    if (sizeof(T) == 4 || shared) {
+        float* to = sizeof(T) == 4 && !shared ? static_cast<float*>(a.dq) + out : part;
+        if constexpr (M1) store_row(to, dq1, a.d, whole, scale, hi);
+        if constexpr (M2) store_row(to + a.d, dq2, a.d, whole, scale, hi);
         return;
     }
     T* dq = static_cast<T*>(a.dq) + out;
-    if constexpr (M1) store_row(dq, dq1, a.d, whole, a.scale, hi);
-    if constexpr (M2) store_row(dq + a.d, dq2, a.d, whole, a.scale, hi);
+    if constexpr (M1) store_row(dq, dq1, a.d, whole, scale, hi);
+    if constexpr (M2) store_row(dq + a.d, dq2, a.d, whole, scale, hi);
 }
 
 // Adds up the parts of workgroups that shared the steps, in their order:

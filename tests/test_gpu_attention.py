@@ -217,3 +217,120 @@ def test_repeatable():
     for r in runs[1:]:
         for x, y in zip(runs[0], r):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("sq,causal", [(1, True), (7, True), (40, False)])
+def test_few_rows_over_many_keys(d, dv, sq, causal, dtype):
+    """The kernel whose workgroups share the keys, with lengths that leave
+    workgroups and waves without any."""
+    n, sk, hq, hk = 5, 900, 4, 2
+    lengths = [900, 1, 0, 470, 33]
+    assert fs.DiffAttention(n, sq, sk, hq, hk, d, dv, dtype=DTYPE[dtype], causal=causal).info.key_splits > 1
+    check(n, sq, sk, hq, hk, d, dv, dtype, causal=causal, lengths=lengths, train=sq == 7)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_tiles(d, dv, causal, dtype):
+    """The kernels that go over all keys or rows in one workgroup (no shared
+    steps), several stages long."""
+    n, s, hq, hk = 40, 150, 16, 16
+    info = fs.DiffAttention(n, s, s, hq, hk, d, dv, dtype=DTYPE[dtype], causal=causal).info
+    assert info.key_splits == 0
+    # most sequences empty, so that the reference stays small
+    check(n, s, s, hq, hk, d, dv, dtype, causal=causal, lengths=[150 if b == 3 else 0 for b in range(n)])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_shared_backward_steps(dtype):
+    """Few tiles of many steps: workgroups share them and their parts are added
+    up; with strides that leave no 16-byte accesses, too."""
+    a = check(1, 310, 290, 4, 2, 32, 64, dtype, causal=True)
+    b = check(1, 310, 290, 4, 2, 32, 64, dtype, causal=True, place=_unaligned)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    check(1, 300, 280, 2, 1, 30, 50, dtype)
+
+
+def test_offsets_beyond_32_bits():
+    """Tokens 2^22 elements apart: the last keys lie 9 GB from the first."""
+    n, sq, sk, h, d, dv = 1, 3, 1100, 1, 32, 64
+    dt = torch.bfloat16
+    q, k, v, lam, do = (_dev(a, dt) for a in make_inputs(11, n, sq, sk, h, h, d, dv))
+    stride = 1 << 22
+    big = torch.empty(sk * stride, dtype=dt, device="cuda")
+    kv = big.as_strided((n, sk, h, 2 * d + dv), (0, stride, 2 * d + dv, 1))
+    kv[..., :2 * d] = k.flatten(3)
+    kv[..., 2 * d:] = v
+    kf, vf = kv[..., :2 * d].unflatten(-1, (2, d)), kv[..., 2 * d:]
+    assert kf.stride(1) == stride
+    plan = fs.DiffAttention(n, sq, sk, h, h, d, dv, dtype=dt)
+    near, far = [], []
+    for out, kk, vv in ((near, k, v), (far, kf, vf)):
+        o, saved = plan.forward(q, kk, vv, lam, save=True)
+        out += [o, *plan.backward(do, q, kk, vv, lam, saved)]
+    torch.cuda.synchronize()
+    for x, y in zip(near, far):
+        assert torch.equal(x, y)
+    too_far = big.as_strided((n, 2, h, 2, d), (0, (1 << 22) + 8, 2 * d, d, 1))
+    small = fs.DiffAttention(n, sq, 2, h, h, d, dv, dtype=dt)
+    with pytest.raises(fs.FftsplitError) as e:
+        small.forward(q, too_far, v[:, :2], lam)
+    assert e.value.status == fs.ERROR_NOT_SUPPORTED
+
+
+def test_refusals():
+    dt = torch.float32
+    q, k, v, lam, do = (_dev(a, dt) for a in make_inputs(2, 2, 8, 300, 4, 2, 16, 32))
+    plan = fs.DiffAttention(2, 8, 300, 4, 2, 16, 32)
+    with pytest.raises(ValueError):
+        plan.forward(q[:, :7], k, v, lam)
+    with pytest.raises(TypeError):
+        plan.forward(q.bfloat16(), k, v, lam)
+    with pytest.raises(TypeError):
+        plan.forward(q.cpu(), k, v, lam)
+    with pytest.raises(ValueError):
+        plan.forward(q, k, v, lam[:3])
+    with pytest.raises(TypeError):
+        plan.forward(q, k, v, lam.double())
+    with pytest.raises(TypeError):
+        plan.forward(q, k, v, lam, key_lengths=torch.ones(2, device="cuda", dtype=torch.int64))
+    with pytest.raises(ValueError):
+        plan.forward(q, k, v, lam, key_lengths=torch.ones(3, device="cuda", dtype=torch.int32))
+    with pytest.raises(ValueError):
+        plan.forward(q.transpose(-1, -2).contiguous().transpose(-1, -2), k, v, lam)
+    with pytest.raises(ValueError):
+        plan.forward(q, k, v, lam, out=torch.empty(3, device="cuda"))
+    assert plan.info.forward_workspace_bytes > 0
+    with pytest.raises(fs.FftsplitError) as e:
+        plan.forward(q, k, v, lam, workspace=torch.empty(16, device="cuda", dtype=torch.uint8))
+    assert e.value.status == fs.ERROR_INSUFFICIENT_WORKSPACE
+    with pytest.raises(fs.FftsplitError) as e:
+        plan.forward(q, k, v, lam, out=v.view(-1)[:8 * 2 * 4 * 32].view(2, 8, 4, 32))
+    assert "overlaps" in str(e.value)
+    # and a sound call still works
+    assert torch.isfinite(plan.forward(q, k, v, lam)).all()
+
+
+def test_another_stream():
+    """Enqueued on the current stream, in its order: the inputs are produced
+    there behind work that takes a while."""
+    n, s, h, d, dv = 2, 128, 4, 64, 128
+    q, k, v, lam, do = (_dev(a, torch.bfloat16) for a in make_inputs(4, n, s, s, h, h, d, dv))
+    plan = fs.DiffAttention(n, s, s, h, h, d, dv, dtype=torch.bfloat16)
+    want = plan.forward(q, k, v, lam)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    q2 = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        w = torch.randn(4096, 4096, device="cuda")
+        for _ in range(4):
+            w = w @ w * 1e-3
+        q2.copy_(q)
+        got = plan.forward(q2, k, v, lam)
+    side.synchronize()
+    assert torch.equal(got, want)
