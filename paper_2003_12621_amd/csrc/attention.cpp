@@ -153,9 +153,8 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
                                               group * ((p.queries + 31LL) / 32));
     plan->query_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_q * ((p.queries + 127LL) / 128),
                                                 (p.keys + 31LL) / 32);
-    const size_t shared = key_part_bytes(p, plan->key_splits), other = query_part_bytes(p, plan->query_splits);
     plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (dlam_parts(p, plan->query_splits) + 1) * 4) +
-                        (shared > other ? shared : other);
+                        key_part_bytes(p, plan->key_splits) + query_part_bytes(p, plan->query_splits);
     // workgroups of the largest launches (a dimension of a grid holds below 2^32 threads)
     const double heads = double(p.batch) * p.heads_q;
     const double groups[] = {heads * ((p.queries + 63) / 64), heads * ((p.keys + 127) / 128) * plan->key_splits,
@@ -360,11 +359,11 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.parts = dlam_parts(p, plan->query_splits);
         a.delta = static_cast<float*>(workspace);
         a.dlam_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + round256(lse_bytes(p)));
-        // (the two kernels' parts in turn)
         a.key_splits = plan->key_splits;
         a.query_splits = plan->query_splits;
         a.lam32 = a.dlam_part + size_t(p.heads_q) * a.parts;
-        a.key_part = a.query_part = a.dlam_part + round256(size_t(p.heads_q) * (a.parts + 1) * 4) / 4;
+        a.key_part = a.dlam_part + round256(size_t(p.heads_q) * (a.parts + 1) * 4) / 4;
+        a.query_part = a.key_part + key_part_bytes(p, plan->key_splits) / 4;
         a.dq = dq;
         a.dk = dk;
         a.dv_out = dv;

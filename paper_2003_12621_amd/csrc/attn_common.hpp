@@ -26,6 +26,26 @@ __device__ __forceinline__ float attn_lambda(const AttnArgs& a, int h) {
     return a.lam_f32 ? static_cast<const float*>(a.lam)[i] : float(static_cast<const __bf16*>(a.lam)[i]);
 }
 
+// Which tile, head and share of it a workgroup takes, of `parts` shares of
+// `tiles` tiles of `heads` heads.  Neighbours share an XCD and its L2.  Under a
+// causal mask tiles differ in length, and `place` counts from the longest: the
+// heads of an XCD, or as many as make 256 workgroups (a quarter of that to four
+// times that are there at once), go through their tiles together, the longest
+// first, and every other round of an XCD's 32 compute units backwards, so that
+// a long and a short tile meet on a unit.
+struct AttnPlace {
+    int place, head, part;
+};
+__device__ __forceinline__ AttnPlace attn_place(const AttnArgs& a, int tiles, int heads, int parts) {
+    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
+    int band = 1;
+    if (a.causal) band = max(1, min(heads / kNumXcd, (256 + tiles * parts - 1) / (tiles * parts)));
+    const int first = id / (band * tiles * parts) * band, n = min(band, heads - first);
+    int i = id - first * tiles * parts;
+    if (a.causal && (i & 32)) i = (i & ~31) + min(i | 31, n * tiles * parts - 1) - i;
+    return {i / (n * parts), first + i / parts % n, i % parts};
+}
+
 // A value at an address that is the same in all lanes, written before this
 // kernel started: by a scalar load, which the vector loads' count leaves out.
 __device__ __forceinline__ float uniform_load(const float* p) {

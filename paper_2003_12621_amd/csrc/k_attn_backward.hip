@@ -10,6 +10,8 @@
 // recompute the scores, rather than one that would add to dq with atomics:
 // results do not depend on the order of workgroups.  D1 and D2 come from the
 // saved outputs; dlam, a sum in which much cancels, from the terms themselves.
+#include <algorithm>
+
 #include "attn_common.hpp"
 
 namespace fftsplit {
@@ -42,7 +44,7 @@ __device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool 
 
 }  // namespace
 
-// D1 and lam D2 of kAttnDeltaRows rows of one head.
+// -D1 and lam D2 of kAttnDeltaRows rows of one head.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
@@ -74,57 +76,53 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
         s2 = row_group_sum(s2);
         if (l == 0) {
             float* delta = a.delta + (size_t(b) * a.hq + h) * 2 * a.sq + row;
-            delta[0] = s1;
+            delta[0] = -s1;
             delta[a.sq] = lam * s2;
         }
     }
 }
 
-// dlam from its parts, in a fixed order: one workgroup a head, or one for all
-// heads together.
-__global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
-    __shared__ float sums[256];
-    const int heads = a.lam_step ? 1 : a.hq;
-    const float* part = a.dlam_part + size_t(blockIdx.x) * a.parts;
-    float t = 0.f;
-    for (long long i = threadIdx.x; i < (long long)heads * a.parts; i += 256) t += part[i];
-    sums[threadIdx.x] = t;
-    __syncthreads();
-    for (int m = 128; m > 0; m /= 2) {
-        if (int(threadIdx.x) < m) sums[threadIdx.x] += sums[threadIdx.x + m];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-        if (a.lam_f32)
-            static_cast<float*>(a.dlam)[blockIdx.x] = sums[0];
-        else
-            static_cast<__bf16*>(a.dlam)[blockIdx.x] = __bf16(sums[0]);
-    }
-}
-
 namespace {
+
+// What a workgroup of the key side computes: all gradients of its keys, those
+// of one map's keys, or those of the values.
+constexpr int kAll = 0, kOneMap = 1, kValues = 2;
 
 constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
 
-template <typename T, int D, int DV>
+// At the largest widths the operands and accumulators of all gradients do not
+// fit a lane's registers: separate workgroups compute them, and what they share
+// (t, the scores) more than once.  In bf16 that is 4/3 of the products, but two
+// workgroups run on a compute unit, not one: 2 x 1999 causal tokens of 8 heads
+// (4 key heads) take 137 us, not 259.  (fp32 at 64 / 128 would fit two as well,
+// at 4/3 of the products; it is bound by those: 466 us, not 342, at 4 x 1024
+// tokens of 8 heads.)
+template <int D> constexpr bool kApart = D == 128;
+
+template <typename T, int D, int DV, int DO>
 struct KeySideShape {
-    // queries per stage: 64 where two such stages fit, which halves the steps' fixed cost
-    static constexpr int kRows = 32;
+    static constexpr int kRows = 32;                                   // queries per stage
+    static constexpr int kMaps = DO == kOneMap ? 1 : 2;
     static constexpr int kQueryBytes = TileShape<T, D>::bytes(kRows);
     static constexpr int kGradBytes = TileShape<T, DV>::bytes(kRows);
-    static constexpr int kStatBytes = 1024;                            // 4 values a row, at most 64 rows; tiles start at multiples of 1024
-    static constexpr int kBufferBytes = 2 * kQueryBytes + kGradBytes + kStatBytes;
-    // The workgroup's keys stay in LDS where two workgroups a compute unit are
-    // aimed at: as operands in registers they would not leave room for that.
+    static constexpr int kStatBytes = 1024;                            // 4 values a row; tiles start at multiples of 1024
+    static constexpr int kQueries = kMaps * kQueryBytes;
+    static constexpr int kBufferBytes = kQueries + kGradBytes + kStatBytes;
+    // workgroups a compute unit aimed at
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 || (sizeof(T) == 2 && kApart<D>) ? 2 : 1;
+    // Where all gradients are computed by two workgroups a compute unit, the keys
+    // stay in LDS: as operands in registers they would not leave room for that.
     static constexpr bool kKeysInLds = sizeof(T) * DV <= 256;
-    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;
-    static constexpr int kAhead = sizeof(T) * DV == 256 ? 0 : 1;
     static constexpr int kKeyBytes = kKeysInLds ? TileShape<T, D>::bytes(kKeySideKeys) : 0;
+    // Operands from LDS are read this many pairs before they are used, where
+    // registers are left for it.
+    static constexpr int kAhead = sizeof(T) * DV == 256 ? 0 : 1;
     // Stages in LDS: one worked on, the others on their way.  With one on its way
     // a step waits for most of the memory's latency.
     static constexpr int kRoom = (163840 / kBlocks - 2 * kKeyBytes) / kBufferBytes;
     static constexpr int kStages = kRoom < 4 ? kRoom : 4;
     static constexpr int kLds = kStages * kBufferBytes + 2 * kKeyBytes;
+    static_assert(kStages >= 2, "a stage on its way");
 };
 
 // Four values of an array in LDS that belong to rows 4 g .. 4 g + 3 of a lane's
@@ -146,28 +144,19 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 
 }  // namespace
 
-// What a launch of either kernel below computes.
-constexpr int kFirst = 1, kSecond = 2, kBoth = 3;    // the gradients of a map's keys or queries
-constexpr int kValues = 4;                           // dv
-constexpr int kAll = 7;
-
 // Key side: one workgroup takes 128 keys of one key head, 32 a wave, and goes
 // over the queries of all heads that share it (or over its share of them).
 // Each wave keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as
 // accumulators in registers.
 template <typename T, int D, int DV, bool WIDE, int DO>
-__global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 2) : 1)) void attn_key_side_kernel(AttnArgs a) {
-    using Shape = KeySideShape<T, D, DV>;
+__device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& place, int map) {
+    using Shape = KeySideShape<T, D, DV, DO>;
     constexpr int kRows = Shape::kRows;
-    constexpr bool DK = (DO & kBoth) != 0, DVAL = (DO & kValues) != 0;
-    constexpr bool M1 = DVAL || (DO & kFirst), M2 = DVAL || (DO & kSecond);      // maps whose scores are needed
-    constexpr bool DK1 = DO & kFirst, DK2 = DO & kSecond;
+    constexpr bool ONE = DO == kOneMap, DK = DO != kValues, DVAL = DO != kOneMap;
+    constexpr bool M2 = !ONE, DK2 = DK && M2;     // (with one map, that takes the first one's place)
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tiles = (a.sk + kKeySideKeys - 1) / kKeySideKeys;
-    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int tile = id % tiles, split = id / tiles % a.key_splits, hkv = id / tiles / a.key_splits % a.hk;
-    const int b = id / tiles / a.key_splits / a.hk;
+    const int tile = place.place, hkv = place.head % a.hk, b = place.head / a.hk, split = place.part % a.key_splits;
     const int group = a.hq / a.hk;
     const int length = attn_length(a, b), offset = length - a.sq;
     const int first = tile * kKeySideKeys, wave_first = first + wave * 32, key = wave_first + (lane & 31);
@@ -179,29 +168,29 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 
 
     constexpr bool kKeysInLds = Shape::kKeysInLds;
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
-    Operand<T> k1[kKeysInLds || !M1 ? 1 : D / 16], k2[kKeysInLds || !M2 ? 1 : D / 16], v[DK ? DV / 16 : 1];
+    Operand<T> k1[kKeysInLds ? 1 : D / 16], k2[kKeysInLds || !M2 ? 1 : D / 16], v[DK ? DV / 16 : 1];
     unsigned key1 = 0;      // LDS address of this lane's key
     {
         if constexpr (kKeysInLds) {
             const unsigned tile1 = base + Shape::kStages * Shape::kBufferBytes;
             const RowCopy<T, D, kKeySideKeys, 256, WIDE> key_copy(a.kt, a.d, tid);
-            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)first * a.kt + hkv * a.kh;
+            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)first * a.kt + hkv * a.kh + map * a.km;
             key_copy.start(tile1, p, a.kt, length - first, tid);
-            key_copy.start(tile1 + Shape::kKeyBytes, p + a.km, a.kt, length - first, tid);
+            if constexpr (M2) key_copy.start(tile1 + Shape::kKeyBytes, p + a.km, a.kt, length - first, tid);
             key1 = tile1 + row_lane<T, D>(lane) + wave * TileShape<T, D>::bytes(32);
         } else {
-            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh;
-            if constexpr (M1) load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
+            const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)key * a.kt + hkv * a.kh + map * a.km;
+            load_row_operands<T, D, WIDE>(k1, p, a.d, exists, lane);
             if constexpr (M2) load_row_operands<T, D, WIDE>(k2, p + a.km, a.d, exists, lane);
         }
         if constexpr (DK)
             load_row_operands<T, DV, WIDE>(v, static_cast<const T*>(a.v) + b * a.vb + (long long)key * a.vt + hkv * a.vh,
                                      a.dv, exists, lane);
     }
-    if constexpr (!kKeysInLds && M1) settle(k1);
+    if constexpr (!kKeysInLds) settle(k1);
     if constexpr (!kKeysInLds && M2) settle(k2);
     if constexpr (DK) settle(v);
-    floatx16 dk1[DK1 ? D / 32 : 1], dk2[DK2 ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
+    floatx16 dk1[DK ? D / 32 : 1], dk2[DK2 ? D / 32 : 1], dval[DVAL ? DV / 32 : 1];
 #pragma unroll
     for (auto& x : dk1) x = zero16();
 #pragma unroll
@@ -218,39 +207,37 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 
     const int begin = int(steps * split / a.key_splits), end = int(steps * (split + 1) / a.key_splits);
 
     // (small tiles: the first half of the threads copies q1, the second q2)
-    constexpr bool kHalves = kRows * TileShape<T, D>::kRowChunks < 256;
+    constexpr bool kHalves = kRows * TileShape<T, D>::kRowChunks < 256 && !ONE;
     using QueryCopy = RowCopy<T, D, kRows, kHalves ? 128 : 256, WIDE>;
     using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
     const QueryCopy query_copy(a.qt, a.d, kHalves ? tid & 127 : tid);
     const GradCopy grad_copy(a.gt, a.dv, tid);
     const unsigned query_row = row_lane<T, D>(lane), query_column = column_lane<T, D>(lane);
-    const unsigned grad_row = row_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
-    const unsigned grad_column = column_lane<T, DV>(lane) + 2 * Shape::kQueryBytes;
+    const unsigned grad_row = row_lane<T, DV>(lane) + Shape::kQueries;
+    const unsigned grad_column = column_lane<T, DV>(lane) + Shape::kQueries;
     constexpr int kStages = Shape::kStages;
     // copies of a wave per stage (the same for all waves)
-    constexpr int kCopies = (kHalves ? 1 : 2) * QueryCopy::kCopies + GradCopy::kCopies + 1;
+    constexpr int kCopies = (kHalves || ONE ? 1 : 2) * QueryCopy::kCopies + GradCopy::kCopies + 1;
     static_assert(QueryCopy::kWhole && GradCopy::kWhole, "waves count their copies alike");
-    // A wave copies 64 of the 4 kRows values of lse of both maps and delta of
-    // both: one of them, or two of 32 rows each (then two waves copy the same).
-    constexpr int kStatRows = kRows == 64 ? 64 : 32;
-    const int stat_row = lane % kStatRows, stat_which = kRows == 64 ? wave : 2 * (wave & 1);
-    const unsigned stat_off = unsigned(stat_row + lane / kStatRows * a.sq) * 4;
+    // A wave copies lse of both maps or delta of both: 2 x 32 values (and two
+    // waves copy the same).
+    const float* const stat = wave & 1 ? a.delta : a.lse;
+    const unsigned stat_off = unsigned((lane & 31) + hi * a.sq) * 4;
     auto fetch = [&](int h, int row0, bool any, unsigned buffer) {
         const int left = any ? a.sq - row0 : 0;
-        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh;
+        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh + map * a.qm;
         if constexpr (kHalves) {
             query_copy.start(buffer + (wave >> 1) * Shape::kQueryBytes, q + (wave >> 1) * a.qm, a.qt, left, tid & 127);
         } else {
             query_copy.start(buffer, q, a.qt, left, tid);
-            query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
+            if constexpr (M2) query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
         }
-        grad_copy.start(buffer + 2 * Shape::kQueryBytes,
+        grad_copy.start(buffer + Shape::kQueries,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
         // Rows beyond the last are zero: their terms are finite, and dO, dP and delta zero.
-        const float* x = (stat_which < 2 ? a.lse : a.delta) + ((size_t(b) * a.hq + h) * 2 + (stat_which & 1)) * a.sq + row0;
-        const int maps = kRows == 64 ? 1 : 2;
-        copy4(copy_source(x, left > 0 ? unsigned(maps * a.sq - row0) * 4 : 0u), stat_row < left ? stat_off : kOutOfRange,
-              __builtin_amdgcn_readfirstlane(buffer + 2 * Shape::kQueryBytes + Shape::kGradBytes + stat_which * kRows * 4));
+        copy4(copy_source(stat + (size_t(b) * a.hq + h) * 2 * a.sq + row0, left > 0 ? unsigned(2 * a.sq - row0) * 4 : 0u),
+              (lane & 31) < left ? stat_off : kOutOfRange,
+              __builtin_amdgcn_readfirstlane(buffer + Shape::kQueries + Shape::kGradBytes + (wave & 1) * 2 * kRows * 4));
     };
     // rows of the steps to come
     int h = hkv * group + (begin < end ? begin / per_head : 0);
@@ -274,120 +261,114 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 
         const unsigned r1 = buffer + query_row, c1 = buffer + query_column;
         const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
         const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
-        const float* stats = reinterpret_cast<const float*>(lds + (buffer - base) + 2 * Shape::kQueryBytes + Shape::kGradBytes);
+        const float* ts = reinterpret_cast<const float*>(lds + (buffer - base) + Shape::kQueries + Shape::kGradBytes);
         // this stage is there, and all waves are done with the one before
         copies_done<(kStages - 2) * kCopies>();
         // (past the last step, copies of nothing keep the count)
         fetch_next(step + kStages - 1 < end);
         buffer = buffer + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : buffer + Shape::kBufferBytes;
-        const int stage_row0 = row0;
-        const float lam = uniform_load(a.lam32 + h);
+        const int block_row0 = row0;
+        const float lam = uniform_load(a.lam32 + h), turn = map ? -lam : 1.f;
         row0 += kRows;
         if (row0 >= a.sq) {
             row0 = tile0 * kRows;
             ++h;
         }
-#pragma unroll 1
-        for (int sub = 0; sub < kRows; sub += 32) {
-            const int block_row0 = stage_row0 + sub;
-            const float* ts = stats + sub;
-            if (sub > 0 && block_row0 >= a.sq) break;
-            // The products after the scores: dv (columns of dO with P1 - lam P2), t
-            // (rows of dO with v) and dk (columns of q with dS), two at a time; their
-            // operands from LDS are read kAhead pairs before they are used.
-            constexpr int N = DV / 32;                                // pairs of each (DV = 2 D)
-            static_assert(DV == 2 * D, "pairs");
-            constexpr int kT = DVAL ? N : 0, kK = kT + (DK ? N : 0), kEnd = kK + (DK ? N : 0), kAhead = Shape::kAhead;
-            Operand<T> ring[kAhead + 1][2];
-            auto read_pair = [&](int pair) {
-                if (pair >= kEnd) return;
-                Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
+        // The products after the scores: dv (columns of dO with P1 - lam P2), t
+        // (rows of dO with v) and dk (columns of q with dS), two at a time; their
+        // operands from LDS are read kAhead pairs before they are used.
+        constexpr int N = DV / 32;                                // pairs of each (DV = 2 D)
+        static_assert(DV == 2 * D, "pairs");
+        constexpr int kT = DVAL ? N : 0, kK = kT + (DK ? N : 0), kEnd = kK + (DK ? N : 0), kAhead = Shape::kAhead;
+        Operand<T> ring[kAhead + 1][2];
+        auto read_pair = [&](int pair) {
+            if (pair >= kEnd) return;
+            Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    if (pair < kT) {
-                        const int i = 2 * pair + e;
-                        o[e] = read_column<T, DV>(cg, sub, 32 * (i % N), i / N);
-                    } else if (pair < kK) {
-                        o[e] = read_row<T, DV>(rg, sub, 2 * (pair - kT) + e);
-                    } else {
-                        const int i = pair - kK;                      // column block i % (D / 32), rows i / (D / 32)
-                        if (e ? DK2 : DK1) o[e] = read_column<T, D>(e ? c2 : c1, sub, 32 * (i % (D / 32)), i / (D / 32));
-                    }
-                }
-            };
-
-            floatx16 p1 = zero16(), p2 = zero16();
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                if constexpr (M1) mma(p1, read_row<T, D>(r1, sub, s), kKeysInLds ? read_row<T, D>(key1, 0, s) : k1[kKeysInLds ? 0 : s]);
-                if constexpr (M2)
-                    mma(p2, read_row<T, D>(r2, sub, s),
-                        kKeysInLds ? read_row<T, D>(key1 + Shape::kKeyBytes, 0, s) : k2[kKeysInLds ? 0 : s]);
-            }
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 l1 = rows_of(ts, g, hi), l2 = rows_of(ts + kRows, g, hi);
-                const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if constexpr (M1) p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
-                    if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j]));
-                }
-            }
-            if (block_row0 < all_from) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const bool hidden = block_row0 + acc_row(r, hi) < from;
-                    p1[r] = hidden ? 0.f : p1[r];
-                    p2[r] = hidden ? 0.f : p2[r];
-                }
-            }
-            floatx16 t = zero16();
-            Operand<T> w[2], s1[2], s2[2];
-            if constexpr (DVAL) {
-                floatx16 difference;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) difference[r] = fmaf(-lam, p2[r], p1[r]);
-                w[0] = acc_operand<T>(difference, 0);
-                w[1] = acc_operand<T>(difference, 1);
-            }
-            in_order();
-#pragma unroll
-            for (int pair = 0; pair < kAhead; ++pair) read_pair(pair);
-#pragma unroll
-            for (int pair = 0; pair < kEnd; ++pair) {
-                if (kAhead) in_order();
-                read_pair(pair + kAhead);
-                if (kAhead) in_order();
-                Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
-                if (DK && pair == kK) {
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const float4 u1 = rows_of(ts + 2 * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
-                        const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if constexpr (DK1) p1[4 * g + j] *= t[4 * g + j] - d1[j];
-                            if constexpr (DK2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
-                        }
-                    }
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        s1[s] = acc_operand<T>(p1, s);
-                        s2[s] = acc_operand<T>(p2, s);
-                    }
-                }
+            for (int e = 0; e < 2; ++e) {
                 if (pair < kT) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) mma(dval[DVAL ? (2 * pair + e) % N : 0], o[e], w[(2 * pair + e) / N % 2]);
+                    const int i = 2 * pair + e;
+                    o[e] = read_column<T, DV>(cg, 0, 32 * (i % N), i / N);
                 } else if (pair < kK) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) mma(t, o[e], v[DK ? 2 * (pair - kT) + e : 0]);
+                    o[e] = read_row<T, DV>(rg, 0, 2 * (pair - kT) + e);
                 } else {
-                    const int i = pair - kK, d = i % (D / 32), s = i / (D / 32) % 2;
-                    if constexpr (DK1) mma(dk1[d], o[0], s1[s]);
-                    if constexpr (DK2) mma(dk2[d], o[1], s2[s]);
+                    const int i = pair - kK;                      // column block i % (D / 32), rows i / (D / 32)
+                    if (e ? DK2 : DK) o[e] = read_column<T, D>(e ? c2 : c1, 0, 32 * (i % (D / 32)), i / (D / 32));
                 }
+            }
+        };
+
+        floatx16 p1 = zero16(), p2 = zero16();
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            mma(p1, read_row<T, D>(r1, 0, s), kKeysInLds ? read_row<T, D>(key1, 0, s) : k1[kKeysInLds ? 0 : s]);
+            if constexpr (M2)
+                mma(p2, read_row<T, D>(r2, 0, s),
+                    kKeysInLds ? read_row<T, D>(key1 + Shape::kKeyBytes, 0, s) : k2[kKeysInLds ? 0 : s]);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 l1 = rows_of(ts + map * kRows, g, hi), l2 = rows_of(ts + kRows, g, hi);
+            const float m1[4] = {l1.x, l1.y, l1.z, l1.w}, m2[4] = {l2.x, l2.y, l2.z, l2.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p1[4 * g + j] = exp2_fast(fmaf(p1[4 * g + j], a.scale_log2, -m1[j]));
+                if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j]));
+            }
+        }
+        if (block_row0 < all_from) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool hidden = block_row0 + acc_row(r, hi) < from;
+                p1[r] = hidden ? 0.f : p1[r];
+                p2[r] = hidden ? 0.f : p2[r];
+            }
+        }
+        floatx16 t = zero16();
+        Operand<T> w[2], s1[2], s2[2];
+        if constexpr (DVAL) {
+            floatx16 difference;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) difference[r] = fmaf(-lam, p2[r], p1[r]);
+            w[0] = acc_operand<T>(difference, 0);
+            w[1] = acc_operand<T>(difference, 1);
+        }
+        in_order();
+#pragma unroll
+        for (int pair = 0; pair < kAhead; ++pair) read_pair(pair);
+#pragma unroll
+        for (int pair = 0; pair < kEnd; ++pair) {
+            if (kAhead) in_order();
+            read_pair(pair + kAhead);
+            if (kAhead) in_order();
+            Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
+            if (DK && pair == kK) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 u1 = rows_of(ts + (2 + map) * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
+                    const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p1[4 * g + j] *= ONE ? fmaf(turn, t[4 * g + j], d1[j]) : t[4 * g + j] + d1[j];
+                        if constexpr (DK2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    s1[s] = acc_operand<T>(p1, s);
+                    s2[s] = acc_operand<T>(p2, s);
+                }
+            }
+            if (pair < kT) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) mma(dval[DVAL ? (2 * pair + e) % N : 0], o[e], w[(2 * pair + e) / N % 2]);
+            } else if (pair < kK) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) mma(t, o[e], v[DK ? 2 * (pair - kT) + e : 0]);
+            } else {
+                const int i = pair - kK, d = i % (D / 32), s = i / (D / 32) % 2;
+                mma(dk1[DK ? d : 0], o[0], s1[s]);
+                if constexpr (DK2) mma(dk2[d], o[1], s2[s]);
             }
         }
     }
@@ -397,24 +378,40 @@ __global__ __launch_bounds__(256, (sizeof(T) * DV <= 256 ? (DO == kValues ? 2 : 
     if (a.key_splits > 1) {
         // [split][key][dk1, dk2, dv], unscaled
         float* part = a.key_part + (size_t(split) * a.n * a.sk * a.hk + at) * (2 * a.d + a.dv);
-        if constexpr (DK1) store_row(part, dk1, a.d, whole && a.o_wide, 1.f, hi);
+        if constexpr (DK) store_row(part + map * a.d, dk1, a.d, whole && a.o_wide, 1.f, hi);
         if constexpr (DK2) store_row(part + a.d, dk2, a.d, whole && a.o_wide, 1.f, hi);
         if constexpr (DVAL) store_row(part + 2 * a.d, dval, a.dv, whole && a.o_wide, 1.f, hi);
         return;
     }
     T* dk = static_cast<T*>(a.dk) + at * 2 * a.d;
-    if constexpr (DK1) store_row(dk, dk1, a.d, whole, a.scale, hi);
+    if constexpr (DK) store_row(dk + map * a.d, dk1, a.d, whole, a.scale, hi);
     if constexpr (DK2) store_row(dk + a.d, dk2, a.d, whole, a.scale, hi);
     if constexpr (DVAL) store_row(static_cast<T*>(a.dv_out) + at * a.dv, dval, a.dv, a.o_wide, 1.f, hi);
+}
+
+template <typename T, int D, int DV, bool WIDE>
+__global__ __launch_bounds__(256, (KeySideShape<T, D, DV, kAll>::kBlocks)) void attn_key_side_kernel(AttnArgs a) {
+    const AttnPlace place = attn_place(a, (a.sk + kKeySideKeys - 1) / kKeySideKeys, a.n * a.hk, a.key_splits * (kApart<D> ? 3 : 1));
+    if constexpr (kApart<D>) {
+        const int which = place.part / a.key_splits;
+        if (which < 2)
+            key_side<T, D, DV, WIDE, kOneMap>(a, place, which);
+        else
+            key_side<T, D, DV, WIDE, kValues>(a, place, 0);
+    } else {
+        key_side<T, D, DV, WIDE, kAll>(a, place, 0);
+    }
 }
 
 namespace {
 template <typename T, int D, int DV>
 struct QuerySideShape {
     static constexpr int kKeys = 32;
+    static constexpr int kMaps = kApart<D> ? 1 : 2;
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
-    static constexpr int kBufferBytes = 2 * kKeyBytes + TileShape<T, DV>::bytes(kKeys);
-    static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 2 : 1;
+    static constexpr int kMapBytes = kMaps * kKeyBytes;
+    static constexpr int kBufferBytes = kMapBytes + TileShape<T, DV>::bytes(kKeys);
+    static constexpr int kBlocks = sizeof(T) * DV <= 256 || (sizeof(T) == 2 && kApart<D>) ? 2 : 1;
     static constexpr int kStages = 2;     // (more were no faster)
     static constexpr int kLds = kStages * kBufferBytes;
 };
@@ -422,17 +419,17 @@ struct QuerySideShape {
 
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does.
-template <typename T, int D, int DV, bool WIDE, int DO>
+template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
     constexpr int kKeys = Shape::kKeys;
-    constexpr bool M1 = DO & kFirst, M2 = DO & kSecond;
+    constexpr bool ONE = kApart<D>, M2 = !ONE;      // (with one map, that takes the first one's place)
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles = (a.sq + kAttnRows - 1) / kAttnRows;
-    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int tile = tiles - 1 - id % tiles, split = id / tiles % a.query_splits;
-    const int h = id / tiles / a.query_splits % a.hq, b = id / tiles / a.query_splits / a.hq;
+    const AttnPlace place = attn_place(a, tiles, a.n * a.hq, a.query_splits * (ONE ? 2 : 1));
+    const int tile = tiles - 1 - place.place, h = place.head % a.hq, b = place.head / a.hq;
+    const int split = place.part % a.query_splits, map = place.part / a.query_splits;
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
     const int first = tile * kAttnRows + wave * 32, row = first + (lane & 31);
@@ -446,42 +443,43 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
     const int end = min(seen, int(stages * (split + 1) / a.query_splits) * kKeys);
     const float lam = attn_lambda(a, h);
 
-    const T* kp = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh;
+    const T* kp = static_cast<const T*>(a.k) + b * a.kb + hkv * a.kh + map * a.km;
     const T* vp = static_cast<const T*>(a.v) + b * a.vb + hkv * a.vh;
     const bool valid = row < a.sq;
-    Operand<T> q1[M1 ? D / 16 : 1], q2[M2 ? D / 16 : 1], g[DV / 16];
+    Operand<T> q1[D / 16], q2[M2 ? D / 16 : 1], g[DV / 16];
     {
-        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh;
-        if constexpr (M1) load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
+        const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row * a.qt + h * a.qh + map * a.qm;
+        load_row_operands<T, D, WIDE>(q1, q, a.d, valid, lane);
         if constexpr (M2) load_row_operands<T, D, WIDE>(q2, q + a.qm, a.d, valid, lane);
         load_row_operands<T, DV, WIDE>(g, static_cast<const T*>(a.dout) + b * a.gb + (long long)row * a.gt + h * a.gh, a.dv,
                                  valid, lane);
     }
-    const size_t at = (size_t(b) * a.hq + h) * 2 * a.sq + row;
-    float lse1 = valid ? a.lse[at] : kInf, lse2 = valid ? a.lse[at + a.sq] : kInf;
-    float d1 = valid ? a.delta[at] : 0.f, d2 = valid ? a.delta[at + a.sq] : 0.f;
+    const size_t at = ((size_t(b) * a.hq + h) * 2 + map) * a.sq + row;
+    float lse1 = valid ? a.lse[at] : kInf, lse2 = valid && M2 ? a.lse[at + a.sq] : kInf;
+    float d1 = valid ? a.delta[at] : 0.f, d2 = valid && M2 ? a.delta[at + a.sq] : 0.f;
+    const float turn = map ? -lam : 1.f;
     asm volatile("" : "+v"(lse1), "+v"(lse2), "+v"(d1), "+v"(d2));
-    if constexpr (M1) settle(q1);
+    settle(q1);
     if constexpr (M2) settle(q2);
     settle(g);
-    floatx16 dq1[M1 ? D / 32 : 1], dq2[M2 ? D / 32 : 1];
+    floatx16 dq1[D / 32], dq2[M2 ? D / 32 : 1];
 #pragma unroll
     for (auto& x : dq1) x = zero16();
 #pragma unroll
     for (auto& x : dq2) x = zero16();
 
     // (small tiles: the first half of the threads copies k1, the second k2)
-    constexpr bool kHalves = kKeys * TileShape<T, D>::kRowChunks < 256 && DO == kBoth;
+    constexpr bool kHalves = kKeys * TileShape<T, D>::kRowChunks < 256 && !ONE;
     using KeyCopy = RowCopy<T, D, kKeys, kHalves ? 128 : 256, WIDE>;
     using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
     const KeyCopy key_copy(a.kt, a.d, kHalves ? tid & 127 : tid);
     const ValueCopy value_copy(a.vt, a.dv, tid);
     constexpr int kStages = Shape::kStages;
-    constexpr int kCopies = (kHalves ? 1 : int(M1) + int(M2)) * KeyCopy::kCopies + ValueCopy::kCopies;
+    constexpr int kCopies = (kHalves || ONE ? 1 : 2) * KeyCopy::kCopies + ValueCopy::kCopies;
     static_assert(KeyCopy::kWhole && ValueCopy::kWhole, "waves count their copies alike");
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
     const unsigned key_row = row_lane<T, D>(lane), key_column = column_lane<T, D>(lane);
-    const unsigned value_row = row_lane<T, DV>(lane) + 2 * Shape::kKeyBytes;
+    const unsigned value_row = row_lane<T, DV>(lane) + Shape::kMapBytes;
     unsigned fill = base;                 // the stage to be filled next
     int fill_key = begin;
     auto fetch_next = [&] {
@@ -490,10 +488,10 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
         if constexpr (kHalves) {
             key_copy.start(fill + (wave >> 1) * Shape::kKeyBytes, k + (wave >> 1) * a.km, a.kt, left, tid & 127);
         } else {
-            if constexpr (M1) key_copy.start(fill, k, a.kt, left, tid);
+            key_copy.start(fill, k, a.kt, left, tid);
             if constexpr (M2) key_copy.start(fill + Shape::kKeyBytes, k + a.km, a.kt, left, tid);
         }
-        value_copy.start(fill + 2 * Shape::kKeyBytes, vp + (long long)fill_key * a.vt, a.vt, left, tid);
+        value_copy.start(fill + Shape::kMapBytes, vp + (long long)fill_key * a.vt, a.vt, left, tid);
         fill_key += kKeys;
         fill = fill + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : fill + Shape::kBufferBytes;
     };
@@ -513,14 +511,14 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            if constexpr (M1) mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
+            mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
             if constexpr (M2) mma(p2, read_row<T, D>(r2, 0, s), q2[s]);
         }
 #pragma unroll
         for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rv, 0, s), g[s]);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            if constexpr (M1) p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
+            p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
             if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2));
         }
         if (key + 31 > first_last) {
@@ -531,13 +529,11 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
                 p2[r] = hidden ? 0.f : p2[r];
             }
         }
-        if constexpr (M2) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) lam_sum = fmaf(p2[r], t[r], lam_sum);
-        }
+        for (int r = 0; r < 16; ++r) lam_sum = fmaf(ONE ? p1[r] : p2[r], t[r], lam_sum);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            if constexpr (M1) p1[r] *= t[r] - d1;
+            p1[r] *= ONE ? fmaf(turn, t[r], d1) : t[r] + d1;
             if constexpr (M2) p2[r] *= fmaf(-lam, t[r], d2);
         }
 #pragma unroll
@@ -545,12 +541,12 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
             const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
-                if constexpr (M1) mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
+                mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
                 if constexpr (M2) mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
             }
         }
     }
-    if constexpr (M2) {
+    if (!ONE || map) {
         // this workgroup's part of dlam, in a fixed order
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) lam_sum += __shfl_xor(lam_sum, m, 64);
@@ -571,58 +567,123 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
     const float scale = shared ? 1.f : a.scale;
     if (sizeof(T) == 4 || shared) {
         float* to = sizeof(T) == 4 && !shared ? static_cast<float*>(a.dq) + out : part;
-        if constexpr (M1) store_row(to, dq1, a.d, whole, scale, hi);
+        store_row(to + map * a.d, dq1, a.d, whole, scale, hi);
         if constexpr (M2) store_row(to + a.d, dq2, a.d, whole, scale, hi);
         return;
     }
     T* dq = static_cast<T*>(a.dq) + out;
-    if constexpr (M1) store_row(dq, dq1, a.d, whole, scale, hi);
+    store_row(dq + map * a.d, dq1, a.d, whole, scale, hi);
     if constexpr (M2) store_row(dq + a.d, dq2, a.d, whole, scale, hi);
 }
 
-// Adds up the parts of workgroups that shared the steps, in their order:
-// rows of `width` values, of which the first `scaled` go to `a0` (times scale),
-// the rest to `a1`.
-template <typename T>
-__global__ __launch_bounds__(256) void attn_parts_kernel(const float* part, int splits, long long rows, int width, int scaled,
-                                                         float scale, T* a0, T* a1) {
-    const long long n = rows * width;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        float t = 0.f;
-        for (int s = 0; s < splits; ++s) t += part[s * n + i];
-        const long long row = i / width;
-        const int col = int(i - row * width);
-        if (col < scaled)
-            a0[row * scaled + col] = T(t * scale);
+namespace {
+
+// Sums of the parts of workgroups that shared their steps, in their order: rows
+// of `width` values, of which the first `scaled` go to `a0` (times scale), the
+// rest to `a1`, by `blocks` workgroups of which this is the one `block`.
+template <typename T, int V>
+__device__ void add_parts(const float* part, int splits, long long rows, int width, int scaled, float scale, T* a0, T* a1,
+                          int block, int blocks) {
+    const long long n = rows * (width / V);
+    for (long long i = (long long)block * 256 + threadIdx.x; i < n; i += (long long)blocks * 256) {
+        float t[V] = {};
+        for (int s = 0; s < splits; ++s) {
+            if constexpr (V == 4) {
+                const float4 x = reinterpret_cast<const float4*>(part)[s * n + i];
+                t[0] += x.x;
+                t[1] += x.y;
+                t[2] += x.z;
+                t[3] += x.w;
+            } else {
+                t[0] += part[s * n + i];
+            }
+        }
+        const int w = width / V;
+        const long long row = n < 0x7fffffff ? unsigned(i) / unsigned(w) : i / w;
+        const int col = int(i - row * w) * V;
+        const long long at = col < scaled ? row * scaled + col : row * (width - scaled) + col - scaled;
+        T* const to = col < scaled ? a0 : a1;
+        const float f = col < scaled ? scale : 1.f;
+        if constexpr (V == 4)
+            store4(to + at, 0, 4, true, t[0] * f, t[1] * f, t[2] * f, t[3] * f);
         else
-            a1[row * (width - scaled) + col - scaled] = T(t);
+            to[at] = T(t[0] * f);
+    }
+}
+template <typename T>
+__device__ void add_parts(const float* part, int splits, long long rows, int width, int scaled, float scale, void* a0, void* a1,
+                          int block, int blocks) {
+    if (width % 4 == 0 && scaled % 4 == 0)
+        add_parts<T, 4>(part, splits, rows, width, scaled, scale, static_cast<T*>(a0), static_cast<T*>(a1), block, blocks);
+    else
+        add_parts<T, 1>(part, splits, rows, width, scaled, scale, static_cast<T*>(a0), static_cast<T*>(a1), block, blocks);
+}
+
+}  // namespace
+
+// What workgroups computed in parts: dlam, by one workgroup a head (or one for
+// all heads together), then dk and dv, by `key_blocks`, and dq, by the others.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int key_blocks, int query_blocks) {
+    const int lams = a.lam_step ? a.hq : 1, block = int(blockIdx.x) - lams;
+    if (block >= key_blocks) {
+        add_parts<T>(a.query_part, a.query_splits, (long long)a.n * a.sq * a.hq, 2 * a.d, 2 * a.d, a.scale, a.dq, nullptr,
+                     block - key_blocks, query_blocks);
+        return;
+    }
+    if (block >= 0) {
+        add_parts<T>(a.key_part, a.key_splits, (long long)a.n * a.sk * a.hk, 2 * a.d + a.dv, 2 * a.d, a.scale, a.dk, a.dv_out,
+                     block, key_blocks);
+        return;
+    }
+    __shared__ float sums[256];
+    const int heads = a.lam_step ? 1 : a.hq;
+    const float* part = a.dlam_part + size_t(blockIdx.x) * a.parts;
+    float t = 0.f;
+    for (long long i = threadIdx.x; i < (long long)heads * a.parts; i += 256) t += part[i];
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    for (int m = 128; m > 0; m /= 2) {
+        if (int(threadIdx.x) < m) sums[threadIdx.x] += sums[threadIdx.x + m];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        if (a.lam_f32)
+            static_cast<float*>(a.dlam)[blockIdx.x] = sums[0];
+        else
+            static_cast<__bf16*>(a.dlam)[blockIdx.x] = __bf16(sums[0]);
     }
 }
 
 namespace {
 
-template <typename T, int D, int DV, int DO>
+template <typename T, int D, int DV>
 hipError_t launch_key_side(const AttnArgs& a, hipStream_t s) {
-    using Shape = KeySideShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hk * a.key_splits * ((a.sk + kKeySideKeys - 1) / kKeySideKeys);
-    auto kernel = a.wide ? attn_key_side_kernel<T, D, DV, true, DO> : attn_key_side_kernel<T, D, DV, false, DO>;
-    if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, nullptr, a);
+    constexpr int kLds = kApart<D> ? std::max(KeySideShape<T, D, DV, kOneMap>::kLds, KeySideShape<T, D, DV, kValues>::kLds)
+                                   : KeySideShape<T, D, DV, kAll>::kLds;
+    const long long blocks =
+        (long long)a.n * a.hk * a.key_splits * ((a.sk + kKeySideKeys - 1) / kKeySideKeys) * (kApart<D> ? 3 : 1);
+    auto kernel = a.wide ? attn_key_side_kernel<T, D, DV, true> : attn_key_side_kernel<T, D, DV, false>;
+    if (hipError_t e = allow_dynamic_lds(kernel, kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), kLds, s, nullptr, nullptr, a);
 }
-template <typename T, int D, int DV, int DO>
+template <typename T, int D, int DV>
 hipError_t launch_query_side(const AttnArgs& a, hipStream_t s) {
     using Shape = QuerySideShape<T, D, DV>;
-    const long long blocks = (long long)a.n * a.hq * a.query_splits * ((a.sq + kAttnRows - 1) / kAttnRows);
-    auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true, DO> : attn_query_side_kernel<T, D, DV, false, DO>;
+    const long long blocks =
+        (long long)a.n * a.hq * a.query_splits * ((a.sq + kAttnRows - 1) / kAttnRows) * (kApart<D> ? 2 : 1);
+    auto kernel = a.wide ? attn_query_side_kernel<T, D, DV, true> : attn_query_side_kernel<T, D, DV, false>;
     if (hipError_t e = allow_dynamic_lds(kernel, Shape::kLds)) return e;
     return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), Shape::kLds, s, nullptr, nullptr, a);
 }
 template <typename T>
-hipError_t launch_parts(const float* part, int splits, long long rows, int width, int scaled, float scale, void* a0, void* a1,
-                        hipStream_t s) {
-    const long long blocks = (rows * width + 255) / 256;
-    return launch_kernel(attn_parts_kernel<T>, dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, nullptr, nullptr,
-                         part, splits, rows, width, scaled, scale, static_cast<T*>(a0), static_cast<T*>(a1));
+hipError_t launch_finish(const AttnArgs& a, hipStream_t s, hipEvent_t stop) {
+    // (workgroups of 256 threads with 4 values each, as many as run at once)
+    const auto blocks = [](int splits, double values) { return splits > 1 ? int(std::min(2048., values / 1024 + 1)) : 0; };
+    const int key_blocks = blocks(a.key_splits, double(a.n) * a.sk * a.hk * (2 * a.d + a.dv));
+    const int query_blocks = blocks(a.query_splits, double(a.n) * a.sq * a.hq * 2 * a.d);
+    return launch_kernel(attn_finish_kernel<T>, dim3((a.lam_step ? a.hq : 1) + key_blocks + query_blocks), dim3(256), 0, s,
+                         nullptr, stop, a, key_blocks, query_blocks);
 }
 
 template <typename T, int D, int DV>
@@ -631,34 +692,9 @@ hipError_t launch_shaped(const AttnArgs& a, hipStream_t s, const LaunchEvents& e
     const long long rows = (long long)a.n * a.hq * chunks;
     if (hipError_t e = launch_kernel(attn_delta_kernel<T>, dim3(unsigned(rows)), dim3(256), 0, s, ev.start, nullptr, a))
         return e;
-    // At the largest widths the operands and accumulators of all gradients do
-    // not fit a lane's registers: there they are computed one after another.
-    constexpr bool kApart = sizeof(T) * D >= 512;
-    if constexpr (kApart) {
-        if (hipError_t e = launch_key_side<T, D, DV, kFirst>(a, s)) return e;
-        if (hipError_t e = launch_key_side<T, D, DV, kSecond>(a, s)) return e;
-        if (hipError_t e = launch_key_side<T, D, DV, kValues>(a, s)) return e;
-    } else if constexpr (sizeof(T) * D >= 256 && sizeof(T) == 2) {
-        if (hipError_t e = launch_key_side<T, D, DV, kBoth>(a, s)) return e;
-        if (hipError_t e = launch_key_side<T, D, DV, kValues>(a, s)) return e;
-    } else {
-        if (hipError_t e = launch_key_side<T, D, DV, kAll>(a, s)) return e;
-    }
-    if (a.key_splits > 1)
-        if (hipError_t e = launch_parts<T>(a.key_part, a.key_splits, (long long)a.n * a.sk * a.hk, 2 * a.d + a.dv, 2 * a.d,
-                                           a.scale, a.dk, a.dv_out, s))
-            return e;
-    if constexpr (kApart) {
-        if (hipError_t e = launch_query_side<T, D, DV, kFirst>(a, s)) return e;
-        if (hipError_t e = launch_query_side<T, D, DV, kSecond>(a, s)) return e;
-    } else {
-        if (hipError_t e = launch_query_side<T, D, DV, kBoth>(a, s)) return e;
-    }
-    if (a.query_splits > 1)
-        if (hipError_t e = launch_parts<T>(a.query_part, a.query_splits, (long long)a.n * a.sq * a.hq, 2 * a.d, 2 * a.d,
-                                           a.scale, a.dq, nullptr, s))
-            return e;
-    return launch_kernel(attn_dlam_kernel, dim3(a.lam_step ? a.hq : 1), dim3(256), 0, s, nullptr, ev.stop, a);
+    if (hipError_t e = launch_key_side<T, D, DV>(a, s)) return e;
+    if (hipError_t e = launch_query_side<T, D, DV>(a, s)) return e;
+    return launch_finish<T>(a, s, ev.stop);
 }
 
 template <typename T>

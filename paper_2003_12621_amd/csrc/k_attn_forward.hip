@@ -92,9 +92,8 @@ attn_forward_kernel(AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, group = wave >> 1;
     const int tiles = (a.sq + kAttnTiledRows - 1) / kAttnTiledRows;
-    const int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int tile = tiles - 1 - id % tiles;           // under a causal mask the longest first
-    const int h = id / tiles % a.hq, b = id / tiles / a.hq;
+    const AttnPlace place = attn_place(a, tiles, a.n * a.hq, 1);
+    const int tile = tiles - 1 - place.place, h = place.head % a.hq, b = place.head / a.hq;
     const int hkv = h / (a.hq / a.hk);
     const int length = attn_length(a, b);
 
