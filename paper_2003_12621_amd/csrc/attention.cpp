@@ -85,10 +85,14 @@ int choose_splits(const fftsplit_attention_problem_t& p, int shape) {
 }
 
 // Workgroups that share the steps of a tile of 128 keys or rows in the backward
-// pass: as many as fill the chip, of at least 8 steps each (bf16; an fp32 step
-// takes four times as long).  Their parts are added up by another launch.
+// pass: as many as run at once, of at least 8 steps each (bf16; an fp32 step
+// takes four times as long).  Two run at once on a compute unit up to bf16 heads
+// of 64 / 128.  Wider heads have two or three workgroups a tile as it is, and
+// one of fp32 keeps a unit's matrix instructions busy: two took 39 and 31 us for
+// the two sides of 6 x 301 tokens of 6 heads of 32 / 64, one takes 35 and 28.
+// Their parts are added up by another launch.
 int choose_backward_splits(const fftsplit_attention_problem_t& p, int shape, long long tiles, long long steps) {
-    const bool two = kAttnShapes[shape].dv * type_bytes(p.dtype) <= 256;     // workgroups a compute unit
+    const bool two = p.dtype == FFTSPLIT_BF16 && shape < 2;
     const long long least = p.dtype == FFTSPLIT_F32 ? 2 : 8;
     long long splits = (two ? 512 : 256) / tiles;
     if (splits > steps / least) splits = steps / least;

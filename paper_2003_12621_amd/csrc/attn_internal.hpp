@@ -74,7 +74,9 @@ hipError_t launch_attn_forward(const fftsplit_attention_plan_s& p, const AttnArg
                                const LaunchEvents& ev);
 hipError_t launch_attn_backward(const fftsplit_attention_plan_s& p, const AttnArgs& a, hipStream_t s,
                                 const LaunchEvents& ev);
-// Rows of one head that a workgroup of the backward's first kernel reduces.
-constexpr int kAttnDeltaRows = 64;
+// Rows of one head that a workgroup of the backward's first kernel reduces: two
+// for each 16 lanes (four took 6.5 us, not 4.9, at 6 x 301 rows of 6 heads; one
+// 15.7, not 14.3, at 4 x 3136 of 8).
+constexpr int kAttnDeltaRows = 32;
 
 }  // namespace fftsplit
