@@ -203,15 +203,14 @@ __device__ __forceinline__ u32x4 copy_source(const void* base, unsigned bytes) {
     rsrc[3] = 0x00020000u;
     return rsrc;
 }
-// All but the last LATER copies that each wave has started are complete, in all waves.
-template <int LATER = 0>
+// The copies that all waves have started are complete.
 __device__ __forceinline__ void copies_done() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 }
 
 // As above for a tile that only this wave copies and reads: all but the last
-// `later` copies it has started are complete.
+// LATER copies it has started are complete.
 template <int LATER>
 __device__ __forceinline__ void own_copies_done() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
@@ -221,8 +220,9 @@ __device__ __forceinline__ void own_reads_done() { asm volatile("s_waitcnt lgkmc
 
 // Copies rows from memory into a tile of ROWS rows of W elements, spread over
 // THREADS threads: chunk place i of thread t is place t + i THREADS in row
-// order.  Tiles are given by their LDS address.  Memory is read through a descriptor of the rows that exist, so rows
-// beyond them become zero and are not touched; so do columns from `cols` on.
+// order.  Tiles are given by their LDS address.  Memory is read through a
+// descriptor of the rows that exist, so rows beyond them become zero and are not
+// touched; so do columns from `cols` on.
 // WIDE: base, stride and cols allow 16-byte accesses, and the copy goes straight
 // into LDS; else elements pass through registers one by one.
 template <typename T, int W, int ROWS, int THREADS, bool WIDE>
@@ -322,10 +322,7 @@ __device__ __forceinline__ void settle(Operand<T> (&o)[N]) {
     for (int s = 0; s < N; ++s) asm volatile("" : "+v"(o[s].v));
 }
 
-// No instruction is moved across this.  Kernels that read their operands in
-// batches, one batch ahead of the products, put it between a batch's reads and
-// the products before it: left to itself the compiler, short of registers, puts
-// every read right before its product and waits for it there.
+// No instruction is moved across this.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Four consecutive elements of an output row, elements from `cols` on left out

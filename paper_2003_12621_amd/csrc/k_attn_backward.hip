@@ -44,7 +44,9 @@ __device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool 
 
 }  // namespace
 
-// -D1 and lam D2 of kAttnDeltaRows rows of one head.
+// -D1 and lam D2 of kAttnDeltaRows rows of one head, 16 lanes a row.  Bound by
+// memory: 14 us for the 77 MB of 4 x 3136 rows of 8 heads of 128 (bf16; 5.4 TB/s,
+// part of it from the caches).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
@@ -92,11 +94,11 @@ constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
 
 // At the largest widths the operands and accumulators of all gradients do not
 // fit a lane's registers: separate workgroups compute them, and what they share
-// (t, the scores) more than once.  In bf16 that is 4/3 of the products, but two
-// workgroups run on a compute unit, not one: 2 x 1999 causal tokens of 8 heads
-// (4 key heads) take 137 us, not 259.  (fp32 at 64 / 128 would fit two as well,
-// at 4/3 of the products; it is bound by those: 466 us, not 342, at 4 x 1024
-// tokens of 8 heads.)
+// (t, the scores) more than once.  In bf16 that is 3/2 and 4/3 of the products, but two
+// workgroups run on a compute unit, not one: the two sides of 2 x 1999 causal
+// tokens of 8 heads (4 key heads) take 136 and 90 us, not 259 and 147.  (fp32 at
+// 64 / 128 would fit two as well; it is bound by the products: 466 and 303 us,
+// not 342 and 256, at 4 x 1024 tokens of 8 heads.)
 template <int D> constexpr bool kApart = D == 128;
 
 template <typename T, int D, int DV, int DO>
@@ -111,18 +113,11 @@ struct KeySideShape {
     // workgroups a compute unit aimed at
     static constexpr int kBlocks = sizeof(T) * DV <= 256 || (sizeof(T) == 2 && kApart<D>) ? 2 : 1;
     // Where all gradients are computed by two workgroups a compute unit, the keys
-    // stay in LDS: as operands in registers they would not leave room for that.
+    // stay in LDS: as operands in registers they would not leave room for that
+    // (D / 2 of a lane's 256 registers, of which 250 are in use as it is).
     static constexpr bool kKeysInLds = sizeof(T) * DV <= 256;
     static constexpr int kKeyBytes = kKeysInLds ? TileShape<T, D>::bytes(kKeySideKeys) : 0;
-    // Operands from LDS are read this many pairs before they are used, where
-    // registers are left for it.
-    static constexpr int kAhead = sizeof(T) * DV == 256 ? 0 : 1;
-    // Stages in LDS: one worked on, the others on their way.  With one on its way
-    // a step waits for most of the memory's latency.
-    static constexpr int kRoom = (163840 / kBlocks - 2 * kKeyBytes) / kBufferBytes;
-    static constexpr int kStages = kRoom < 4 ? kRoom : 4;
-    static constexpr int kLds = kStages * kBufferBytes + 2 * kKeyBytes;
-    static_assert(kStages >= 2, "a stage on its way");
+    static constexpr int kLds = 2 * kBufferBytes + 2 * kKeyBytes;
 };
 
 // Four values of an array in LDS that belong to rows 4 g .. 4 g + 3 of a lane's
@@ -145,9 +140,20 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 }  // namespace
 
 // Key side: one workgroup takes 128 keys of one key head, 32 a wave, and goes
-// over the queries of all heads that share it (or over its share of them).
-// Each wave keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as
-// accumulators in registers.
+// over the queries of all heads that share it (or over its share of them), 32 a
+// step, double buffered in LDS with the statistics of their rows.  Each wave
+// keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as accumulators in
+// registers.  (Heads that share a key head are summed in the accumulators: their
+// gradients need no other sum.)  Deeper buffers, and operands read from LDS ahead
+// of their products, were no faster.  P1 - lam P2 and dS enter the products
+// rounded to bf16, as in the forward pass.
+//
+// Bound by the chain scores - terms - t - dS - dk of a step, which two workgroups
+// a compute unit (registers allow no third) do not hide: matrix instructions
+// take 37 %, vector instructions 41 % of a unit's busy time, and with 3.1
+// workgroups a unit its last ones run alone (units are busy 82 % of the launch).
+// Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136 tokens, 8 heads of
+// 64 / 128 513 us, 630 TFLOP/s.
 template <typename T, int D, int DV, bool WIDE, int DO>
 __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& place, int map) {
     using Shape = KeySideShape<T, D, DV, DO>;
@@ -172,7 +178,7 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
     unsigned key1 = 0;      // LDS address of this lane's key
     {
         if constexpr (kKeysInLds) {
-            const unsigned tile1 = base + Shape::kStages * Shape::kBufferBytes;
+            const unsigned tile1 = base + 2 * Shape::kBufferBytes;
             const RowCopy<T, D, kKeySideKeys, 256, WIDE> key_copy(a.kt, a.d, tid);
             const T* p = static_cast<const T*>(a.k) + b * a.kb + (long long)first * a.kt + hkv * a.kh + map * a.km;
             key_copy.start(tile1, p, a.kt, length - first, tid);
@@ -206,98 +212,49 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
     const long long steps = (long long)per_head * group;
     const int begin = int(steps * split / a.key_splits), end = int(steps * (split + 1) / a.key_splits);
 
-    // (small tiles: the first half of the threads copies q1, the second q2)
-    constexpr bool kHalves = kRows * TileShape<T, D>::kRowChunks < 256 && !ONE;
-    using QueryCopy = RowCopy<T, D, kRows, kHalves ? 128 : 256, WIDE>;
+    using QueryCopy = RowCopy<T, D, kRows, 256, WIDE>;
     using GradCopy = RowCopy<T, DV, kRows, 256, WIDE>;
-    const QueryCopy query_copy(a.qt, a.d, kHalves ? tid & 127 : tid);
+    const QueryCopy query_copy(a.qt, a.d, tid);
     const GradCopy grad_copy(a.gt, a.dv, tid);
     const unsigned query_row = row_lane<T, D>(lane), query_column = column_lane<T, D>(lane);
     const unsigned grad_row = row_lane<T, DV>(lane) + Shape::kQueries;
     const unsigned grad_column = column_lane<T, DV>(lane) + Shape::kQueries;
-    constexpr int kStages = Shape::kStages;
-    // copies of a wave per stage (the same for all waves)
-    constexpr int kCopies = (kHalves || ONE ? 1 : 2) * QueryCopy::kCopies + GradCopy::kCopies + 1;
-    static_assert(QueryCopy::kWhole && GradCopy::kWhole, "waves count their copies alike");
     // A wave copies lse of both maps or delta of both: 2 x 32 values (and two
     // waves copy the same).
     const float* const stat = wave & 1 ? a.delta : a.lse;
     const unsigned stat_off = unsigned((lane & 31) + hi * a.sq) * 4;
-    auto fetch = [&](int h, int row0, bool any, unsigned buffer) {
-        const int left = any ? a.sq - row0 : 0;
+    auto fetch = [&](int h, int row0, unsigned buffer) {
+        const int left = a.sq - row0;
         const T* q = static_cast<const T*>(a.q) + b * a.qb + (long long)row0 * a.qt + h * a.qh + map * a.qm;
-        if constexpr (kHalves) {
-            query_copy.start(buffer + (wave >> 1) * Shape::kQueryBytes, q + (wave >> 1) * a.qm, a.qt, left, tid & 127);
-        } else {
-            query_copy.start(buffer, q, a.qt, left, tid);
-            if constexpr (M2) query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
-        }
+        query_copy.start(buffer, q, a.qt, left, tid);
+        if constexpr (M2) query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
         grad_copy.start(buffer + Shape::kQueries,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
         // Rows beyond the last are zero: their terms are finite, and dO, dP and delta zero.
-        copy4(copy_source(stat + (size_t(b) * a.hq + h) * 2 * a.sq + row0, left > 0 ? unsigned(2 * a.sq - row0) * 4 : 0u),
+        copy4(copy_source(stat + (size_t(b) * a.hq + h) * 2 * a.sq + row0, unsigned(2 * a.sq - row0) * 4),
               (lane & 31) < left ? stat_off : kOutOfRange,
               __builtin_amdgcn_readfirstlane(buffer + Shape::kQueries + Shape::kGradBytes + (wave & 1) * 2 * kRows * 4));
     };
-    // rows of the steps to come
+    // the rows of this step
     int h = hkv * group + (begin < end ? begin / per_head : 0);
     int row0 = (tile0 + (begin < end ? begin % per_head : 0)) * kRows;
-    int next_h = h, next_row0 = row0;
-    unsigned fill = base;                 // the stage to be filled next
-    auto fetch_next = [&](bool any) {
-        fetch(next_h, next_row0, any, fill);
-        next_row0 += kRows;
-        if (next_row0 >= a.sq) {
-            next_row0 = tile0 * kRows;
-            ++next_h;
-        }
-        fill = fill + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : fill + Shape::kBufferBytes;
-    };
-    if (begin < end)
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) fetch_next(begin + i < end);
-    unsigned buffer = base;
+    if (begin < end) fetch(h, row0, base);
     for (int step = begin; step < end; ++step) {
+        const unsigned buffer = base + ((step - begin) & 1) * Shape::kBufferBytes;
         const unsigned r1 = buffer + query_row, c1 = buffer + query_column;
         const unsigned r2 = r1 + Shape::kQueryBytes, c2 = c1 + Shape::kQueryBytes;
         const unsigned rg = buffer + grad_row, cg = buffer + grad_column;
         const float* ts = reinterpret_cast<const float*>(lds + (buffer - base) + Shape::kQueries + Shape::kGradBytes);
-        // this stage is there, and all waves are done with the one before
-        copies_done<(kStages - 2) * kCopies>();
-        // (past the last step, copies of nothing keep the count)
-        fetch_next(step + kStages - 1 < end);
-        buffer = buffer + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : buffer + Shape::kBufferBytes;
-        const int block_row0 = row0;
         const float lam = uniform_load(a.lam32 + h), turn = map ? -lam : 1.f;
+        const int block_row0 = row0;
         row0 += kRows;
         if (row0 >= a.sq) {
             row0 = tile0 * kRows;
             ++h;
         }
-        // The products after the scores: dv (columns of dO with P1 - lam P2), t
-        // (rows of dO with v) and dk (columns of q with dS), two at a time; their
-        // operands from LDS are read kAhead pairs before they are used.
-        constexpr int N = DV / 32;                                // pairs of each (DV = 2 D)
-        static_assert(DV == 2 * D, "pairs");
-        constexpr int kT = DVAL ? N : 0, kK = kT + (DK ? N : 0), kEnd = kK + (DK ? N : 0), kAhead = Shape::kAhead;
-        Operand<T> ring[kAhead + 1][2];
-        auto read_pair = [&](int pair) {
-            if (pair >= kEnd) return;
-            Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (pair < kT) {
-                    const int i = 2 * pair + e;
-                    o[e] = read_column<T, DV>(cg, 0, 32 * (i % N), i / N);
-                } else if (pair < kK) {
-                    o[e] = read_row<T, DV>(rg, 0, 2 * (pair - kT) + e);
-                } else {
-                    const int i = pair - kK;                      // column block i % (D / 32), rows i / (D / 32)
-                    if (e ? DK2 : DK) o[e] = read_column<T, D>(e ? c2 : c1, 0, 32 * (i % (D / 32)), i / (D / 32));
-                }
-            }
-        };
-
+        // this stage is there, and all waves are done with the other buffer
+        copies_done();
+        if (step + 1 < end) fetch(h, row0, base + ((step + 1 - begin) & 1) * Shape::kBufferBytes);
         floatx16 p1 = zero16(), p2 = zero16();
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
@@ -324,51 +281,39 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
                 p2[r] = hidden ? 0.f : p2[r];
             }
         }
-        floatx16 t = zero16();
-        Operand<T> w[2], s1[2], s2[2];
         if constexpr (DVAL) {
             floatx16 difference;
 #pragma unroll
             for (int r = 0; r < 16; ++r) difference[r] = fmaf(-lam, p2[r], p1[r]);
-            w[0] = acc_operand<T>(difference, 0);
-            w[1] = acc_operand<T>(difference, 1);
+            const Operand<T> w[2] = {acc_operand<T>(difference, 0), acc_operand<T>(difference, 1)};
+            in_order();
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(cg, 0, 32 * d, s), w[s]);
         }
-        in_order();
+        if constexpr (DK) {
+            floatx16 t = zero16();
 #pragma unroll
-        for (int pair = 0; pair < kAhead; ++pair) read_pair(pair);
+            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rg, 0, s), v[s]);
 #pragma unroll
-        for (int pair = 0; pair < kEnd; ++pair) {
-            if (kAhead) in_order();
-            read_pair(pair + kAhead);
-            if (kAhead) in_order();
-            Operand<T> (&o)[2] = ring[pair % (kAhead + 1)];
-            if (DK && pair == kK) {
+            for (int g = 0; g < 4; ++g) {
+                const float4 u1 = rows_of(ts + (2 + map) * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
+                const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 u1 = rows_of(ts + (2 + map) * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
-                    const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        p1[4 * g + j] *= ONE ? fmaf(turn, t[4 * g + j], d1[j]) : t[4 * g + j] + d1[j];
-                        if constexpr (DK2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
-                    }
-                }
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    s1[s] = acc_operand<T>(p1, s);
-                    s2[s] = acc_operand<T>(p2, s);
+                for (int j = 0; j < 4; ++j) {
+                    p1[4 * g + j] *= ONE ? fmaf(turn, t[4 * g + j], d1[j]) : t[4 * g + j] + d1[j];
+                    if constexpr (M2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
                 }
             }
-            if (pair < kT) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) mma(dval[DVAL ? (2 * pair + e) % N : 0], o[e], w[(2 * pair + e) / N % 2]);
-            } else if (pair < kK) {
+            for (int s = 0; s < 2; ++s) {
+                const Operand<T> s1 = acc_operand<T>(p1, s), s2 = acc_operand<T>(p2, s);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) mma(t, o[e], v[DK ? 2 * (pair - kT) + e : 0]);
-            } else {
-                const int i = pair - kK, d = i % (D / 32), s = i / (D / 32) % 2;
-                mma(dk1[DK ? d : 0], o[0], s1[s]);
-                if constexpr (DK2) mma(dk2[d], o[1], s2[s]);
+                for (int d = 0; d < D / 32; ++d) {
+                    mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), s1);
+                    if constexpr (M2) mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), s2);
+                }
             }
         }
     }
@@ -412,13 +357,16 @@ struct QuerySideShape {
     static constexpr int kMapBytes = kMaps * kKeyBytes;
     static constexpr int kBufferBytes = kMapBytes + TileShape<T, DV>::bytes(kKeys);
     static constexpr int kBlocks = sizeof(T) * DV <= 256 || (sizeof(T) == 2 && kApart<D>) ? 2 : 1;
-    static constexpr int kStages = 2;     // (more were no faster)
-    static constexpr int kLds = kStages * kBufferBytes;
+    static constexpr int kLds = 2 * kBufferBytes;
 };
 }  // namespace
 
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
-// goes over the keys, as the forward kernel does.
+// goes over the keys, as the forward kernel does; q1, q2 and dO are operands, dq1
+// and dq2 accumulators in registers.  Bound as the key side is (matrix
+// instructions 45 %, vector instructions 58 % of busy time).  Measured (bf16,
+// 8 d + 2 dv operations a pair): 4 x 3136 tokens, 8 heads of 64 / 128 341 us, 710
+// TFLOP/s; with 64 rows a workgroup 371 us.
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;
@@ -468,45 +416,28 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
 #pragma unroll
     for (auto& x : dq2) x = zero16();
 
-    // (small tiles: the first half of the threads copies k1, the second k2)
-    constexpr bool kHalves = kKeys * TileShape<T, D>::kRowChunks < 256 && !ONE;
-    using KeyCopy = RowCopy<T, D, kKeys, kHalves ? 128 : 256, WIDE>;
+    using KeyCopy = RowCopy<T, D, kKeys, 256, WIDE>;
     using ValueCopy = RowCopy<T, DV, kKeys, 256, WIDE>;
-    const KeyCopy key_copy(a.kt, a.d, kHalves ? tid & 127 : tid);
+    const KeyCopy key_copy(a.kt, a.d, tid);
     const ValueCopy value_copy(a.vt, a.dv, tid);
-    constexpr int kStages = Shape::kStages;
-    constexpr int kCopies = (kHalves || ONE ? 1 : 2) * KeyCopy::kCopies + ValueCopy::kCopies;
-    static_assert(KeyCopy::kWhole && ValueCopy::kWhole, "waves count their copies alike");
     const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds));
     const unsigned key_row = row_lane<T, D>(lane), key_column = column_lane<T, D>(lane);
     const unsigned value_row = row_lane<T, DV>(lane) + Shape::kMapBytes;
-    unsigned fill = base;                 // the stage to be filled next
-    int fill_key = begin;
-    auto fetch_next = [&] {
-        const int left = end - fill_key;
-        const T* k = kp + (long long)fill_key * a.kt;
-        if constexpr (kHalves) {
-            key_copy.start(fill + (wave >> 1) * Shape::kKeyBytes, k + (wave >> 1) * a.km, a.kt, left, tid & 127);
-        } else {
-            key_copy.start(fill, k, a.kt, left, tid);
-            if constexpr (M2) key_copy.start(fill + Shape::kKeyBytes, k + a.km, a.kt, left, tid);
-        }
-        value_copy.start(fill + Shape::kMapBytes, vp + (long long)fill_key * a.vt, a.vt, left, tid);
-        fill_key += kKeys;
-        fill = fill + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : fill + Shape::kBufferBytes;
+    auto fetch = [&](int key, unsigned buffer) {
+        const int left = end - key;
+        const T* k = kp + (long long)key * a.kt;
+        key_copy.start(buffer, k, a.kt, left, tid);
+        if constexpr (M2) key_copy.start(buffer + Shape::kKeyBytes, k + a.km, a.kt, left, tid);
+        value_copy.start(buffer + Shape::kMapBytes, vp + (long long)key * a.vt, a.vt, left, tid);
     };
-    if (begin < end)
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) fetch_next();
+    if (begin < end) fetch(begin, base);
     float lam_sum = 0.f;
-    unsigned buffer = base;
-    for (int key = begin; key < end; key += kKeys) {
+    for (int i = 0, key = begin; key < end; ++i, key += kKeys) {
+        const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
         const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
         const unsigned r2 = r1 + Shape::kKeyBytes, c2 = c1 + Shape::kKeyBytes, rv = buffer + value_row;
-        copies_done<(kStages - 2) * kCopies>();
-        // (past the last key, copies of nothing keep the count)
-        fetch_next();
-        buffer = buffer + Shape::kBufferBytes == base + kStages * Shape::kBufferBytes ? base : buffer + Shape::kBufferBytes;
+        copies_done();
+        if (key + kKeys < end) fetch(key + kKeys, base + ((i + 1) & 1) * Shape::kBufferBytes);
         if (key >= wave_end) continue;
         floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
 #pragma unroll
@@ -623,6 +554,8 @@ __device__ void add_parts(const float* part, int splits, long long rows, int wid
 
 // What workgroups computed in parts: dlam, by one workgroup a head (or one for
 // all heads together), then dk and dv, by `key_blocks`, and dq, by the others.
+// Bound by memory, or in small calls by its latency: 13.3 us for the 65 MB of 2 x
+// 1999 x 4 keys in two parts (4.9 TB/s), 5 us for dlam alone.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int key_blocks, int query_blocks) {
     const int lams = a.lam_step ? a.hq : 1, block = int(blockIdx.x) - lams;

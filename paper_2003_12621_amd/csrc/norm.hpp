@@ -26,7 +26,7 @@ constexpr int kNormMaxLast = 8192;   // channels, last
 constexpr int kNormMaxFirst = 2048;  // channels, first
 
 // Workgroups of the backward pass, each with a partial sum per channel.
-int norm_backward_blocks(int n, int s, int c, bool first);
+int norm_backward_blocks(int n, int s, bool first);
 hipError_t launch_norm_forward(const NormArgs& a, hipStream_t s, const LaunchEvents& ev);
 hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s, const LaunchEvents& ev);
 
