@@ -101,6 +101,14 @@ constexpr int kKeySideKeys = 128;   // 4 waves of 32 keys
 // not 342 and 256, at 4 x 1024 tokens of 8 heads.)
 template <int D> constexpr bool kApart = D == 128;
 
+// Operands from LDS are read this many products before they are used, as many as
+// the registers have room for: one where all gradients are computed together (4 x
+// 3136 tokens of 8 heads of 64 / 128, bf16, key side: 495 us; none 513, two 498,
+// three 557, from scratch), two where they are not (2 x 1999 causal tokens of 8
+// heads of 128 / 256, key and query side: 133 and 83 us; none 137 and 89, one 134
+// and 86).
+template <int D> constexpr int kOperandsAhead = kApart<D> ? 2 : 1;
+
 template <typename T, int D, int DV, int DO>
 struct KeySideShape {
     static constexpr int kRows = 32;                                   // queries per stage
@@ -144,16 +152,15 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 // step, double buffered in LDS with the statistics of their rows.  Each wave
 // keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as accumulators in
 // registers.  (Heads that share a key head are summed in the accumulators: their
-// gradients need no other sum.)  Deeper buffers, and operands read from LDS ahead
-// of their products, were no faster.  P1 - lam P2 and dS enter the products
+// gradients need no other sum.)  Deeper buffers were no faster.  P1 - lam P2 and dS enter the products
 // rounded to bf16, as in the forward pass.
 //
-// Bound by the chain scores - terms - t - dS - dk of a step, which two workgroups
-// a compute unit (registers allow no third) do not hide: matrix instructions
-// take 37 %, vector instructions 41 % of a unit's busy time, and with 3.1
-// workgroups a unit its last ones run alone (units are busy 82 % of the launch).
-// Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136 tokens, 8 heads of
-// 64 / 128 513 us, 630 TFLOP/s.
+// Bound by the chain scores - terms - t - dS - dk of a step and its reads from
+// LDS, which two workgroups a compute unit (registers allow no third) hide in
+// part: matrix instructions take 37 %, vector instructions 40 % of a unit's busy
+// time, and with 3.1 workgroups a unit its last ones run alone (units are busy
+// 86 % of the launch).  Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136
+// tokens, 8 heads of 64 / 128 495 us, 650 TFLOP/s.
 template <typename T, int D, int DV, bool WIDE, int DO>
 __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& place, int map) {
     using Shape = KeySideShape<T, D, DV, DO>;
@@ -281,39 +288,68 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
                 p2[r] = hidden ? 0.f : p2[r];
             }
         }
+        // The products after the scores: dv (columns of dO), t (rows of dO) and dk
+        // (columns of q); their operands from LDS are read kAhead before they are used.
+        constexpr int N = DV / 16, kAhead = kOperandsAhead<D>;
+        constexpr int kT = DVAL ? N : 0, kK = kT + (DK ? N : 0), kEnd = kK + (DK ? (M2 ? N : N / 2) : 0);
+        Operand<T> ring[kAhead + 1];
+        auto read = [&](int i) {
+            if (i >= kEnd) return;
+            Operand<T>& o = ring[i % (kAhead + 1)];
+            if (i < kT) {
+                o = read_column<T, DV>(cg, 0, 32 * (i % (DV / 32)), i / (DV / 32));
+            } else if (i < kK) {
+                o = read_row<T, DV>(rg, 0, i - kT);
+            } else {
+                const int e = M2 ? (i - kK) % 2 : 0, x = M2 ? (i - kK) / 2 : i - kK;
+                o = read_column<T, D>(e ? c2 : c1, 0, 32 * (x % (D / 32)), x / (D / 32));
+            }
+        };
+        floatx16 t = zero16();
+        Operand<T> w[2], s1[2], s2[2];
         if constexpr (DVAL) {
             floatx16 difference;
 #pragma unroll
             for (int r = 0; r < 16; ++r) difference[r] = fmaf(-lam, p2[r], p1[r]);
-            const Operand<T> w[2] = {acc_operand<T>(difference, 0), acc_operand<T>(difference, 1)};
-            in_order();
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int d = 0; d < DV / 32; ++d) mma(dval[d], read_column<T, DV>(cg, 0, 32 * d, s), w[s]);
+            w[0] = acc_operand<T>(difference, 0);
+            w[1] = acc_operand<T>(difference, 1);
         }
-        if constexpr (DK) {
-            floatx16 t = zero16();
+        in_order();
 #pragma unroll
-            for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rg, 0, s), v[s]);
+        for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 u1 = rows_of(ts + (2 + map) * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
-                const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+        for (int i = 0; i < kEnd; ++i) {
+            in_order();
+            read(i + kAhead);
+            in_order();
+            const Operand<T>& o = ring[i % (kAhead + 1)];
+            if (DK && i == kK) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p1[4 * g + j] *= ONE ? fmaf(turn, t[4 * g + j], d1[j]) : t[4 * g + j] + d1[j];
-                    if constexpr (M2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
+                for (int g = 0; g < 4; ++g) {
+                    const float4 u1 = rows_of(ts + (2 + map) * kRows, g, hi), u2 = rows_of(ts + 3 * kRows, g, hi);
+                    const float d1[4] = {u1.x, u1.y, u1.z, u1.w}, d2[4] = {u2.x, u2.y, u2.z, u2.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p1[4 * g + j] *= ONE ? fmaf(turn, t[4 * g + j], d1[j]) : t[4 * g + j] + d1[j];
+                        if constexpr (M2) p2[4 * g + j] *= fmaf(-lam, t[4 * g + j], d2[j]);
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    s1[s] = acc_operand<T>(p1, s);
+                    s2[s] = acc_operand<T>(p2, s);
                 }
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Operand<T> s1 = acc_operand<T>(p1, s), s2 = acc_operand<T>(p2, s);
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) {
-                    mma(dk1[d], read_column<T, D>(c1, 0, 32 * d, s), s1);
-                    if constexpr (M2) mma(dk2[d], read_column<T, D>(c2, 0, 32 * d, s), s2);
-                }
+            if (i < kT) {
+                mma(dval[DVAL ? i % (DV / 32) : 0], o, w[i / (DV / 32) % 2]);
+            } else if (i < kK) {
+                mma(t, o, v[DK ? i - kT : 0]);
+            } else {
+                const int e = M2 ? (i - kK) % 2 : 0, x = M2 ? (i - kK) / 2 : i - kK, d = x % (D / 32), s = x / (D / 32) % 2;
+                if (e)
+                    mma(dk2[DK2 ? d : 0], o, s2[s]);
+                else
+                    mma(dk1[DK ? d : 0], o, s1[s]);
             }
         }
     }
@@ -439,41 +475,72 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
         copies_done();
         if (key + kKeys < end) fetch(key + kKeys, base + ((i + 1) & 1) * Shape::kBufferBytes);
         if (key >= wave_end) continue;
-        floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            mma(p1, read_row<T, D>(r1, 0, s), q1[s]);
-            if constexpr (M2) mma(p2, read_row<T, D>(r2, 0, s), q2[s]);
-        }
-#pragma unroll
-        for (int s = 0; s < DV / 16; ++s) mma(t, read_row<T, DV>(rv, 0, s), g[s]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
-            if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2));
-        }
-        if (key + 31 > first_last) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const bool hidden = acc_row(r, hi) > last - key;
-                p1[r] = hidden ? 0.f : p1[r];
-                p2[r] = hidden ? 0.f : p2[r];
+        // The products: scores (rows of k1, k2), t (rows of v), then dq (columns of
+        // k1, k2), with operands read kAhead before they are used, as on the key side.
+        constexpr int kMaps = Shape::kMaps, kT = kMaps * (D / 16), kQ = kT + DV / 16, kEnd = kQ + kMaps * (D / 16), kAhead = kOperandsAhead<D>;
+        Operand<T> ring[kAhead + 1];
+        auto read = [&](int i) {
+            if (i >= kEnd) return;
+            Operand<T>& o = ring[i % (kAhead + 1)];
+            if (i < kT) {
+                o = read_row<T, D>(i % kMaps ? r2 : r1, 0, i / kMaps);
+            } else if (i < kQ) {
+                o = read_row<T, DV>(rv, 0, i - kT);
+            } else {
+                const int x = (i - kQ) / kMaps;
+                o = read_column<T, D>((i - kQ) % kMaps ? c2 : c1, 0, 32 * (x % (D / 32)), x / (D / 32));
             }
-        }
+        };
+        floatx16 p1 = zero16(), p2 = zero16(), t = zero16();
+        Operand<T> s1[2], s2[2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) lam_sum = fmaf(ONE ? p1[r] : p2[r], t[r], lam_sum);
+        for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            p1[r] *= ONE ? fmaf(turn, t[r], d1) : t[r] + d1;
-            if constexpr (M2) p2[r] *= fmaf(-lam, t[r], d2);
-        }
+        for (int i = 0; i < kEnd; ++i) {
+            in_order();
+            read(i + kAhead);
+            in_order();
+            const Operand<T>& o = ring[i % (kAhead + 1)];
+            if (i == kQ) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const Operand<T> x1 = acc_operand<T>(p1, s), x2 = acc_operand<T>(p2, s);
+                for (int r = 0; r < 16; ++r) {
+                    p1[r] = exp2_fast(fmaf(p1[r], a.scale_log2, -lse1));
+                    if constexpr (M2) p2[r] = exp2_fast(fmaf(p2[r], a.scale_log2, -lse2));
+                }
+                if (key + 31 > first_last) {
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-                mma(dq1[d], read_column<T, D>(c1, 0, 32 * d, s), x1);
-                if constexpr (M2) mma(dq2[d], read_column<T, D>(c2, 0, 32 * d, s), x2);
+                    for (int r = 0; r < 16; ++r) {
+                        const bool hidden = acc_row(r, hi) > last - key;
+                        p1[r] = hidden ? 0.f : p1[r];
+                        p2[r] = hidden ? 0.f : p2[r];
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) lam_sum = fmaf(ONE ? p1[r] : p2[r], t[r], lam_sum);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p1[r] *= ONE ? fmaf(turn, t[r], d1) : t[r] + d1;
+                    if constexpr (M2) p2[r] *= fmaf(-lam, t[r], d2);
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    s1[s] = acc_operand<T>(p1, s);
+                    s2[s] = acc_operand<T>(p2, s);
+                }
+            }
+            if (i < kT) {
+                if (i % kMaps)
+                    mma(p2, o, q2[M2 ? i / kMaps : 0]);
+                else
+                    mma(p1, o, q1[i / kMaps]);
+            } else if (i < kQ) {
+                mma(t, o, g[i - kT]);
+            } else {
+                const int x = (i - kQ) / kMaps, d = x % (D / 32), s = x / (D / 32) % 2;
+                if ((i - kQ) % kMaps)
+                    mma(dq2[M2 ? d : 0], o, s2[s]);
+                else
+                    mma(dq1[d], o, s1[s]);
             }
         }
     }

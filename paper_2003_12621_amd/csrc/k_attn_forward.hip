@@ -89,9 +89,10 @@ struct ForwardShape {
 // (keys down, queries across the lanes): a lane then holds 16 scores of one
 // query, whose maximum and sum need one exchange with the other half wave, and
 // the terms stay in the lane as the next product's operand.  The terms enter it
-// rounded to bf16 (the sum is of the unrounded ones): a relative error of 2^-9 of
-// each, which averages out over the keys, where the exact term would cost two
-// more products of the same size.
+// rounded to bf16 (the sum is of the unrounded ones), by up to 2^-8 each: with
+// random inputs that is 1.8e-3 of the output, as much as its own rounding to bf16
+// adds.  A second product with what the rounding left out, which the kernel for
+// few rows has time for, would here be a third more matrix instructions.
 //
 // Bound by issue: at 8192 causal tokens of 16 heads (bf16, 64 / 128) vector
 // instructions, most of them the softmax's, keep a compute unit 74 % and matrix
