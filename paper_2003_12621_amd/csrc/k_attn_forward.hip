@@ -74,6 +74,13 @@ struct ForwardShape {
     // Keys per stage: 64 where four such double buffers fit a compute unit's LDS
     // (4 x 1024 tokens of 8 heads of 32 / 64: 30.9 us; with 32 keys 34.1).
     static constexpr int kKeys = sizeof(T) * DV <= 128 ? 64 : 32;
+    // Operands from LDS are read this many products before they are used: one,
+    // and two where two waves a SIMD have the registers for it (2 x 1999 causal
+    // tokens of 8 heads of 128 / 256, bf16: 83.5 us; none 88.5, one 85.3, four
+    // 83.9).  With four waves a SIMD one is no faster than none in bf16 (4 x 3136,
+    // 64 / 128: 303 and 306 us), but in fp32 (6 x 301, 32 / 64: 26.7 and 28.1 us),
+    // and two do not fit.
+    static constexpr int kAhead = sizeof(T) == 2 && D == 128 ? 2 : 1;
     // workgroups per compute unit aimed at
     static constexpr int kBlocks = sizeof(T) * DV <= 256 ? 4 : (sizeof(T) * DV <= 512 ? 2 : 1);
     static constexpr int kKeyBytes = TileShape<T, D>::bytes(kKeys);
@@ -102,7 +109,7 @@ struct ForwardShape {
 //     8192 x 8192 causal, 16 heads (4 of keys), 64 / 128    407 us  1010 TFLOP/s
 //     4 x 3136 x 3136, 8 heads, 64 / 128                    305 us   790 TFLOP/s
 //     8 x 784 x 784, 8 heads, 64 / 128                       48 us   630 TFLOP/s
-//     2 x 1999 x 1999 causal, 8 heads (4), 128 / 256         87 us   560 TFLOP/s
+//     2 x 1999 x 1999 causal, 8 heads (4), 128 / 256         84 us   590 TFLOP/s
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__((ForwardShape<T, D, DV>::kThreads), (ForwardShape<T, D, DV>::kBlocks)) void
 attn_forward_kernel(AttnArgs a) {
@@ -161,15 +168,34 @@ attn_forward_kernel(AttnArgs a) {
             const int key0 = key + sub;
             if (key0 >= wave_end) break;
             floatx16 c = zero16();
+            constexpr int kT = D / 16, kEnd = kT + DV / 16, kAhead = Shape::kAhead;
+            Operand<T> ring[kAhead + 1];
+            auto read = [&](int i) {
+                if (i >= kEnd) return;
+                if (i < kT)
+                    ring[i % (kAhead + 1)] = read_row<T, D>(tk, sub, i);
+                else
+                    ring[i % (kAhead + 1)] = read_column<T, DV>(tv, sub, 32 * ((i - kT) % DT), (i - kT) / DT);
+            };
+            Operand<T> p[2];
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s) mma(c, read_row<T, D>(tk, sub, s), q[s]);
-            if (key0 + 31 > first_last) mask_scores(c, key0, last, hi);
-            softmax_step(c, st, o, a.scale_log2);
+            for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const Operand<T> p = acc_operand<T>(c, s);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) mma(o[d], read_column<T, DV>(tv, sub, 32 * d, s), p);
+            for (int i = 0; i < kEnd; ++i) {
+                in_order();
+                read(i + kAhead);
+                in_order();
+                const Operand<T>& x = ring[i % (kAhead + 1)];
+                if (i == kT) {
+                    if (key0 + 31 > first_last) mask_scores(c, key0, last, hi);
+                    softmax_step(c, st, o, a.scale_log2);
+                    p[0] = acc_operand<T>(c, 0);
+                    p[1] = acc_operand<T>(c, 1);
+                }
+                if (i < kT)
+                    mma(c, x, q[i]);
+                else
+                    mma(o[(i - kT) % DT], x, p[(i - kT) / DT % 2]);
             }
         }
     }
