@@ -157,9 +157,9 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 //
 // Bound by the chain scores - terms - t - dS - dk of a step and its reads from
 // LDS, which two workgroups a compute unit (registers allow no third) hide in
-// part: matrix instructions take 37 %, vector instructions 40 % of a unit's busy
+// part: matrix instructions take 40 %, vector instructions 43 % of a unit's busy
 // time, and with 3.1 workgroups a unit its last ones run alone (units are busy
-// 86 % of the launch).  Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136
+// 81 % of the launch).  Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136
 // tokens, 8 heads of 64 / 128 495 us, 650 TFLOP/s.
 template <typename T, int D, int DV, bool WIDE, int DO>
 __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& place, int map) {
@@ -400,7 +400,7 @@ struct QuerySideShape {
 // Query side: one workgroup takes 128 query rows of one head, 32 a wave, and
 // goes over the keys, as the forward kernel does; q1, q2 and dO are operands, dq1
 // and dq2 accumulators in registers.  Bound as the key side is (matrix
-// instructions 45 %, vector instructions 58 % of busy time).  Measured (bf16,
+// instructions 45 %, vector instructions 57 % of busy time).  Measured (bf16,
 // 8 d + 2 dv operations a pair): 4 x 3136 tokens, 8 heads of 64 / 128 341 us, 710
 // TFLOP/s; with 64 rows a workgroup 371 us.
 template <typename T, int D, int DV, bool WIDE>

@@ -102,9 +102,9 @@ struct ForwardShape {
 // few rows has time for, would here be a third more matrix instructions.
 //
 // Bound by issue: at 8192 causal tokens of 16 heads (bf16, 64 / 128) vector
-// instructions, most of them the softmax's, keep a compute unit 74 % and matrix
-// instructions 60 % of its busy time, and no LDS read conflicts; the units are
-// busy 89 % of the launch (what is left is its ends).  Measured (bf16, 4 d + 4 dv
+// instructions, most of them the softmax's, take 77 % and matrix instructions
+// 62 % of a compute unit's busy time, and no LDS read conflicts; the units are
+// busy 86 % of the launch (what is left is its ends).  Measured (bf16, 4 d + 4 dv
 // operations for each visible pair):
 //     8192 x 8192 causal, 16 heads (4 of keys), 64 / 128    407 us  1010 TFLOP/s
 //     4 x 3136 x 3136, 8 heads, 64 / 128                    305 us   790 TFLOP/s
