@@ -99,6 +99,10 @@ int choose_backward_splits(const fftsplit_attention_problem_t& p, int shape, lon
     if (splits > 8) splits = 8;
     return splits < 1 ? 1 : int(splits);
 }
+// fp32 plans keep every row's D2 for dlam.
+size_t second_bytes(const fftsplit_attention_problem_t& p) {
+    return p.dtype == FFTSPLIT_F32 ? round256(size_t(p.batch) * p.heads_q * p.queries * 4) : 0;
+}
 size_t key_part_bytes(const fftsplit_attention_problem_t& p, int splits) {
     return splits > 1 ? round256(size_t(splits) * p.batch * p.keys * p.heads_k * (2 * p.dim + p.dim_v) * 4) : 0;
 }
@@ -158,7 +162,7 @@ fftsplit_status_t build(const fftsplit_attention_problem_t* prob, int device, co
     plan->query_splits = choose_backward_splits(p, shape, (long long)p.batch * p.heads_q * ((p.queries + 127LL) / 128),
                                                 (p.keys + 31LL) / 32);
     plan->backward_ws = round256(lse_bytes(p)) + round256(size_t(p.heads_q) * (dlam_parts(p, plan->query_splits) + 1) * 4) +
-                        key_part_bytes(p, plan->key_splits) + query_part_bytes(p, plan->query_splits);
+                        key_part_bytes(p, plan->key_splits) + query_part_bytes(p, plan->query_splits) + second_bytes(p);
     // workgroups of the largest launches (a dimension of a grid holds below 2^32 threads)
     const double heads = double(p.batch) * p.heads_q;
     const double groups[] = {heads * ((p.queries + 63) / 64), heads * ((p.keys + 127) / 128) * plan->key_splits,
@@ -368,6 +372,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         a.lam32 = a.dlam_part + size_t(p.heads_q) * a.parts;
         a.key_part = a.dlam_part + round256(size_t(p.heads_q) * (a.parts + 1) * 4) / 4;
         a.query_part = a.key_part + key_part_bytes(p, plan->key_splits) / 4;
+        a.second = a.query_part + query_part_bytes(p, plan->query_splits) / 4;
         a.dq = dq;
         a.dk = dk;
         a.dv_out = dv;

@@ -60,7 +60,8 @@ struct AttnArgs {
     // backward
     const void* dout;
     long long gb, gt, gh;            // batch, token, head strides of dout
-    float* delta;                    // [n][hq][2][sq]
+    float* delta;                    // [n][hq][2][sq]: - D1, lam D2
+    float* second;                   // [n][hq][sq]: D2 (fp32)
     float* dlam_part;                // [hq][parts]
     float* lam32;                    // [hq]: lam in fp32
     int parts;

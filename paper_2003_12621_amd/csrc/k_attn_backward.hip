@@ -9,7 +9,10 @@
 // the query side (dq) are two kernels that each own their outputs and
 // recompute the scores, rather than one that would add to dq with atomics:
 // results do not depend on the order of workgroups.  D1 and D2 come from the
-// saved outputs; dlam, a sum in which much cancels, from the terms themselves.
+// saved outputs.  dlam, a sum in which much cancels, comes in bf16 from the terms
+// themselves (the saved outputs are rounded: 3.8e-3 of dlam, not 1.7e-3, at 4 x
+// 3136 tokens), and in fp32 from the saved outputs, as - sum D2 (the log sums, of
+// about 10, are rounded to 5e-7, which is each term's relative error).
 #include <algorithm>
 
 #include "attn_common.hpp"
@@ -80,6 +83,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
             float* delta = a.delta + (size_t(b) * a.hq + h) * 2 * a.sq + row;
             delta[0] = -s1;
             delta[a.sq] = lam * s2;
+            if constexpr (sizeof(T) == 4) a.second[(size_t(b) * a.hq + h) * a.sq + row] = s2;
         }
     }
 }
@@ -467,7 +471,11 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
         value_copy.start(buffer + Shape::kMapBytes, vp + (long long)key * a.vt, a.vt, left, tid);
     };
     if (begin < end) fetch(begin, base);
+    // of bf16 terms over the keys, or fp32 rows' D2 (once)
     float lam_sum = 0.f;
+    if constexpr (sizeof(T) == 4)
+        if (valid && hi == 0 && split == 0) lam_sum = a.second[(size_t(b) * a.hq + h) * a.sq + row];
+    asm volatile("" : "+v"(lam_sum));
     for (int i = 0, key = begin; key < end; ++i, key += kKeys) {
         const unsigned buffer = base + (i & 1) * Shape::kBufferBytes;
         const unsigned r1 = buffer + key_row, c1 = buffer + key_column;
@@ -515,8 +523,13 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
                         p2[r] = hidden ? 0.f : p2[r];
                     }
                 }
+                if constexpr (sizeof(T) == 2) {
+                    // (a step's terms first, so that the long sum is of few)
+                    float step_sum = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) lam_sum = fmaf(ONE ? p1[r] : p2[r], t[r], lam_sum);
+                    for (int r = 0; r < 16; ++r) step_sum = fmaf(ONE ? p1[r] : p2[r], t[r], step_sum);
+                    lam_sum += step_sum;
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     p1[r] *= ONE ? fmaf(turn, t[r], d1) : t[r] + d1;
