@@ -29,10 +29,12 @@ __device__ __forceinline__ float attn_lambda(const AttnArgs& a, int h) {
 // Which tile, head and share of it a workgroup takes, of `parts` shares of
 // `tiles` tiles of `heads` heads.  Neighbours share an XCD and its L2.  Under a
 // causal mask tiles differ in length, and `place` counts from the longest: the
-// heads of an XCD, or as many as make 256 workgroups (a quarter of that to four
-// times that are there at once), go through their tiles together, the longest
-// first, and every other round of an XCD's 32 compute units backwards, so that
-// a long and a short tile meet on a unit.
+// heads of an XCD (as many as make 256 workgroups, which is at least as many as
+// it runs at once) go through their tiles together, the longest first, and every
+// other round of its 32 compute units backwards, so that a long and a short tile
+// meet on a unit.  Head by head, longest first, 8192 tokens of 16 heads took 466
+// us, not 433, and 2 x 1999 of 8 wide heads 104, not 87; every other head
+// backwards, 536 and 90.
 struct AttnPlace {
     int place, head, part;
 };
