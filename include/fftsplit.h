@@ -386,8 +386,8 @@ typedef struct {
  *     batch, token, head, map;
  *   v [batch][keys][heads_k][dim_v]: batch, token, head;
  * the last dimension is dense, no stride is negative and those of tokens are at
- * most 2^22.  q, k and v may be
- * slices of one tensor.  Pointers need only their type's alignment; where
+ * most 2^22.  q, k and v may be slices of one tensor, and rows of each may
+ * overlap or be one row for all (stride 0).  Pointers need only their type's alignment; where
  * pointers, strides and widths allow 16-byte accesses those are used.
  *   lam: one value for all heads or one per query head (lam_count 1 or
  *     heads_q), of type lam_dtype;

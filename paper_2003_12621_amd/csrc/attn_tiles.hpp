@@ -221,8 +221,12 @@ __device__ __forceinline__ void own_reads_done() { asm volatile("s_waitcnt lgkmc
 // Copies rows from memory into a tile of ROWS rows of W elements, spread over
 // THREADS threads: chunk place i of thread t is place t + i THREADS in row
 // order.  Tiles are given by their LDS address.  Memory is read through a
-// descriptor of the rows that exist, so rows beyond them become zero and are not
-// touched; so do columns from `cols` on.
+// descriptor that ends with the last row that exists, so nothing beyond it is
+// touched, and columns from `cols` on become zero.  What rows beyond the last
+// hold is zero only where the stride is at least `cols`: where rows overlap, or are
+// one and the same (stride 0), their offsets lie before that end, and the one row
+// of a tensor may have any stride, so that they wrap round.  They then hold
+// elements of rows that exist, and their terms have to be hidden.
 // WIDE: base, stride and cols allow 16-byte accesses, and the copy goes straight
 // into LDS; else elements pass through registers one by one.
 template <typename T, int W, int ROWS, int THREADS, bool WIDE>

@@ -178,8 +178,8 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
     const int length = attn_length(a, b), offset = length - a.sq;
     const int first = tile * kKeySideKeys, wave_first = first + wave * 32, key = wave_first + (lane & 31);
     const bool exists = key < length;
-    // rows from which on this lane's key is visible (none: beyond all rows)
-    const int from = !exists ? 0x7fffffff : (a.causal ? key - offset : 0);
+    // this lane's key is visible to rows from `from` on, `seen` of them
+    const int from = !exists ? a.sq : (a.causal ? max(0, key - offset) : 0), seen = max(0, a.sq - from);
     // every row from here on sees all of the wave's keys
     const int all_from = wave_first + 31 >= length ? 0x7fffffff : (a.causal ? wave_first + 31 - offset : 0);
 
@@ -241,7 +241,7 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
         if constexpr (M2) query_copy.start(buffer + Shape::kQueryBytes, q + a.qm, a.qt, left, tid);
         grad_copy.start(buffer + Shape::kQueries,
                         static_cast<const T*>(a.dout) + b * a.gb + (long long)row0 * a.gt + h * a.gh, a.gt, left, tid);
-        // Rows beyond the last are zero: their terms are finite, and dO, dP and delta zero.
+        // (Rows beyond the last have zero log sums and delta.)
         copy4(copy_source(stat + (size_t(b) * a.hq + h) * 2 * a.sq + row0, unsigned(2 * a.sq - row0) * 4),
               (lane & 31) < left ? stat_off : kOutOfRange,
               __builtin_amdgcn_readfirstlane(buffer + Shape::kQueries + Shape::kGradBytes + (wave & 1) * 2 * kRows * 4));
@@ -284,10 +284,11 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
                 if constexpr (M2) p2[4 * g + j] = exp2_fast(fmaf(p2[4 * g + j], a.scale_log2, -m2[j]));
             }
         }
-        if (block_row0 < all_from) {
+        // rows that do not see the key, and rows beyond the last
+        if (block_row0 < all_from || block_row0 + kRows > a.sq) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const bool hidden = block_row0 + acc_row(r, hi) < from;
+                const bool hidden = unsigned(block_row0 + acc_row(r, hi) - from) >= unsigned(seen);
                 p1[r] = hidden ? 0.f : p1[r];
                 p2[r] = hidden ? 0.f : p2[r];
             }
