@@ -449,7 +449,9 @@ __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
     for (int s = 0; s < a.splits; ++s) {
         const float4 st = stats[s];
         const float m = map ? st.z : st.x, l = map ? st.w : st.y;
-        if (m == kNoMax) continue;
+        // (no key was visible.  A share whose only scores are NaN has no maximum
+        // either, but a sum, which makes the row NaN.)
+        if (l == 0.f) continue;
         const float f = exp2_fast(m - top);
         sum = fmaf(l, f, sum);
         if (col < DV) {
