@@ -353,9 +353,11 @@ typedef enum {
  *   Pm[j] = softmax_j(scale <q[b][i][h][m], k[b][j][g][m]>)  over the visible j.
  * Key j is visible to row i if j < key_lengths[b] and, with causal set, if
  * j <= i + key_lengths[b] - queries (the last row sees every key).  A row
- * that sees no key gives o = 0 and contributes to no gradient.  What lies in
- * k and v from row key_lengths[b] on is not read.  What causal hides is: it has
- * to be finite, as a row takes zero times it.
+ * that sees no key gives o = 0 and contributes to no gradient, whatever it
+ * holds.  What lies in k and v from row key_lengths[b] on is not read.  What
+ * causal hides from a row that sees other keys is: it has to be finite, as the
+ * row takes zero times it (and in the backward pass the keys take zero times
+ * the row's q and dout).
  * Scores, the softmax statistics and all sums are fp32; with bf16 tensors the
  * terms of the softmax (and the score gradients) are rounded to bf16 as
  * operands of the matrix products. */

@@ -215,10 +215,10 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
 #pragma unroll
     for (auto& x : dval) x = zero16();
 
-    // row tiles that see any of the workgroup's keys
-    const int row_tiles = (a.sq + kRows - 1) / kRows;
-    const int tile0 = !a.causal ? 0 : max(0, first - offset) / kRows;
-    const int per_head = first >= length ? 0 : max(0, row_tiles - tile0);
+    // The steps start at the first row that sees any of the workgroup's keys: rows
+    // that see no key are not read, whatever they hold.
+    const int first_row = !a.causal ? 0 : max(0, first - offset);
+    const int per_head = first >= length ? 0 : max(0, a.sq - first_row + kRows - 1) / kRows;
     // this workgroup's share of the steps
     const long long steps = (long long)per_head * group;
     const int begin = int(steps * split / a.key_splits), end = int(steps * (split + 1) / a.key_splits);
@@ -248,7 +248,7 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
     };
     // the rows of this step
     int h = hkv * group + (begin < end ? begin / per_head : 0);
-    int row0 = (tile0 + (begin < end ? begin % per_head : 0)) * kRows;
+    int row0 = first_row + (begin < end ? begin % per_head : 0) * kRows;
     if (begin < end) fetch(h, row0, base);
     for (int step = begin; step < end; ++step) {
         const unsigned buffer = base + ((step - begin) & 1) * Shape::kBufferBytes;
@@ -260,7 +260,7 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
         const int block_row0 = row0;
         row0 += kRows;
         if (row0 >= a.sq) {
-            row0 = tile0 * kRows;
+            row0 = first_row;
             ++h;
         }
         // this stage is there, and all waves are done with the other buffer
@@ -359,6 +359,14 @@ __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& pla
         }
     }
     if (key >= a.sk) return;
+    if (!exists) {      // (a row that is not finite would leave zero times it)
+#pragma unroll
+        for (auto& x : dk1) x = zero16();
+#pragma unroll
+        for (auto& x : dk2) x = zero16();
+#pragma unroll
+        for (auto& x : dval) x = zero16();
+    }
     const size_t at = (size_t(b) * a.sk + key) * a.hk + hkv;
     const bool whole = a.d % 4 == 0;
     if (a.key_splits > 1) {
@@ -557,6 +565,13 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
                     mma(dq1[d], o, s1[s]);
             }
         }
+    }
+    if (last < 0) {      // a row that sees no key: no gradient, whatever q and dO hold
+        lam_sum = 0.f;
+#pragma unroll
+        for (auto& x : dq1) x = zero16();
+#pragma unroll
+        for (auto& x : dq2) x = zero16();
     }
     if (!ONE || map) {
         // this workgroup's part of dlam, in a fixed order

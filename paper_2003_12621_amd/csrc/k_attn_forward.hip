@@ -206,7 +206,7 @@ attn_forward_kernel(AttnArgs a) {
     const float2 halves = both_halves(st.l);
     const float l = halves.x + halves.y;
     const bool none = last < 0;                        // no key is visible: the row is zero
-    const float inv = none ? 0.f : 1.f / l;
+    const float inv = 1.f / l;
     const bool valid = row < a.sq;
     const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
     T* own = a.o1 && valid ? static_cast<T*>(map ? a.o2 : a.o1) + at : nullptr;
@@ -216,7 +216,7 @@ attn_forward_kernel(AttnArgs a) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[d][4 * g + j] *= inv;
+            for (int j = 0; j < 4; ++j) o[d][4 * g + j] = none ? 0.f : o[d][4 * g + j] * inv;
             const float4 y = make_float4(o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]);
             if (own) store4(own, 32 * d + acc_row(4 * g, hi), a.dv, a.o_wide, y.x, y.y, y.z, y.w);
             if (map) join[(d * 4 + g) * 64] = make_float4(y.x * lam, y.y * lam, y.z * lam, y.w * lam);
@@ -460,8 +460,8 @@ __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
         }
     }
     const bool none = attn_last_key(a, i, attn_length(a, b)) < 0;
-    const float inv = none ? 0.f : 1.f / sum;
-    y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+    const float inv = 1.f / sum;
+    y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     const size_t at = ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
     if (a.o1) store4(static_cast<T*>(map ? a.o2 : a.o1) + at, col, a.dv, a.o_wide, y.x, y.y, y.z, y.w);
     if (a.lse && col == 0)

@@ -54,3 +54,51 @@ def test_nan_in_a_visible_key_of_many_rows(d, dv, dtype):
     assert torch.isnan(o[1, 70:, 3]).all()
     o[1, 70:, 3] = want[1, 70:, 3]
     assert torch.equal(o, want)
+
+
+def _all(plan, q, k, v, lam, do, lengths):
+    o, saved = plan.forward(q, k, v, lam, key_lengths=lengths, save=True)
+    return (o, *plan.backward(do, q, k, v, lam, saved, key_lengths=lengths))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("sq,sk,filled", [(90, 60, [60, 20, 0, 33, 1]), (5, 900, [2, 900, 0, 4, 1]), (300, 290, [290, 7, 0, 64, 129])])
+def test_rows_that_see_no_key_reach_nothing(sq, sk, filled, d, dv, dtype):
+    """Whatever q and dout hold there: zero output, zero gradient of the row, and
+    no part in any other."""
+    n, hq, hk, dt = len(filled), 4, 2, DTYPE[dtype]
+    print(f"[case] {sq}x{sk} {filled} {d}/{dv} {dtype}", flush=True)
+    q, k, v, lam, do = (_dev(a, dt) for a in make_inputs(6, n, sq, sk, hq, hk, d, dv))
+    lengths = torch.tensor(filled, dtype=torch.int32, device="cuda")
+    plan = fs.DiffAttention(n, sq, sk, hq, hk, d, dv, dtype=dt, causal=True)
+    outs = []
+    for fill in (0.0, float("nan"), float("inf")):
+        for b, l in enumerate(filled):
+            q[b, :max(0, sq - l)], do[b, :max(0, sq - l)] = fill, fill
+        outs.append(_all(plan, q, k, v, lam, do, lengths))
+    torch.cuda.synchronize()
+    for other in outs:
+        for name, x, y in zip(("o", "dq", "dk", "dv", "dlam"), outs[0], other):
+            assert torch.isfinite(x).all() and torch.equal(x, y), name
+        for b, l in enumerate(filled):
+            assert not other[0][b, :max(0, sq - l)].any() and not other[1][b, :max(0, sq - l)].any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("sq,sk", [(90, 60), (5, 900)])
+def test_rows_that_see_no_key_stay_zero_beside_a_nan(sq, sk, d, dv, dtype):
+    """Next to rows that see one: NaN in the first value, and in a row's q."""
+    n, h, length, dt = 2, 2, 3, DTYPE[dtype]
+    q, k, v, lam, do = (_dev(a, dt) for a in make_inputs(7, n, sq, sk, h, h, d, dv))
+    lengths = torch.tensor([length, 0], dtype=torch.int32, device="cuda")
+    v[0, 0], q[0, sq - 1] = float("nan"), float("nan")
+    plan = fs.DiffAttention(n, sq, sk, h, h, d, dv, dtype=dt, causal=True)
+    o, saved = plan.forward(q, k, v, lam, key_lengths=lengths, save=True)
+    dq, dk, dval, _ = plan.backward(do, q, k, v, lam, saved, key_lengths=lengths)
+    torch.cuda.synchronize()
+    assert torch.isnan(o[0, sq - length:]).all() and torch.isnan(dk[0, :length]).all()
+    for t in (o, dq, *saved[:2]):
+        assert not t[0, :sq - length].any() and not t[1].any()
+    assert not dk[0, length:].any() and not dval[0, length:].any() and not dk[1].any() and not dval[1].any()
