@@ -158,17 +158,32 @@ namespace {
 struct Heads {
     const char* name;
     uintptr_t p;
-    size_t batch, token;     // strides
-    size_t row, span;        // from a token's first byte to its last, from the tensor's
+    size_t count[3], stride[3];   // batch, token, head
+    size_t row, span;             // from a head's first byte to its last, from the tensor's
 };
 
-// Whether two tensors share no byte: apart as a whole, or slices of one
-// tensor whose rows lie side by side in every token.
+// Bytes that a tensor takes up modulo `period`, from its first on: dimensions
+// that step by whole periods add none.
+size_t extent_modulo(const Heads& a, size_t period) {
+    size_t bytes = a.row;
+    for (int i = 0; i < 3; ++i)
+        if (a.stride[i] % period) bytes += (a.count[i] - 1) * a.stride[i];
+    return bytes;
+}
+
+// Whether two tensors share no byte: apart as a whole, or side by side modulo
+// one of their strides, as slices of one tensor are (in every token, in every
+// head, ...).
 bool apart(const Heads& a, const Heads& b) {
     if (a.p + a.span <= b.p || b.p + b.span <= a.p) return true;
-    if (a.token != b.token || a.batch != b.batch || a.token == 0 || a.batch % a.token) return false;
-    const size_t t = a.token, delta = b.p >= a.p ? (b.p - a.p) % t : (t - (a.p - b.p) % t) % t;
-    return delta >= a.row && delta + b.row <= t;
+    for (const Heads* x : {&a, &b})
+        for (int i = 0; i < 3; ++i) {
+            const size_t t = x->stride[i];
+            if (x->count[i] == 1 || t == 0) continue;
+            const size_t delta = b.p >= a.p ? (b.p - a.p) % t : (t - (a.p - b.p) % t) % t;
+            if (delta >= extent_modulo(a, t) && delta + extent_modulo(b, t) <= t) return true;
+        }
+    return false;
 }
 
 // Checks one tensor pair of the rotation and describes its two tensors.
@@ -190,14 +205,16 @@ fftsplit_status_t check_rotary_tensor(const fftsplit_rotary_t* d, int which, con
             if (dims[i] > 1 && x == y && xs[i] != ys[i])
                 return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: in place needs equal strides");
         }
-        // dimensions of one token (or one sequence) have no stride that matters
+        // (the stride of a dimension of one does not matter)
         Heads& h = desc[2 * which + t];
         h.name = names[t];
         h.p = reinterpret_cast<uintptr_t>(t ? y : x);
-        h.row = (size_t(d->dim) + size_t(dims[2] - 1) * size_t(st[2])) * es;
-        h.token = dims[1] > 1 ? size_t(st[1]) * es : 0;
-        h.batch = dims[0] > 1 ? size_t(st[0]) * es : 0;
-        h.span = h.row + size_t(dims[1] - 1) * h.token + size_t(dims[0] - 1) * h.batch;
+        h.row = h.span = size_t(d->dim) * es;
+        for (int i = 0; i < 3; ++i) {
+            h.count[i] = size_t(dims[i]);
+            h.stride[i] = dims[i] > 1 ? size_t(st[i]) * es : 0;
+            h.span += (h.count[i] - 1) * h.stride[i];
+        }
     }
     // no two elements of the output coincide: each dimension steps over the smaller ones
     long long order[3] = {0, 1, 2};
