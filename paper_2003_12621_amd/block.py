@@ -27,7 +27,6 @@ class AttentionBlock:
         tokens, dim_v = height * width, 2 * dim
         self.attention = DiffAttention(batch, tokens, tokens, heads, heads_k, dim, dim_v, dtype=torch.bfloat16,
                                        device=dev.index)
-        self.workspace = self.attention.new_workspace(backward=True)
         self.widths = [heads * 2 * dim, heads_k * 2 * dim, heads_k * dim_v]
         gen = torch.Generator(device=dev).manual_seed(seed)
 
@@ -49,9 +48,10 @@ class AttentionBlock:
         return (q.view(n, s, self.heads, 2, self.dim), k.view(n, s, self.heads_k, 2, self.dim),
                 v.view(n, s, self.heads_k, 2 * self.dim))
 
-    def forward(self, x, save=False):
+    def forward(self, x, save=False, workspace=None):
         """x [n, c, h, w] (fp32) -> x + attention(norm(x)), and with save=True
-        what backward needs."""
+        what backward needs.  `workspace`: as the attention's; by default each
+        call allocates its own, so that calls on several streams stay apart."""
         import torch
         p = self.params
         tokens, mean, rstd = layer_norm(x, p["norm_weight"], p["norm_bias"], layout="first", out_layout="last",
@@ -60,13 +60,13 @@ class AttentionBlock:
         q, k = rotary(q, self.positions, self.freqs, self.sections, other=k)
         args = (q, k, v, p["lam"])
         if save:
-            o, kept = self.attention.forward(*args, workspace=self.workspace, save=True)
+            o, kept = self.attention.forward(*args, workspace=workspace, save=True)
         else:
-            o, kept = self.attention.forward(*args, workspace=self.workspace), None
+            o, kept = self.attention.forward(*args, workspace=workspace), None
         y = (o.flatten(2) @ p["merge"].t()).transpose(1, 2).reshape(x.shape).float() + x
         return (y, (tokens, mean, rstd, args, o, kept)) if save else y
 
-    def backward(self, dy, x, saved):
+    def backward(self, dy, x, saved, workspace=None):
         """dx and the gradients of the parameters (a dict like `params`)."""
         import torch
         p = self.params
@@ -75,7 +75,7 @@ class AttentionBlock:
         dout = dy.flatten(2).transpose(1, 2).to(torch.bfloat16).reshape(n * s, c)
         grads = {"merge": dout.t() @ o.view(n * s, -1)}
         do = (dout @ p["merge"]).view(o.shape)
-        dq, dk, dv, grads["lam"] = self.attention.backward(do, *args, kept, workspace=self.workspace)
+        dq, dk, dv, grads["lam"] = self.attention.backward(do, *args, kept, workspace=workspace)
         dqkv = torch.empty((n, s, sum(self.widths)), dtype=torch.bfloat16, device=x.device)
         q, k, v = self._split(dqkv)
         rotary(dq, self.positions, self.freqs, self.sections, other=dk, inverse=True, out=q, out_other=k)
