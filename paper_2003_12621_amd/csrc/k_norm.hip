@@ -496,10 +496,27 @@ namespace {
 
 template <typename TX, typename TY, int G, int NV, int N>
 hipError_t last(bool backward, const NormArgs& a, hipStream_t s, const LaunchEvents& ev) {
-    const long long rows = (long long)a.n * a.s;
-    if (!backward)
-        return launch_kernel(norm_last_forward_kernel<TX, TY, G, NV, N>, dim3(unsigned((rows + 256 / G - 1) / (256 / G))),
-                             dim3(256), 0, s, ev.start, ev.stop, a);
+    if (!backward) {
+        // a grid holds below 2^32 threads: more rows than that go in several launches
+        constexpr int kRows = 256 / G;
+        const long long rows = (long long)a.n * a.s, most = 0xffffffLL * kRows;
+        for (long long row = 0; row < rows; row += most) {
+            NormArgs part = a;
+            part.n = 1;
+            part.s = int(rows - row < most ? rows - row : most);
+            part.x = static_cast<const TX*>(a.x) + row * a.c;
+            part.y = static_cast<TY*>(a.y) + row * a.c;
+            if (a.mean) {
+                part.mean = a.mean + row;
+                part.rstd = a.rstd + row;
+            }
+            if (hipError_t e = launch_kernel(norm_last_forward_kernel<TX, TY, G, NV, N>, dim3(unsigned((part.s + kRows - 1) / kRows)),
+                                             dim3(256), 0, s, row == 0 ? ev.start : nullptr,
+                                             row + most >= rows ? ev.stop : nullptr, part))
+                return e;
+        }
+        return hipSuccess;
+    }
     const int lds = 256 / G * 2 * a.c * 4 > 16 ? 256 / G * 2 * a.c * 4 : 16;
     auto kernel = norm_last_backward_kernel<TX, TY, G, NV, N>;
     if (hipError_t e = allow_dynamic_lds(kernel, lds)) return e;
