@@ -445,8 +445,8 @@ enum {
 };
 typedef struct {
     /* At most 8192 channels, with x channels first 2048 and 2^22 positions.
-     * batch * positions: at most 2^25 (2^23 above 1024 channels); with x
-     * channels first batch * ceil(positions / 16) at most 2^21. */
+     * batch * positions: below 2^25 (2^23 above 1024 channels); with x
+     * channels first batch * ceil(positions / 16) below 2^21. */
     int batch, positions, channels;
     int x_dtype, y_dtype;             /* fftsplit_dtype_t; both the same, or fp32 to bf16 */
     int x_layout, y_layout;           /* both the same, or a feature map to tokens */

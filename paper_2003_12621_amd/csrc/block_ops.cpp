@@ -28,9 +28,9 @@ fftsplit_status_t check_norm(const fftsplit_layer_norm_t* d, NormArgs& a) {
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: at most 8192 channels, 2048 with channels first");
     if (!(d->eps >= 0.f) || !std::isfinite(d->eps))
         return fail(FFTSPLIT_ERROR_INVALID_VALUE, "layer norm: eps must be finite and not negative");
-    // a grid holds below 2^32 threads: 16 positions a workgroup of 1024, or up to 256 threads a position
+    // a grid holds below 2^32 threads: channels first, 8 positions or more a workgroup of up to 1024 threads
     const long long rows = (long long)d->batch * d->positions;
-    if (first ? (long long)d->batch * ((d->positions + 15) / 16) > (1 << 21) : rows * (d->channels > 1024 ? 256 : 64) > 0x7fffffffLL)
+    if (first ? (long long)d->batch * ((d->positions + 15) / 16) >= (1 << 21) : rows * (d->channels > 1024 ? 256 : 64) > 0x7fffffffLL)
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: too many positions");
     if (first && d->positions > (1 << 22))
         return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "layer norm: at most 2^22 positions of a feature map");
