@@ -32,8 +32,8 @@ constexpr int kAttnRows = 128;
 // Query rows, packed over the heads that share a key head, of the kernel for few rows.
 constexpr int kAttnFewRows = 32;
 
-// Tiles hold at most 64 rows of 4-byte elements: their byte offsets stay below
-// 2^31.
+// Tiles hold at most 128 rows of at most 4-byte elements: their byte offsets stay
+// below 2^31.
 constexpr long long kAttnMaxTokenStride = 1 << 22;
 
 // What the attention kernels get.  Strides are in elements.

@@ -588,7 +588,9 @@ __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn
     if (!valid) return;
     const size_t out = ((size_t(b) * a.sq + row) * a.hq + h) * 2 * a.d;
     const bool whole = a.d % 4 == 0;
-    // a part of the sum, unscaled, or the gradient
+    // A part of the sum, unscaled, or the gradient.  (Rows of fp32, parts or not, take
+    // one path: of two, the compiler makes code in which the scan for overwritten
+    // store data in the tests takes a store's address registers for its data.)
     const bool shared = a.query_splits > 1;
     float* part = a.query_part + (shared ? size_t(split) * a.n * a.sq * a.hq * 2 * a.d + out : 0);
     const float scale = shared ? 1.f : a.scale;
