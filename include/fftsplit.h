@@ -412,14 +412,15 @@ fftsplit_status_t fftsplit_attention_plan_info(fftsplit_attention_plan_t plan, f
 void fftsplit_attention_plan_destroy(fftsplit_attention_plan_t plan);   /* NULL is ignored */
 
 /* o (device) [batch][queries][heads_q][dim_v], dense, 16-byte aligned.
- * For a backward pass also o1 and o2 (like o: the maps' own outputs) and lse
- * (device, info.lse_bytes: fp32 [batch][heads_q][2][queries], log2 of the sum
- * of exp2 of the scaled scores); all NULL otherwise.  Outputs must not
+ * For a backward pass also o1 and o2 (device, the maps' own outputs: fp32
+ * whatever o is, laid out as o, 16-byte aligned) and lse (device,
+ * info.lse_bytes: fp32 [batch][heads_q][2][queries], log2 of the sum of
+ * exp2 of the scaled scores); all NULL otherwise.  Outputs must not
  * overlap the inputs or the workspace (of info.forward_workspace_bytes; NULL
  * allowed if that is 0).  The result does not depend on what runs beside it:
  * no atomics are used. */
 fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_plan_t plan, const fftsplit_attention_inputs_t* in /* host */,
-                                             void* o, void* o1, void* o2, float* lse, void* workspace, size_t workspace_bytes,
+                                             void* o, float* o1, float* o2, float* lse, void* workspace, size_t workspace_bytes,
                                              hipStream_t stream);
 
 /* Gradients of fftsplit_attention_forward's inputs from that of o.
@@ -431,8 +432,8 @@ fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_plan_t plan, con
  *     them) are zero; a key head's sums over its query heads;
  *   dlam (device): like lam (type and count; one value sums over heads). */
 fftsplit_status_t fftsplit_attention_backward(fftsplit_attention_plan_t plan, const fftsplit_attention_inputs_t* in /* host */,
-                                              const void* dout, const long long dout_stride[3], const void* o1,
-                                              const void* o2, const float* lse, void* dq, void* dk, void* dv,
+                                              const void* dout, const long long dout_stride[3], const float* o1,
+                                              const float* o2, const float* lse, void* dq, void* dk, void* dv,
                                               void* dlam, void* workspace, size_t workspace_bytes,
                                               hipStream_t stream);
 

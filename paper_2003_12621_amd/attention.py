@@ -221,7 +221,7 @@ class DiffAttention:
         saved = None
         sp = (None, None, None)
         if save:
-            saved = (torch.empty_like(o), torch.empty_like(o),
+            saved = (torch.empty_like(o, dtype=torch.float32), torch.empty_like(o, dtype=torch.float32),
                      torch.empty(self.info.lse_bytes // 4, dtype=torch.float32, device=self.device))
             sp = tuple(t.data_ptr() for t in saved)
         ws, nbytes = self._workspace(workspace, self.info.forward_workspace_bytes)
@@ -238,8 +238,8 @@ class DiffAttention:
         gp = _strided(dout, "dout", self.dtype, self.out_shape, dev)
         gs = (ctypes.c_longlong * 3)(*dout.stride()[:3])
         numel = _fs._prod(self.out_shape)
-        o1 = _dense(saved[0], "saved[0]", self.dtype, numel, dev)
-        o2 = _dense(saved[1], "saved[1]", self.dtype, numel, dev)
+        o1 = _dense(saved[0], "saved[0]", torch.float32, numel, dev)
+        o2 = _dense(saved[1], "saved[1]", torch.float32, numel, dev)
         lse = _dense(saved[2], "saved[2]", torch.float32, self.info.lse_bytes // 4, dev)
         dq = torch.empty(self.q_shape, dtype=self.dtype, device=dev)
         dk = torch.empty(self.k_shape, dtype=self.dtype, device=dev)

@@ -52,6 +52,9 @@ size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 size_t output_bytes(const fftsplit_attention_problem_t& p) {
     return size_t(p.batch) * p.queries * p.heads_q * p.dim_v * type_bytes(p.dtype);
 }
+size_t map_output_bytes(const fftsplit_attention_problem_t& p) {
+    return size_t(p.batch) * p.queries * p.heads_q * p.dim_v * 4;
+}
 size_t lse_bytes(const fftsplit_attention_problem_t& p) { return size_t(p.batch) * p.heads_q * 2 * p.queries * 4; }
 
 // How many workgroups share the keys of a tile of the kernel for few rows, or
@@ -281,8 +284,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_plan_info(fftsplit_attentio
 FFTSPLIT_EXPORT void fftsplit_attention_plan_destroy(fftsplit_attention_plan_t plan) { delete plan; }
 
 FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_plan_t plan,
-                                                             const fftsplit_attention_inputs_t* in, void* o, void* o1,
-                                                             void* o2, float* lse, void* workspace, size_t workspace_bytes,
+                                                             const fftsplit_attention_inputs_t* in, void* o, float* o1,
+                                                             float* o2, float* lse, void* workspace, size_t workspace_bytes,
                                                              hipStream_t stream) {
     return guarded([&] {
         if (fftsplit_status_t s = check_plan(plan)) return s;
@@ -299,8 +302,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_
         }
         if (fftsplit_status_t s = check_scratch(workspace, workspace_bytes, plan->forward_ws)) return s;
         outs.add(o, output_bytes(plan->prob), "o");
-        outs.add(o1, output_bytes(plan->prob), "o1");
-        outs.add(o2, output_bytes(plan->prob), "o2");
+        outs.add(o1, map_output_bytes(plan->prob), "o1");
+        outs.add(o2, map_output_bytes(plan->prob), "o2");
         outs.add(lse, lse_bytes(plan->prob), "lse");
         outs.add(workspace, plan->forward_ws, "the workspace");
         if (fftsplit_status_t s = check_apart(ins, outs)) return s;
@@ -323,8 +326,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_forward(fftsplit_attention_
 
 FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention_plan_t plan,
                                                               const fftsplit_attention_inputs_t* in, const void* dout,
-                                                              const long long dout_stride[3], const void* o1,
-                                                              const void* o2, const float* lse, void* dq, void* dk,
+                                                              const long long dout_stride[3], const float* o1,
+                                                              const float* o2, const float* lse, void* dq, void* dk,
                                                               void* dv, void* dlam, void* workspace,
                                                               size_t workspace_bytes, hipStream_t stream) {
     return guarded([&] {
@@ -347,8 +350,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         if (fftsplit_status_t s = check_device_ptr(dlam, "dlam", type_bytes(in->lam_dtype))) return s;
         if (fftsplit_status_t s = check_scratch(workspace, workspace_bytes, plan->backward_ws)) return s;
         ins.add(dout, extent(gd, dout_stride, 3, p.dim_v, es), "dout");
-        ins.add(o1, output_bytes(p), "o1");
-        ins.add(o2, output_bytes(p), "o2");
+        ins.add(o1, map_output_bytes(p), "o1");
+        ins.add(o2, map_output_bytes(p), "o2");
         ins.add(lse, lse_bytes(p), "lse");
         outs.add(dq, size_t(p.batch) * p.queries * p.heads_q * 2 * p.dim * es, "dq");
         outs.add(dk, size_t(p.batch) * p.keys * p.heads_k * 2 * p.dim * es, "dk");
@@ -356,8 +359,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_attention_backward(fftsplit_attention
         outs.add(dlam, size_t(in->lam_count) * type_bytes(in->lam_dtype), "dlam");
         outs.add(workspace, plan->backward_ws, "the workspace");
         if (fftsplit_status_t s = check_apart(ins, outs)) return s;
-        a.o1 = const_cast<void*>(o1);
-        a.o2 = const_cast<void*>(o2);
+        a.o1 = const_cast<float*>(o1);
+        a.o2 = const_cast<float*>(o2);
         a.lse = const_cast<float*>(lse);
         a.dout = dout;
         a.gb = dout_stride[0];

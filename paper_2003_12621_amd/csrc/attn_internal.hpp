@@ -50,7 +50,7 @@ struct AttnArgs {
     long long vb, vt, vh;
     int wide;                        // 16-byte accesses of all input rows allowed
     void* o;                         // [n][sq][hq][dv]
-    void *o1, *o2;                   // the maps' own outputs, same layout, or null
+    float *o1, *o2;                  // the maps' own outputs, same layout, or null
     float* lse;                      // [n][hq][2][sq]: log2 of the sum of exp2, or null
     int o_wide;
     // few rows

@@ -9,10 +9,13 @@
 // the query side (dq) are two kernels that each own their outputs and
 // recompute the scores, rather than one that would add to dq with atomics:
 // results do not depend on the order of workgroups.  D1 and D2 come from the
-// saved outputs.  dlam, a sum in which much cancels, comes in bf16 from the terms
-// themselves (the saved outputs are rounded: 3.8e-3 of dlam, not 1.7e-3, at 4 x
-// 3136 tokens), and in fp32 from the saved outputs, as - sum D2 (the log sums, of
-// about 10, are rounded to 5e-7, which is each term's relative error).
+// saved outputs, which are fp32: dS sums to zero over a row's keys, and an error
+// of D is one of that sum, which a common part of the keys carries into dq (saved
+// in bf16, 2e-2 of dq at 2 x 333 tokens with keys of mean 0.5 and values of mean
+// 2; in fp32 3e-3).  dlam, a sum in which much cancels, comes in bf16 from the
+// terms themselves (those of o1 and o2 are rounded), and in fp32 from the saved
+// outputs, as - sum D2 (the log sums, of about 10, are rounded to 5e-7, which is
+// each term's relative error).
 #include <algorithm>
 
 #include "attn_common.hpp"
@@ -48,8 +51,8 @@ __device__ __forceinline__ void load8(float (&y)[8], const T* p, int left, bool 
 }  // namespace
 
 // -D1 and lam D2 of kAttnDeltaRows rows of one head, 16 lanes a row.  Bound by
-// memory: 14 us for the 77 MB of 4 x 3136 rows of 8 heads of 128 (bf16; 5.4 TB/s,
-// part of it from the caches).
+// memory: 20 us for the 128 MB of 4 x 3136 rows of 8 heads of 128 (dO in bf16;
+// 6.4 TB/s, part of it from the caches).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
     const int chunks = (a.sq + kAttnDeltaRows - 1) / kAttnDeltaRows;
@@ -62,8 +65,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
         const int row = c * kAttnDeltaRows + i;
         if (row >= a.sq) break;      // (the same in all lanes of the group)
         const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
-        const T* o1 = static_cast<const T*>(a.o1) + at;
-        const T* o2 = static_cast<const T*>(a.o2) + at;
+        const float *o1 = a.o1 + at, *o2 = a.o2 + at;
         const T* g = static_cast<const T*>(a.dout) + b * a.gb + row * a.gt + h * a.gh;
         float s1 = 0.f, s2 = 0.f;
         for (int col = l * 8; col < a.dv; col += kDeltaLanes * 8) {

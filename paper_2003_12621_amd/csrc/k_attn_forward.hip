@@ -209,7 +209,7 @@ attn_forward_kernel(AttnArgs a) {
     const float inv = 1.f / l;
     const bool valid = row < a.sq;
     const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
-    T* own = a.o1 && valid ? static_cast<T*>(map ? a.o2 : a.o1) + at : nullptr;
+    float* own = a.o1 && valid ? (map ? a.o2 : a.o1) + at : nullptr;
     __syncthreads();
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
     const float inv = 1.f / sum;
     y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     const size_t at = ((size_t(b) * a.sq + i) * a.hq + h) * a.dv;
-    if (a.o1) store4(static_cast<T*>(map ? a.o2 : a.o1) + at, col, a.dv, a.o_wide, y.x, y.y, y.z, y.w);
+    if (a.o1) store4((map ? a.o2 : a.o1) + at, col, a.dv, a.o_wide, y.x, y.y, y.z, y.w);
     if (a.lse && col == 0)
         a.lse[((size_t(b) * a.hq + h) * 2 + map) * a.sq + i] = none ? 0.f : top + log2f(sum);
     if (map) second[threadIdx.x & 63] = y;
