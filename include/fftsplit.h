@@ -360,7 +360,9 @@ typedef enum {
  * the row's q and dout).
  * Scores, the softmax statistics and all sums are fp32; with bf16 tensors the
  * terms of the softmax (and the score gradients) are rounded to bf16 as
- * operands of the matrix products. */
+ * operands of the matrix products, those of the forward pass by each map: what
+ * that leaves out, 1.7e-3 of either map's output, stays where the maps cancel
+ * (plans with key_splits keep it).  fp32 tensors are rounded nowhere. */
 typedef struct {
     int batch;            /* sequences */
     int queries, keys;    /* query rows; room for keys (each sequence may fill less); at most 2^28 */

@@ -158,15 +158,20 @@ __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[N], int co
 // step, double buffered in LDS with the statistics of their rows.  Each wave
 // keeps its rows of k1, k2 and v as operands and dk1, dk2, dv as accumulators in
 // registers.  (Heads that share a key head are summed in the accumulators: their
-// gradients need no other sum.)  Deeper buffers were no faster.  P1 - lam P2 and dS enter the products
-// rounded to bf16, as in the forward pass.
+// gradients need no other sum.)  Deeper buffers were no faster.
+//
+// P1 - lam P2 and dS enter the products rounded to bf16, 1.66e-3 of a gradient of
+// random inputs, as much as its own rounding adds; a common part of the other
+// factor magnifies it.  Second products with what that leaves out find no
+// registers at 64 / 128: the key side took 1010 us with them for dS and 1240 for
+// both, not 505, and the query side 445, not 350 (4 x 3136 tokens of 8 heads).
 //
 // Bound by the chain scores - terms - t - dS - dk of a step and its reads from
 // LDS, which two workgroups a compute unit (registers allow no third) hide in
 // part: matrix instructions take 40 %, vector instructions 43 % of a unit's busy
 // time, and with 3.1 workgroups a unit its last ones run alone (units are busy
-// 81 % of the launch).  Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136
-// tokens, 8 heads of 64 / 128 495 us, 650 TFLOP/s.
+// 80 % of the launch).  Measured (bf16, 8 d + 4 dv operations a pair): 4 x 3136
+// tokens, 8 heads of 64 / 128 477 to 521 us, 620 to 680 TFLOP/s.
 template <typename T, int D, int DV, bool WIDE, int DO>
 __device__ __forceinline__ void key_side(const AttnArgs& a, const AttnPlace& place, int map) {
     using Shape = KeySideShape<T, D, DV, DO>;
@@ -416,8 +421,8 @@ struct QuerySideShape {
 // goes over the keys, as the forward kernel does; q1, q2 and dO are operands, dq1
 // and dq2 accumulators in registers.  Bound as the key side is (matrix
 // instructions 45 %, vector instructions 57 % of busy time).  Measured (bf16,
-// 8 d + 2 dv operations a pair): 4 x 3136 tokens, 8 heads of 64 / 128 341 us, 710
-// TFLOP/s; with 64 rows a workgroup 371 us.
+// 8 d + 2 dv operations a pair): 4 x 3136 tokens, 8 heads of 64 / 128 328 to 361
+// us, 670 to 740 TFLOP/s (with 64 rows a workgroup 371 us, not 352).
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__(256, (QuerySideShape<T, D, DV>::kBlocks)) void attn_query_side_kernel(AttnArgs a) {
     using Shape = QuerySideShape<T, D, DV>;

@@ -66,7 +66,7 @@ __device__ __forceinline__ void mask_scores(floatx16& s, int key0, int last, int
 // values, so that four workgroups a compute unit hide one another's waits: with
 // 64 rows a wave, which reads half as many operands from LDS, and two
 // workgroups, 4 x 8 heads of 3136 x 3136 (bf16, 64 / 128 wide) took 366 us, not
-// the 305 below.
+// 305.
 template <typename T, int D, int DV>
 struct ForwardShape {
     static constexpr int kWaves = 4;
@@ -96,20 +96,26 @@ struct ForwardShape {
 // (keys down, queries across the lanes): a lane then holds 16 scores of one
 // query, whose maximum and sum need one exchange with the other half wave, and
 // the terms stay in the lane as the next product's operand.  The terms enter it
-// rounded to bf16 (the sum is of the unrounded ones), by up to 2^-8 each: with
-// random inputs that is 1.8e-3 of the output, as much as its own rounding to bf16
-// adds.  A second product with what the rounding left out, which the kernel for
-// few rows has time for, would here be a third more matrix instructions.
+// rounded to bf16 (the sum is of the unrounded ones): 1.66e-3 of each map's output
+// with random inputs, as much as the output's own rounding to bf16 adds.  Where
+// the maps cancel it is that of the maps, not of their difference: with a
+// difference of a tenth of either, 1e-2 of the output (fp32 tensors keep all).  A
+// second product with what the rounding left out, which the kernel for few rows
+// has time for, is two thirds more matrix instructions here: 441, 285, 50 and 81
+// us of the four calls below became 705, 409, 68 and 102.
 //
 // Bound by issue: at 8192 causal tokens of 16 heads (bf16, 64 / 128) vector
-// instructions, most of them the softmax's, take 77 % and matrix instructions
-// 62 % of a compute unit's busy time, and no LDS read conflicts; the units are
-// busy 86 % of the launch (what is left is its ends).  Measured (bf16, 4 d + 4 dv
-// operations for each visible pair):
-//     8192 x 8192 causal, 16 heads (4 of keys), 64 / 128    407 us  1010 TFLOP/s
-//     4 x 3136 x 3136, 8 heads, 64 / 128                    305 us   790 TFLOP/s
-//     8 x 784 x 784, 8 heads, 64 / 128                       48 us   630 TFLOP/s
-//     2 x 1999 x 1999 causal, 8 heads (4), 128 / 256         84 us   590 TFLOP/s
+// instructions are issued 77 % and matrix instructions run 62 % of a compute
+// unit's busy time, both 32 %, with no LDS read conflicts; the units are busy 86 %
+// of the launch (what is left is its ends).  Of the cycles that issue vector
+// instructions the matrix instructions take 10 %, and the softmax's fma,
+// exponential (two cycles), sum and conversion of each term 61 %.  Measured (bf16,
+// 4 d + 4 dv operations for each visible pair; from many calls in a stream to a
+// few under the profiler, on several machines):
+//     8192 x 8192 causal, 16 heads (4 of keys), 64 / 128    407-489 us  840-1010 TFLOP/s
+//     4 x 3136 x 3136, 8 heads, 64 / 128                    285-305 us  790-850 TFLOP/s
+//     8 x 784 x 784, 8 heads, 64 / 128                        46-51 us  590-660 TFLOP/s
+//     2 x 1999 x 1999 causal, 8 heads (4), 128 / 256          80-86 us  570-610 TFLOP/s
 template <typename T, int D, int DV, bool WIDE>
 __global__ __launch_bounds__((ForwardShape<T, D, DV>::kThreads), (ForwardShape<T, D, DV>::kBlocks)) void
 attn_forward_kernel(AttnArgs a) {
@@ -238,8 +244,8 @@ attn_forward_kernel(AttnArgs a) {
 
 // ---- few rows: single tokens over a long cache ----
 //
-// Bound by reading k and v once: 45 us for the 201 MB of 16 sequences' caches of
-// up to 8192 keys (4.5 TB/s; a copy reaches 4.8).  The rows of all heads that share a key head
+// Bound by reading k and v once: 41 to 44 us for the 201 MB of 16 sequences' caches
+// of up to 8192 keys (4.6 to 4.9 TB/s; a copy reaches 4.8).  The rows of all heads that share a key head
 // are packed into tiles of 32, and the keys of a tile are shared by several
 // workgroups, whose partial results a second kernel joins.  Within a
 // workgroup every wave goes over key blocks of its own, copied into LDS of its
@@ -433,7 +439,7 @@ __global__ __launch_bounds__((FewShape<T, D, DV>::kThreads)) void attn_few_rows_
 }
 
 // Joins the workgroups that shared a row's keys: 128 threads a row, 64 a map, 4
-// columns each.  Bound by its own latency: 4.7 us for 256 rows of 4 parts.
+// columns each.  Bound by its own latency: 4.2 to 4.8 us for 256 rows of 4 parts.
 template <typename T, int DV>
 __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
     __shared__ float4 second[64];

@@ -5,7 +5,7 @@
 // a few tokens, computes their sines and cosines once into LDS (they serve
 // all heads) and then streams the heads through in 16-byte accesses.  Measured:
 // 4 x 16384 tokens of 40 heads of 64 (bf16) 135 us, 5.0 TB/s (a copy of 4 GiB
-// reaches 4.8); 196 tokens of 32 heads of 32 (fp32) 3.9 us, a launch's latency.
+// reaches 4.8); 196 tokens of 32 heads of 32 (fp32) 3.4 to 3.9 us, a launch's latency.
 #include "fftsplit_internal.hpp"
 #include "launch_util.hpp"
 #include "rotary.hpp"
