@@ -207,11 +207,11 @@ attn_forward_kernel(AttnArgs a) {
     }
 
     // each map's own output, then the second map's scaled by lam to the waves of the first
-    const float lam = attn_lambda(a, h);
+    const bool none = last < 0;                        // no key is visible: the row is zero, whatever lam is
+    const float lam = none ? 0.f : attn_lambda(a, h);
     float4* join = reinterpret_cast<float4*>(lds) + group * (DT * 4 * 64) + lane;
     const float2 halves = both_halves(st.l);
     const float l = halves.x + halves.y;
-    const bool none = last < 0;                        // no key is visible: the row is zero
     const float inv = 1.f / l;
     const bool valid = row < a.sq;
     const size_t at = ((size_t(b) * a.sq + row) * a.hq + h) * a.dv;
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(128) void attn_few_rows_join_kernel(AttnArgs a) {
     __syncthreads();
     if (map) return;
     const float4 z = second[threadIdx.x];
-    const float lam = attn_lambda(a, h);
+    const float lam = none ? 0.f : attn_lambda(a, h);
     store4(static_cast<T*>(a.o) + at, col, a.dv, a.o_wide, y.x - lam * z.x, y.y - lam * z.y, y.z - lam * z.z,
            y.w - lam * z.w);
 }

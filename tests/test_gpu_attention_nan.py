@@ -102,3 +102,21 @@ def test_rows_that_see_no_key_stay_zero_beside_a_nan(sq, sk, d, dv, dtype):
     for t in (o, dq, *saved[:2]):
         assert not t[0, :sq - length].any() and not t[1].any()
     assert not dk[0, length:].any() and not dval[0, length:].any() and not dk[1].any() and not dval[1].any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("sq,sk", [(90, 60), (5, 900)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_rows_that_see_no_key_do_not_depend_on_lam(value, sq, sk, dtype):
+    n, h, d, dv, length, dt = 2, 2, 32, 64, 3, DTYPE[dtype]
+    q, k, v, lam, do = (_dev(a, dt) for a in make_inputs(8, n, sq, sk, h, h, d, dv))
+    lam[1] = value
+    lengths = torch.tensor([length, 0], dtype=torch.int32, device="cuda")
+    plan = fs.DiffAttention(n, sq, sk, h, h, d, dv, dtype=dt, causal=True)
+    o, *grads = _all(plan, q, k, v, lam, do, lengths)
+    torch.cuda.synchronize()
+    assert torch.isfinite(o[:, :, 0]).all() and not torch.isfinite(o[0, sq - length:, 1]).any()
+    for t in (o, grads[0]):
+        assert not t[0, :sq - length].any() and not t[1].any()
+    for t in grads[1:3]:
+        assert not t[0, length:].any() and not t[1].any()
