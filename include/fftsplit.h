@@ -334,8 +334,9 @@ fftsplit_status_t fftsplit_maxpool2x2(const float* x, float* y, int n, int c, in
                                       hipStream_t stream);
 
 /* ---------------------------------------------------------------------
- * Operators of the attention block that follows a convolution backbone:
- * layer norm, rotary positions over several axes, differential attention.
+ * Operators of the attention blocks that follow a convolution backbone:
+ * layer norm, rotary positions over several axes, differential attention,
+ * norms of query and key heads with their rotation, linear attention.
  * They are not part of the paper's method.  The conventions above hold,
  * except that tensors may also be bf16 and that attention and the rotation
  * take strides where they say so.
@@ -500,6 +501,134 @@ fftsplit_status_t fftsplit_rotary(const fftsplit_rotary_t* desc /* host */, cons
                                   const void* x0, const long long x0_stride[3], void* y0, const long long y0_stride[3],
                                   const void* x1, const long long x1_stride[3], void* y1, const long long y1_stride[3],
                                   hipStream_t stream);
+
+/* Norm of every head and rotation in one pass, as for queries and keys between
+ * a projection and attention.  Of a head x of a token:
+ *   y = R (weight * x * rstd),  rstd = 1 / sqrt(mean(x^2) + eps),
+ * with the mean over all `dim` elements and the rotation R of fftsplit_rotary
+ * (rotary.inverse must be 0).  Everything is fp32 until y is rounded. */
+typedef struct {
+    fftsplit_rotary_t rotary;
+    float eps;                     /* finite, not negative */
+} fftsplit_head_norm_t;
+
+/* One of the two tensors (strides as for fftsplit_rotary). */
+typedef struct {
+    const void* x;                 /* device */
+    void* y;                       /* device; may be x (in place, with equal strides), no other overlap */
+    long long x_stride[3], y_stride[3];
+    const float* weight;           /* device, fp32 [dim], or NULL: 1 */
+} fftsplit_head_norm_tensor_t;
+
+/* t1 is NULL unless rotary.heads1.  Runs on the current device. */
+fftsplit_status_t fftsplit_head_norm_rotary(const fftsplit_head_norm_t* desc /* host */, const int* positions,
+                                            const float* freqs, const fftsplit_head_norm_tensor_t* t0 /* host */,
+                                            const fftsplit_head_norm_tensor_t* t1 /* host */, hipStream_t stream);
+
+/* Gradients of one tensor's input and weight; x and weight as in the forward
+ * pass, nothing else is saved from it. */
+typedef struct {
+    const void *dy, *x;            /* device */
+    void* dx;                      /* device; may be dy (in place, with equal strides), no other overlap */
+    long long dy_stride[3], x_stride[3], dx_stride[3];
+    const float* weight;
+    float* dweight;                /* device, fp32 [dim]: the sum over all tokens and heads, in a fixed order;
+                                    * NULL: not computed */
+} fftsplit_head_norm_gradient_t;
+
+/* workspace: device, of the bytes that fftsplit_head_norm_rotary_workspace gives. */
+fftsplit_status_t fftsplit_head_norm_rotary_workspace(const fftsplit_head_norm_t* desc /* host */, size_t* bytes /* host */);
+fftsplit_status_t fftsplit_head_norm_rotary_backward(const fftsplit_head_norm_t* desc /* host */, const int* positions,
+                                                     const float* freqs,
+                                                     const fftsplit_head_norm_gradient_t* t0 /* host */,
+                                                     const fftsplit_head_norm_gradient_t* t1 /* host */, void* workspace,
+                                                     size_t workspace_bytes, hipStream_t stream);
+
+/* Linear attention with a decay for each head: causal, with a state of fixed
+ * size in place of a cache.  For sequence b and key head g, with
+ * decay = exp(log_decay[g]),
+ *   S_t = decay S_(t-1) + k_t v_t^T              (dim x dim_v),
+ *   o_t = scale S_t^T q_t                        for the query heads h of g = h / (heads_q / heads_k),
+ * from the state that the caller gives, or zero.  Tokens from lengths[b] on are
+ * not read; their outputs and gradients are zero, and the state is the one after
+ * the last token that is there.  What the order of tokens hides from a row has to
+ * be finite, as it is multiplied by zero.
+ * States, products and sums are fp32.  With bf16 tensors the scores q k^T (with
+ * their decay) and the state as an operand are rounded to bf16 in calls of more
+ * than a few tokens, and the terms of the state are good to 2^-18; fp32 tensors
+ * are rounded nowhere. */
+typedef struct {
+    int batch;                     /* sequences */
+    int tokens;                    /* of the longest; at most 2^28 */
+    int heads_q, heads_k;          /* heads_k divides heads_q; v has heads_k heads */
+    int dim, dim_v;                /* widths of q and k, and of v and o; at most 256 */
+    int dtype;                     /* fftsplit_dtype_t of q, k, v, o and their gradients */
+    float scale;                   /* 0: 1 / sqrt(dim) */
+} fftsplit_linear_attention_problem_t;
+
+typedef struct fftsplit_linear_attention_plan_s* fftsplit_linear_attention_plan_t;   /* opaque, host-side */
+
+typedef struct {
+    size_t forward_workspace_bytes, backward_workspace_bytes;
+    size_t state_bytes;            /* fp32 [batch][heads_k][dim][dim_v] */
+    /* Kernel choice: 1 if the forward pass goes token by token, else 0 (chunks
+     * of 32 tokens); into how many parts a sequence is cut that are worked on
+     * side by side, in either pass (1: it is not). */
+    int recurrent, forward_segments, backward_segments;
+} fftsplit_linear_attention_info_t;
+
+/* Input tensors (device).  Strides are in elements, of the dimensions
+ *   q [batch][tokens][heads_q][dim], k [batch][tokens][heads_k][dim],
+ *   v [batch][tokens][heads_k][dim_v]: batch, token, head;
+ * the last dimension is dense, no stride is negative and those of tokens are at
+ * most 2^22.  q, k and v may be slices of one tensor and overlap.  Pointers need
+ * only their type's alignment; where pointers, strides and widths allow 16-byte
+ * accesses those are used.
+ *   log_decay: fp32 [heads_k]; values above 0 are taken as 0.  No gradient of it
+ *     is computed: decays are constants of a model.
+ *   lengths: [batch], or NULL: every sequence has `tokens` tokens.  Values
+ *     outside [0, tokens] are taken as the nearest of the two.
+ *   state: fp32 [batch][heads_k][dim][dim_v], dense, 16-byte aligned, or NULL: zero. */
+typedef struct {
+    const void *q, *k, *v;
+    const float* log_decay;
+    const int* lengths;
+    const float* state;
+    long long q_stride[3], k_stride[3], v_stride[3];
+} fftsplit_linear_attention_inputs_t;
+
+/* Validate `prob` and create a plan for `device`, as fftsplit_plan does; the
+ * _for_arch form makes one that can be queried but not run. */
+fftsplit_status_t fftsplit_linear_attention_plan(const fftsplit_linear_attention_problem_t* prob, int device,
+                                                 fftsplit_linear_attention_plan_t* out);
+fftsplit_status_t fftsplit_linear_attention_plan_for_arch(const fftsplit_linear_attention_problem_t* prob,
+                                                          const char* arch, fftsplit_linear_attention_plan_t* out);
+fftsplit_status_t fftsplit_linear_attention_plan_info(fftsplit_linear_attention_plan_t plan,
+                                                      fftsplit_linear_attention_info_t* out /* host */);
+void fftsplit_linear_attention_plan_destroy(fftsplit_linear_attention_plan_t plan);   /* NULL is ignored */
+
+/* o (device) [batch][tokens][heads_q][dim_v], dense, 16-byte aligned; state_out
+ * (device): laid out as state, the state after each sequence's last token, or
+ * NULL.  It may be `state` (in place); outputs and the workspace (of
+ * info.forward_workspace_bytes; NULL allowed if that is 0) must not overlap
+ * anything else.  No atomics are used. */
+fftsplit_status_t fftsplit_linear_attention_forward(fftsplit_linear_attention_plan_t plan,
+                                                    const fftsplit_linear_attention_inputs_t* in /* host */, void* o,
+                                                    float* state_out, void* workspace, size_t workspace_bytes,
+                                                    hipStream_t stream);
+
+/* Gradients of fftsplit_linear_attention_forward's inputs.
+ *   dout (device): the gradient of o, strides batch, token, head in elements,
+ *     last dimension dense; dstate_out (device): that of state_out, laid out as
+ *     state, or NULL: zero;
+ *   dq, dk, dv (device): dense, 16-byte aligned, laid out as q, k and v are
+ *     declared above; a key head's are sums over its query heads;
+ *   dstate (device): the gradient of state, or NULL: not computed. */
+fftsplit_status_t fftsplit_linear_attention_backward(fftsplit_linear_attention_plan_t plan,
+                                                     const fftsplit_linear_attention_inputs_t* in /* host */,
+                                                     const void* dout, const long long dout_stride[3],
+                                                     const float* dstate_out, void* dq, void* dk, void* dv, float* dstate,
+                                                     void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Benchmark hook (host, per calling thread): until called again with
  * NULL, NULL, every later fftsplit_transform_weights / fftsplit_conv2d /

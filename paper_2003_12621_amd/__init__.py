@@ -442,6 +442,10 @@ def bin_coords(L: int):
 
 
 from . import attention as _attention  # noqa: E402
-from .attention import DiffAttention, layer_norm, layer_norm_backward, rotary  # noqa: E402,F401
+from .attention import (DiffAttention, head_norm_rotary, head_norm_rotary_backward, layer_norm,  # noqa: E402,F401
+                        layer_norm_backward, rotary)
+from . import linear_attention as _linear_attention  # noqa: E402
+from .linear_attention import LinearAttention  # noqa: E402,F401
 
 _SIGNATURES.update(_attention.SIGNATURES)
+_SIGNATURES.update(_linear_attention.SIGNATURES)

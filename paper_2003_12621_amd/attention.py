@@ -49,6 +49,21 @@ class Rotary(ctypes.Structure):
                 + [(f, ctypes.c_int) for f in ("positions_per_batch", "inverse", "interleaved")])
 
 
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("rotary", Rotary), ("eps", ctypes.c_float)]
+
+
+class HeadNormTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_longlong * 3),
+                ("y_stride", ctypes.c_longlong * 3), ("weight", ctypes.c_void_p)]
+
+
+class HeadNormGradient(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("dy_stride", ctypes.c_longlong * 3), ("x_stride", ctypes.c_longlong * 3),
+                ("dx_stride", ctypes.c_longlong * 3), ("weight", ctypes.c_void_p), ("dweight", ctypes.c_void_p)]
+
+
 _P, _SZ = ctypes.c_void_p, ctypes.c_size_t
 _STRIDES = ctypes.POINTER(ctypes.c_longlong)
 SIGNATURES = {
@@ -67,6 +82,12 @@ SIGNATURES = {
                                                     _SZ, _P]),
     "fftsplit_rotary": (ctypes.c_int, [ctypes.POINTER(Rotary), _P, _P, _P, _STRIDES, _P, _STRIDES, _P, _STRIDES, _P,
                                        _STRIDES, _P]),
+    "fftsplit_head_norm_rotary": (ctypes.c_int, [ctypes.POINTER(HeadNorm), _P, _P, ctypes.POINTER(HeadNormTensor),
+                                                 ctypes.POINTER(HeadNormTensor), _P]),
+    "fftsplit_head_norm_rotary_workspace": (ctypes.c_int, [ctypes.POINTER(HeadNorm), ctypes.POINTER(_SZ)]),
+    "fftsplit_head_norm_rotary_backward": (ctypes.c_int, [ctypes.POINTER(HeadNorm), _P, _P,
+                                                          ctypes.POINTER(HeadNormGradient),
+                                                          ctypes.POINTER(HeadNormGradient), _P, _SZ, _P]),
 }
 
 
@@ -418,3 +439,102 @@ def rotary(x, positions, freqs, sections, other=None, interleaved=False, inverse
     _launch(dev, "fftsplit_rotary", ctypes.byref(desc), pp, fp, x.data_ptr(), v[0], out.data_ptr(), v[1],
             None if other is None else other.data_ptr(), v[2], None if other is None else out_other.data_ptr(), v[3])
     return out if other is None else (out, out_other)
+
+
+@functools.lru_cache(maxsize=256)
+def _head_norm_desc(shape, other_shape, strides, dtype, pos_shape, sections, interleaved, eps):
+    """The description and strides of a call, and the bytes of the backward
+    pass's workspace.  `strides`: of x and its companions (output, or gradient
+    and output), then of other and its."""
+    per = len(strides) // 2
+    views, rot = [], None
+    # (the rotation's description takes tensors in pairs)
+    for i in range(0, per, 2):
+        pair = (strides[i], strides[min(i + 1, per - 1)])
+        pair += (None, None) if other_shape is None else (strides[per + i], strides[per + min(i + 1, per - 1)])
+        rot, v = _rotary_desc(shape, other_shape, pair, dtype, pos_shape, sections, interleaved, False)
+        views.append(v)
+    first = [views[i // 2][i % 2] for i in range(per)]
+    second = [views[i // 2][2 + i % 2] for i in range(per)]
+    desc = HeadNorm(rot, eps)
+    need = ctypes.c_size_t()
+    _fs._check(_fs.lib().fftsplit_head_norm_rotary_workspace(ctypes.byref(desc), ctypes.byref(need)),
+               "fftsplit_head_norm_rotary_workspace")
+    return desc, first, second, need.value
+
+
+def head_norm_rotary(x, weight, positions, freqs, sections, other=None, other_weight=None, eps=1e-6,
+                     interleaved=False, out=None, out_other=None):
+    """rotary(x / sqrt(mean(x^2) + eps) * weight) in one pass, the mean over each
+    head of x [batch, tokens, heads, dim]; weight fp32 [dim] or None.  The rest
+    as for rotary: `other` (the keys) is done in the same launch, with a weight
+    of its own; out=x works in place."""
+    torch, dev = _torch(), _device_of(x, "x")
+    if other is None and (out_other is not None or other_weight is not None):
+        raise ValueError("out_other or other_weight given without other")
+    sections = tuple(sections)
+    out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
+    _like(out, "output of x", x, x)
+    strides = (x.stride(), out.stride(), None, None)
+    if other is not None:
+        _device_of(other, "other")
+        out_other = torch.empty(other.shape, dtype=other.dtype, device=dev) if out_other is None else out_other
+        _like(other, "other", other, x)
+        _like(out_other, "output of other", other, x)
+        strides = strides[:2] + (other.stride(), out_other.stride())
+    desc, v, w, _ = _head_norm_desc(x.shape, None if other is None else other.shape, strides, x.dtype, positions.shape,
+                                    sections, bool(interleaved), float(eps))
+    pp = _dense(positions, "positions", torch.int32, None, dev)
+    fp = _dense(freqs, "freqs", torch.float32, sum(sections), dev)
+    t0 = HeadNormTensor(x.data_ptr(), out.data_ptr(), v[0], v[1], _param(weight, "weight", desc.rotary.dim, dev))
+    t1 = None
+    if other is not None:
+        t1 = ctypes.byref(HeadNormTensor(other.data_ptr(), out_other.data_ptr(), w[0], w[1],
+                                         _param(other_weight, "other_weight", desc.rotary.dim, dev)))
+    _launch(dev, "fftsplit_head_norm_rotary", ctypes.byref(desc), pp, fp, ctypes.byref(t0), t1)
+    return out if other is None else (out, out_other)
+
+
+def head_norm_rotary_backward(dy, x, weight, positions, freqs, sections, dy_other=None, other=None, other_weight=None,
+                              eps=1e-6, interleaved=False, out=None, out_other=None, workspace=None):
+    """(dx, dweight) from the gradient of head_norm_rotary's output, with `other`
+    (dx, dweight, dother, dother_weight); the weights' gradients are fp32.
+    out=dy works in place."""
+    torch, dev = _torch(), _device_of(x, "x")
+    _device_of(dy, "dy")
+    if (other is None) != (dy_other is None):
+        raise ValueError("other and dy_other must both be given or both be None")
+    if other is None and (out_other is not None or other_weight is not None):
+        raise ValueError("out_other or other_weight given without other")
+    sections = tuple(sections)
+    out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
+    _like(dy, "dy", x, x)
+    _like(out, "gradient of x", x, x)
+    strides = (dy.stride(), out.stride(), x.stride())
+    if other is not None:
+        _device_of(other, "other")
+        _device_of(dy_other, "dy_other")
+        out_other = torch.empty(other.shape, dtype=other.dtype, device=dev) if out_other is None else out_other
+        _like(other, "other", other, x)
+        _like(dy_other, "dy_other", other, x)
+        _like(out_other, "gradient of other", other, x)
+        strides += (dy_other.stride(), out_other.stride(), other.stride())
+    else:
+        strides += (None, None, None)
+    desc, v, w, need = _head_norm_desc(x.shape, None if other is None else other.shape, strides, x.dtype,
+                                       positions.shape, sections, bool(interleaved), float(eps))
+    dim = desc.rotary.dim
+    pp = _dense(positions, "positions", torch.int32, None, dev)
+    fp = _dense(freqs, "freqs", torch.float32, sum(sections), dev)
+    dweight = torch.empty((1 if other is None else 2, dim), dtype=torch.float32, device=dev)
+    t0 = HeadNormGradient(dy.data_ptr(), x.data_ptr(), out.data_ptr(), v[0], v[2], v[1],
+                          _param(weight, "weight", dim, dev), dweight.data_ptr())
+    t1 = None
+    if other is not None:
+        t1 = ctypes.byref(HeadNormGradient(dy_other.data_ptr(), other.data_ptr(), out_other.data_ptr(), w[0], w[2], w[1],
+                                           _param(other_weight, "other_weight", dim, dev),
+                                           dweight.data_ptr() + 4 * dim))
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
+    _launch(dev, "fftsplit_head_norm_rotary_backward", ctypes.byref(desc), pp, fp, ctypes.byref(t0), t1,
+            _dense(ws, "workspace", None, None, dev), ws.numel() * ws.element_size())
+    return (out, dweight[0]) if other is None else (out, dweight[0], out_other, dweight[1])

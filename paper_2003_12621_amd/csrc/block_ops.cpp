@@ -1,7 +1,8 @@
-// Layer norm and rotary positions: argument checks and launches.
+// Layer norm, rotary positions and head norms: argument checks and launches.
 #include <cmath>
 
 #include "entry_checks.hpp"
+#include "head_norm.hpp"
 #include "launch_util.hpp"
 #include "norm.hpp"
 #include "rotary.hpp"
@@ -186,34 +187,42 @@ bool apart(const Heads& a, const Heads& b) {
     return false;
 }
 
+// Checks the address and strides of a tensor of the rotation, and describes it.
+fftsplit_status_t describe_heads(const fftsplit_rotary_t* d, int heads, const char* name, const void* p,
+                                 const long long* strides, Heads& h) {
+    const int es = type_bytes(d->dtype), dims[3] = {d->batch, d->tokens, heads};
+    if (fftsplit_status_t s = check_device_ptr(p, name, es)) return s;
+    h.name = name;
+    h.p = reinterpret_cast<uintptr_t>(p);
+    h.row = h.span = size_t(d->dim) * es;
+    for (int i = 0; i < 3; ++i) {
+        if (strides[i] < 0 || (dims[i] > 1 && size_t(strides[i]) > (size_t(1) << 58) / size_t(dims[i])))
+            return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(name) + " has a stride out of range");
+        // (the stride of a dimension of one does not matter)
+        h.count[i] = size_t(dims[i]);
+        h.stride[i] = dims[i] > 1 ? size_t(strides[i]) * es : 0;
+        h.span += (h.count[i] - 1) * h.stride[i];
+    }
+    return FFTSPLIT_SUCCESS;
+}
+
 // Checks one tensor pair of the rotation and describes its two tensors.
 fftsplit_status_t check_rotary_tensor(const fftsplit_rotary_t* d, int which, const void* x, const long long* xs, void* y,
                                       const long long* ys, RotaryArgs& a, Heads* desc) {
     const char* names[2] = {which ? "x1" : "x0", which ? "y1" : "y0"};
-    const int es = type_bytes(d->dtype), per = 16 / es;
+    const int per = 16 / type_bytes(d->dtype);
     const int dims[3] = {d->batch, d->tokens, a.heads[which]};
-    if (fftsplit_status_t s = check_device_ptr(x, names[0], es)) return s;
-    if (fftsplit_status_t s = check_device_ptr(y, names[1], es)) return s;
+    if (fftsplit_status_t s = check_device_ptr(x, names[0], type_bytes(d->dtype))) return s;
+    if (fftsplit_status_t s = check_device_ptr(y, names[1], type_bytes(d->dtype))) return s;
     if (!xs || !ys) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: strides are NULL");
     for (int t = 0; t < 2; ++t) {
         const long long* st = t ? ys : xs;
+        if (fftsplit_status_t s = describe_heads(d, a.heads[which], names[t], t ? y : x, st, desc[2 * which + t])) return s;
         for (int i = 0; i < 3; ++i) {
-            if (st[i] < 0 || (dims[i] > 1 && size_t(st[i]) > (size_t(1) << 58) / size_t(dims[i])))
-                return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(names[t]) + " has a stride out of range");
             a.wide = a.wide && (dims[i] == 1 || st[i] % per == 0);
             (t ? a.ys : a.xs)[which][i] = st[i];
             if (dims[i] > 1 && x == y && xs[i] != ys[i])
                 return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: in place needs equal strides");
-        }
-        // (the stride of a dimension of one does not matter)
-        Heads& h = desc[2 * which + t];
-        h.name = names[t];
-        h.p = reinterpret_cast<uintptr_t>(t ? y : x);
-        h.row = h.span = size_t(d->dim) * es;
-        for (int i = 0; i < 3; ++i) {
-            h.count[i] = size_t(dims[i]);
-            h.stride[i] = dims[i] > 1 ? size_t(st[i]) * es : 0;
-            h.span += (h.count[i] - 1) * h.stride[i];
         }
     }
     // no two elements of the output coincide: each dimension steps over the smaller ones
@@ -239,6 +248,75 @@ fftsplit_status_t check_rotary_tensor(const fftsplit_rotary_t* d, int which, con
     return FFTSPLIT_SUCCESS;
 }
 
+// Checks the description of a rotation.
+fftsplit_status_t check_rotation(const fftsplit_rotary_t* d, RotaryArgs& a) {
+    if (!d) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: description is NULL");
+    if (d->batch <= 0 || d->tokens <= 0 || d->heads0 <= 0 || d->heads1 < 0 || d->dim <= 0)
+        return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: all dimensions must be positive");
+    if (!known_type(d->dtype)) return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: fp32 and bf16 only");
+    if (d->axes < 1 || d->axes > FFTSPLIT_ROTARY_MAX_AXES)
+        return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: 1 to 4 axes");
+    long long pairs = 0;
+    for (int i = 0; i < d->axes; ++i) {
+        if (d->sections[i] < 0) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: a section is negative");
+        pairs += d->sections[i];
+        a.section_end[i] = int(pairs < 0x7fffffff ? pairs : 0x7fffffff);
+    }
+    if (pairs < 1 || 2 * pairs > d->dim)
+        return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: the sections must hold 1 to dim / 2 pairs");
+    if (d->dim > 1024 || d->heads0 > 65536 || d->heads1 > 65536 ||
+        (long long)d->batch * d->tokens > (1 << 26))
+        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: dim at most 1024, 65536 heads, 2^26 tokens");
+    a.n = d->batch;
+    a.s = d->tokens;
+    a.d = d->dim;
+    a.pairs = int(pairs);
+    a.axes = d->axes;
+    a.pos_batch = d->positions_per_batch ? (long long)d->tokens * d->axes : 0;
+    a.inverse = d->inverse != 0;
+    a.interleaved = d->interleaved != 0;
+    a.dtype = d->dtype;
+    a.heads[0] = d->heads0;
+    a.heads[1] = d->heads1;
+    const int per = 16 / type_bytes(d->dtype);
+    a.wide = d->dim % per == 0 && (a.interleaved ? 2 * a.pairs % per == 0 : a.pairs % per == 0);
+    // Eight tokens share a workgroup's sines where that leaves four
+    // workgroups a compute unit, fewer tokens in smaller calls (196 tokens:
+    // 3.9 us with one, 5.9 with eight; 65536: 139 us with one, 135 with eight).
+    const long long tokens = (long long)a.n * a.s;
+    a.block_tokens = int(tokens / 1024 < 1 ? 1 : (tokens / 1024 > 8 ? 8 : tokens / 1024));
+    return FFTSPLIT_SUCCESS;
+}
+
+// Checks its tables.
+fftsplit_status_t check_tables(const fftsplit_rotary_t* d, const int* positions, const float* freqs, RotaryArgs& a,
+                               Spans& tables) {
+    if (fftsplit_status_t s = check_device_ptr(positions, "positions", 4)) return s;
+    if (fftsplit_status_t s = check_device_ptr(freqs, "freqs", 4)) return s;
+    a.positions = positions;
+    a.freqs = freqs;
+    tables.add(positions, size_t(d->positions_per_batch ? d->batch : 1) * d->tokens * d->axes * 4, "positions");
+    tables.add(freqs, size_t(a.pairs) * 4, "freqs");
+    return FFTSPLIT_SUCCESS;
+}
+
+// No output shares an element with another tensor (but with the one at `pair`
+// less than its own place, in place) or a byte with a dense buffer.
+fftsplit_status_t check_heads_apart(const Heads* desc, int tensors, int step, int pair, const Spans& dense) {
+    for (int i = step - 1; i < tensors; i += step) {
+        for (int j = 0; j < tensors; ++j) {
+            const bool in_place = j == i - pair && desc[i].p == desc[j].p;
+            if (j != i && !in_place && !apart(desc[i], desc[j]))
+                return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(desc[i].name) + " overlaps " + desc[j].name);
+        }
+        for (int j = 0; j < dense.count; ++j)
+            if (desc[i].p < reinterpret_cast<uintptr_t>(dense.p[j]) + dense.n[j] &&
+                reinterpret_cast<uintptr_t>(dense.p[j]) < desc[i].p + desc[i].span)
+                return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(desc[i].name) + " overlaps " + dense.name[j]);
+    }
+    return FFTSPLIT_SUCCESS;
+}
+
 }  // namespace
 
 FFTSPLIT_EXPORT fftsplit_status_t fftsplit_rotary(const fftsplit_rotary_t* d, const int* positions, const float* freqs,
@@ -247,65 +325,159 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_rotary(const fftsplit_rotary_t* d, co
                                                   const long long x1_stride[3], void* y1,
                                                   const long long y1_stride[3], hipStream_t stream) {
     return guarded([&] {
-        if (!d) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: description is NULL");
-        if (d->batch <= 0 || d->tokens <= 0 || d->heads0 <= 0 || d->heads1 < 0 || d->dim <= 0)
-            return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: all dimensions must be positive");
-        if (!known_type(d->dtype)) return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: fp32 and bf16 only");
-        if (d->axes < 1 || d->axes > FFTSPLIT_ROTARY_MAX_AXES)
-            return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: 1 to 4 axes");
         RotaryArgs a{};
-        long long pairs = 0;
-        for (int i = 0; i < d->axes; ++i) {
-            if (d->sections[i] < 0) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: a section is negative");
-            pairs += d->sections[i];
-            a.section_end[i] = int(pairs < 0x7fffffff ? pairs : 0x7fffffff);
-        }
-        if (pairs < 1 || 2 * pairs > d->dim)
-            return fail(FFTSPLIT_ERROR_INVALID_VALUE, "rotary: the sections must hold 1 to dim / 2 pairs");
-        if (d->dim > 1024 || d->heads0 > 65536 || d->heads1 > 65536 ||
-            (long long)d->batch * d->tokens > (1 << 26))
-            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "rotary: dim at most 1024, 65536 heads, 2^26 tokens");
-        if (fftsplit_status_t s = check_device_ptr(positions, "positions", 4)) return s;
-        if (fftsplit_status_t s = check_device_ptr(freqs, "freqs", 4)) return s;
-        const int es = type_bytes(d->dtype), per = 16 / es;
-        a.positions = positions;
-        a.freqs = freqs;
-        a.n = d->batch;
-        a.s = d->tokens;
-        a.d = d->dim;
-        a.pairs = int(pairs);
-        a.axes = d->axes;
-        a.pos_batch = d->positions_per_batch ? (long long)d->tokens * d->axes : 0;
-        a.inverse = d->inverse != 0;
-        a.interleaved = d->interleaved != 0;
-        a.dtype = d->dtype;
-        a.heads[0] = d->heads0;
-        a.heads[1] = d->heads1;
-        a.wide = d->dim % per == 0 && (a.interleaved ? 2 * a.pairs % per == 0 : a.pairs % per == 0);
+        Spans tables;
+        if (fftsplit_status_t s = check_rotation(d, a)) return s;
+        if (fftsplit_status_t s = check_tables(d, positions, freqs, a, tables)) return s;
         Heads desc[4];
-        const int tensors = d->heads1 ? 4 : 2;
         if (fftsplit_status_t s = check_rotary_tensor(d, 0, x0, x0_stride, y0, y0_stride, a, desc)) return s;
         if (d->heads1)
             if (fftsplit_status_t s = check_rotary_tensor(d, 1, x1, x1_stride, y1, y1_stride, a, desc)) return s;
-        for (int i = 1; i < tensors; i += 2)
-            for (int j = 0; j < tensors; ++j) {
-                const bool in_place = j == i - 1 && desc[i].p == desc[j].p;
-                if (j != i && !in_place && !apart(desc[i], desc[j]))
-                    return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(desc[i].name) + " overlaps " + desc[j].name);
-            }
-        Spans in;
-        in.add(positions, size_t(d->positions_per_batch ? d->batch : 1) * d->tokens * d->axes * 4, "positions");
-        in.add(freqs, size_t(pairs) * 4, "freqs");
-        for (int i = 1; i < tensors; i += 2)
-            for (int j = 0; j < in.count; ++j)
-                if (desc[i].p < reinterpret_cast<uintptr_t>(in.p[j]) + in.n[j] &&
-                    reinterpret_cast<uintptr_t>(in.p[j]) < desc[i].p + desc[i].span)
-                    return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(desc[i].name) + " overlaps " + in.name[j]);
-        // Eight tokens share a workgroup's sines where that leaves four
-        // workgroups a compute unit, fewer tokens in smaller calls (196 tokens:
-        // 3.9 us with one, 5.9 with eight; 65536: 139 us with one, 135 with eight).
-        const long long tokens = (long long)a.n * a.s;
-        a.block_tokens = int(tokens / 1024 < 1 ? 1 : (tokens / 1024 > 8 ? 8 : tokens / 1024));
+        if (fftsplit_status_t s = check_heads_apart(desc, d->heads1 ? 4 : 2, 2, 1, tables)) return s;
         return launched_ok(launch_rotary(a, stream, timing_events()), "rotary launch");
+    });
+}
+
+namespace {
+
+fftsplit_status_t check_head_norm(const fftsplit_head_norm_t* d, HeadNormArgs& a) {
+    if (!d) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "head norm: description is NULL");
+    if (fftsplit_status_t s = check_rotation(&d->rotary, a.r)) return s;
+    if (d->rotary.inverse) return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "head norm: only rotated forwards");
+    if (!(d->eps >= 0.f) || !std::isfinite(d->eps))
+        return fail(FFTSPLIT_ERROR_INVALID_VALUE, "head norm: eps must be finite and not negative");
+    a.eps = d->eps;
+    a.access = 16 / type_bytes(d->rotary.dtype);
+    const long long groups = ((long long)a.r.n * a.r.s + a.r.block_tokens - 1) / a.r.block_tokens;
+    a.blocks = int(groups < kHeadNormBlocks ? groups : kHeadNormBlocks);
+    return FFTSPLIT_SUCCESS;
+}
+
+size_t part_bytes(const HeadNormArgs& a) { return size_t(a.blocks) * 2 * a.r.d * 4; }
+
+// Narrows the accesses to what a tensor's address and strides allow.
+void fit_access(HeadNormArgs& a, const void* p, const long long* strides, int heads) {
+    const int es = type_bytes(a.r.dtype), dims[3] = {a.r.n, a.r.s, heads};
+    while (a.access > 1) {
+        bool ok = reinterpret_cast<uintptr_t>(p) % size_t(a.access * es) == 0;
+        for (int i = 0; i < 3; ++i) ok = ok && (dims[i] == 1 || strides[i] % a.access == 0);
+        if (ok) return;
+        a.access /= 2;
+    }
+}
+
+// Deals a head out to lanes once the accesses are known.
+void share_heads(HeadNormArgs& a) {
+    const RotaryArgs& r = a.r;
+    while (a.access > 1 && (r.d % a.access || (r.interleaved ? 2 * r.pairs : r.pairs) % a.access)) a.access /= 2;
+    const int n = a.access;
+    const int turned = r.interleaved && n > 1 ? (2 * r.pairs / n + 1) / 2 : r.pairs / n;
+    const int pieces = turned + (r.d - 2 * r.pairs + 2 * n - 1) / (2 * n);
+    a.row_lanes = 0;
+    for (int lanes = 1; lanes <= 64 && !a.row_lanes; lanes *= 2)
+        if (pieces <= lanes) a.row_lanes = lanes;
+}
+
+}  // namespace
+
+FFTSPLIT_EXPORT fftsplit_status_t fftsplit_head_norm_rotary(const fftsplit_head_norm_t* d, const int* positions,
+                                                            const float* freqs, const fftsplit_head_norm_tensor_t* t0,
+                                                            const fftsplit_head_norm_tensor_t* t1, hipStream_t stream) {
+    return guarded([&] {
+        HeadNormArgs a{};
+        Spans dense;
+        if (fftsplit_status_t s = check_head_norm(d, a)) return s;
+        if (fftsplit_status_t s = check_tables(&d->rotary, positions, freqs, a.r, dense)) return s;
+        const int tensors = d->rotary.heads1 ? 2 : 1;
+        const fftsplit_head_norm_tensor_t* t[2] = {t0, t1};
+        Heads desc[4];
+        for (int i = 0; i < tensors; ++i) {
+            if (!t[i]) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "head norm: a tensor is NULL");
+            if (fftsplit_status_t s = check_rotary_tensor(&d->rotary, i, t[i]->x, t[i]->x_stride, t[i]->y, t[i]->y_stride,
+                                                          a.r, desc))
+                return s;
+            if (t[i]->weight) {
+                if (fftsplit_status_t s = check_device_ptr(t[i]->weight, i ? "weight of x1" : "weight of x0", 4)) return s;
+                dense.add(t[i]->weight, size_t(a.r.d) * 4, i ? "weight of x1" : "weight of x0");
+            }
+            a.weight[i] = t[i]->weight;
+            fit_access(a, t[i]->x, t[i]->x_stride, a.r.heads[i]);
+            fit_access(a, t[i]->y, t[i]->y_stride, a.r.heads[i]);
+        }
+        if (fftsplit_status_t s = check_heads_apart(desc, 2 * tensors, 2, 1, dense)) return s;
+        share_heads(a);
+        return launched_ok(launch_head_norm(a, stream, timing_events()), "head norm launch");
+    });
+}
+
+FFTSPLIT_EXPORT fftsplit_status_t fftsplit_head_norm_rotary_workspace(const fftsplit_head_norm_t* d, size_t* bytes) {
+    return guarded([&] {
+        HeadNormArgs a{};
+        if (!bytes) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "bytes is NULL");
+        if (fftsplit_status_t s = check_head_norm(d, a)) return s;
+        *bytes = part_bytes(a);
+        return FFTSPLIT_SUCCESS;
+    });
+}
+
+FFTSPLIT_EXPORT fftsplit_status_t fftsplit_head_norm_rotary_backward(const fftsplit_head_norm_t* d, const int* positions,
+                                                                     const float* freqs,
+                                                                     const fftsplit_head_norm_gradient_t* t0,
+                                                                     const fftsplit_head_norm_gradient_t* t1,
+                                                                     void* workspace, size_t workspace_bytes,
+                                                                     hipStream_t stream) {
+    return guarded([&] {
+        HeadNormArgs a{};
+        Spans dense, outs;
+        if (fftsplit_status_t s = check_head_norm(d, a)) return s;
+        if (fftsplit_status_t s = check_tables(&d->rotary, positions, freqs, a.r, dense)) return s;
+        const int tensors = d->rotary.heads1 ? 2 : 1;
+        const fftsplit_head_norm_gradient_t* t[2] = {t0, t1};
+        Heads desc[6];      // of each: x, dy, dx
+        size_t need = 0;
+        for (int i = 0; i < tensors; ++i) {
+            if (!t[i]) return fail(FFTSPLIT_ERROR_INVALID_VALUE, "head norm: a tensor is NULL");
+            const int heads = a.r.heads[i];
+            Heads pair[4];
+            if (fftsplit_status_t s = describe_heads(&d->rotary, heads, i ? "x1" : "x0", t[i]->x, t[i]->x_stride, desc[3 * i]))
+                return s;
+            if (fftsplit_status_t s = check_rotary_tensor(&d->rotary, i, t[i]->dy, t[i]->dy_stride, t[i]->dx,
+                                                          t[i]->dx_stride, a.r, pair))
+                return s;
+            desc[3 * i + 1] = pair[2 * i];
+            desc[3 * i + 1].name = i ? "dy1" : "dy0";
+            desc[3 * i + 2] = pair[2 * i + 1];
+            desc[3 * i + 2].name = i ? "dx1" : "dx0";
+            a.x[i] = t[i]->x;
+            for (int j = 0; j < 3; ++j) a.xs[i][j] = t[i]->x_stride[j];
+            if (t[i]->weight) {
+                if (fftsplit_status_t s = check_device_ptr(t[i]->weight, i ? "weight of x1" : "weight of x0", 4)) return s;
+                dense.add(t[i]->weight, size_t(a.r.d) * 4, i ? "weight of x1" : "weight of x0");
+            }
+            a.weight[i] = t[i]->weight;
+            if (t[i]->dweight) {
+                if (fftsplit_status_t s = check_device_ptr(t[i]->dweight, i ? "dweight1" : "dweight0", 4)) return s;
+                outs.add(t[i]->dweight, size_t(a.r.d) * 4, i ? "dweight1" : "dweight0");
+                need = part_bytes(a);
+            }
+            a.dweight[i] = t[i]->dweight;
+            fit_access(a, t[i]->x, t[i]->x_stride, heads);
+            fit_access(a, t[i]->dy, t[i]->dy_stride, heads);
+            fit_access(a, t[i]->dx, t[i]->dx_stride, heads);
+        }
+        if (fftsplit_status_t s = check_scratch(workspace, workspace_bytes, need)) return s;
+        outs.add(workspace, need, "the workspace");
+        if (fftsplit_status_t s = check_apart(dense, outs)) return s;
+        // the dense outputs count as buffers that no tensor may touch
+        for (int j = 0; j < outs.count; ++j) {
+            for (int i = 0; i < 3 * tensors; ++i)
+                if (desc[i].p < reinterpret_cast<uintptr_t>(outs.p[j]) + outs.n[j] &&
+                    reinterpret_cast<uintptr_t>(outs.p[j]) < desc[i].p + desc[i].span)
+                    return fail(FFTSPLIT_ERROR_INVALID_VALUE, std::string(outs.name[j]) + " overlaps " + desc[i].name);
+        }
+        if (fftsplit_status_t s = check_heads_apart(desc, 3 * tensors, 3, 1, dense)) return s;
+        a.part = static_cast<float*>(workspace);
+        share_heads(a);
+        return launched_ok(launch_head_norm_backward(a, stream, timing_events()), "head norm gradient launch");
     });
 }

@@ -1,0 +1,28 @@
+// What the kernels of the head norms get.
+#pragma once
+
+#include "rotary.hpp"
+
+namespace fftsplit {
+
+struct HeadNormArgs {
+    // x (forward) or dy (backward) -> y or dx; inverse, copy_rest and wide are not used
+    RotaryArgs r;
+    const void* x[2];                // backward: the forward pass's input
+    long long xs[2][3];
+    const float* weight[2];          // or null: 1
+    float* dweight[2];               // or null: not computed
+    float* part;                     // [blocks][2][d]: the sums of each workgroup
+    float eps;
+    int access;                      // elements an access: 16 bytes' worth, or fewer where alignment asks for it
+    int row_lanes;                   // lanes that share a head (a power of two), or 0: 64 with several pieces each
+    int blocks;                      // workgroups of the backward kernel
+};
+
+// Workgroups of the backward kernel: each keeps the weights' sums of its share.
+constexpr int kHeadNormBlocks = 1024;
+
+hipError_t launch_head_norm(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev);
+hipError_t launch_head_norm_backward(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev);
+
+}  // namespace fftsplit

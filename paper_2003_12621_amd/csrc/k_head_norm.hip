@@ -1,0 +1,321 @@
+// Norm of every head by its root mean square, and rotation, in one pass; and the
+// gradient of both.
+//
+// With r = 1 / sqrt(mean(x^2) + eps) and z = x r the forward pass is
+// y = R (w z).  Backwards, u = R^T dy is the gradient behind the rotation, and
+//     dx = r (w u - z mean(w u z)),    dw = sum over tokens and heads of u z,
+// from x and dy alone: r is computed again from x, which has to be read anyway.
+//
+// Bound by memory: every element is read and written once.  A few lanes share a
+// head: each takes two accesses' worth of elements that are turned into one
+// another (or two neighbouring ones), so that the sums over the head are the
+// only exchange, and a lane's elements are the same ones of every head, so that
+// the weights and their gradient stay in registers.  As in the rotation alone a
+// workgroup computes its tokens' sines and cosines once for all heads.
+#include "head_norm.hpp"
+#include "launch_util.hpp"
+#include "rotary_turn.hpp"
+
+namespace fftsplit {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// What a lane takes of a head: N elements from e0 and N from e1.
+struct Piece {
+    int e0, e1;
+    bool turned, first, second;      // rotated; which of the two there are
+};
+template <int N, bool INTERLEAVED>
+__device__ __forceinline__ Piece piece_of(const RotaryArgs& a, int i) {
+    Piece p;
+    const int turned = INTERLEAVED && N > 1 ? (2 * a.pairs / N + 1) / 2 : a.pairs / N;
+    p.turned = i < turned;
+    if (p.turned && !(INTERLEAVED && N > 1)) {
+        p.e0 = INTERLEAVED ? 2 * i : i * N;
+        p.e1 = INTERLEAVED ? p.e0 + 1 : p.e0 + a.pairs;
+        p.first = p.second = true;
+        return p;
+    }
+    const int start = p.turned ? 0 : 2 * a.pairs, end = p.turned ? 2 * a.pairs : a.d;
+    p.e0 = start + 2 * N * (p.turned ? i : i - turned);
+    p.e1 = p.e0 + N;
+    p.first = p.e0 < end;
+    p.second = p.e1 < end;
+    return p;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void load_piece(float (&u)[N], const T* p, bool there) {
+    Pack<T, N> x;
+#pragma unroll
+    for (int j = 0; j < N; ++j) x.v[j] = T(0.f);
+    if (there) x = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+    for (int j = 0; j < N; ++j) u[j] = float(x.v[j]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_piece(T* p, const float (&u)[N], bool there) {
+    Pack<T, N> x;
+#pragma unroll
+    for (int j = 0; j < N; ++j) x.v[j] = T(u[j]);
+    if (there) *reinterpret_cast<Pack<T, N>*>(p) = x;
+}
+
+// Turns a lane's elements by the token's angles (BACK: by minus them).
+template <int N, bool INTERLEAVED, bool BACK>
+__device__ __forceinline__ void turn_piece(float (&u)[N], float (&v)[N], const Piece& p, const float2* cs) {
+    if (!p.turned) return;
+    auto by = [](float& x, float& y, float2 w) {
+        const float s = BACK ? -w.y : w.y, t = x * w.x - y * s;
+        y = y * w.x + x * s;
+        x = t;
+    };
+    if constexpr (INTERLEAVED && N > 1) {
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) by(u[2 * j], u[2 * j + 1], cs[p.e0 / 2 + j]);
+        if (p.second)
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) by(v[2 * j], v[2 * j + 1], cs[p.e1 / 2 + j]);
+    } else {
+        const float2* w = cs + (INTERLEAVED ? p.e0 / 2 : p.e0);
+#pragma unroll
+        for (int j = 0; j < N; ++j) by(u[j], v[j], w[j]);
+    }
+}
+
+// The sum over the lanes that share a head.
+__device__ __forceinline__ float head_sum(float x, int lanes) {
+    for (int m = 1; m < lanes; m *= 2) x += __shfl_xor(x, m);
+    return x;
+}
+
+// The angles of the tokens from token0 on, into LDS.
+__device__ __forceinline__ void fill_turns(const RotaryArgs& a, float2* turns, int token0, int tokens) {
+    for (int i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
+        const int pair = i % a.pairs, t = token0 + i / a.pairs;
+        int axis = 0;
+        while (axis + 1 < a.axes && pair >= a.section_end[axis]) ++axis;
+        const int b = t / a.s;
+        turns[i] = turn(a.positions[b * a.pos_batch + (long long)(t - b * a.s) * a.axes + axis], a.freqs[pair]);
+    }
+}
+
+}  // namespace
+
+// ONE: a lane has one piece of a head, which it keeps in registers; else heads
+// are so wide that 64 lanes take several pieces each, and read them again after
+// the sums.  BACK: the gradients.
+template <typename T, int N, bool INTERLEAVED, bool ONE, bool BACK>
+__global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
+    extern __shared__ float2 turns[];
+    const RotaryArgs& r = a.r;
+    const int lanes = a.row_lanes, part = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes;
+    const int all = r.n * r.s, token_groups = (all + r.block_tokens - 1) / r.block_tokens;
+    // BACK: [groups][d] in place of the angles, for either tensor in turn; where
+    // heads do not fit the registers, [2][groups][d] behind them
+    float* sums = reinterpret_cast<float*>(ONE ? turns : turns + r.block_tokens * r.pairs);
+    if constexpr (BACK && !ONE) {
+        for (int i = threadIdx.x; i < 2 * groups * r.d; i += kThreads) sums[i] = 0.f;
+    }
+    float w0[2][N], w1[2][N], d0[2][N], d1[2][N];
+    const Piece own = piece_of<N, INTERLEAVED>(r, part);
+    auto load_weight = [&](float (&u)[N], float (&v)[N], int which, const Piece& p) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            u[j] = p.first && a.weight[which] ? a.weight[which][p.e0 + j] : 1.f;
+            v[j] = p.second && a.weight[which] ? a.weight[which][p.e1 + j] : 1.f;
+        }
+    };
+    if constexpr (ONE) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (r.heads[which]) load_weight(w0[which], w1[which], which, own);
+#pragma unroll
+            for (int j = 0; j < N; ++j) d0[which][j] = d1[which][j] = 0.f;
+        }
+    }
+    for (int tg = blockIdx.x; tg < token_groups; tg += gridDim.x) {
+        const int token0 = tg * r.block_tokens, tokens = min(r.block_tokens, all - token0);
+        if (BACK) __syncthreads();                   // (the last round's angles are no longer read)
+        fill_turns(r, turns, token0, tokens);
+        __syncthreads();
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const int heads = r.heads[which];
+            for (int i = group; i < tokens * heads; i += groups) {
+                const int tok = i / heads, head = i - tok * heads, t = token0 + tok, b = t / r.s, pos = t - b * r.s;
+                const T* in = static_cast<const T*>(r.x[which]) + b * r.xs[which][0] + pos * r.xs[which][1] +
+                              head * r.xs[which][2];
+                T* out = static_cast<T*>(r.y[which]) + b * r.ys[which][0] + pos * r.ys[which][1] + head * r.ys[which][2];
+                const T* x = in;
+                if constexpr (BACK)
+                    x = static_cast<const T*>(a.x[which]) + b * a.xs[which][0] + pos * a.xs[which][1] +
+                        head * a.xs[which][2];
+                const float2* cs = turns + tok * r.pairs;
+                float u[N], v[N], gu[N], gv[N];
+                float square = 0.f, cross = 0.f;
+                // one piece: its part of the sums over the head.  Backwards gu, gv
+                // are the gradients behind the rotation.
+                auto take = [&](const Piece& p, const float (&wu)[N], const float (&wv)[N]) {
+                    load_piece<T, N>(u, x + p.e0, p.first);
+                    load_piece<T, N>(v, x + p.e1, p.second);
+                    if constexpr (BACK) {
+                        load_piece<T, N>(gu, in + p.e0, p.first);
+                        load_piece<T, N>(gv, in + p.e1, p.second);
+                        turn_piece<N, INTERLEAVED, true>(gu, gv, p, cs);
+                    }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        square = fmaf(u[j], u[j], fmaf(v[j], v[j], square));
+                        if constexpr (BACK) cross = fmaf(gu[j] * wu[j], u[j], fmaf(gv[j] * wv[j], v[j], cross));
+                    }
+                };
+                float rstd = 0.f, mean = 0.f;
+                auto give = [&](const Piece& p, const float (&wu)[N], const float (&wv)[N], float (&su)[N], float (&sv)[N]) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        u[j] *= rstd;
+                        v[j] *= rstd;
+                        if constexpr (BACK) {
+                            su[j] = fmaf(gu[j], u[j], su[j]);
+                            sv[j] = fmaf(gv[j], v[j], sv[j]);
+                            u[j] = rstd * fmaf(-mean, u[j], gu[j] * wu[j]);
+                            v[j] = rstd * fmaf(-mean, v[j], gv[j] * wv[j]);
+                        } else {
+                            u[j] *= wu[j];
+                            v[j] *= wv[j];
+                        }
+                    }
+                    if constexpr (!BACK) turn_piece<N, INTERLEAVED, false>(u, v, p, cs);
+                    store_piece<T, N>(out + p.e0, u, p.first);
+                    store_piece<T, N>(out + p.e1, v, p.second);
+                };
+                auto statistics = [&] {
+                    rstd = 1.f / sqrtf(head_sum(square, lanes) / float(r.d) + a.eps);
+                    if constexpr (BACK) mean = head_sum(cross, lanes) * rstd / float(r.d);
+                };
+                if constexpr (ONE) {
+                    take(own, w0[which], w1[which]);
+                    statistics();
+                    give(own, w0[which], w1[which], d0[which], d1[which]);
+                } else {
+                    float wu[N], wv[N];
+                    for (int k = part;; k += lanes) {
+                        const Piece p = piece_of<N, INTERLEAVED>(r, k);
+                        if (!p.first) break;
+                        load_weight(wu, wv, which, p);
+                        take(p, wu, wv);
+                    }
+                    statistics();
+                    for (int k = part;; k += lanes) {
+                        const Piece p = piece_of<N, INTERLEAVED>(r, k);
+                        if (!p.first) break;
+                        load_weight(wu, wv, which, p);
+                        take(p, wu, wv);
+                        float su[N], sv[N];
+#pragma unroll
+                        for (int j = 0; j < N; ++j) su[j] = sv[j] = 0.f;
+                        give(p, wu, wv, su, sv);
+                        if constexpr (BACK) {
+                            float* s = sums + (which * groups + group) * r.d;
+#pragma unroll
+                            for (int j = 0; j < N; ++j) {
+                                s[p.e0 + j] += su[j];
+                                if (p.second) s[p.e1 + j] += sv[j];
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (BACK) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (!a.dweight[which]) continue;
+            const float* from = sums + (ONE ? 0 : which * groups * r.d);
+            __syncthreads();
+            if constexpr (ONE) {
+                float* s = sums + group * r.d;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if (own.first) s[own.e0 + j] = d0[which][j];
+                    if (own.second) s[own.e1 + j] = d1[which][j];
+                }
+                __syncthreads();
+            }
+            for (int i = threadIdx.x; i < r.d; i += kThreads) {
+                float sum = 0.f;
+                for (int g = 0; g < groups; ++g) sum += from[g * r.d + i];
+                a.part[(size_t(blockIdx.x) * 2 + which) * r.d + i] = sum;
+            }
+        }
+    }
+}
+
+// The weights' gradients from the workgroups' sums: 16 elements a workgroup.
+__global__ __launch_bounds__(256) void head_norm_sum_kernel(HeadNormArgs a) {
+    __shared__ float sums[16][17];
+    const int column = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    float sum = 0.f;
+    if (column < 2 * a.r.d && a.dweight[column / a.r.d])
+        for (int i = row; i < a.blocks; i += 16) sum += a.part[size_t(i) * 2 * a.r.d + column];
+    sums[row][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (row || column >= 2 * a.r.d) return;
+    sum = 0.f;
+    for (int i = 0; i < 16; ++i) sum += sums[i][threadIdx.x];
+    const int which = column / a.r.d;
+    if (a.dweight[which]) a.dweight[which][column % a.r.d] = sum;
+}
+
+namespace {
+
+template <typename T, int N, bool BACK>
+hipError_t launch_pieces(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    const RotaryArgs& r = a.r;
+    const bool one = a.row_lanes > 0;
+    HeadNormArgs b = a;
+    if (!one) b.row_lanes = 64;
+    auto kernel = r.interleaved ? (one ? head_norm_kernel<T, N, true, true, BACK> : head_norm_kernel<T, N, true, false, BACK>)
+                                : (one ? head_norm_kernel<T, N, false, true, BACK> : head_norm_kernel<T, N, false, false, BACK>);
+    const long long token_groups = ((long long)r.n * r.s + r.block_tokens - 1) / r.block_tokens;
+    const int turns = r.block_tokens * r.pairs * 8, sums = BACK ? kThreads / b.row_lanes * r.d * 4 : 0;
+    const int lds = one ? (turns > sums ? turns : sums) : turns + 2 * sums;
+    if (hipError_t e = allow_dynamic_lds(kernel, lds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(BACK ? a.blocks : token_groups)), dim3(kThreads), unsigned(lds), s, ev.start,
+                         ev.stop, b);
+}
+
+template <bool BACK>
+hipError_t launch_typed(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    if (a.r.dtype == FFTSPLIT_BF16) {
+        switch (a.access) {
+            case 8: return launch_pieces<__bf16, 8, BACK>(a, s, ev);
+            case 4: return launch_pieces<__bf16, 4, BACK>(a, s, ev);
+            case 2: return launch_pieces<__bf16, 2, BACK>(a, s, ev);
+            default: return launch_pieces<__bf16, 1, BACK>(a, s, ev);
+        }
+    }
+    switch (a.access) {
+        case 4: return launch_pieces<float, 4, BACK>(a, s, ev);
+        case 2: return launch_pieces<float, 2, BACK>(a, s, ev);
+        default: return launch_pieces<float, 1, BACK>(a, s, ev);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_head_norm(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    return launch_typed<false>(a, s, ev);
+}
+
+hipError_t launch_head_norm_backward(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev) {
+    if (!a.dweight[0] && !a.dweight[1]) return launch_typed<true>(a, s, ev);
+    if (hipError_t e = launch_typed<true>(a, s, LaunchEvents{ev.start, nullptr})) return e;
+    return launch_kernel(head_norm_sum_kernel, dim3(unsigned((2 * a.r.d + 15) / 16)), dim3(256), 0, s, nullptr, ev.stop, a);
+}
+
+}  // namespace fftsplit

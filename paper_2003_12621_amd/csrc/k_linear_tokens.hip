@@ -1,0 +1,141 @@
+// Linear attention of a few tokens: the recurrence itself,
+//     S = decay S + k_t v_t^T,   o_t = scale q_t^T S,
+// in fp32, with the state read once and written once.
+//
+// Bound by the state's bytes.  A workgroup takes 64 columns of one key head's
+// state: 16 lanes a row, 4 columns a lane, rows dealt out to 16 groups, so that
+// every row is one run of 256 bytes and the state stays in registers over the
+// tokens.  The sums over the rows are joined through LDS.
+#include "linear_common.hpp"
+
+namespace fftsplit {
+
+namespace {
+constexpr int kTokenColumns = 64, kTokenGroups = 16;
+// Query heads whose outputs are joined at once.
+constexpr int kTokenHeads = 4;
+}  // namespace
+
+// ROWS: of the state in a thread.
+template <typename T, int ROWS, bool WIDE>
+__global__ __launch_bounds__(256) void linear_tokens_kernel(LinearTokens a) {
+    __shared__ float4 join[2][kTokenHeads][4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = tid >> 4;
+    const int slices = (a.dv + kTokenColumns - 1) / kTokenColumns;
+    const int slice = blockIdx.x % slices, head = blockIdx.x / slices, h = head % a.hk, b = head / a.hk;
+    const int column = slice * kTokenColumns + 4 * (tid & 15), heads = a.hq / a.hk;
+    const int length = linear_length(a.lengths, a.s, b);
+    const float less_one = decay_less_one(decay_log2(a.log_decay[h]), 1);
+    const size_t at = size_t(head) * a.d * a.dv + column;
+
+    float4 state[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = group + kTokenGroups * i;
+        float e[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.state && row < a.d) {
+            const float* p = a.state + at + size_t(row) * a.dv;
+            if constexpr (WIDE) {
+                if (column < a.dv) *reinterpret_cast<float4*>(e) = *reinterpret_cast<const float4*>(p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (column + j < a.dv) e[j] = p[j];
+            }
+        }
+        state[i] = make_float4(e[0], e[1], e[2], e[3]);
+    }
+    T* o = static_cast<T*>(a.o) + (size_t(b) * a.s * a.hq + size_t(h) * heads) * a.dv + column;
+    int buffer = 0;
+    for (int t = 0; t < a.s; ++t, o += size_t(a.hq) * a.dv) {
+        if (t >= length) {
+            for (int g = group; g < heads; g += kTokenGroups)
+                store4(o + size_t(g) * a.dv, 0, a.dv - column, WIDE, 0.f, 0.f, 0.f, 0.f);
+            continue;
+        }
+        const T* k = static_cast<const T*>(a.k.p) + b * a.k.b + t * a.k.t + h * a.k.h;
+        const T* v = static_cast<const T*>(a.v.p) + b * a.v.b + t * a.v.t + h * a.v.h + column;
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = column + j < a.dv ? float(v[j]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int row = group + kTokenGroups * i;
+            const float y = row < a.d ? float(k[row]) : 0.f;
+            float4& s = state[i];
+            s.x = fmaf(y, x[0], fmaf(s.x, less_one, s.x));
+            s.y = fmaf(y, x[1], fmaf(s.y, less_one, s.y));
+            s.z = fmaf(y, x[2], fmaf(s.z, less_one, s.z));
+            s.w = fmaf(y, x[3], fmaf(s.w, less_one, s.w));
+        }
+        for (int g0 = 0; g0 < heads; g0 += kTokenHeads, buffer ^= 1) {
+            const int n = min(heads - g0, kTokenHeads);
+#pragma unroll
+            for (int g = 0; g < kTokenHeads; ++g) {
+                if (g >= n) break;
+                const T* q = static_cast<const T*>(a.q.p) + b * a.q.b + t * a.q.t + (long long)(h * heads + g0 + g) * a.q.h;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    const int row = group + kTokenGroups * i;
+                    if (row >= a.d) continue;
+                    const float y = float(q[row]);
+                    sum.x = fmaf(y, state[i].x, sum.x);
+                    sum.y = fmaf(y, state[i].y, sum.y);
+                    sum.z = fmaf(y, state[i].z, sum.z);
+                    sum.w = fmaf(y, state[i].w, sum.w);
+                }
+#pragma unroll
+                for (int m = 16; m < 64; m *= 2) {
+                    sum.x += __shfl_xor(sum.x, m);
+                    sum.y += __shfl_xor(sum.y, m);
+                    sum.z += __shfl_xor(sum.z, m);
+                    sum.w += __shfl_xor(sum.w, m);
+                }
+                if (lane < 16) join[buffer][g][wave][lane] = sum;
+            }
+            // (the other buffer's readers are past the barrier after it)
+            __syncthreads();
+            if (group < n) {
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float4 z = join[buffer][group][w][tid & 15];
+                    y = make_float4(y.x + z.x, y.y + z.y, y.z + z.z, y.w + z.w);
+                }
+                store4(o + size_t(g0 + group) * a.dv, 0, a.dv - column, WIDE, y.x * a.scale, y.y * a.scale, y.z * a.scale,
+                       y.w * a.scale);
+            }
+        }
+    }
+    if (!a.state_out) return;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = group + kTokenGroups * i;
+        if (row >= a.d) continue;
+        store4(a.state_out + at + size_t(row) * a.dv, 0, a.dv - column, WIDE, state[i].x, state[i].y, state[i].z, state[i].w);
+    }
+}
+
+namespace {
+template <typename T, int ROWS>
+hipError_t launch_rows(const LinearTokens& a, hipStream_t s, const LaunchEvents& ev) {
+    const long long blocks = (long long)a.n * a.hk * ((a.dv + kTokenColumns - 1) / kTokenColumns);
+    auto kernel = a.state_wide ? linear_tokens_kernel<T, ROWS, true> : linear_tokens_kernel<T, ROWS, false>;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(256), 0, s, ev.start, ev.stop, a);
+}
+
+template <typename T>
+hipError_t launch_typed(const LinearTokens& a, hipStream_t s, const LaunchEvents& ev) {
+    if (a.d <= 32) return launch_rows<T, 2>(a, s, ev);
+    if (a.d <= 64) return launch_rows<T, 4>(a, s, ev);
+    if (a.d <= 128) return launch_rows<T, 8>(a, s, ev);
+    return launch_rows<T, 16>(a, s, ev);
+}
+}  // namespace
+
+hipError_t launch_linear_tokens(const LinearTokens& a, int dtype, hipStream_t s, const LaunchEvents& ev) {
+    return dtype == FFTSPLIT_BF16 ? launch_typed<__bf16>(a, s, ev) : launch_typed<float>(a, s, ev);
+}
+
+}  // namespace fftsplit

@@ -1,0 +1,371 @@
+"""Linear attention with a decay for each head on the GPU against its recurrence
+in 64 bits.
+
+Tolerances.  u = 2^-24 is half a step of fp32, e = 2^-8 one of bf16.  |o| below is
+the same formula of the inputs' magnitudes, which bounds the sum of the terms'
+magnitudes; the gradients likewise.
+
+fp32: a product over d, dv or 32 tokens is a chain of as many roundings, the
+state a chain over the chunks whose older links decay with the terms they hold,
+and factors are good to 4 u: (2 d + 2 dv + 32 + 3 chunks + 16) u |o| in all.
+bf16, chunks: the scores, or the state as an operand, are rounded once, e |o|,
+and the output once more, e of itself.  Random inputs: each of these two is
+1.66e-3 of the output in the mean square, 2.35e-3 together, tested as 3e-3.
+The state's terms are kept as two bf16 numbers, e^2 each at most: e^2 |S|; in the
+mean square 2.8e-6, tested as 4e-6.  bf16, token by token: only the output is
+rounded.
+"""
+import numpy as np
+import pytest
+
+from linear_reference import reference
+
+torch = pytest.importorskip("torch")
+fs = pytest.importorskip("paper_2003_12621_amd")
+
+pytestmark = pytest.mark.gpu
+
+DTYPE = {"fp32": torch.float32, "bf16": torch.bfloat16}
+U, E = 2.0 ** -24, 2.0 ** -8
+NAMES = ("o", "state", "dq", "dk", "dv", "dstate")
+
+
+def _np(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def make(seed, n, s, hq, hk, d, dv, dtype, state=True, ragged=False, shift=0):
+    """q, k, v, do, log_decay, state, dstate, lengths; `shift`: elements that
+    put rows off their alignment."""
+    rng = np.random.default_rng(seed)
+
+    def rows(h, w):
+        x = torch.from_numpy(rng.standard_normal((n, s, h, w + shift)).astype(np.float32)).to(DTYPE[dtype]).cuda()
+        return x[..., shift:]
+
+    log_decay = torch.from_numpy(-np.exp2(-1 - 8 * rng.random(hk)).astype(np.float32)).cuda()
+    states = [torch.from_numpy(rng.standard_normal((n, hk, d, dv)).astype(np.float32)).cuda() if state else None
+              for _ in range(2)]
+    lengths = None
+    if ragged:
+        lengths = torch.from_numpy(rng.integers(0, s + 1, n).astype(np.int32)).cuda()
+        lengths[n // 2] = 0
+    return rows(hq, d), rows(hk, d), rows(hk, dv), rows(hq, dv), log_decay, *states, lengths
+
+
+def both(q, k, v, do, log_decay, state, dstate, lengths, plan=None, scale=None):
+    n, s, hq, d = q.shape
+    plan = plan or fs.LinearAttention(n, s, hq, k.shape[2], d, v.shape[3], dtype=q.dtype, scale=scale)
+    o, last = plan.forward(q, k, v, log_decay, state=state, lengths=lengths, return_state=True)
+    grads = plan.backward(do, q, k, v, log_decay, state=state, dstate=dstate, lengths=lengths)
+    torch.cuda.synchronize()
+    return plan, (o, last, *grads)
+
+
+def check(plan, got, q, k, v, do, log_decay, state, dstate, lengths, random=True, scale=None):
+    args = [_np(x) for x in (q, k, v, log_decay, state, lengths)]
+    want = reference(*args, scale, _np(do), _np(dstate))
+    size = reference(*[np.abs(x) if i not in (3, 5) and x is not None else x for i, x in enumerate(args)], scale,
+                     np.abs(_np(do)), None if dstate is None else np.abs(_np(dstate)))
+    chunks = -(-q.shape[1] // 32)
+    chain = (2 * q.shape[3] + 2 * v.shape[3] + 32 + 3 * chunks + 16) * U
+    for name, g, w, m in zip(NAMES, got, want, size):
+        if g is None:
+            continue
+        g, off = _np(g), None
+        if q.dtype == torch.float32:
+            bound, off = chain * m, None
+        elif name in ("state", "dstate"):
+            bound, off = (E * E + chain) * m, 4e-6
+        elif name == "o" and plan.info.recurrent:
+            bound, off = E * np.abs(w) + chain * m, 2e-3
+        else:
+            bound, off = E * np.abs(w) + (E + E * E + chain) * m, 3e-3
+        assert (np.abs(g - w) <= bound + 1e-30).all(), (name, float(np.max(np.abs(g - w) - bound)))
+        if random and off and np.linalg.norm(w) > 0 and w.size >= 1024:
+            assert np.linalg.norm(g - w) <= off * np.linalg.norm(w), (name, np.linalg.norm(g - w) / np.linalg.norm(w))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("s", [1, 2, 7, 8, 9, 31, 32, 33, 64, 65, 200, 517])
+def test_lengths_of_sequences(s, dtype):
+    x = make(s, 2, s, 4, 2, 32, 64, dtype)
+    print(f"[case] linear attention {s} tokens {dtype}", flush=True)
+    plan, got = both(*x)
+    assert plan.info.recurrent == (s <= 8)
+    check(plan, got, *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,dv", [(1, 1), (8, 8), (32, 32), (33, 5), (40, 72), (48, 96), (64, 128), (128, 64), (128, 256),
+                                  (256, 128), (256, 256), (100, 130)])
+@pytest.mark.parametrize("s", [3, 70])
+def test_widths(s, d, dv, dtype):
+    x = make(d + dv, 2, s, 4, 2, d, dv, dtype)
+    print(f"[case] linear attention {s} tokens of {d} / {dv} {dtype}", flush=True)
+    check(*both(*x), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (3, 3), (8, 1), (10, 2), (12, 3)])
+@pytest.mark.parametrize("s", [4, 75])
+def test_heads(s, hq, hk, dtype):
+    x = make(hq, 2, s, hq, hk, 32, 40, dtype)
+    check(*both(*x), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("s", [6, 150, 600])
+@pytest.mark.parametrize("state", [False, True])
+def test_ragged(s, state, dtype):
+    """Lengths from zero on; what lies behind a sequence's end is not read, and
+    its outputs and gradients are zero."""
+    x = make(s, 5, s, 4, 2, 32, 64, dtype, state=state, ragged=True)
+    lengths = x[7].clone()
+    lengths[0], lengths[1] = -3, s + 9          # taken as 0 and s
+    plan, want = both(*x[:7], lengths)
+    check(plan, want, *x[:7], lengths)
+    hidden = torch.arange(s, device="cuda")[None, :] >= lengths[:, None]
+    for t in x[:4]:
+        t[hidden] = float("nan")
+    _, got = both(*x[:7], lengths)
+    for name, g, w in zip(NAMES, got, want):
+        assert (g is None and w is None) or torch.equal(g, w), name
+    for i in (0, 2, 3, 4):
+        assert (got[i][hidden] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shift", [1, 4])
+@pytest.mark.parametrize("s", [5, 90])
+def test_alignment(s, shift, dtype):
+    x = make(shift, 2, s, 4, 2, 64, 64, dtype, shift=shift)
+    check(*both(*x), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_long_sequences_in_segments(dtype):
+    """Sequences that are cut into parts: with and without a state, ragged, with
+    ends before, in and at the end of a part."""
+    n, s, hq, hk, d, dv = 4, 1500, 2, 1, 32, 64
+    x = make(1, n, s, hq, hk, d, dv, dtype)
+    plan = fs.LinearAttention(n, s, hq, hk, d, dv, dtype=DTYPE[dtype])
+    assert plan.info.forward_segments > 2 and plan.info.backward_segments > 2
+    # heads that remember over many parts
+    x[4][:] = -0.002
+    lengths = torch.tensor([s, s // 2, 33, 1], dtype=torch.int32, device="cuda")
+    check(*both(*x), *x)
+    check(*both(*x[:7], lengths), *x[:7], lengths)
+    check(*both(*x[:5], None, None, lengths), *x[:5], None, None, lengths)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("s", [5, 100])
+def test_decays(s, dtype):
+    """No decay, one that leaves nothing, and values out of range."""
+    x = make(3, 2, s, 6, 6, 32, 32, dtype)
+    x[4][:] = torch.tensor([0.0, 0.7, -float("inf"), -1e6, -90.0, -1e-9])
+    plan, got = both(*x)
+    check(plan, got, *x)
+    x[4][1] = float("nan")
+    _, got = both(*x)
+    for i, name in enumerate(NAMES):
+        bad = torch.isnan(got[i].float())
+        head = 1 if name in ("state", "dstate") else 2
+        assert not bad.index_select(head, torch.tensor([0, 2, 3, 4, 5], device="cuda")).any(), name
+        assert bad.select(head, 1).any(), name
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_layouts(dtype):
+    """Slices of one projection, sequences behind tokens, one row for all."""
+    n, s, hq, hk, d, dv = 3, 70, 4, 2, 32, 64
+    q, k, v, do, *rest = make(4, n, s, hq, hk, d, dv, dtype)
+    plan, want = both(q, k, v, do, *rest)
+    packed = torch.cat([q.flatten(2), k.flatten(2), v.flatten(2)], -1)
+    pq, pk, pv = packed.split([hq * d, hk * d, hk * dv], -1)
+    _, got = both(pq.unflatten(-1, (hq, d)), pk.unflatten(-1, (hk, d)), pv.unflatten(-1, (hk, dv)), do, *rest)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    turned = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v, do)]
+    _, got = both(*turned, *rest)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    heads = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k, v, do)]
+    _, got = both(*heads, *rest)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    one = do[:, :1].expand(-1, s, -1, -1)
+    x = (q, k[:, :1].expand(-1, s, -1, -1), v, one, *rest)
+    check(*both(*x), *x, random=False)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_single_token_rows_of_any_stride(dtype):
+    """Tensors of one token or one sequence, whose strides say nothing."""
+    q, k, v, do, ld, s0, ds, _ = make(5, 1, 1, 2, 1, 32, 32, dtype)
+    odd = lambda t: t.as_strided(t.shape, (1 << 40, 1 << 30, t.stride(2), 1))
+    x = (odd(q), odd(k), odd(v), odd(do), ld, s0, ds, None)
+    check(*both(*x), *x, random=False)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hq,hk,s", [(4, 4, 100), (4, 2, 100), (4, 2, 6), (2, 1, 1500)])
+def test_state_in_place(hq, hk, s, dtype):
+    x = make(6, 2, s, hq, hk, 32, 64, dtype)
+    plan, want = both(*x)
+    state = x[5].clone()
+    o, last = plan.forward(*x[:3], x[4], state=state, out_state=state)
+    torch.cuda.synchronize()
+    assert last is state and torch.equal(state, want[1]) and torch.equal(o, want[0])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_pieces_continue_one_another(dtype):
+    """A prompt, a few tokens and single tokens, with the state handed on, are
+    the whole sequence; its gradients handed back are the whole gradient."""
+    n, hq, hk, d, dv = 2, 4, 2, 32, 64
+    cuts = [0, 70, 75, 76, 77]
+    x = make(7, n, cuts[-1], hq, hk, d, dv, dtype)
+    q, k, v, do, ld, s0, ds, _ = x
+    plan, whole = both(*x)
+    plans, states, outs = [], [s0], []
+    for a, b in zip(cuts, cuts[1:]):
+        p = fs.LinearAttention(n, b - a, hq, hk, d, dv, dtype=DTYPE[dtype])
+        o, last = p.forward(q[:, a:b], k[:, a:b], v[:, a:b], ld, state=states[-1], return_state=True)
+        plans.append(p)
+        states.append(last)
+        outs.append(o)
+    check(plan, (torch.cat(outs, 1), states[-1]) + (None,) * 4, *x)
+    grads, g = [], ds
+    for i in range(len(plans) - 1, -1, -1):
+        a, b = cuts[i], cuts[i + 1]
+        r = plans[i].backward(do[:, a:b], q[:, a:b], k[:, a:b], v[:, a:b], ld, state=states[i], dstate=g)
+        grads.insert(0, r[:3])
+        g = r[3]
+    # (two more roundings of the states handed on in fp32 are within the chain)
+    check(plan, (None, None) + tuple(torch.cat(t, 1) for t in zip(*grads)) + (g,), *x)
+
+
+def test_gradient_against_differences():
+    x = make(8, 1, 40, 2, 1, 8, 8, "fp32")
+    q, k, v, do, ld, s0, ds, _ = x
+    _, got = both(*x)
+    args = [_np(t) for t in (q, k, v, s0)]
+    rng = np.random.default_rng(1)
+
+    def value(a):
+        o, last = reference(a[0], a[1], a[2], _np(ld), a[3])
+        return (_np(do) * o).sum() + (_np(ds) * last).sum()
+
+    h = 1e-4
+    for i, grad in enumerate((got[2], got[3], got[4], got[5])):
+        e = rng.standard_normal(args[i].shape)
+        move = lambda sign: [t + sign * h * e if j == i else t for j, t in enumerate(args)]
+        slope = (value(move(1)) - value(move(-1))) / (2 * h)
+        size = (np.abs(_np(grad)) * np.abs(e)).sum()
+        # (the function is quadratic at most in each argument: the difference is exact)
+        assert abs((_np(grad) * e).sum() - slope) <= 2e-5 * size, i
+
+
+def test_scale():
+    x = make(9, 2, 50, 2, 2, 16, 16, "fp32")
+    check(*both(*x, scale=0.37), *x, scale=0.37)
+
+
+def test_drift_of_a_long_memory():
+    """8192 tokens of a decay next to 1, in pieces of 8 token by token and in
+    chunks: the state keeps fp32's precision (a factor rounded to fp32 would be
+    off by up to 3e-8 at every token, 2.4e-4 at the end)."""
+    n, s, d = 1, 8192, 8
+    q, k, v, _, ld, _, _, _ = make(10, n, s, 1, 1, d, d, "fp32", state=False)
+    ld[0] = -1.7e-4
+    k, v = torch.ones_like(k), torch.ones_like(v)
+    decay = np.exp(np.float64(ld[0].item()))
+    want = (1 - decay ** s) / (1 - decay)
+    plan = fs.LinearAttention(n, s, 1, 1, d, d)
+    _, chunks = plan.forward(q, k, v, ld, return_state=True)
+    step = fs.LinearAttention(n, 8, 1, 1, d, d)
+    state = torch.zeros(n, 1, d, d, device="cuda")
+    for t in range(0, s, 8):
+        step.forward(q[:, t:t + 8], k[:, t:t + 8], v[:, t:t + 8], ld, state=state, out_state=state)
+    torch.cuda.synchronize()
+    # the roundings of 8192 sums of which each is kept for 5900 tokens in the
+    # mean: a random walk of 2^-24 steps, below 77 u; all with one sign 5900 u
+    for got in (chunks, state):
+        assert float((got.double() / want - 1).abs().max()) <= 5e-5
+
+
+def test_two_streams():
+    """Calls on two streams, with workspaces of their own."""
+    x = make(11, 2, 2000, 2, 1, 64, 64, "bf16")
+    plan, want = both(*x)
+    assert plan.info.forward_workspace_bytes > 0
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            o, last = plan.forward(*x[:3], x[4], state=x[5], return_state=True)
+            got.append((o, last, *plan.backward(x[3], *x[:3], x[4], state=x[5], dstate=x[6])))
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,s,hq,hk", [(2, 200, 4, 2), (1, 2000, 2, 1), (3, 1, 4, 2)])
+def test_graph(n, s, hq, hk, dtype):
+    d, dv = 64, 128
+    e = lambda *shape: torch.empty(shape, dtype=dtype, device="cuda")
+    q, k, v, do = e(n, s, hq, d), e(n, s, hk, d), e(n, s, hk, dv), e(n, s, hq, dv)
+    s0, ds = (torch.empty(n, hk, d, dv, device="cuda") for _ in range(2))
+    ld = -torch.rand(hk, device="cuda")
+    lengths = torch.tensor([s - b // 2 for b in range(n)], dtype=torch.int32, device="cuda")
+    plan = fs.LinearAttention(n, s, hq, hk, d, dv, dtype=dtype)
+    ws = plan.new_workspace(backward=True)
+
+    def make_calls():
+        kw = dict(state=s0, lengths=lengths, workspace=ws)
+        o, last = plan.forward(q, k, v, ld, return_state=True, **kw)
+        return [o, last, *plan.backward(do, q, k, v, ld, dstate=ds, **kw)]
+
+    def fill(i):
+        gen = torch.Generator(device="cuda").manual_seed(i)
+        for t in (q, k, v, do, s0, ds):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+
+    fill(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        make_calls()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = make_calls()
+    for i in range(1, 5):
+        fill(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        want = make_calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want)), i
+
+
+def test_offsets_past_32_bits():
+    """A sequence whose rows lie 2^21 elements apart: the last at 2^32 and more."""
+    s, step = 2100, 1 << 21
+    room = torch.empty((s - 1) * step + 64, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    small = torch.randn(1, s, 1, 32, generator=gen, device="cuda").bfloat16()
+    far = room.as_strided((1, s, 1, 32), (step, step, 32, 1))
+    far.copy_(small)
+    ld = torch.full((1,), -0.1, device="cuda")
+    plan = fs.LinearAttention(1, s, 1, 1, 32, 32, dtype=torch.bfloat16)
+    want = plan.forward(small, small, small, ld)
+    grads = plan.backward(small, small, small, small, ld)
+    got = plan.forward(far, far, far, ld)
+    far_grads = plan.backward(far, far, far, far, ld)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert all(torch.equal(a, b) for a, b in zip(far_grads[:3], grads[:3]))
