@@ -554,9 +554,9 @@ fftsplit_status_t fftsplit_head_norm_rotary_backward(const fftsplit_head_norm_t*
  * the last token that is there.  What the order of tokens hides from a row has to
  * be finite, as it is multiplied by zero.
  * States, products and sums are fp32.  With bf16 tensors the scores q k^T (with
- * their decay) and the state as an operand are rounded to bf16 in calls of more
- * than a few tokens, and the terms of the state are good to 2^-18; fp32 tensors
- * are rounded nowhere. */
+ * their decay) and the state that a segment begins with are rounded to bf16 once, as
+ * operands, in calls of more than a few tokens; what a call returns of a state or its
+ * gradient is a sum of unrounded products.  fp32 tensors are rounded nowhere. */
 typedef struct {
     int batch;                     /* sequences */
     int tokens;                    /* of the longest; at most 2^28 */
@@ -571,10 +571,11 @@ typedef struct fftsplit_linear_attention_plan_s* fftsplit_linear_attention_plan_
 typedef struct {
     size_t forward_workspace_bytes, backward_workspace_bytes;
     size_t state_bytes;            /* fp32 [batch][heads_k][dim][dim_v] */
-    /* Kernel choice: 1 if the forward pass goes token by token, else 0 (chunks
-     * of 32 tokens); into how many parts a sequence is cut that are worked on
-     * side by side, in either pass (1: it is not). */
-    int recurrent, forward_segments, backward_segments;
+    /* Kernel choice: 1 if the forward pass goes token by token, else 0; tokens of
+     * a segment, within which pairs of tokens are taken one by one and between
+     * which a state is carried, and how many a sequence is cut into (a short one
+     * is taken as one where no state is returned). */
+    int recurrent, segment_tokens, segments;
 } fftsplit_linear_attention_info_t;
 
 /* Input tensors (device).  Strides are in elements, of the dimensions

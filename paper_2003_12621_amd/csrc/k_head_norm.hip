@@ -255,20 +255,32 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
     }
 }
 
-// The weights' gradients from the workgroups' sums: 16 elements a workgroup.
-__global__ __launch_bounds__(256) void head_norm_sum_kernel(HeadNormArgs a) {
-    __shared__ float sums[16][17];
-    const int column = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+// The weights' gradients from the workgroups' sums, in a fixed order: 8 columns a
+// workgroup, 8 loads a lane in flight.
+__global__ __launch_bounds__(1024) void head_norm_sum_kernel(HeadNormArgs a) {
+    constexpr int kColumns = 8, kLanes = 1024 / kColumns, kAhead = 8;
+    __shared__ float sums[kLanes][kColumns + 1];
+    const int column = blockIdx.x * kColumns + threadIdx.x % kColumns, row = threadIdx.x / kColumns, width = 2 * a.r.d;
     float sum = 0.f;
-    if (column < 2 * a.r.d && a.dweight[column / a.r.d])
-        for (int i = row; i < a.blocks; i += 16) sum += a.part[size_t(i) * 2 * a.r.d + column];
-    sums[row][threadIdx.x & 15] = sum;
-    __syncthreads();
-    if (row || column >= 2 * a.r.d) return;
-    sum = 0.f;
-    for (int i = 0; i < 16; ++i) sum += sums[i][threadIdx.x];
+    if (column < width && a.dweight[column / a.r.d])
+        for (int i = row; i < a.blocks; i += kAhead * kLanes) {
+            float v[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int at = i + j * kLanes;
+                v[j] = a.part[size_t(at < a.blocks ? at : i) * width + column];
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) sum += i + j * kLanes < a.blocks ? v[j] : 0.f;
+        }
+    sums[row][threadIdx.x % kColumns] = sum;
+    for (int half = kLanes / 2; half; half /= 2) {
+        __syncthreads();
+        if (row < half) sums[row][threadIdx.x % kColumns] += sums[row + half][threadIdx.x % kColumns];
+    }
+    if (row || column >= width) return;
     const int which = column / a.r.d;
-    if (a.dweight[which]) a.dweight[which][column % a.r.d] = sum;
+    if (a.dweight[which]) a.dweight[which][column % a.r.d] = sums[0][threadIdx.x];
 }
 
 namespace {
@@ -315,7 +327,7 @@ hipError_t launch_head_norm(const HeadNormArgs& a, hipStream_t s, const LaunchEv
 hipError_t launch_head_norm_backward(const HeadNormArgs& a, hipStream_t s, const LaunchEvents& ev) {
     if (!a.dweight[0] && !a.dweight[1]) return launch_typed<true>(a, s, ev);
     if (hipError_t e = launch_typed<true>(a, s, LaunchEvents{ev.start, nullptr})) return e;
-    return launch_kernel(head_norm_sum_kernel, dim3(unsigned((2 * a.r.d + 15) / 16)), dim3(256), 0, s, nullptr, ev.stop, a);
+    return launch_kernel(head_norm_sum_kernel, dim3(unsigned((2 * a.r.d + 7) / 8)), dim3(1024), 0, s, nullptr, ev.stop, a);
 }
 
 }  // namespace fftsplit

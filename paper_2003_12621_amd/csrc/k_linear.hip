@@ -1,21 +1,22 @@
-// Linear attention with a decay for each head, in chunks of 32 tokens.
+// Linear attention with a decay for each head.
 //
-// With S the state (d x dv) before a chunk and D[i][j] = decay^(i - j) for
-// j <= i, the chunk's outputs and the state behind it are
-//     O = (Q K^T . D) V + diag(decay^(i+1)) Q S
-//     S' = decay^32 S + (diag(decay^(31-j)) K)^T V,
-// four matrix products.  A wave owns 32 columns of V, O and S; the state stays
-// in its accumulators from chunk to chunk.  The scores are computed transposed
-// (keys down, queries across the lanes), so that they are in place as the
-// operand of the product with V; the state's accumulators are the operand of
-// the product with Q as they stand.
+// A sequence is cut into segments.  Within one, the terms of all pairs of tokens
+// are taken one by one, as in attention without a softmax: a wave owns 32 query
+// rows, goes over the keys of its segment in tiles of 32 and adds
+//     decay^(i - j) (q_i . k_j) v_j
+// to its outputs.  What lies before the segment comes from the state S (d x dv)
+// before it, as decay^i q_i^T S.  So no wave waits for another one's state:
+//   parts  adds up what each segment adds to the state,
+//   join   makes of these the state before each segment,
+//   pass   computes the outputs of all rows at once.
+// The recurrence over tiles that this replaces has a chain of products, roundings
+// and weights per tile of 3000 cycles, in every wave; here 12 products and 55
+// vector instructions a tile depend on nothing but the keys.
 //
 // The gradients are the same sums with other roles: dq that of (dO, v, k), and
 // dk and dv those of (v, dO, q) and (k, q, dO) from the last token to the first.
-//
-// Sequences with too few heads to fill the chip are cut into segments: a kernel
-// that only adds up each segment's own state, one that joins them to the state
-// before each, and then all segments side by side.
+#include <type_traits>
+
 #include "linear_common.hpp"
 
 namespace fftsplit {
@@ -38,283 +39,688 @@ __device__ __forceinline__ unsigned state_column_lane(int lane) {
     return Shape::at(4 * (lane >> 5) + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + (lane & 1)) + ((lane >> 1) & 1) * 8;
 }
 
-// An operand's elements times factors.  The state is a sum over all tokens and
-// an output in fp32, so bf16 elements are kept as two numbers (rounded, and what
-// that left out), together good to 2^-18; fp32 ones as one.
-template <typename T>
+// An operand's elements times factors, as the sum of PARTS operands.  bf16 elements
+// times fp32 factors have 24 significant bits, three bf16 numbers of 8, cut off one
+// after the other: that is what a state that the caller gets is summed from.  Where
+// it only serves as an operand, rounded to 8 bits, two of them (good to 2^-16) do.
+// fp32 elements are one.
+template <typename T, int PARTS>
 struct Weighted {
-    static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
-    Operand<T> part[kParts];
+    Operand<T> part[PARTS];
     __device__ __forceinline__ Weighted(const Operand<T>& x, const float* w) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) part[0].v[e] = x.v[e] * w[e];
         } else {
-            u32x4 whole, rest;
+            u32x4 p[PARTS];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float a = float(x.v[2 * e]) * w[2 * e], b = float(x.v[2 * e + 1]) * w[2 * e + 1];
-                whole[e] = pack_bf16(a, b);
-                rest[e] = pack_bf16(a - __uint_as_float(whole[e] << 16), b - __uint_as_float(whole[e] & 0xffff0000u));
+                float a = float(x.v[2 * e]) * w[2 * e], b = float(x.v[2 * e + 1]) * w[2 * e + 1];
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    // (the upper halves)
+                    p[i][e] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+                    a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+                    b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+                }
             }
-            part[0].v = __builtin_bit_cast(bf16x8, whole);
-            part[1].v = __builtin_bit_cast(bf16x8, rest);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) part[i].v = __builtin_bit_cast(bf16x8, p[i]);
         }
     }
 };
 
-template <typename T, int D, int WAVES>
-struct ScanShape {
-    static constexpr int kThreads = 64 * WAVES;
-    static constexpr int kColumns = 32 * WAVES;
-    static constexpr int kRowBytes = TileShape<T, D>::bytes(kLinearChunk);          // a chunk of q or k
-    static constexpr int kPairBytes = kRowBytes + TileShape<T, kColumns>::bytes(kLinearChunk);   // of k and v
-    static constexpr int lds(bool main) { return 2 * (kPairBytes + (main ? kRowBytes : 0)); }
+// A stage: some rows of k and of v, of D and COLUMNS columns, on their way from
+// memory straight into LDS, in pieces of 1024 bytes that are dealt out to the waves
+// alike, so that every wave has the same number of copies in flight.  (What rows
+// beyond the last hold is as for RowCopy.)
+template <typename T, int D, int COLUMNS, int WAVES>
+struct StageShape {
+    // Whether the pass's accumulators leave room for three waves a SIMD: then stages of
+    // one tile and fewer operands read ahead, which at 64 / 128 take 33 us where two waves
+    // with two tiles take 37 (training of 4 x 3136 tokens of 8 heads, forwards).
+    static constexpr bool kLean = sizeof(T) == 2 && D * COLUMNS <= 8192;
+    static constexpr int kPassOccupancy = kLean ? 3 : D <= 128 ? 2 : 1;
+    // Two tiles a stage, where two workgroups' rings fit a compute unit
+    static constexpr int kRows = !kLean && 64 * (D + COLUMNS) * int(sizeof(T)) <= 40960 ? 64 : 32;
+    static constexpr int kRowBytes = TileShape<T, D>::bytes(kRows);
+    static constexpr int kUsedBytes = kRowBytes + TileShape<T, COLUMNS>::bytes(kRows);
+    static constexpr int kPer = (kUsedBytes / 1024 + WAVES - 1) / WAVES;             // copies of a wave
+    static constexpr int kStageBytes = kPer * WAVES * 1024;
+    // Stages in LDS: the one worked on, and those on their way.
+    static constexpr int kStages = 3 * kStageBytes <= 81920 ? 3 : 2;
+    static constexpr int kLds = kStages * kStageBytes;
 };
+
+template <typename T, int D, int COLUMNS, int WAVES, bool WIDE>
+struct StageCopy {
+    using Shape = StageShape<T, D, COLUMNS, WAVES>;
+    using Rows = TileShape<T, D>;
+    using Values = TileShape<T, COLUMNS>;
+    static constexpr int kRowPieces = Shape::kRowBytes / 1024, kPieces = Shape::kUsedBytes / 1024;
+    unsigned off[Shape::kPer];
+    int row[Shape::kPer];
+
+    // Which tensor a wave's piece i belongs to: 0 k, 1 v, in this order in LDS (or
+    // 2: none, filled up with zeros).
+    static __device__ __forceinline__ int tensor(int wave, int i) {
+        // (where all waves have the same, that is known here)
+        const int piece = i * WAVES + (kRowPieces % WAVES || kPieces % WAVES ? wave : 0);
+        return piece < kRowPieces ? 0 : piece < kPieces ? 1 : 2;
+    }
+    // Column of a lane's chunk of that piece, and its row.
+    static __device__ __forceinline__ int place(int wave, int lane, int i, int& row) {
+        const int which = tensor(wave, i), at = (wave + i * WAVES - (which ? kRowPieces : 0)) * 64 + lane;
+        row = which ? at / Values::kRowChunks : at / Rows::kRowChunks;
+        return which ? ((at % Values::kRowChunks) ^ Values::swizzle(row)) * Values::kChunk
+                     : ((at % Rows::kRowChunks) ^ Rows::swizzle(row)) * Rows::kChunk;
+    }
+    __device__ __forceinline__ StageCopy(long long k_stride, int k_cols, long long v_stride, int v_cols, int wave,
+                                         int lane) {
+#pragma unroll
+        for (int i = 0; i < Shape::kPer; ++i) {
+            const int which = tensor(wave, i), col = place(wave, lane, i, row[i]);
+            off[i] = which < 2 && col < (which ? v_cols : k_cols)
+                         ? unsigned((row[i] * (which ? v_stride : k_stride) + col) * int(sizeof(T))) : kOutOfRange;
+        }
+    }
+    // Starts the copies of the first `rows` rows (of a stage, with zeros for the rest;
+    // at most all, possibly none or less) from k and v on, which reach `size` bytes.
+    __device__ __forceinline__ void start(unsigned stage, const char* k, const char* v, unsigned size_k, unsigned size_v,
+                                          int rows, int k_cols, int v_cols, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < Shape::kPer; ++i) {
+            const int which = tensor(wave, i);
+            const unsigned to = stage + (wave + i * WAVES) * 1024, at = row[i] < rows ? off[i] : kOutOfRange;
+            const char* from = which ? v : k;
+            const unsigned size = which ? size_v : size_k;
+            if constexpr (WIDE) {
+                copy16(copy_source(from, size), at, __builtin_amdgcn_readfirstlane(to));
+            } else {
+                const BufRsrc rsrc = make_rsrc(from, size);
+                int unused;
+                const int col = place(wave, lane, i, unused);
+                constexpr int kChunk = 16 / sizeof(T);
+                T e[kChunk];
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    const unsigned o = col + j < (which ? v_cols : k_cols) ? at + j * unsigned(sizeof(T)) : kOutOfRange;
+                    if constexpr (sizeof(T) == 4)
+                        e[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, o, 0, 0));
+                    else
+                        e[j] = __builtin_bit_cast(__bf16, __builtin_amdgcn_raw_buffer_load_b16(rsrc, o, 0, 0));
+                }
+                u32x4 u;
+                __builtin_memcpy(&u, e, 16);
+                *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(
+                    (__attribute__((address_space(3))) char*)(to + lane * 16)) = u;
+            }
+        }
+    }
+};
+
+// The keys that a workgroup goes over in stages, of each the heads of k and v that
+// share a state one after another: copies them into a ring.  First the tokens from
+// `first` on to `end`, then those from `other` on to `other_end` (either possibly
+// none); rows of the last stage that are not there become zero.
+template <typename T, int D, int COLUMNS, int WAVES, bool WIDE>
+struct KeyStream {
+    using Shape = StageShape<T, D, COLUMNS, WAVES>;
+    static constexpr int kBytes = sizeof(T);
+    const StageCopy<T, D, COLUMNS, WAVES, WIDE> copy;
+    const char *k, *v;
+    // to the next head; further from the last one to the next stage's first; and further
+    // to the first of the other tokens
+    long long to_head_k, to_head_v, to_next_k, to_next_v, to_other_k, to_other_v;
+    unsigned size_k, size_v;
+    int own, stages, heads, k_cols, v_cols, next_stage = 0, next_head = 0, rows, to_other_rows;
+    unsigned base, next;             // LDS: of the ring, and of the stage to fill next
+
+    __device__ __forceinline__ KeyStream(const LinearPass& a, unsigned ring, int b, int h, int column0, int first, int end,
+                                         int other, int other_end, int wave, int lane)
+        : copy(a.k.t, a.d, a.v.t, min(a.dv - column0, COLUMNS), wave, lane) {
+        base = next = ring;
+        heads = linear_scalar(a.k_heads);
+        k_cols = a.d;
+        v_cols = min(a.dv - column0, COLUMNS);
+        rows = end - first;
+        const int other_rows = other_end - other;
+        own = rows > 0 ? (rows + Shape::kRows - 1) / Shape::kRows : 0;
+        stages = own + (other_rows > 0 ? (other_rows + Shape::kRows - 1) / Shape::kRows : 0);
+        to_other_rows = other_rows + own * Shape::kRows - rows;
+        k = static_cast<const char*>(a.k.p) + (b * a.k.b + (long long)h * heads * a.k.h + first * a.k.t) * kBytes;
+        v = static_cast<const char*>(a.v.p) + (b * a.v.b + (long long)h * heads * a.v.h + first * a.v.t + column0) * kBytes;
+        to_head_k = a.k.h * kBytes;
+        to_head_v = a.v.h * kBytes;
+        to_next_k = Shape::kRows * kBytes * a.k.t - heads * to_head_k;
+        to_next_v = Shape::kRows * kBytes * a.v.t - heads * to_head_v;
+        const long long jump = (long long)(other - first) - own * Shape::kRows;
+        to_other_k = jump * kBytes * a.k.t;
+        to_other_v = jump * kBytes * a.v.t;
+        size_k = unsigned(((Shape::kRows - 1) * a.k.t + k_cols) * kBytes);
+        size_v = unsigned(((Shape::kRows - 1) * a.v.t + v_cols) * kBytes);
+    }
+    // Starts the copy of the next step; behind the last, of nothing.
+    __device__ __forceinline__ void fetch(int wave, int lane) {
+        copy.start(next, k, v, size_k, size_v, next_stage < stages ? rows : 0, k_cols, v_cols, wave, lane);
+        next = next + Shape::kStageBytes == base + Shape::kLds ? base : next + Shape::kStageBytes;
+        // (sums, not a choice among members, for which the compiler keeps them in memory)
+        const bool last_head = next_head + 1 == heads, jump = last_head && next_stage == own - 1;
+        k += to_head_k + (last_head ? to_next_k : 0) + (jump ? to_other_k : 0);
+        v += to_head_v + (last_head ? to_next_v : 0) + (jump ? to_other_v : 0);
+        rows += (last_head ? -Shape::kRows : 0) + (jump ? to_other_rows : 0);
+        next_stage += last_head ? 1 : 0;
+        next_head = last_head ? 0 : next_head + 1;
+    }
+    // The next stage is there, and all waves are done with the one before, whose
+    // place the copy that starts here fills.
+    __device__ __forceinline__ void advance(int wave, int lane) {
+        own_copies_done<(Shape::kStages - 2) * Shape::kPer>();
+        __syncthreads();
+        fetch(wave, lane);
+    }
+};
+
+struct PassPair {
+    LinearPass pass[2];
+    int first_blocks;                // of pass[0]; the rest belong to pass[1]
+};
+
+// Columns of the values that a workgroup of the pass takes, and waves of it (one
+// for each 32 columns) of the kernel that adds up the parts.
+constexpr int kPassWaves = kLinearRows / kLinearTile;
+constexpr int kDiagonalBytes = kLinearTile * kLinearTile * 4;
 
 }  // namespace
 
-// One workgroup: one segment of one head and 32 WAVES columns.  MAIN: the
-// outputs; else only the state that the segment adds, from zero.
-template <typename T, int D, int WAVES, bool WIDE, bool MAIN>
-__global__ __launch_bounds__(64 * WAVES) void linear_scan_kernel(LinearScan a) {
-    using Shape = ScanShape<T, D, WAVES>;
-    constexpr int kChunk = kLinearChunk, DT = D / 32, kSteps = D / 16;
+// One workgroup: 128 query rows of one head, COLUMNS columns; a wave takes 32 of
+// the rows.  Scores are computed transposed (keys down, queries across the
+// lanes), so that they are in place as the operand of the product with the values.
+//
+// The decay of a pair in tiles m >= 1 apart, with a the query's and b the key's
+// place in its tile, is decay^(32 (m - 1) + a) of the lane times decay^(32 - b) of
+// the register, neither of which can overflow.
+template <typename T, int D, int COLUMNS, bool WIDE>
+__global__ __launch_bounds__(64 * kPassWaves, (StageShape<T, D, COLUMNS, kPassWaves>::kPassOccupancy))
+void linear_pass_kernel(PassPair pair) {
+    using Shape = StageShape<T, D, COLUMNS, kPassWaves>;
+    constexpr int kTile = kLinearTile, kSteps = D / 16, kBlocks = COLUMNS / 32;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int slices = (a.dv + Shape::kColumns - 1) / Shape::kColumns, q_heads = MAIN ? a.q_heads : 1;
-    // (the columns and query heads of one segment next to one another)
-    int id = xcd_logical_block(blockIdx.x, gridDim.x);
-    const int slice = id % slices;
+    const bool second = int(blockIdx.x) >= pair.first_blocks;
+    const LinearPass& a = pair.pass[second];
+    const int lane = threadIdx.x & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // (the tiles, columns and query heads of one head next to one another, the
+    // tiles with most keys first)
+    const int slices = (a.dv + COLUMNS - 1) / COLUMNS, row_tiles = (a.s + kLinearRows - 1) / kLinearRows;
+    const int blocks = second ? int(gridDim.x) - pair.first_blocks : pair.first_blocks;
+    int id = xcd_logical_block(int(blockIdx.x) - (second ? pair.first_blocks : 0), blocks);
+    const int column0 = linear_scalar(id % slices * COLUMNS);
     id /= slices;
-    const int member = id % q_heads;
-    id /= q_heads;
-    const int segments = MAIN ? a.segments : a.segments - 1;
-    int segment = id % segments;
-    const int head = id / segments, h = head % a.hk, b = head / a.hk;
-    if (!MAIN && a.reverse) ++segment;               // the last one's own state is not needed
+    const int member = linear_scalar(id % a.q_heads);
+    id /= a.q_heads;
+    const int place = linear_scalar(id % row_tiles), head = linear_scalar(id / row_tiles);
+    const int h = linear_scalar(head % a.hk), b = linear_scalar(head / a.hk);
+    const int row0 = (a.reverse ? place : row_tiles - 1 - place) * kLinearRows;
+    const float log2_decay = decay_log2(linear_uniform(a.log_decay + h));
     const int length = linear_length(a.lengths, a.s, b);
-    const int begin = segment * a.segment_tokens;
-    const int room = int(min((long long)begin + a.segment_tokens, (long long)a.s)), end = min(room, length);
-    const int chunks = end > begin ? (end - begin + kChunk - 1) / kChunk : 0;
-    const float log2_decay = decay_log2(a.log_decay[h]);
-    const int column0 = slice * Shape::kColumns, columns = min(a.dv - column0, Shape::kColumns);
+    const size_t o_row = size_t(a.hk) * a.q_heads * a.dv;
+    const int own0 = row0 + kTile * wave, row = own0 + (lane & 31);
+    T* o = static_cast<T*>(a.o) + (size_t(b) * a.s + row) * o_row + (size_t(h) * a.q_heads + member) * a.dv;
+    floatx16 out[kBlocks];
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) out[c] = zero16();
 
+    if (row0 < length) {
+        const int segment = linear_scalar(row0 / a.segment_tokens), begin = segment * a.segment_tokens;
+        const int end = int(min((long long)begin + a.segment_tokens, (long long)length));
+        // first the keys of the workgroup's own rows, then those further on (all of them
+        // before its rows, backwards behind them)
+        const int own_end = min(row0 + kLinearRows, end);
+        KeyStream<T, D, COLUMNS, kPassWaves, WIDE> stream(a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, row0,
+                                                          own_end, a.reverse ? own_end : begin, a.reverse ? end : row0, wave,
+                                                          lane);
+        for (int i = 0; i + 1 < Shape::kStages; ++i) stream.fetch(wave, lane);
+        Operand<T> q[kSteps];
+        load_row_operands<T, D, WIDE>(q, static_cast<const T*>(a.q.p) + b * a.q.b + row * a.q.t +
+                                             ((long long)h * a.q_heads + member) * a.q.h, a.d, row < length, lane);
+        const int query = lane & 31;
+        // (in registers: what is read again behind a copy's start would be loaded again)
+        const int reverse = linear_scalar(a.reverse), k_heads = linear_scalar(a.k_heads);
+        const float pair_scale = linear_scalar(a.pair_scale), way = reverse ? -1.f : 1.f;
+        // decay^(32 - b) (backwards decay^b) of b = acc_row(r, hi), as a product
+        float eights[4], ones[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            eights[r] = pair_scale * decay_power(log2_decay, reverse ? 8 * r : 24 - 8 * r);
+            ones[r] = decay_power(log2_decay, reverse ? 4 * hi + r : 8 - 4 * hi - r);
+        }
+        const float place0 = float(reverse ? kTile - query : query) - float(kTile);
+        // the factors of a wave's own tile, which no such product can give: in LDS, as
+        // the registers of a lane
+        float4* diagonal = reinterpret_cast<float4*>(lds + Shape::kLds);
+        {
+            const int i = threadIdx.x >> 6;
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = acc_row(4 * i + j, hi), apart = reverse ? key - query : query - key;
+                e[j] = apart >= 0 ? pair_scale * decay_power(log2_decay, apart) : 0.f;
+            }
+            diagonal[i * 64 + lane] = make_float4(e[0], e[1], e[2], e[3]);
+        }
+        if (a.starts) {
+            // what came before the segment
+            const int rows = linear_steps(a.d), all = (a.dv + 31) / 32;
+            const Operand<T>* p =
+                static_cast<const Operand<T>*>(a.starts) + (size_t(head) * a.segments + segment) * all * rows * 64 + lane;
+            // (loads side by side, of strips that exist: the columns behind the last
+            // are not stored)
+            constexpr int kHalf = kSteps * sizeof(T) <= 16 ? kSteps : 16 / int(sizeof(T));
+            Operand<T> x[2][kHalf];
+            auto load = [&](int j) {
+                const int strip = min(column0 / 32 + j * kHalf / kSteps, all - 1);
+                const Operand<T>* at = p + size_t(strip * rows + j * kHalf % kSteps) * 64;
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) x[j % 2][i] = at[i * 64];
+            };
+            load(0);
+#pragma unroll
+            for (int j = 0; j < kBlocks * kSteps / kHalf; ++j) {
+                if (j + 1 < kBlocks * kSteps / kHalf) load(j + 1);
+                in_order();
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) mma(out[j * kHalf / kSteps], x[j % 2][i], q[(j * kHalf + i) % kSteps]);
+            }
+            const float f = a.inter_scale * decay_power(log2_decay, max(a.reverse ? end - 1 - row : row - begin + 1, 0));
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) out[c][r] *= f;
+        }
+        settle(q);
+        const unsigned k_row = stream.base + row_lane<T, D>(lane);
+        const unsigned v_column = stream.base + column_lane<T, COLUMNS>(lane) + Shape::kRowBytes;
+        constexpr int kTiles = Shape::kRows / kTile;
+        // TILES tiles of a stage, from its tile j on, side by side; operands are read
+        // kAhead products before they are used.  weigh(s, t): scores become terms.
+        auto take = [&](auto tiles, int stage, int j, auto weigh) {
+            constexpr int TILES = decltype(tiles)::value;
+            constexpr int kScores = TILES * kSteps, kEnd = kScores + 2 * TILES * kBlocks, kAhead = Shape::kLean ? 2 : 3;
+            const unsigned k_at = k_row + stage + j * kTile * int(sizeof(T)) * D;
+            const unsigned v_at = v_column + stage + j * kTile * int(sizeof(T)) * COLUMNS;
+            floatx16 s[TILES];
+            Operand<T> ring[kAhead + 1], p[2 * TILES];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) s[t] = zero16();
+            auto read = [&](int i) {
+                if (i >= kEnd) return;
+                const int v = i - kScores;
+                ring[i % (kAhead + 1)] =
+                    i < kScores ? read_row<T, D>(k_at, kTile * (i % TILES), i / TILES)
+                                : read_column<T, COLUMNS>(v_at, kTile * (v / kBlocks / 2), 32 * (v % kBlocks), v / kBlocks % 2);
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) read(i);
+#pragma unroll
+            for (int i = 0; i < kEnd; ++i) {
+                in_order();
+                read(i + kAhead);
+                in_order();
+                if (i == kScores) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        weigh(s[t], t);
+                        p[2 * t] = acc_operand<T>(s[t], 0);
+                        p[2 * t + 1] = acc_operand<T>(s[t], 1);
+                    }
+                }
+                const Operand<T>& x = ring[i % (kAhead + 1)];
+                const int v = i - kScores;
+                if (i < kScores)
+                    mma(s[i % TILES], x, q[i / TILES]);
+                else
+                    mma(out[v % kBlocks], x, p[v / kBlocks]);
+            }
+        };
+        // Terms of a tile `between` tokens from the wave's own.
+        auto apart = [&](floatx16& s, int between) {
+            const float far = __builtin_amdgcn_exp2f(log2_decay * (place0 + float(between)));
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= eights[r / 4] * far * ones[r % 4];
+        };
+        int stage = 0;
+        const int own_tile = wave, step = reverse ? 1 : -1;
+        for (int n = 0; n < stream.own; ++n)
+            for (int g = 0; g < k_heads; ++g) {
+                stream.advance(wave, lane);
+#pragma unroll 1
+                for (int j = 0; j < kTiles; ++j) {
+                    const int between = (n * kTiles + j - own_tile) * step;
+                    if (between < 0) continue;
+                    take(std::integral_constant<int, 1>{}, stage, j, [&](floatx16& s, int) {
+                        if (between) {
+                            apart(s, between * kTile);
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const float4 e = diagonal[r * 64 + lane];
+                                s[4 * r] *= e.x;
+                                s[4 * r + 1] *= e.y;
+                                s[4 * r + 2] *= e.z;
+                                s[4 * r + 3] *= e.w;
+                            }
+                        }
+                    });
+                }
+                stage = stage + Shape::kStageBytes == Shape::kLds ? 0 : stage + Shape::kStageBytes;
+            }
+        int between = reverse ? kLinearRows - own_tile * kTile : own0 - begin;
+        for (int n = stream.own; n < stream.stages; ++n, between += step * Shape::kRows)
+            for (int g = 0; g < k_heads; ++g) {
+                stream.advance(wave, lane);
+                take(std::integral_constant<int, kTiles>{}, stage, 0,
+                     [&](floatx16& s, int t) { apart(s, between + step * kTile * t); });
+                stage = stage + Shape::kStageBytes == Shape::kLds ? 0 : stage + Shape::kStageBytes;
+            }
+        // (no copy may be on its way to the LDS of a workgroup that has ended)
+        own_copies_done<0>();
+    }
+    if (row >= a.s) return;
+    const bool there = row < length;                 // (tokens behind the last: zero)
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            store4(o, column0 + 32 * c + acc_row(4 * r, hi), a.dv, WIDE || a.o_wide, there ? out[c][4 * r] : 0.f,
+                   there ? out[c][4 * r + 1] : 0.f, there ? out[c][4 * r + 2] : 0.f, there ? out[c][4 * r + 3] : 0.f);
+}
+
+// What one segment of one head adds to the state, from zero: 32 WAVES columns, 32 a
+// wave, whose accumulators keep the state while the keys pass.  PARTS: of the
+// weighted values (Weighted).
+template <typename T, int D, int WAVES, bool WIDE, int PARTS>
+__global__ __launch_bounds__(64 * WAVES, (D <= 128 ? 2 : 1)) void linear_parts_kernel(PassPair pair) {
+    constexpr int kTile = kLinearTile, DT = D / 32, kColumns = 32 * WAVES;
+    using Shape = StageShape<T, D, kColumns, WAVES>;
+    extern __shared__ __align__(16) char lds[];
+    const bool second = int(blockIdx.x) >= pair.first_blocks;
+    const LinearPass& a = pair.pass[second];
+    const int lane = threadIdx.x & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int slices = (a.dv + kColumns - 1) / kColumns;
+    const int blocks = second ? int(gridDim.x) - pair.first_blocks : pair.first_blocks;
+    int id = xcd_logical_block(int(blockIdx.x) - (second ? pair.first_blocks : 0), blocks);
+    const int column0 = linear_scalar(id % slices * kColumns);
+    id /= slices;
+    const int segment = linear_scalar(id % a.part_count) + a.first_part, head = linear_scalar(id / a.part_count);
+    const int h = linear_scalar(head % a.hk), b = linear_scalar(head / a.hk);
+    const int begin = segment * a.segment_tokens;
+    const float log2_decay = decay_log2(linear_uniform(a.log_decay + h));
+    const int end = int(min((long long)begin + a.segment_tokens, (long long)linear_length(a.lengths, a.s, b)));
+
+    KeyStream<T, D, kColumns, WAVES, WIDE> stream(a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, begin, end, 0,
+                                                  0, wave, lane);
+    for (int i = 0; i + 1 < Shape::kStages; ++i) stream.fetch(wave, lane);
+    // a token's weight is decay to its distance from the segment's end (backwards,
+    // from one before its beginning): of its place in the tile, times the tile's
+    const int reverse = linear_scalar(a.reverse), k_heads = linear_scalar(a.k_heads);
+    const float update_scale = linear_scalar(a.update_scale);
+    float weight[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int key = acc_row(r, hi);
+        weight[r] = update_scale * decay_power(log2_decay, reverse ? key + 1 : kTile - 1 - key);
+    }
     floatx16 state[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) state[d] = zero16();
+    const unsigned k_column = stream.base + state_column_lane<T, D>(lane);
+    const unsigned v_column = stream.base + column_lane<T, kColumns>(lane) + Shape::kRowBytes;
+    int stage = 0;
+    for (int n = 0; n < stream.stages; ++n) {
+        for (int g = 0; g < k_heads; ++g) {
+            stream.advance(wave, lane);
+#pragma unroll
+            for (int j = 0; j < Shape::kRows / kTile; ++j) {
+                const int first = n * Shape::kRows + j * kTile, keys = end - begin - first;
+                float w[16];
+                const float far = decay_power(log2_decay, reverse ? first : max(keys - kTile, 0));
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w[r] = weight[r] * far;
+                if (keys < kTile && !reverse) {
+                    // (behind the last, values are zero)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        w[r] = update_scale * decay_power(log2_decay, max(keys - 1 - acc_row(r, hi), 0));
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const Weighted<T, PARTS> x(read_column<T, kColumns>(v_column + stage, kTile * j, 32 * wave, i), w + 8 * i);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const Operand<T> y = read_column<T, D>(k_column + stage, kTile * j, 32 * d, i);
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) mma(state[d], y, x.part[p]);
+                    }
+                }
+            }
+            stage = stage + Shape::kStageBytes == Shape::kLds ? 0 : stage + Shape::kStageBytes;
+        }
+    }
+    own_copies_done<0>();
     const int column = column0 + 32 * wave + (lane & 31);
-    if (MAIN && a.init) {
-        const float* p = a.init + head * a.init_head + segment * a.init_segment + column * a.init_column;
+    float* to = a.parts + (size_t(head) * a.segments + segment) * a.d * a.dv + column;
+    if (column < a.dv)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int row = 32 * d + state_row(r, hi);
-                if (row < a.d && column < a.dv) state[d][r] = p[row * a.init_row];
+                if (row < a.d) to[unsigned(row * a.dv)] = state[d][r];
             }
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(state[d]));
-
-    // factors of a pair (key acc_row(r, hi), query lane % 32) and of a token's
-    // term of the state, in a chunk of n tokens
-    float pair[16], update[16];
-    int factors_of = 0;
-    float inter = 0.f, carry = 0.f;
-    const int query = lane & 31;
-    auto set_factors = [&](int n) {
-        factors_of = n;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int key = acc_row(r, hi), apart = a.reverse ? key - query : query - key;
-            pair[r] = apart >= 0 && key < n ? a.pair_scale * decay_power(log2_decay, apart) : -1.f;
-            const int left = a.reverse ? key + 1 : n - 1 - key;
-            update[r] = key < n ? a.update_scale * decay_power(log2_decay, left) : 0.f;
-        }
-        inter = a.inter_scale * decay_power(log2_decay, max(a.reverse ? n - 1 - query : query + 1, 0));
-        carry = decay_less_one(log2_decay, n);
-    };
-
-    using QueryCopy = RowCopy<T, D, kChunk, Shape::kThreads, WIDE>;
-    using ValueCopy = RowCopy<T, Shape::kColumns, kChunk, Shape::kThreads, WIDE>;
-    const QueryCopy query_copy(a.q.t, a.d, tid), key_copy(a.k.t, a.d, tid);
-    const ValueCopy value_copy(a.v.t, columns, tid);
-    const T* q = static_cast<const T*>(a.q.p) + b * a.q.b + (h * a.q_heads + member) * a.q.h;
-    const T* k = static_cast<const T*>(a.k.p) + b * a.k.b + (long long)h * a.k_heads * a.k.h;
-    const T* v = static_cast<const T*>(a.v.p) + b * a.v.b + (long long)h * a.k_heads * a.v.h + column0;
-    const unsigned base = unsigned(reinterpret_cast<uintptr_t>(lds)), queries = base + 2 * Shape::kPairBytes;
-    // Chunk and head of step i: the heads of k and v that share a state follow one
-    // another within a chunk.
-    auto fetch = [&](int chunk, int g, int step) {
-        const int row = begin + (a.reverse ? chunks - 1 - chunk : chunk) * kChunk, rows = end - row;
-        const unsigned to = base + (step & 1) * Shape::kPairBytes;
-        key_copy.start(to, k + g * a.k.h + (long long)row * a.k.t, a.k.t, rows, tid);
-        value_copy.start(to + Shape::kRowBytes, v + g * a.v.h + (long long)row * a.v.t, a.v.t, rows, tid);
-        if (MAIN && g == 0)
-            query_copy.start(queries + (chunk & 1) * Shape::kRowBytes, q + (long long)row * a.q.t, a.q.t, rows, tid);
-    };
-    const unsigned row_at = row_lane<T, D>(lane), key_column_at = state_column_lane<T, D>(lane);
-    const unsigned value_at = column_lane<T, Shape::kColumns>(lane) + Shape::kRowBytes;
-    const size_t o_row = size_t(a.hk) * a.q_heads * a.dv;
-    T* o = MAIN ? static_cast<T*>(a.o) + size_t(b) * a.s * o_row + (size_t(h) * a.q_heads + member) * a.dv : nullptr;
-
-    floatx16 out = zero16();
-    if (chunks > 0) fetch(0, 0, 0);
-    copies_done();
-    for (int chunk = 0, g = 0, step = 0; chunk < chunks; ++step) {
-        const bool last_head = g + 1 == a.k_heads;
-        if (!last_head)
-            fetch(chunk, g + 1, step + 1);
-        else if (chunk + 1 < chunks)
-            fetch(chunk + 1, 0, step + 1);
-        const int row = begin + (a.reverse ? chunks - 1 - chunk : chunk) * kChunk, n = min(end - row, kChunk);
-        if (n != factors_of) set_factors(n);
-        const unsigned pairs = base + (step & 1) * Shape::kPairBytes;
-        const unsigned tq = queries + (chunk & 1) * Shape::kRowBytes + row_at;
-        if (MAIN && g == 0) {
-            // what came before the chunk
-            out = zero16();
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) mma(out, acc_operand<T>(state[s / 2], s % 2), read_row<T, D>(tq, 0, s));
-#pragma unroll
-            for (int r = 0; r < 16; ++r) out[r] *= inter;
-        }
-        if (g == 0) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) state[d][r] = fmaf(state[d][r], carry, state[d][r]);
-        }
-        Operand<T> x[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) x[s] = read_column<T, Shape::kColumns>(pairs + value_at, 0, 32 * wave, s);
-        if (MAIN) {
-            floatx16 c = zero16();
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) mma(c, read_row<T, D>(pairs + row_at, 0, s), read_row<T, D>(tq, 0, s));
-#pragma unroll
-            for (int r = 0; r < 16; ++r) c[r] = pair[r] < 0.f ? 0.f : c[r] * pair[r];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) mma(out, x[s], acc_operand<T>(c, s));
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const Weighted<T> w(x[s], update + 8 * s);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const Operand<T> y = read_column<T, D>(pairs + key_column_at, 0, 32 * d, s);
-#pragma unroll
-                for (int p = 0; p < Weighted<T>::kParts; ++p) mma(state[d], y, w.part[p]);
-            }
-        }
-        // the next stage is there, and all waves are done with this one
-        copies_done();
-        if (MAIN && last_head && query < n) {
-            // (after the wait, so that it is not for these stores)
-            T* p = o + size_t(row + query) * o_row;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                store4(p, column0 + 32 * wave + acc_row(4 * r, hi), a.dv, a.o_wide, out[4 * r], out[4 * r + 1], out[4 * r + 2],
-                       out[4 * r + 3]);
-        }
-        g = last_head ? 0 : g + 1;
-        chunk += last_head;
-    }
-
-    if (MAIN) {
-        // tokens behind the last
-        for (int row = max(end, begin) + tid / Shape::kColumns; row < room; row += Shape::kThreads / Shape::kColumns) {
-            const int c = tid % Shape::kColumns;
-            if (c < columns) o[size_t(row) * o_row + column0 + c] = T(0.f);
-        }
-    }
-    float* to = MAIN ? a.last : a.parts;
-    if (!to) return;
-    if (MAIN) {
-        if (member != 0 || segment != (a.reverse ? 0 : a.segments - 1)) return;
-        to += size_t(head) * a.d * a.dv;
-    } else {
-        to += (size_t(head) * a.segments + segment) * a.d * a.dv;
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = 32 * d + state_row(r, hi);
-            if (row < a.d && column < a.dv) to[size_t(row) * a.dv + column] = state[d][r];
-        }
 }
 
-// One thread an element: the state before each segment from what each adds.
-__global__ __launch_bounds__(256) void linear_join_kernel(LinearJoin a) {
-    const int blocks = (a.elements + 255) / 256;
-    const int head = blockIdx.x / blocks, i = blockIdx.x % blocks * 256 + threadIdx.x;
-    if (i >= a.elements) return;
-    const int length = linear_length(a.lengths, a.s, head / a.hk);
-    const float log2_decay = decay_log2(a.log_decay[head % a.hk]);
-    float* p = a.parts + size_t(head) * a.segments * a.elements + i;
-    float state = a.init ? a.init[size_t(head) * a.elements + i] : 0.f;
-    constexpr int kAhead = 8;
-    for (int m0 = 0; m0 < a.segments; m0 += kAhead) {
-        float added[kAhead];
+struct JoinJobs {
+    LinearJoin job[3];
+    int end[3];                      // workgroups up to and including each
+};
+
+// A lane: 8 rows of one column of the operands.  The segments are taken kJoinWaves * RUN
+// at a time, a run of RUN of them to a wave, whose loads are in flight together; each
+// wave adds up its own run, reads the other waves' sums for the state before it, and
+// goes through its run once more.  The order is that of the segments, whatever the
+// timing.  VEC: the 8 rows lie side by side in a state.
+constexpr int kJoinWaves = 8;
+
+template <typename T, int RUN, bool VEC>
+__device__ __forceinline__ void linear_join(const LinearJoin& a, int block, float (&sums)[kJoinWaves][8][64]) {
+    const int items = a.rows / 8 * a.columns, per = items / 64;
+    const int head = block / per, lane = threadIdx.x & 63, item = block % per * 64 + lane;
+    const int wave = linear_scalar(int(threadIdx.x >> 6));
+    const int step = item / 64 % (a.rows / 16), strip = item / 64 / (a.rows / 16);
+    const int row0 = 16 * step + 8 * (lane >> 5), column = 32 * strip + (lane & 31);
+    const int length = linear_scalar(linear_length(a.lengths, a.s, head / a.hk));
+    const float log2_decay = decay_log2(linear_uniform(a.log_decay + head % a.hk));
+    const int elements = a.d * a.dv, row_step = a.turned ? 1 : a.dv, column_step = a.turned ? a.dv : 1;
+    const int rows = min((a.turned ? a.dv : a.d) - row0, 8);
+    const bool there = column < (a.turned ? a.d : a.dv);
+    const int at = row0 * row_step + column * column_step;
+    // (loads that do not branch, for many at a time: what is not there reads element 0)
+    auto load = [&](float (&e)[8], const float* p) {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int m = a.reverse ? a.segments - 1 - (m0 + j) : m0 + j;
-            added[j] = m0 + j + 1 < a.segments ? p[size_t(m) * a.elements] : 0.f;   // (the last is not there)
+            for (int j = 0; j < 8; j += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(p + (there && j < rows ? at + j : 0));
+                e[j] = v.x;
+                e[j + 1] = v.y;
+                e[j + 2] = v.z;
+                e[j + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = p[there && j < rows ? at + j * row_step : 0];
+        }
+    };
+    auto keep = [&](float (&e)[8], bool given) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = given && there && j < rows ? e[j] : 0.f;
+    };
+    const float whole = decay_less_one(log2_decay, a.segment_tokens);
+    const float whole_run = decay_less_one(log2_decay, RUN * a.segment_tokens);
+    // decay over the segments from `first` on, in the order of the join, less one
+    auto carry_over = [&](int first, int count) {
+        const int low = a.reverse ? a.segments - first - count : first;
+        const int tokens = max(0, min(length - low * a.segment_tokens, count * a.segment_tokens));
+        if (tokens == a.segment_tokens) return whole;
+        if (tokens == RUN * a.segment_tokens) return whole_run;
+        return tokens ? decay_less_one(log2_decay, tokens) : 0.f;
+    };
+    auto advance = [&](float (&state)[8], float carry, const float (&added)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) state[j] = fmaf(state[j], carry, state[j]) + added[j];
+    };
+    float state[8];
+    load(state, a.init ? a.init + size_t(head) * elements : a.parts);
+    keep(state, a.init != nullptr);
+    const float* parts = a.parts + size_t(head) * a.segments * elements;
+    Operand<T>* starts = static_cast<Operand<T>*>(a.starts) + (size_t(head) * a.segments * items + item);
+    for (int m0 = 0; m0 < a.segments; m0 += RUN * kJoinWaves) {
+        // the run of any wave in this turn
+        auto first_of = [&](int w) { return min(m0 + w * RUN, a.segments); };
+        const int first = first_of(wave), count = first_of(wave + 1) - first;
+        auto segment = [&](int i) {
+            const int m = min(first + i, a.segments - 1);
+            return a.reverse ? a.segments - 1 - m : m;
+        };
+        float added[RUN][8], sum[8] = {};
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) load(added[i], parts + (long long)segment(i) * elements);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            const int m = segment(i);
+            keep(added[i], i < count && m >= a.first_part && m < a.first_part + a.part_count);
+            if (i < count) advance(sum, carry_over(first + i, 1), added[i]);
+        }
+        if (m0) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[wave][j][lane] = sum[j];
+        __syncthreads();
+        // the state before this wave's run, and before the next turn
+        float next[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) next[j] = state[j];
+        for (int w = 0; w < kJoinWaves; ++w) {
+            const int f = first_of(w), c = first_of(w + 1) - f;
+            if (!c) break;
+            float other[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) other[j] = sums[w][j][lane];
+            advance(next, carry_over(f, c), other);
+            if (w < wave)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) state[j] = next[j];
         }
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (m0 + j >= a.segments) break;
-            const int m = a.reverse ? a.segments - 1 - (m0 + j) : m0 + j;
-            p[size_t(m) * a.elements] = state;
-            const int n = max(0, min(length - m * a.segment_tokens, a.segment_tokens));
-            state = fmaf(state, decay_less_one(log2_decay, n), state) + added[j];
+        for (int i = 0; i < RUN; ++i) {
+            if (i >= count) break;
+            if (a.starts) {
+                floatx16 c;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) c[j] = state[j];
+                starts[size_t(segment(i)) * items] = acc_operand<T>(c, 0);
+            }
+            advance(state, carry_over(first + i, 1), added[i]);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) state[j] = next[j];
     }
+    if (a.last && there && !wave)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < rows) a.last[size_t(head) * elements + at + j * row_step] = state[j];
+}
+
+template <typename T, int RUN>
+__global__ __launch_bounds__(64 * kJoinWaves, 4) void linear_join_kernel(JoinJobs jobs) {
+    __shared__ float sums[kJoinWaves][8][64];
+    const int which = int(blockIdx.x) < jobs.end[0] ? 0 : int(blockIdx.x) < jobs.end[1] ? 1 : 2;
+    const LinearJoin& a = jobs.job[which];
+    const int block = blockIdx.x - (which ? jobs.end[which - 1] : 0);
+    if (a.turned && a.dv % 4 == 0)
+        linear_join<T, RUN, true>(a, block, sums);
+    else
+        linear_join<T, RUN, false>(a, block, sums);
 }
 
 namespace {
 
-template <typename T, int D, int WAVES, bool MAIN>
-hipError_t launch_shaped(const LinearScan& a, hipStream_t s, const LaunchEvents& ev) {
-    using Shape = ScanShape<T, D, WAVES>;
-    const int slices = (a.dv + Shape::kColumns - 1) / Shape::kColumns;
-    const long long blocks = (long long)a.n * a.hk * (MAIN ? (long long)a.q_heads * a.segments : a.segments - 1) * slices;
-    auto kernel = a.wide ? linear_scan_kernel<T, D, WAVES, true, MAIN> : linear_scan_kernel<T, D, WAVES, false, MAIN>;
-    if (hipError_t e = allow_dynamic_lds(kernel, Shape::lds(MAIN))) return e;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(Shape::kThreads), Shape::lds(MAIN), s, ev.start, ev.stop, a);
+long long pass_blocks(const LinearPass& a, int columns) {
+    return (long long)a.n * a.hk * a.q_heads * ((a.dv + columns - 1) / columns) * ((a.s + kLinearRows - 1) / kLinearRows);
+}
+long long part_blocks(const LinearPass& a, int columns) {
+    return (long long)a.n * a.hk * a.part_count * ((a.dv + columns - 1) / columns);
 }
 
-template <typename T, int D, bool MAIN>
-hipError_t launch_columns(const LinearScan& a, hipStream_t s, const LaunchEvents& ev) {
-    // (fp32 rows of 256: two buffers of 128 columns fill all of a compute unit's LDS)
-    if (a.dv > 64 && sizeof(T) * D < 1024) return launch_shaped<T, D, 4, MAIN>(a, s, ev);
-    return launch_shaped<T, D, 2, MAIN>(a, s, ev);
+// MAIN: the pass; else the parts.
+template <typename T, int D, int COLUMNS, bool MAIN>
+hipError_t launch_shaped(const LinearPass& a, const LinearPass* b, hipStream_t s, const LaunchEvents& ev) {
+    constexpr int kWaves = MAIN ? kPassWaves : COLUMNS / 32;
+    using Shape = StageShape<T, D, COLUMNS, kWaves>;
+    auto blocks = [](const LinearPass& p) { return MAIN ? pass_blocks(p, COLUMNS) : part_blocks(p, COLUMNS); };
+    const PassPair pair{{a, b ? *b : a}, int(blocks(a))};
+    void (*kernel)(PassPair);
+    if constexpr (MAIN) {
+        kernel = a.wide ? linear_pass_kernel<T, D, COLUMNS, true> : linear_pass_kernel<T, D, COLUMNS, false>;
+    } else {
+        constexpr int kAll = sizeof(T) == 2 ? 3 : 1, kSome = sizeof(T) == 2 ? 2 : 1;
+        if (a.exact || (b && b->exact))
+            kernel = a.wide ? linear_parts_kernel<T, D, kWaves, true, kAll> : linear_parts_kernel<T, D, kWaves, false, kAll>;
+        else
+            kernel = a.wide ? linear_parts_kernel<T, D, kWaves, true, kSome> : linear_parts_kernel<T, D, kWaves, false, kSome>;
+    }
+    constexpr int kLds = Shape::kLds + (MAIN ? kDiagonalBytes : 0);
+    if (hipError_t e = allow_dynamic_lds(kernel, kLds)) return e;
+    return launch_kernel(kernel, dim3(unsigned(blocks(a) + (b ? blocks(*b) : 0))), dim3(64 * kWaves), kLds, s, ev.start, ev.stop,
+                         pair);
 }
 
 template <typename T, bool MAIN>
-hipError_t launch_typed(const LinearScan& a, hipStream_t s, const LaunchEvents& ev) {
-    if (a.d <= 32) return launch_columns<T, 32, MAIN>(a, s, ev);
-    if (a.d <= 64) return launch_columns<T, 64, MAIN>(a, s, ev);
-    if (a.d <= 128) return launch_columns<T, 128, MAIN>(a, s, ev);
-    return launch_columns<T, 256, MAIN>(a, s, ev);
+hipError_t launch_typed(const LinearPass& a, const LinearPass* b, hipStream_t s, const LaunchEvents& ev) {
+    const bool few = linear_columns(a.dv) == 64;
+    switch (linear_padded(a.d)) {
+        case 32: return few ? launch_shaped<T, 32, 64, MAIN>(a, b, s, ev) : launch_shaped<T, 32, 128, MAIN>(a, b, s, ev);
+        case 64: return few ? launch_shaped<T, 64, 64, MAIN>(a, b, s, ev) : launch_shaped<T, 64, 128, MAIN>(a, b, s, ev);
+        case 128: return few ? launch_shaped<T, 128, 64, MAIN>(a, b, s, ev) : launch_shaped<T, 128, 128, MAIN>(a, b, s, ev);
+        default: return few ? launch_shaped<T, 256, 64, MAIN>(a, b, s, ev) : launch_shaped<T, 256, 128, MAIN>(a, b, s, ev);
+    }
 }
 
 }  // namespace
 
-hipError_t launch_linear_scan(const LinearScan& a, int dtype, hipStream_t s, const LaunchEvents& ev) {
-    return dtype == FFTSPLIT_BF16 ? launch_typed<__bf16, true>(a, s, ev) : launch_typed<float, true>(a, s, ev);
+hipError_t launch_linear_pass(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev) {
+    return dtype == FFTSPLIT_BF16 ? launch_typed<__bf16, true>(a, b, s, ev) : launch_typed<float, true>(a, b, s, ev);
 }
 
-hipError_t launch_linear_parts(const LinearScan& a, int dtype, hipStream_t s, const LaunchEvents& ev) {
-    return dtype == FFTSPLIT_BF16 ? launch_typed<__bf16, false>(a, s, ev) : launch_typed<float, false>(a, s, ev);
+hipError_t launch_linear_parts(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev) {
+    return dtype == FFTSPLIT_BF16 ? launch_typed<__bf16, false>(a, b, s, ev) : launch_typed<float, false>(a, b, s, ev);
 }
 
-hipError_t launch_linear_join(const LinearJoin& a, hipStream_t s, const LaunchEvents& ev) {
-    const long long blocks = (long long)a.heads * ((a.elements + 255) / 256);
-    return launch_kernel(linear_join_kernel, dim3(unsigned(blocks)), dim3(256), 0, s, ev.start, ev.stop, a);
+hipError_t launch_linear_join(const LinearJoin* jobs, int count, int dtype, hipStream_t s, const LaunchEvents& ev) {
+    JoinJobs j{};
+    int blocks = 0;
+    for (int i = 0; i < 3; ++i) {
+        j.job[i] = jobs[i < count ? i : 0];
+        if (i < count) blocks += j.job[i].heads * (j.job[i].rows / 8 * j.job[i].columns / 64);
+        j.end[i] = blocks;
+    }
+    const int run = (jobs[0].segments + kJoinWaves - 1) / kJoinWaves;
+    auto kernel = dtype == FFTSPLIT_BF16
+                      ? run <= 1   ? linear_join_kernel<__bf16, 1>
+                        : run <= 2 ? linear_join_kernel<__bf16, 2>
+                                   : linear_join_kernel<__bf16, 4>
+                  : run <= 1 ? linear_join_kernel<float, 1>
+                  : run <= 2 ? linear_join_kernel<float, 2>
+                             : linear_join_kernel<float, 4>;
+    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(64 * kJoinWaves), 0, s, ev.start, ev.stop, j);
 }
 
 }  // namespace fftsplit

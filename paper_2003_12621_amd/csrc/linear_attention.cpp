@@ -56,20 +56,42 @@ size_t state_bytes(const fftsplit_linear_attention_problem_t& p) {
     return size_t(p.batch) * p.heads_k * p.dim * p.dim_v * 4;
 }
 
-// Into how many parts to cut the sequences so that the waves of `workgroups` of
-// them fill the chip.
-void choose_segments(const fftsplit_linear_attention_problem_t& p, long long waves, int& segments, int& tokens) {
-    const long long chunks = (p.tokens + kLinearChunk - 1) / kLinearChunk;
-    long long want = (1024 + waves - 1) / waves;
-    if (want > chunks / 4) want = chunks / 4;
-    if (want > kLinearMaxSegments) want = kLinearMaxSegments;
-    if (want < 1) want = 1;
-    const long long per = (chunks + want - 1) / want;
-    segments = int((chunks + per - 1) / per);
-    tokens = int(per * kLinearChunk < p.tokens ? per * kLinearChunk : p.tokens);
+// Tokens of a segment, a multiple of a workgroup's rows.  Long segments cost pairs of
+// tokens, short ones states, written and read.  Measured (us of all kernels, segments of
+// 128 / 256 / 384) where the short segments' states take up to 16 MiB: 8192 tokens of 16
+// heads (4) of 64 / 128 in bf16 48 / 53 / 68, training of 2 x 1999 tokens of 8 heads (4)
+// of 128 / 256 127 / 136 / 154; and where they take more: 4 x 16384 tokens of 16 heads
+// 465 / 407 / 398, training of 4 x 3136 tokens of 8 heads 190 / 177 / 185, of 2 x 4000
+// tokens of 16 heads (8) of 256 679 / 569.  Products of fp32 take 16 times as long as
+// those of bf16, so that pairs weigh more: training of 6 x 301 tokens 95 / 133 / 146.
+void choose_segments(const fftsplit_linear_attention_problem_t& p, int& tokens, int& segments) {
+    const double states = double(state_bytes(p)) * ((p.tokens + kLinearRows - 1) / kLinearRows);
+    tokens = p.dtype == FFTSPLIT_F32 || states <= 16 << 20 ? kLinearRows : 2 * kLinearRows;
+    segments = (p.tokens + tokens - 1) / tokens;
 }
 
-long long slices(int width) { return (width + 31) / 32; }
+// Whether a call that returns no state takes a sequence as one segment, which saves two
+// launches and the states, for pairs of all its tokens (us, in segments / in one): bf16
+// forward passes of 8 x 784 tokens of 8 heads of 64 / 128 38 / 27, of 1000 of 16 heads 21
+// / 24, of 512 20 / 16, of 4 x 300 tokens of 8 heads of 64 19 / 9; backward passes, whose
+// key heads take the pairs of all the query heads that share them, of 8 x 784 tokens 77 /
+// 63, of 256 tokens of 16 heads (4) 47 / 44, of 512 48 / 74.
+bool one_segment(const fftsplit_linear_attention_problem_t& p, bool backward) {
+    const long long pairs = (long long)p.tokens * (backward ? p.heads_q / p.heads_k : 1);
+    return pairs <= (p.dtype == FFTSPLIT_F32 ? 256 : 1024);
+}
+
+int padded32(int width) { return (width + 31) / 32 * 32; }
+
+// Bytes of the parts of the segments' states, and of the operands made of them
+// (rows padded as the passes that read them pad their widths).
+size_t parts_bytes(const fftsplit_linear_attention_problem_t& p, int segments) {
+    return round256(state_bytes(p) * size_t(segments));
+}
+size_t starts_bytes(const fftsplit_linear_attention_problem_t& p, int segments, bool turned) {
+    const size_t rows = linear_padded(turned ? p.dim_v : p.dim), columns = padded32(turned ? p.dim : p.dim_v);
+    return round256(size_t(p.batch) * p.heads_k * segments * rows * columns * type_bytes(p.dtype));
+}
 
 fftsplit_status_t build(const fftsplit_linear_attention_problem_t* prob, int device, const char* arch,
                         fftsplit_linear_attention_plan_t* out) {
@@ -107,23 +129,22 @@ fftsplit_status_t build(const fftsplit_linear_attention_problem_t* prob, int dev
     plan->device = device;
     plan->scale = p.scale > 0.f ? p.scale : float(1.0 / std::sqrt(double(p.dim)));
     plan->recurrent = p.tokens <= kLinearRecurrentTokens;
-    const long long heads_k = (long long)p.batch * p.heads_k, heads_q = (long long)p.batch * p.heads_q;
-    choose_segments(p, heads_q * slices(p.dim_v), plan->segments[0], plan->segment_tokens[0]);
-    choose_segments(p, heads_k * slices(p.dim), plan->segments[1], plan->segment_tokens[1]);
-    // (one segment of several query heads: the state that all of them start from
-    // has to stay while one of them writes the last)
-    const bool shared = p.heads_q > p.heads_k;
-    plan->forward_ws = plan->recurrent || (plan->segments[0] == 1 && !shared)
-                           ? 0 : round256(state_bytes(p) * size_t(plan->segments[0]));
-    plan->backward_ws = plan->segments[1] == 1 ? 0 : 2 * round256(state_bytes(p) * size_t(plan->segments[1]));
+    choose_segments(p, plan->segment_tokens, plan->segments);
+    plan->forward_ws = plan->recurrent ? 0 : parts_bytes(p, plan->segments) + starts_bytes(p, plan->segments, false);
+    plan->backward_ws = 2 * parts_bytes(p, plan->segments) + starts_bytes(p, plan->segments, false) +
+                        2 * starts_bytes(p, plan->segments, true);
     // workgroups of the largest launches (a dimension of a grid holds below 2^32 threads)
-    const double most = double(heads_q) * slices(p.dim > p.dim_v ? p.dim : p.dim_v) *
-                        (plan->segments[0] > plan->segments[1] ? plan->segments[0] : plan->segments[1]);
-    const double joined = double(heads_k) * ((double(p.dim) * p.dim_v + 255) / 256);
-    if (most > double(1 << 22) || joined > double(1 << 22)) {
-        delete plan;
-        return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "linear attention: too many heads over all sequences");
-    }
+    const double heads_q = double(p.batch) * p.heads_q, heads_k = double(p.batch) * p.heads_k;
+    auto slices = [](int width) { return (width + linear_columns(width) - 1) / linear_columns(width); };
+    const int wider = slices(p.dim) > slices(p.dim_v) ? slices(p.dim) : slices(p.dim_v);
+    const double groups[] = {(heads_q + heads_k) * wider * ((p.tokens + kLinearRows - 1) / kLinearRows),
+                             2 * heads_k * wider * plan->segments,
+                             6 * heads_k * (double(linear_padded(p.dim)) * linear_padded(p.dim_v) / 512)};
+    for (double g : groups)
+        if (g > double(1 << 23)) {
+            delete plan;
+            return fail(FFTSPLIT_ERROR_NOT_SUPPORTED, "linear attention: too many tokens and heads over all sequences");
+        }
     *out = plan;
     return FFTSPLIT_SUCCESS;
 }
@@ -163,24 +184,28 @@ fftsplit_status_t check_inputs(fftsplit_linear_attention_plan_t plan, const ffts
     return FFTSPLIT_SUCCESS;
 }
 
-// What all scans of a call share; the caller sets their rows, widths and factors.
-LinearScan scan_of(fftsplit_linear_attention_plan_t plan, const fftsplit_linear_attention_inputs_t* in, int pass) {
+// What all passes of a call share; the caller sets their rows, widths and factors.
+LinearPass pass_of(fftsplit_linear_attention_plan_t plan, const fftsplit_linear_attention_inputs_t* in, int wide, bool one) {
     const fftsplit_linear_attention_problem_t& p = plan->prob;
-    LinearScan a{};
+    LinearPass a{};
     a.log_decay = in->log_decay;
     a.lengths = in->lengths;
     a.n = p.batch;
     a.s = p.tokens;
     a.hk = p.heads_k;
-    a.segments = plan->segments[pass];
-    a.segment_tokens = plan->segment_tokens[pass];
+    a.segments = one ? 1 : plan->segments;
+    a.segment_tokens = one ? (p.tokens + kLinearRows - 1) / kLinearRows * kLinearRows : plan->segment_tokens;
+    a.wide = wide;
     return a;
 }
 
-LinearJoin join_of(const LinearScan& a, float* parts, const float* init, int reverse, int elements) {
+// The join of the parts of `a`, of states dim x dim_v.
+LinearJoin join_of(const LinearPass& a, int dim, int dim_v, bool turned, const float* init, void* starts, float* last) {
     LinearJoin j{};
-    j.parts = parts;
+    j.parts = a.parts;
     j.init = init;
+    j.starts = starts;
+    j.last = last;
     j.log_decay = a.log_decay;
     j.lengths = a.lengths;
     j.heads = a.n * a.hk;
@@ -188,20 +213,27 @@ LinearJoin join_of(const LinearScan& a, float* parts, const float* init, int rev
     j.s = a.s;
     j.segments = a.segments;
     j.segment_tokens = a.segment_tokens;
-    j.reverse = reverse;
-    j.elements = elements;
+    j.reverse = a.reverse;
+    j.d = dim;
+    j.dv = dim_v;
+    j.turned = turned;
+    j.rows = linear_padded(turned ? dim_v : dim);
+    j.columns = padded32(turned ? dim : dim_v);
+    j.first_part = a.first_part;
+    j.part_count = a.part_count;
     return j;
 }
 
-// The states that a scan starts its segments from: `p` [head][segment][dim][dim_v],
-// with rows along dim (or, turned, along dim_v).
-void start_from(LinearScan& a, const float* p, int segments, int dim, int dim_v, bool turned) {
-    a.init = p;
-    a.init_segment = (long long)dim * dim_v;
-    a.init_head = a.init_segment * segments;
-    a.init_row = turned ? 1 : dim_v;
-    a.init_column = turned ? dim_v : 1;
-}
+// The launches of a call: only the first records when the call begins, and only
+// the last when it ends.
+struct Launches {
+    LaunchEvents ev;
+    LaunchEvents next(bool last) {
+        const LaunchEvents e{ev.start, last ? ev.stop : nullptr};
+        ev.start = nullptr;
+        return e;
+    }
+};
 
 }  // namespace
 
@@ -231,8 +263,8 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_plan_info(fftsplit_l
         i.backward_workspace_bytes = plan->backward_ws;
         i.state_bytes = state_bytes(plan->prob);
         i.recurrent = plan->recurrent;
-        i.forward_segments = plan->recurrent ? 1 : plan->segments[0];
-        i.backward_segments = plan->segments[1];
+        i.segment_tokens = plan->segment_tokens;
+        i.segments = plan->segments;
         *out = i;
         return FFTSPLIT_SUCCESS;
     });
@@ -284,11 +316,10 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_forward(fftsplit_lin
             return launched_ok(launch_linear_tokens(a, p.dtype, stream, ev), "linear attention launch");
         }
 
-        LinearScan a = scan_of(plan, in, 0);
+        LinearPass a = pass_of(plan, in, x.wide, !state_out && one_segment(p, false));
         a.q = x.q;
         a.k = x.k;
         a.v = x.v;
-        a.wide = x.wide;
         a.o = o;
         a.o_wide = p.dim_v % 4 == 0;
         a.q_heads = p.heads_q / p.heads_k;
@@ -297,27 +328,22 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_forward(fftsplit_lin
         a.dv = p.dim_v;
         a.pair_scale = a.inter_scale = plan->scale;
         a.update_scale = 1.f;
-        a.last = state_out;
-        // the states before the segments, where they are more than one or the
-        // only one's is shared
-        const bool parts = a.segments > 1 || (a.q_heads > 1 && in->state && in->state == state_out);
-        LaunchEvents first = ev, last = ev;
-        if (parts) {
-            first.stop = last.start = nullptr;
-            LaunchEvents middle{a.segments > 1 ? nullptr : ev.start, nullptr};
-            a.parts = static_cast<float*>(workspace);
-            if (a.segments > 1)
-                if (fftsplit_status_t s = launched_ok(launch_linear_parts(a, p.dtype, stream, first), "linear attention launch"))
-                    return s;
-            if (fftsplit_status_t s = launched_ok(
-                    launch_linear_join(join_of(a, a.parts, in->state, 0, p.dim * p.dim_v), stream, middle),
-                    "linear attention launch"))
+        a.part_count = state_out ? a.segments : a.segments - 1;
+        a.exact = state_out != nullptr;
+        a.parts = static_cast<float*>(workspace);
+        auto launched = [](hipError_t e) { return launched_ok(e, "linear attention launch"); };
+        Launches launches{ev};
+        if (a.part_count)
+            if (fftsplit_status_t s = launched(launch_linear_parts(a, nullptr, p.dtype, stream, launches.next(false))))
                 return s;
-            start_from(a, a.parts, a.segments, p.dim, p.dim_v, false);
-        } else if (in->state) {
-            start_from(a, in->state, 1, p.dim, p.dim_v, false);
+        const bool before = a.segments > 1 || in->state;
+        if (before || state_out) {
+            void* starts = before ? static_cast<char*>(workspace) + parts_bytes(p, a.segments) : nullptr;
+            const LinearJoin j = join_of(a, p.dim, p.dim_v, false, in->state, starts, state_out);
+            if (fftsplit_status_t s = launched(launch_linear_join(&j, 1, p.dtype, stream, launches.next(false)))) return s;
+            a.starts = starts;
         }
-        return launched_ok(launch_linear_scan(a, p.dtype, stream, last), "linear attention launch");
+        return launched(launch_linear_pass(a, nullptr, p.dtype, stream, launches.next(true)));
     });
 }
 
@@ -356,79 +382,86 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_backward(
         if (fftsplit_status_t s = check_apart(ins, outs)) return s;
         DeviceGuard guard(plan->device);
         if (!guard.ok()) return fail(FFTSPLIT_ERROR_DEVICE, "cannot select the plan's device");
-        const LaunchEvents ev = timing_events(), none;
         auto launched = [](hipError_t e) { return launched_ok(e, "linear attention gradient launch"); };
+        Launches launches{timing_events()};
 
         // The forward pass's state, of (k, v), serves dq; its gradient, of (q,
         // dout) from the last token on, dk and dv.
         const int group = p.heads_q / p.heads_k;
-        LinearScan a = scan_of(plan, in, 1);
-        a.wide = x.wide;
-        LinearScan sq = a, sk = a, sv = a;
-        sq.q = g;                       // dq = scan(dout, v, k)
-        sq.k = x.v;
-        sq.v = x.k;
-        sq.o = dq;
-        sq.q_heads = group;
-        sq.k_heads = 1;
-        sq.pair_scale = sq.inter_scale = plan->scale;
-        sq.update_scale = 1.f;
-        sv.q = x.k;                     // dv = scan back(k, q, dout)
-        sv.k = x.q;
-        sv.v = g;
-        sv.o = dv;
-        sk.q = x.v;                     // dk = scan back(v, dout, q)
-        sk.k = g;
-        sk.v = x.q;
-        sk.o = dk;
-        for (LinearScan* s : {&sk, &sv}) {
-            s->q_heads = 1;
-            s->k_heads = group;
-            s->reverse = 1;
-            s->pair_scale = s->update_scale = plan->scale;
-            s->inter_scale = 1.f;
+        const LinearPass a = pass_of(plan, in, x.wide, !dstate && one_segment(p, true));
+        LinearPass pq = a, pk = a, pv = a;
+        pq.q = g;                       // dq: (dout, v, k)
+        pq.k = x.v;
+        pq.v = x.k;
+        pq.o = dq;
+        pq.q_heads = group;
+        pq.k_heads = 1;
+        pq.pair_scale = pq.inter_scale = plan->scale;
+        pv.q = x.k;                     // dv: back (k, q, dout)
+        pv.k = x.q;
+        pv.v = g;
+        pv.o = dv;
+        pk.q = x.v;                     // dk: back (v, dout, q)
+        pk.k = g;
+        pk.v = x.q;
+        pk.o = dk;
+        for (LinearPass* b : {&pk, &pv}) {
+            b->q_heads = 1;
+            b->k_heads = group;
+            b->reverse = 1;
+            b->pair_scale = plan->scale;
+            b->inter_scale = 1.f;
         }
-        sv.d = p.dim;
-        sv.dv = p.dim_v;
-        sq.d = sk.d = p.dim_v;
-        sq.dv = sk.dv = p.dim;
-        sv.o_wide = p.dim_v % 4 == 0;
-        sq.o_wide = sk.o_wide = p.dim % 4 == 0;
-        sv.last = dstate;
+        pv.d = p.dim;
+        pv.dv = p.dim_v;
+        pq.d = pk.d = p.dim_v;
+        pq.dv = pk.dv = p.dim;
+        pv.o_wide = p.dim_v % 4 == 0;
+        pq.o_wide = pk.o_wide = p.dim % 4 == 0;
+
         const int segments = a.segments;
-        if (segments > 1) {
-            float* forward = static_cast<float*>(workspace);
-            float* backward = forward + plan->backward_ws / 8;
-            LinearScan pf = sv;          // the state's own parts: of (k, v), d x dv
-            pf.q = LinearRows{};
-            pf.k = x.k;
-            pf.v = x.v;
-            pf.k_heads = 1;
-            pf.reverse = 0;
-            pf.update_scale = 1.f;
-            pf.parts = forward;
-            if (fftsplit_status_t s = launched(launch_linear_parts(pf, p.dtype, stream, LaunchEvents{ev.start, nullptr}))) return s;
-            LinearScan pb = sv;
-            pb.parts = backward;
-            if (fftsplit_status_t s = launched(launch_linear_parts(pb, p.dtype, stream, none))) return s;
-            if (fftsplit_status_t s = launched(launch_linear_join(join_of(a, forward, in->state, 0, p.dim * p.dim_v), stream, none)))
+        char* ws = static_cast<char*>(workspace);
+        LinearPass state = a, gradient = pv;      // what adds to the state, and to its gradient
+        state.k = x.k;
+        state.v = x.v;
+        state.k_heads = 1;
+        state.d = p.dim;
+        state.dv = p.dim_v;
+        state.update_scale = 1.f;
+        state.parts = reinterpret_cast<float*>(ws);
+        state.part_count = segments - 1;
+        gradient.update_scale = plan->scale;
+        gradient.parts = reinterpret_cast<float*>(ws + parts_bytes(p, segments));
+        gradient.first_part = dstate ? 0 : 1;
+        gradient.part_count = segments - gradient.first_part;
+        gradient.exact = dstate != nullptr;
+        ws += 2 * parts_bytes(p, segments);
+        if (state.part_count) {
+            if (fftsplit_status_t s = launched(launch_linear_parts(state, &gradient, p.dtype, stream, launches.next(false))))
                 return s;
-            if (fftsplit_status_t s = launched(launch_linear_join(join_of(a, backward, dstate_out, 1, p.dim * p.dim_v), stream, none)))
+        } else if (gradient.part_count) {
+            if (fftsplit_status_t s = launched(launch_linear_parts(gradient, nullptr, p.dtype, stream, launches.next(false))))
                 return s;
-            start_from(sq, forward, segments, p.dim, p.dim_v, true);
-            start_from(sk, backward, segments, p.dim, p.dim_v, true);
-            start_from(sv, backward, segments, p.dim, p.dim_v, false);
-        } else {
-            if (in->state) start_from(sq, in->state, 1, p.dim, p.dim_v, true);
-            if (dstate_out) {
-                start_from(sk, dstate_out, 1, p.dim, p.dim_v, true);
-                start_from(sv, dstate_out, 1, p.dim, p.dim_v, false);
-            }
         }
-        if (fftsplit_status_t s =
-                launched(launch_linear_scan(sq, p.dtype, stream, LaunchEvents{segments > 1 ? nullptr : ev.start, nullptr})))
-            return s;
-        if (fftsplit_status_t s = launched(launch_linear_scan(sk, p.dtype, stream, none))) return s;
-        return launched(launch_linear_scan(sv, p.dtype, stream, LaunchEvents{nullptr, ev.stop}));
+        LinearJoin jobs[3];
+        int count = 0;
+        if (segments > 1 || in->state) {
+            jobs[count++] = join_of(state, p.dim, p.dim_v, true, in->state, ws, nullptr);
+            pq.starts = ws;
+        }
+        ws += starts_bytes(p, segments, true);
+        if (segments > 1 || dstate_out) {
+            jobs[count++] = join_of(gradient, p.dim, p.dim_v, true, dstate_out, ws, nullptr);
+            pk.starts = ws;
+            pv.starts = ws + starts_bytes(p, segments, true);
+        }
+        ws += starts_bytes(p, segments, true);
+        if (pv.starts || dstate)
+            jobs[count++] = join_of(gradient, p.dim, p.dim_v, false, dstate_out, const_cast<void*>(pv.starts), dstate);
+        if (count)
+            if (fftsplit_status_t s = launched(launch_linear_join(jobs, count, p.dtype, stream, launches.next(false))))
+                return s;
+        if (fftsplit_status_t s = launched(launch_linear_pass(pq, &pk, p.dtype, stream, launches.next(false)))) return s;
+        return launched(launch_linear_pass(pv, nullptr, p.dtype, stream, launches.next(true)));
     });
 }

@@ -7,11 +7,31 @@
 
 namespace fftsplit {
 
+// A value that is the same in all lanes, in a scalar register: quotients come from
+// vector instructions, and what is derived from them would stay in vector ones,
+// branches included.
+__device__ __forceinline__ int linear_scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float linear_scalar(float x) {
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
+}
+
+// A value at an address that is the same in all lanes, which no kernel writes while
+// this one runs: by a scalar load.
+template <typename V>
+__device__ __forceinline__ V linear_uniform(const V* p) {
+    return *(const __attribute__((address_space(4))) V*)(p);
+}
+
 // Tokens of sequence b that exist.
 __device__ __forceinline__ int linear_length(const int* lengths, int s, int b) {
     if (!lengths) return s;
-    const int l = lengths[b];
+    const int l = linear_scalar(linear_uniform(lengths + b));
     return l < 0 ? 0 : (l > s ? s : l);
+}
+
+// Steps of 16 along a row that the kernels pad its width to.
+__device__ __forceinline__ int linear_steps(int width) {
+    return width <= 32 ? 2 : width <= 64 ? 4 : width <= 128 ? 8 : 16;
 }
 
 // log2 of a head's decay.  Values above 0 are taken as 0; below -10^4 nothing is

@@ -8,9 +8,9 @@ struct fftsplit_linear_attention_plan_s {
     int device;              // HIP ordinal, or -1 for an architecture-only plan
     float scale;
     int recurrent;           // the forward pass goes token by token
-    // Parts of a sequence that workgroups take side by side (1: each goes over
-    // all of it), and their tokens, in the forward and in the backward pass.
-    int segments[2], segment_tokens[2];
+    // Tokens of a segment, within which pairs of tokens are taken one by one
+    // and which only a state carries over, and how many make up a sequence.
+    int segment_tokens, segments;
     size_t forward_ws, backward_ws;
 };
 
@@ -18,10 +18,9 @@ namespace fftsplit {
 
 // Widths of a head (rows of a state) the kernels are compiled for.
 constexpr int kLinearMaxDim = 256;
-// Tokens of a chunk: one 32 x 32 tile of scores.
-constexpr int kLinearChunk = 32;
-constexpr int kLinearMaxSegments = 64;
-// A chunk's rows are addressed with 32-bit offsets from its first.
+// Tokens of a tile, and query rows of a workgroup (four waves' tiles).
+constexpr int kLinearTile = 32, kLinearRows = 128;
+// A tile's rows are addressed with 32-bit offsets from its first.
 constexpr long long kLinearMaxTokenStride = 1 << 22;
 
 // Tokens up to which the forward pass goes token by token.
@@ -33,41 +32,45 @@ struct LinearRows {
     long long b, t, h;
 };
 
-// One scan over the tokens, which the forward pass and each gradient are:
+// One sum over the tokens, which the forward pass and each gradient are:
 //   out_i = sum over the j up to i of decay^|i - j| pair_scale (q_i . k_j) v_j
 //           + inter_scale q_i^T S,
-//   S     = the state before i, of the terms update_scale k_j v_j^T.
-// Forwards j is up to i from the first token on; backwards from the last, and
-// the state is one step of decay behind (it holds the gradient that the tokens
-// behind i gave to the state after i).
-struct LinearScan {
+//   S     = the state before i's segment, times decay to the distance.
+// Forwards j is up to i from the segment's first token on; backwards from its
+// last, and the state is one step of decay behind (it holds the gradient that the
+// tokens behind the segment gave to the state after it).
+struct LinearPass {
     LinearRows q, k, v;
     void* o;                         // [n][s][hk q_heads][dv], dense
     int q_heads, k_heads;            // of either, those that share a key head; one of them is 1
     int d, dv;                       // widths of q and k, and of v
     int reverse;
     float pair_scale, update_scale, inter_scale;
-    // State at the start of a segment, and after the last: of head g (over all
-    // sequences) and segment m element (row, column) is
-    //   g * head + m * segment + row * row_step + column * column_step.
-    const float* init;               // or null: zero
-    long long init_head, init_segment, init_row, init_column;
-    float* last;                     // [n hk][d][dv], or null
-    float* parts;                    // of the kernel that only computes states: [n hk][segments][d][dv]
+    const void* starts;              // operands of the states before the segments, or null: zero
+    float* parts;                    // what each segment adds to the state: [n hk][segments][d][dv]
     const float* log_decay;
     const int* lengths;
     int n, s, hk, segments, segment_tokens;
+    int first_part, part_count;      // the segments whose parts are needed
+    int exact;                       // the caller gets the state, in fp32
     int wide, o_wide;
 };
 
-// States at the start of the segments from what each segment adds.
+// The state before each segment from the parts, as the operand of the product
+// with a tile of queries: [head][segment][column / 32][row / 16][lane][8], lane =
+// 32 (row / 8 % 2) + column % 32, in the tensors' type; rows are those of the
+// state, columns its columns, or (turned) the other way round.
 struct LinearJoin {
-    float* parts;                    // [heads][segments][elements], in place
-    const float* init;               // [heads][elements] or null
+    const float* parts;              // [heads][segments][d][dv]
+    const float* init;               // [heads][d][dv] or null
+    void* starts;                    // or null
+    float* last;                     // [heads][d][dv]: the state behind the last segment, or null
     const float* log_decay;
     const int* lengths;
     int heads, hk, s, segments, segment_tokens, reverse;
-    int elements;
+    int d, dv, turned;
+    int rows, columns;               // of the operands, rounded up to whole tiles
+    int first_part, part_count;
 };
 
 struct LinearTokens {
@@ -82,9 +85,14 @@ struct LinearTokens {
     int state_wide;
 };
 
-hipError_t launch_linear_scan(const LinearScan& a, int dtype, hipStream_t s, const LaunchEvents& ev);
-hipError_t launch_linear_parts(const LinearScan& a, int dtype, hipStream_t s, const LaunchEvents& ev);
-hipError_t launch_linear_join(const LinearJoin& a, hipStream_t s, const LaunchEvents& ev);
+// Widths that the kernels pad a pass's rows and a workgroup's columns to.
+inline int linear_padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 128 ? 128 : 256; }
+inline int linear_columns(int width) { return width <= 64 ? 64 : 128; }
+
+// Two passes of the same widths in one launch, or one (b null).
+hipError_t launch_linear_pass(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev);
+hipError_t launch_linear_parts(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev);
+hipError_t launch_linear_join(const LinearJoin* jobs, int count, int dtype, hipStream_t s, const LaunchEvents& ev);
 hipError_t launch_linear_tokens(const LinearTokens& a, int dtype, hipStream_t s, const LaunchEvents& ev);
 
 }  // namespace fftsplit

@@ -28,8 +28,8 @@ class LinearAttentionProblem(ctypes.Structure):
 
 class LinearAttentionInfo(ctypes.Structure):
     _fields_ = [("forward_workspace_bytes", ctypes.c_size_t), ("backward_workspace_bytes", ctypes.c_size_t),
-                ("state_bytes", ctypes.c_size_t), ("recurrent", ctypes.c_int), ("forward_segments", ctypes.c_int),
-                ("backward_segments", ctypes.c_int)]
+                ("state_bytes", ctypes.c_size_t), ("recurrent", ctypes.c_int), ("segment_tokens", ctypes.c_int),
+                ("segments", ctypes.c_int)]
 
 
 class LinearAttentionInputs(ctypes.Structure):

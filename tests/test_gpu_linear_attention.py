@@ -107,6 +107,21 @@ def test_widths(s, d, dv, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("s", [5, 130, 256, 257, 1000, 1024, 1025])
+@pytest.mark.parametrize("state", [False, True])
+def test_no_state_returned(s, state, dtype):
+    """Calls that return no state may take the whole sequence at once."""
+    x = make(s, 2, s, 2, 2, 40, 32, dtype, state=state, ragged=True)
+    q, k, v, do, log_decay, st, _, lengths = x
+    x = (*x[:6], None, lengths)
+    plan = fs.LinearAttention(2, s, 2, 2, 40, 32, dtype=DTYPE[dtype])
+    o = plan.forward(q, k, v, log_decay, state=st, lengths=lengths)
+    grads = plan.backward(do, q, k, v, log_decay, state=st, lengths=lengths)
+    torch.cuda.synchronize()
+    check(plan, (o, None, *grads[:3], grads[3]), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("hq,hk", [(1, 1), (3, 3), (8, 1), (10, 2), (12, 3)])
 @pytest.mark.parametrize("s", [4, 75])
 def test_heads(s, hq, hk, dtype):
@@ -150,7 +165,7 @@ def test_long_sequences_in_segments(dtype):
     n, s, hq, hk, d, dv = 4, 1500, 2, 1, 32, 64
     x = make(1, n, s, hq, hk, d, dv, dtype)
     plan = fs.LinearAttention(n, s, hq, hk, d, dv, dtype=DTYPE[dtype])
-    assert plan.info.forward_segments > 2 and plan.info.backward_segments > 2
+    assert plan.info.segments > 1
     # heads that remember over many parts
     x[4][:] = -0.002
     lengths = torch.tensor([s, s // 2, 33, 1], dtype=torch.int32, device="cuda")

@@ -75,21 +75,19 @@ def test_arch_only_plan_cannot_run():
 
 
 def test_plan_choices():
-    """Few tokens go one by one and need no workspace; few heads of long
-    sequences are cut into parts, whose states the workspace holds."""
+    """Few tokens go one by one and need no workspace; longer sequences are cut
+    into segments, whose states the workspace holds."""
     one = plan(tokens=1)
     assert one.info.recurrent == 1 and one.info.forward_workspace_bytes == 0
     assert one.info.state_bytes == 2 * 2 * 64 * 128 * 4
     long = plan(batch=1, tokens=8192)
-    assert long.info.recurrent == 0 and long.info.forward_segments > 8
-    assert long.info.forward_workspace_bytes >= long.info.forward_segments * long.info.state_bytes
-    assert long.info.backward_workspace_bytes >= 2 * long.info.backward_segments * long.info.state_bytes
-    many = plan(batch=256, heads_q=8, heads_k=8, tokens=1000)
-    assert many.info.forward_segments == 1 and many.info.backward_segments == 1
-    assert many.info.forward_workspace_bytes == 0 and many.info.backward_workspace_bytes == 0
+    assert long.info.recurrent == 0 and long.info.segments > 8
+    assert long.info.forward_workspace_bytes >= long.info.segments * long.info.state_bytes
+    assert long.info.backward_workspace_bytes >= 2 * long.info.segments * long.info.state_bytes
     for tokens in (9, 33, 1000, 12345, 1 << 20, 1 << 28):
-        info = plan(batch=1, heads_q=1, heads_k=1, tokens=tokens).info
-        assert 1 <= info.forward_segments <= 64 and 1 <= info.backward_segments <= 64
+        for dtype in (torch.float32, torch.bfloat16):
+            info = plan(batch=1, heads_q=1, heads_k=1, tokens=tokens, dtype=dtype).info
+            assert info.segment_tokens % 128 == 0 and info.segments == -(-tokens // info.segment_tokens)
 
 
 def rotary(**kw):
