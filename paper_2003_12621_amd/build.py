@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libfftsplit.so")
 SOURCES = ["plan.cpp", "api.cpp", "k_weights.hip", "k_forward.hip", "k_contract.hip", "k_contract_split.hip", "k_inverse.hip", "k_pool.hip",
            "k_direct.hip", "k_oaa.hip", "noalloc.hip", "k_probe.hip", "attention.cpp", "k_attn_forward.hip",
            "k_attn_backward.hip", "block_ops.cpp", "k_norm.hip", "k_rotary.hip",
-           "linear_attention.cpp", "k_linear.hip", "k_linear_tokens.hip", "k_head_norm.hip"]
+           "linear_attention.cpp", "k_linear.hip", "k_linear_gradients.hip", "k_linear_tokens.hip",
+           "k_head_norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -137,7 +137,7 @@ fftsplit_status_t build(const fftsplit_linear_attention_problem_t* prob, int dev
     const double heads_q = double(p.batch) * p.heads_q, heads_k = double(p.batch) * p.heads_k;
     auto slices = [](int width) { return (width + linear_columns(width) - 1) / linear_columns(width); };
     const int wider = slices(p.dim) > slices(p.dim_v) ? slices(p.dim) : slices(p.dim_v);
-    const double groups[] = {(heads_q + heads_k) * wider * ((p.tokens + kLinearRows - 1) / kLinearRows),
+    const double groups[] = {(heads_q + 2 * heads_k) * wider * ((p.tokens + kLinearRows - 1) / kLinearRows),
                              2 * heads_k * wider * plan->segments,
                              6 * heads_k * (double(linear_padded(p.dim)) * linear_padded(p.dim_v) / 512)};
     for (double g : groups)
@@ -461,6 +461,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_backward(
         if (count)
             if (fftsplit_status_t s = launched(launch_linear_join(jobs, count, p.dtype, stream, launches.next(false))))
                 return s;
+        if (x.wide) return launched(launch_linear_gradients(pq, pk, pv, p.dtype, stream, launches.next(true)));
         if (fftsplit_status_t s = launched(launch_linear_pass(pq, &pk, p.dtype, stream, launches.next(false)))) return s;
         return launched(launch_linear_pass(pv, nullptr, p.dtype, stream, launches.next(true)));
     });

@@ -86,11 +86,14 @@ struct LinearTokens {
 };
 
 // Widths that the kernels pad a pass's rows and a workgroup's columns to.
-inline int linear_padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 128 ? 128 : 256; }
-inline int linear_columns(int width) { return width <= 64 ? 64 : 128; }
+constexpr int linear_padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 128 ? 128 : 256; }
+constexpr int linear_columns(int width) { return width <= 64 ? 64 : 128; }
 
 // Two passes of the same widths in one launch, or one (b null).
 hipError_t launch_linear_pass(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev);
+// The three passes of the gradients, of aligned tensors, in one launch.
+hipError_t launch_linear_gradients(const LinearPass& dq, const LinearPass& dk, const LinearPass& dv, int dtype, hipStream_t s,
+                                   const LaunchEvents& ev);
 hipError_t launch_linear_parts(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev);
 hipError_t launch_linear_join(const LinearJoin* jobs, int count, int dtype, hipStream_t s, const LaunchEvents& ev);
 hipError_t launch_linear_tokens(const LinearTokens& a, int dtype, hipStream_t s, const LaunchEvents& ev);
