@@ -122,6 +122,14 @@ def test_no_state_returned(s, state, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("s,hq,d,dv", [(8, 12, 256, 70), (3, 60, 256, 8), (2, 100, 250, 5), (8, 40, 33, 64)])
+def test_many_query_heads_of_few_tokens(s, hq, d, dv, dtype):
+    """Rows of all tokens, or of all heads of one, that do not fit together."""
+    x = make(hq, 2, s, hq, 1, d, dv, dtype, ragged=True)
+    check(*both(*x), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("hq,hk", [(1, 1), (3, 3), (8, 1), (10, 2), (12, 3)])
 @pytest.mark.parametrize("s", [4, 75])
 def test_heads(s, hq, hk, dtype):
