@@ -349,7 +349,9 @@ fftsplit_status_t check_head_norm(const fftsplit_head_norm_t* d, HeadNormArgs& a
     a.eps = d->eps;
     a.access = 16 / type_bytes(d->rotary.dtype);
     const long long groups = ((long long)a.r.n * a.r.s + a.r.block_tokens - 1) / a.r.block_tokens;
-    a.blocks = int(groups < kHeadNormBlocks ? groups : kHeadNormBlocks);
+    // (each with the same number of token groups, or one less)
+    const long long rounds = (groups + kHeadNormBlocks - 1) / kHeadNormBlocks;
+    a.blocks = int((groups + rounds - 1) / rounds);
     return FFTSPLIT_SUCCESS;
 }
 

@@ -10,7 +10,7 @@
 // head: each takes two accesses' worth of elements that are turned into one
 // another (or two neighbouring ones), so that the sums over the head are the
 // only exchange, and a lane's elements are the same ones of every head, so that
-// the weights and their gradient stay in registers.  As in the rotation alone a
+// the weights' gradient stays in registers.  As in the rotation alone a
 // workgroup computes its tokens' sines and cosines once for all heads.
 #include "head_norm.hpp"
 #include "launch_util.hpp"
@@ -47,14 +47,23 @@ __device__ __forceinline__ Piece piece_of(const RotaryArgs& a, int i) {
 }
 
 template <typename T, int N>
-__device__ __forceinline__ void load_piece(float (&u)[N], const T* p, bool there) {
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p, bool there) {
     Pack<T, N> x;
 #pragma unroll
     for (int j = 0; j < N; ++j) x.v[j] = T(0.f);
     if (there) x = *reinterpret_cast<const Pack<T, N>*>(p);
+    return x;
+}
+template <typename T, int N>
+__device__ __forceinline__ void widen(float (&u)[N], const Pack<T, N>& x) {
 #pragma unroll
     for (int j = 0; j < N; ++j) u[j] = float(x.v[j]);
 }
+// A piece of x and (backwards) of dy, as they are in memory.
+template <typename T, int N>
+struct Loaded {
+    Pack<T, N> u, v, gu, gv;
+};
 template <typename T, int N>
 __device__ __forceinline__ void store_piece(T* p, const float (&u)[N], bool there) {
     Pack<T, N> x;
@@ -92,12 +101,13 @@ __device__ __forceinline__ float head_sum(float x, int lanes) {
 }
 
 // The angles of the tokens from token0 on, into LDS.
-__device__ __forceinline__ void fill_turns(const RotaryArgs& a, float2* turns, int token0, int tokens) {
+__device__ __forceinline__ void fill_turns(const HeadNormArgs& args, float2* turns, int token0, int tokens) {
+    const RotaryArgs& a = args.r;
     for (int i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
-        const int pair = i % a.pairs, t = token0 + i / a.pairs;
+        const int row = args.by_pairs.quotient(i), pair = i - row * a.pairs, t = token0 + row;
         int axis = 0;
         while (axis + 1 < a.axes && pair >= a.section_end[axis]) ++axis;
-        const int b = t / a.s;
+        const int b = args.by_s.quotient(t);
         turns[i] = turn(a.positions[b * a.pos_batch + (long long)(t - b * a.s) * a.axes + axis], a.freqs[pair]);
     }
 }
@@ -108,7 +118,7 @@ __device__ __forceinline__ void fill_turns(const RotaryArgs& a, float2* turns, i
 // are so wide that 64 lanes take several pieces each, and read them again after
 // the sums.  BACK: the gradients.
 template <typename T, int N, bool INTERLEAVED, bool ONE, bool BACK>
-__global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
+__global__ __launch_bounds__(kThreads, BACK ? 4 : 6) void head_norm_kernel(HeadNormArgs a) {
     extern __shared__ float2 turns[];
     const RotaryArgs& r = a.r;
     const int lanes = a.row_lanes, part = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes;
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
     if constexpr (BACK && !ONE) {
         for (int i = threadIdx.x; i < 2 * groups * r.d; i += kThreads) sums[i] = 0.f;
     }
-    float w0[2][N], w1[2][N], d0[2][N], d1[2][N];
+    float d0[2][N], d1[2][N];
     const Piece own = piece_of<N, INTERLEAVED>(r, part);
     auto load_weight = [&](float (&u)[N], float (&v)[N], int which, const Piece& p) {
 #pragma unroll
@@ -128,42 +138,97 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
             v[j] = p.second && a.weight[which] ? a.weight[which][p.e1 + j] : 1.f;
         }
     };
+    // The weights stay in LDS, [2][d] behind the angles: in registers they cost waves
+    // (4 x 16384 tokens of 32 + 8 heads of 64 in bf16 133 us, so 123; backwards of 4 x
+    // 3136 tokens of 8 + 8 heads three waves a SIMD and 31 us, so four and 24).
+    float* weights = reinterpret_cast<float*>(turns + r.block_tokens * r.pairs);
+    auto kept_weight = [&](float (&u)[N], float (&v)[N], int which) {
+        const auto x = *reinterpret_cast<const Pack<float, N>*>(weights + which * r.d + (own.first ? own.e0 : 0));
+        const auto y = *reinterpret_cast<const Pack<float, N>*>(weights + which * r.d + (own.second ? own.e1 : 0));
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            u[j] = x.v[j];
+            v[j] = y.v[j];
+        }
+    };
+    if constexpr (ONE) {
+        for (int i = threadIdx.x; i < 2 * r.d; i += kThreads) {
+            const int which = i >= r.d;
+            weights[i] = r.heads[which] && a.weight[which] ? a.weight[which][i - which * r.d] : 1.f;
+        }
+    }
     if constexpr (ONE) {
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            if (r.heads[which]) load_weight(w0[which], w1[which], which, own);
 #pragma unroll
             for (int j = 0; j < N; ++j) d0[which][j] = d1[which][j] = 0.f;
         }
     }
     for (int tg = blockIdx.x; tg < token_groups; tg += gridDim.x) {
         const int token0 = tg * r.block_tokens, tokens = min(r.block_tokens, all - token0);
+        // the rows of unit i of a tensor: x, dy (forwards x again) and the output
+        struct Unit {
+            const T *x, *in;
+            T* out;
+            int token;
+        };
+        auto unit = [&](int which, int i) {
+            const int heads = r.heads[which], tok = a.by_heads[which].quotient(i), head = i - tok * heads, t = token0 + tok;
+            const int b = a.by_s.quotient(t), pos = t - b * r.s;
+            Unit w;
+            w.token = tok;
+            w.in = static_cast<const T*>(r.x[which]) + b * r.xs[which][0] + pos * r.xs[which][1] + head * r.xs[which][2];
+            w.out = static_cast<T*>(r.y[which]) + b * r.ys[which][0] + pos * r.ys[which][1] + head * r.ys[which][2];
+            w.x = w.in;
+            if constexpr (BACK)
+                w.x = static_cast<const T*>(a.x[which]) + b * a.xs[which][0] + pos * a.xs[which][1] + head * a.xs[which][2];
+            return w;
+        };
+        auto fetch = [&](Loaded<T, N>& x, const Unit& w, const Piece& p) {
+            x.u = load_pack<T, N>(w.x + p.e0, p.first);
+            x.v = load_pack<T, N>(w.x + p.e1, p.second);
+            if constexpr (BACK) {
+                x.gu = load_pack<T, N>(w.in + p.e0, p.first);
+                x.gv = load_pack<T, N>(w.in + p.e1, p.second);
+            }
+        };
+        // The first rows are on their way while the angles are computed, the next ones
+        // while one is worked on: 150 -> 133 us of the former.  (Backwards, with twice the
+        // rows, it costs a wave: 31 -> 40 us of the latter.)
+        Loaded<T, N> loaded[2];
+        if constexpr (ONE && !BACK) {
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+                if (r.heads[which]) fetch(loaded[which], unit(which, min(group, tokens * r.heads[which] - 1)), own);
+        }
         if (BACK) __syncthreads();                   // (the last round's angles are no longer read)
-        fill_turns(r, turns, token0, tokens);
+        fill_turns(a, turns, token0, tokens);
         __syncthreads();
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const int heads = r.heads[which];
-            for (int i = group; i < tokens * heads; i += groups) {
-                const int tok = i / heads, head = i - tok * heads, t = token0 + tok, b = t / r.s, pos = t - b * r.s;
-                const T* in = static_cast<const T*>(r.x[which]) + b * r.xs[which][0] + pos * r.xs[which][1] +
-                              head * r.xs[which][2];
-                T* out = static_cast<T*>(r.y[which]) + b * r.ys[which][0] + pos * r.ys[which][1] + head * r.ys[which][2];
-                const T* x = in;
-                if constexpr (BACK)
-                    x = static_cast<const T*>(a.x[which]) + b * a.xs[which][0] + pos * a.xs[which][1] +
-                        head * a.xs[which][2];
-                const float2* cs = turns + tok * r.pairs;
+            const int count = tokens * r.heads[which];
+            for (int first = 0; first < count; first += groups) {
+                const int i = first + group;
+                const Unit w = unit(which, min(i, count - 1));
+                T* out = w.out;
+                const float2* cs = turns + w.token * r.pairs;
+                Loaded<T, N> x;
+                if constexpr (ONE && !BACK) {
+                    x = loaded[which];
+                    if (first + groups < count) fetch(loaded[which], unit(which, min(i + groups, count - 1)), own);
+                }
+                if (i >= count) continue;
                 float u[N], v[N], gu[N], gv[N];
                 float square = 0.f, cross = 0.f;
                 // one piece: its part of the sums over the head.  Backwards gu, gv
                 // are the gradients behind the rotation.
                 auto take = [&](const Piece& p, const float (&wu)[N], const float (&wv)[N]) {
-                    load_piece<T, N>(u, x + p.e0, p.first);
-                    load_piece<T, N>(v, x + p.e1, p.second);
+                    if constexpr (!ONE || BACK) fetch(x, w, p);
+                    widen(u, x.u);
+                    widen(v, x.v);
                     if constexpr (BACK) {
-                        load_piece<T, N>(gu, in + p.e0, p.first);
-                        load_piece<T, N>(gv, in + p.e1, p.second);
+                        widen(gu, x.gu);
+                        widen(gv, x.gv);
                         turn_piece<N, INTERLEAVED, true>(gu, gv, p, cs);
                     }
 #pragma unroll
@@ -197,9 +262,12 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
                     if constexpr (BACK) mean = head_sum(cross, lanes) * rstd / float(r.d);
                 };
                 if constexpr (ONE) {
-                    take(own, w0[which], w1[which]);
+                    float wu[N], wv[N];
+                    if constexpr (BACK) kept_weight(wu, wv, which);
+                    take(own, wu, wv);
                     statistics();
-                    give(own, w0[which], w1[which], d0[which], d1[which]);
+                    if constexpr (!BACK) kept_weight(wu, wv, which);
+                    give(own, wu, wv, d0[which], d1[which]);
                 } else {
                     float wu[N], wv[N];
                     for (int k = part;; k += lanes) {
@@ -246,10 +314,26 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs a) {
                 }
                 __syncthreads();
             }
-            for (int i = threadIdx.x; i < r.d; i += kThreads) {
+            // (slices of the groups side by side, where there are threads for them)
+            float* partial = sums + (ONE ? 1 : 2) * groups * r.d;
+            const int slices = kThreads / r.d > 1 ? kThreads / r.d : 1;
+            const int slice = slices > 1 ? int(threadIdx.x) / r.d : 0;
+            for (int i = threadIdx.x - slice * r.d; i < r.d && slice < slices; i += kThreads) {
                 float sum = 0.f;
-                for (int g = 0; g < groups; ++g) sum += from[g * r.d + i];
-                a.part[(size_t(blockIdx.x) * 2 + which) * r.d + i] = sum;
+#pragma unroll 8
+                for (int g = slice; g < groups; g += slices) sum += from[g * r.d + i];
+                if (slices == 1)
+                    a.part[(size_t(blockIdx.x) * 2 + which) * r.d + i] = sum;
+                else
+                    partial[threadIdx.x] = sum;
+            }
+            if (slices > 1) {
+                __syncthreads();
+                if (int(threadIdx.x) < r.d) {
+                    float sum = 0.f;
+                    for (int g = 0; g < slices; ++g) sum += partial[g * r.d + threadIdx.x];
+                    a.part[(size_t(blockIdx.x) * 2 + which) * r.d + threadIdx.x] = sum;
+                }
             }
         }
     }
@@ -291,11 +375,17 @@ hipError_t launch_pieces(const HeadNormArgs& a, hipStream_t s, const LaunchEvent
     const bool one = a.row_lanes > 0;
     HeadNormArgs b = a;
     if (!one) b.row_lanes = 64;
-    auto kernel = r.interleaved ? (one ? head_norm_kernel<T, N, true, true, BACK> : head_norm_kernel<T, N, true, false, BACK>)
-                                : (one ? head_norm_kernel<T, N, false, true, BACK> : head_norm_kernel<T, N, false, false, BACK>);
+    for (int i = 0; i < 2; ++i) b.by_heads[i] = fast_div(r.heads[i]);
+    b.by_s = fast_div(r.s);
+    b.by_pairs = fast_div(r.pairs);
+    auto kernel = r.interleaved
+                      ? (one ? head_norm_kernel<T, N, true, true, BACK> : head_norm_kernel<T, N, true, false, BACK>)
+                      : (one ? head_norm_kernel<T, N, false, true, BACK> : head_norm_kernel<T, N, false, false, BACK>);
     const long long token_groups = ((long long)r.n * r.s + r.block_tokens - 1) / r.block_tokens;
     const int turns = r.block_tokens * r.pairs * 8, sums = BACK ? kThreads / b.row_lanes * r.d * 4 : 0;
-    const int lds = one ? (turns > sums ? turns : sums) : turns + 2 * sums;
+    const int partial = BACK ? kThreads * 4 : 0;
+    const int angles = turns + 2 * r.d * 4;
+    const int lds = one ? (angles > sums + partial ? angles : sums + partial) : turns + 2 * sums + partial;
     if (hipError_t e = allow_dynamic_lds(kernel, lds)) return e;
     return launch_kernel(kernel, dim3(unsigned(BACK ? a.blocks : token_groups)), dim3(kThreads), unsigned(lds), s, ev.start,
                          ev.stop, b);
