@@ -172,15 +172,13 @@ struct JoinJobs {
     int end[3];                      // workgroups up to and including each
 };
 
-// A lane: 8 rows of one column of the operands.  The segments are taken kJoinWaves * RUN
-// at a time, a run of RUN of them to a wave, whose loads are in flight together; each
-// wave adds up its own run, reads the other waves' sums for the state before it, and
-// goes through its run once more.  The order is that of the segments, whatever the
-// timing.  VEC: the 8 rows lie side by side in a state.
-constexpr int kJoinWaves = 8;
-
-template <typename T, int RUN, bool VEC>
-__device__ __forceinline__ void linear_join(const LinearJoin& a, int block, float (&sums)[kJoinWaves][8][64]) {
+// A lane: 8 rows of one column of the operands.  The segments are taken WAVES * RUN at a
+// time, a run of RUN of them to a wave, whose loads are in flight together; each wave
+// adds up its own run, reads the other waves' sums for the state before it, and goes
+// through its run once more.  The order is that of the segments, whatever the timing.
+// VEC: the 8 rows lie side by side in a state.
+template <typename T, int WAVES, int RUN, bool VEC>
+__device__ __forceinline__ void linear_join(const LinearJoin& a, int block, float (&sums)[WAVES][8][64]) {
     const int items = a.rows / 8 * a.columns, per = items / 64;
     const int head = block / per, lane = threadIdx.x & 63, item = block % per * 64 + lane;
     const int wave = linear_scalar(int(threadIdx.x >> 6));
@@ -231,7 +229,7 @@ __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, floa
     keep(state, a.init != nullptr);
     const float* parts = a.parts + size_t(head) * a.segments * elements;
     Operand<T>* starts = static_cast<Operand<T>*>(a.starts) + (size_t(head) * a.segments * items + item);
-    for (int m0 = 0; m0 < a.segments; m0 += RUN * kJoinWaves) {
+    for (int m0 = 0; m0 < a.segments; m0 += RUN * WAVES) {
         // the run of any wave in this turn
         auto first_of = [&](int w) { return min(m0 + w * RUN, a.segments); };
         const int first = first_of(wave), count = first_of(wave + 1) - first;
@@ -256,7 +254,7 @@ __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, floa
         float next[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) next[j] = state[j];
-        for (int w = 0; w < kJoinWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const int f = first_of(w), c = first_of(w + 1) - f;
             if (!c) break;
             float other[8];
@@ -287,16 +285,16 @@ __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, floa
             if (j < rows) a.last[size_t(head) * elements + at + j * row_step] = state[j];
 }
 
-template <typename T, int RUN>
-__global__ __launch_bounds__(64 * kJoinWaves, 4) void linear_join_kernel(JoinJobs jobs) {
-    __shared__ float sums[kJoinWaves][8][64];
+template <typename T, int WAVES, int RUN>
+__global__ __launch_bounds__(64 * WAVES, 4) void linear_join_kernel(JoinJobs jobs) {
+    __shared__ float sums[WAVES][8][64];
     const int which = int(blockIdx.x) < jobs.end[0] ? 0 : int(blockIdx.x) < jobs.end[1] ? 1 : 2;
     const LinearJoin& a = jobs.job[which];
     const int block = blockIdx.x - (which ? jobs.end[which - 1] : 0);
     if (a.turned && a.dv % 4 == 0)
-        linear_join<T, RUN, true>(a, block, sums);
+        linear_join<T, WAVES, RUN, true>(a, block, sums);
     else
-        linear_join<T, RUN, false>(a, block, sums);
+        linear_join<T, WAVES, RUN, false>(a, block, sums);
 }
 
 namespace {
@@ -339,6 +337,23 @@ hipError_t launch_typed(const LinearPass& a, const LinearPass* b, hipStream_t s,
     }
 }
 
+// Few waves, each with a longer run, cost less where one turn goes over all segments; for
+// more, more waves save turns.  Measured, 4 / 8 waves (us): 13 and 16 segments of the
+// three joins of a training step of 4 x 3136 tokens of 8 heads of 64 / 128 17 / 20, of 2 x
+// 1999 tokens of 8 heads (4) of 128 / 256 21 / 24; 64 segments of 4 heads 14 / 11 (of 64
+// heads 42 / 42, which is their bytes).
+template <typename T>
+hipError_t launch_join(const JoinJobs& j, int blocks, hipStream_t s, const LaunchEvents& ev) {
+    const int segments = j.job[0].segments;
+    auto launch = [&](auto kernel, int waves) {
+        return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(64 * waves), 0, s, ev.start, ev.stop, j);
+    };
+    if (segments <= 4) return launch(linear_join_kernel<T, 4, 1>, 4);
+    if (segments <= 8) return launch(linear_join_kernel<T, 4, 2>, 4);
+    if (segments <= 16) return launch(linear_join_kernel<T, 4, 4>, 4);
+    return launch(linear_join_kernel<T, 8, 4>, 8);
+}
+
 }  // namespace
 
 hipError_t launch_linear_pass(const LinearPass& a, const LinearPass* b, int dtype, hipStream_t s, const LaunchEvents& ev) {
@@ -357,15 +372,7 @@ hipError_t launch_linear_join(const LinearJoin* jobs, int count, int dtype, hipS
         if (i < count) blocks += j.job[i].heads * (j.job[i].rows / 8 * j.job[i].columns / 64);
         j.end[i] = blocks;
     }
-    const int run = (jobs[0].segments + kJoinWaves - 1) / kJoinWaves;
-    auto kernel = dtype == FFTSPLIT_BF16
-                      ? run <= 1   ? linear_join_kernel<__bf16, 1>
-                        : run <= 2 ? linear_join_kernel<__bf16, 2>
-                                   : linear_join_kernel<__bf16, 4>
-                  : run <= 1 ? linear_join_kernel<float, 1>
-                  : run <= 2 ? linear_join_kernel<float, 2>
-                             : linear_join_kernel<float, 4>;
-    return launch_kernel(kernel, dim3(unsigned(blocks)), dim3(64 * kJoinWaves), 0, s, ev.start, ev.stop, j);
+    return dtype == FFTSPLIT_BF16 ? launch_join<__bf16>(j, blocks, s, ev) : launch_join<float>(j, blocks, s, ev);
 }
 
 }  // namespace fftsplit
