@@ -183,6 +183,28 @@ def test_long_sequences_in_segments(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_more_segments_than_a_turn_of_the_join(dtype):
+    n, s, hq, hk, d, dv = 2, 4700, 2, 1, 20, 12
+    x = make(12, n, s, hq, hk, d, dv, dtype)
+    plan = fs.LinearAttention(n, s, hq, hk, d, dv, dtype=DTYPE[dtype])
+    assert plan.info.segment_tokens == 128 and plan.info.segments > 32
+    x[4][:] = -0.001
+    x = (*x[:7], torch.tensor([s, 4099], dtype=torch.int32, device="cuda"))
+    check(*both(*x, plan=plan), *x)
+    state = x[5].clone()
+    plan.forward(*x[:3], x[4], state=state, out_state=state, lengths=x[7])
+    assert torch.equal(state, plan.forward(*x[:3], x[4], state=x[5], lengths=x[7], return_state=True)[1])
+
+
+def test_segments_of_256_tokens():
+    n, s, hq, hk, d, dv = 4, 2200, 4, 4, 128, 128
+    x = make(13, n, s, hq, hk, d, dv, "bf16", ragged=True)
+    plan = fs.LinearAttention(n, s, hq, hk, d, dv, dtype=torch.bfloat16)
+    assert plan.info.segment_tokens == 256
+    check(*both(*x, plan=plan), *x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("s", [5, 100])
 def test_decays(s, dtype):
     """No decay, one that leaves nothing, and values out of range."""
