@@ -7,7 +7,9 @@
 // every row is one run of 256 bytes and the state stays in registers over the
 // tokens.  The sums over the rows are joined through LDS.  The tokens' rows are
 // read into LDS side by side with the state, as many as fit: one after the other
-// they cost a wait for memory each (5 tokens of 32 key heads of 64 / 128 17 us).
+// they cost a wait for memory each (5 tokens of 16 sequences of 16 heads (4) of 64 /
+// 128 18 us, so 11; single tokens of 64 sequences of 16 heads 15 us either way, 67 MB
+// of states at a copy's rate).
 #include "linear_common.hpp"
 
 namespace fftsplit {
