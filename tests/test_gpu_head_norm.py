@@ -138,6 +138,28 @@ def test_two_tensors_strides_and_in_place(dtype):
     assert torch.equal(x, before[0]) and torch.equal(dy[..., rest], before[1][..., rest])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,s,h,h1,d", [(1, 9001, 9, 5, 64), (2, 3, 100, 37, 128), (3, 5, 1, 70, 32)])
+def test_in_place_rounds_of_heads(n, s, h, h1, d, dtype):
+    """More heads than a workgroup takes at once, of two slices of one tensor:
+    rows are read while the ones before them are written, forwards and back."""
+    sections = (d // 4, d // 4)
+    x, dy, w, pos, freqs = make(15, n, s, h + h1, d, sections, dtype)
+    w1 = w.flip(0).contiguous()
+    both, grads = x.clone(), dy.clone()
+    fs.head_norm_rotary(both[:, :, :h], w, pos, freqs, sections, other=both[:, :, h:], other_weight=w1, eps=EPS,
+                        out=both[:, :, :h], out_other=both[:, :, h:])
+    _, dw, _, dw1 = fs.head_norm_rotary_backward(
+        grads[:, :, :h], x[:, :, :h], w, pos, freqs, sections, dy_other=grads[:, :, h:], other=x[:, :, h:], other_weight=w1,
+        eps=EPS, out=grads[:, :, :h], out_other=grads[:, :, h:])
+    torch.cuda.synchronize()
+    for part, weight, got in ((slice(0, h), w, dw), (slice(h, None), w1, dw1)):
+        y, dx, want, size = wanted(x[:, :, part], weight, pos, freqs, sections, dy=dy[:, :, part])
+        assert err(both[:, :, part], y) <= TOL[dtype] and err(grads[:, :, part], dx) <= TOL_DX[dtype]
+        rows = n * s * x[:, :, part].shape[2]
+        assert (np.abs(_np(got) - want) <= (rows + 1240) * U * size).all()
+
+
 @pytest.mark.parametrize("d", [64, 1024])
 def test_in_place_wide(d):
     """Heads that 64 lanes take in several pieces, too, may be written in place."""
