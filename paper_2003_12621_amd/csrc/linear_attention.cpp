@@ -71,14 +71,16 @@ void choose_segments(const fftsplit_linear_attention_problem_t& p, int& tokens, 
 }
 
 // Whether a call that returns no state takes a sequence as one segment, which saves two
-// launches and the states, for pairs of all its tokens (us, in segments / in one): bf16
-// forward passes of 8 x 784 tokens of 8 heads of 64 / 128 38 / 27, of 1000 of 16 heads 21
-// / 24, of 512 20 / 16, of 4 x 300 tokens of 8 heads of 64 19 / 9; backward passes, whose
-// key heads take the pairs of all the query heads that share them, of 8 x 784 tokens 77 /
-// 63, of 256 tokens of 16 heads (4) 47 / 44, of 512 48 / 74.
+// launches and the states, for pairs of all its tokens; backwards two of the three sums
+// have a key head's pairs with all the query heads that share it.  Measured, in segments
+// / as one (us): bf16 forward passes of one sequence of 8 heads of 64 / 128 and 300, 600,
+// 1000 tokens 19 / 10, 20 / 16, 20 / 23, of 8 sequences 24 / 11, 32 / 20, 37 / 33; backward
+// passes of the former 21 / 12, 23 / 17, 25 / 25, of 16 heads (4) of 64 29 / 22, 30 / 36,
+// 31 / 56, of 8 heads (4) of 128 26 / 16, 28 / 25, 31 / 36.  fp32, 160, 300, 600 tokens of 8
+// heads of 64 / 128: forward 37 / 20, 37 / 36, 38 / 64, backward 39 / 22, 40 / 38, 43 / 68.
 bool one_segment(const fftsplit_linear_attention_problem_t& p, bool backward) {
-    const long long pairs = (long long)p.tokens * (backward ? p.heads_q / p.heads_k : 1);
-    return pairs <= (p.dtype == FFTSPLIT_F32 ? 256 : 1024);
+    const long long sums = backward ? 2 * (p.heads_q / p.heads_k) + 1 : 3;
+    return p.tokens * sums <= 3 * (p.dtype == FFTSPLIT_F32 ? 320 : 900);
 }
 
 int padded32(int width) { return (width + 31) / 32 * 32; }

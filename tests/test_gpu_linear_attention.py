@@ -107,7 +107,7 @@ def test_widths(s, d, dv, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("s", [5, 130, 256, 257, 1000, 1024, 1025])
+@pytest.mark.parametrize("s", [5, 130, 320, 321, 900, 901, 1025])
 @pytest.mark.parametrize("state", [False, True])
 def test_no_state_returned(s, state, dtype):
     """Calls that return no state may take the whole sequence at once."""
