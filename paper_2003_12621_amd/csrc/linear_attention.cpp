@@ -59,11 +59,13 @@ size_t state_bytes(const fftsplit_linear_attention_problem_t& p) {
 // Tokens of a segment, a multiple of a workgroup's rows.  Long segments cost pairs of
 // tokens, short ones states, written and read.  Measured (us of all kernels, segments of
 // 128 / 256 / 384) where the short segments' states take up to 16 MiB: 8192 tokens of 16
-// heads (4) of 64 / 128 in bf16 48 / 53 / 68, training of 2 x 1999 tokens of 8 heads (4)
-// of 128 / 256 127 / 136 / 154; and where they take more: 4 x 16384 tokens of 16 heads
-// 465 / 407 / 398, training of 4 x 3136 tokens of 8 heads 190 / 177 / 185, of 2 x 4000
-// tokens of 16 heads (8) of 256 679 / 569.  Products of fp32 take 16 times as long as
-// those of bf16, so that pairs weigh more: training of 6 x 301 tokens 95 / 133 / 146.
+// heads (4) of 64 / 128 in bf16 47 / 51 / 56, gradients of 16384 tokens of 32 heads (4) 221
+// / 250 / 291, training of 2 x 1999 tokens of 8 heads (4) of 128 / 256 113 / 118 / 131; and
+// where they take more: 4 x 16384 tokens of 16 heads 440 / 392 / 379, training of 4 x 3136
+// tokens of 8 heads 168 / 149 / 151, of 2 x 4000 tokens of 16 heads (8) of 256 663 / 551 /
+// 544.  Products of fp32 take 16 times as long as those of bf16, so that pairs weigh more:
+// training of 6 x 301 tokens 73 / 102 / 111, of 4 x 3000 tokens of 8 heads of 64 287 / 363 /
+// 369.
 void choose_segments(const fftsplit_linear_attention_problem_t& p, int& tokens, int& segments) {
     const double states = double(state_bytes(p)) * ((p.tokens + kLinearRows - 1) / kLinearRows);
     tokens = p.dtype == FFTSPLIT_F32 || states <= 16 << 20 ? kLinearRows : 2 * kLinearRows;

@@ -15,8 +15,9 @@ namespace fftsplit {
 template <typename T, int D, int COLUMNS, int WAVES>
 struct StageShape {
     // Whether the pass's accumulators leave room for three waves a SIMD: then stages of
-    // one tile and fewer operands read ahead, which at 64 / 128 take 33 us where two waves
-    // with two tiles take 37 (training of 4 x 3136 tokens of 8 heads, forwards).
+    // one tile and fewer operands read ahead, which take 9 % off all kernels of 4 x 16384
+    // tokens of 16 heads of 64 / 128 and of training of 4 x 3136 tokens of 8 heads (443 ->
+    // 405 and 188 -> 172 us when it was chosen); of 128 / 256 nothing.
     static constexpr bool kLean = sizeof(T) == 2 && D * COLUMNS <= 8192;
     static constexpr int kPassOccupancy = kLean ? 3 : D <= 128 || sizeof(T) == 2 ? 2 : 1;
     // (as many as the registers hold)
