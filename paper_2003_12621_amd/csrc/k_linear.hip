@@ -231,7 +231,9 @@ __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, floa
     load(state, a.init ? a.init + size_t(head) * elements : a.parts);
     keep(state, a.init != nullptr);
     const float* parts = a.parts + size_t(head) * a.segments * elements;
-    Operand<T>* starts = static_cast<Operand<T>*>(a.starts) + (size_t(head) * a.segments * items + item);
+    constexpr int kParts = Precise<T>::kParts;
+    Operand<T>* starts =
+        static_cast<Operand<T>*>(a.starts) + (size_t(head) * a.segments * items + item / 64 * 64) * kParts + lane;
     for (int m0 = 0; m0 < a.segments; m0 += RUN * WAVES) {
         // the run of any wave in this turn
         auto first_of = [&](int w) { return min(m0 + w * RUN, a.segments); };
@@ -275,7 +277,10 @@ __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, floa
                 floatx16 c;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) c[j] = state[j];
-                starts[size_t(segment(i)) * items] = acc_operand<T>(c, 0);
+                Precise<T> x;
+                x.set(c, 0);
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) starts[size_t(segment(i)) * items * kParts + 64 * p] = x.part[p];
             }
             advance(state, carry_over(first + i, 1), added[i]);
         }

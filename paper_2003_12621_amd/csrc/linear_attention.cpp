@@ -88,13 +88,14 @@ bool one_segment(const fftsplit_linear_attention_problem_t& p, bool backward) {
 int padded32(int width) { return (width + 31) / 32 * 32; }
 
 // Bytes of the parts of the segments' states, and of the operands made of them
-// (rows padded as the passes that read them pad their widths).
+// (rows padded as the passes that read them pad their widths; of fp32 one operand of
+// 4 bytes a value, of bf16 two of 2).
 size_t parts_bytes(const fftsplit_linear_attention_problem_t& p, int segments) {
     return round256(state_bytes(p) * size_t(segments));
 }
 size_t starts_bytes(const fftsplit_linear_attention_problem_t& p, int segments, bool turned) {
     const size_t rows = linear_padded(turned ? p.dim_v : p.dim), columns = padded32(turned ? p.dim : p.dim_v);
-    return round256(size_t(p.batch) * p.heads_k * segments * rows * columns * type_bytes(p.dtype));
+    return round256(size_t(p.batch) * p.heads_k * segments * rows * columns * 4);
 }
 
 fftsplit_status_t build(const fftsplit_linear_attention_problem_t* prob, int device, const char* arch,

@@ -57,9 +57,10 @@ struct LinearPass {
 };
 
 // The state before each segment from the parts, as the operand of the product
-// with a tile of queries: [head][segment][column / 32][row / 16][lane][8], lane =
-// 32 (row / 8 % 2) + column % 32, in the tensors' type; rows are those of the
-// state, columns its columns, or (turned) the other way round.
+// with a tile of queries: [head][segment][column / 32][row / 16][part][lane][8], lane
+// = 32 (row / 8 % 2) + column % 32, in the tensors' type, of which bf16 takes two
+// parts; rows are those of the state, columns its columns, or (turned) the other way
+// round.
 struct LinearJoin {
     const float* parts;              // [heads][segments][d][dv]
     const float* init;               // [heads][d][dv] or null

@@ -250,17 +250,20 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
         }
         if (a.starts) {
             // what came before the segment
+            constexpr int kParts = Precise<T>::kParts;
             const int rows = linear_steps(a.d), all = (a.dv + 31) / 32;
-            const Operand<T>* p =
-                static_cast<const Operand<T>*>(a.starts) + (size_t(head) * a.segments + segment) * all * rows * 64 + lane;
+            const Operand<T>* p = static_cast<const Operand<T>*>(a.starts) +
+                                  (size_t(head) * a.segments + segment) * all * rows * kParts * 64 + lane;
             // (as many loads side by side as the registers hold, of strips that exist: the
             // columns behind the last are not stored)
-            constexpr int kAll = kBlocks * kSteps, kGroup = kAll < 16 / int(sizeof(T)) ? kAll : 16 / int(sizeof(T));
+            constexpr int kAll = kBlocks * kSteps * kParts, kGroup = kAll < 16 / int(sizeof(T)) ? kAll : 16 / int(sizeof(T));
             Operand<T> x[2][kGroup];
             auto load = [&](int j) {
 #pragma unroll
                 for (int i = j; i < j + kGroup; ++i)
-                    x[j / kGroup % 2][i - j] = p[size_t(min(column0 / 32 + i / kSteps, all - 1) * rows + i % kSteps) * 64];
+                    x[j / kGroup % 2][i - j] =
+                        p[size_t((min(column0 / 32 + i / kParts / kSteps, all - 1) * rows + i / kParts % kSteps) * kParts +
+                                 i % kParts) * 64];
             };
             load(0);
 #pragma unroll
@@ -268,7 +271,7 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
                 if (j + kGroup < kAll) load(j + kGroup);
                 in_order();
 #pragma unroll
-                for (int i = j; i < j + kGroup; ++i) mma(out[i / kSteps], x[j / kGroup % 2][i - j], q[i % kSteps]);
+                for (int i = j; i < j + kGroup; ++i) mma(out[i / kParts / kSteps], x[j / kGroup % 2][i - j], q[i / kParts % kSteps]);
             }
             const float f = a.inter_scale * decay_power(log2_decay, max(a.reverse ? end - 1 - row : row - begin + 1, 0));
 #pragma unroll
