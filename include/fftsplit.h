@@ -554,10 +554,10 @@ fftsplit_status_t fftsplit_head_norm_rotary_backward(const fftsplit_head_norm_t*
  * the last token that is there.  What the order of tokens hides from a row has to
  * be finite, as it is multiplied by zero.
  * States, products and sums are fp32.  With bf16 tensors the scores q k^T (with
- * their decay) are rounded to bf16 once, as operands, in calls of more than a few
- * tokens, and the state that a segment begins with is good to 2^-16 there; what a
- * call returns of a state or its gradient is a sum of unrounded products.  fp32
- * tensors are rounded nowhere. */
+ * their decay) and the state that a segment begins with are good to 2^-14 as operands,
+ * in calls of more than a few tokens, and only outputs are rounded; what a call returns
+ * of a state or its gradient is a sum of unrounded products.  fp32 tensors are rounded
+ * nowhere. */
 typedef struct {
     int batch;                     /* sequences */
     int tokens;                    /* of the longest; at most 2^28 */

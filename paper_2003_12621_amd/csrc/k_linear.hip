@@ -40,8 +40,8 @@ __device__ __forceinline__ unsigned state_column_lane(int lane) {
 // An operand's elements times factors, as the sum of PARTS operands.  bf16 elements
 // times fp32 factors have 24 significant bits, three bf16 numbers of 8, cut off one
 // after the other: that is what a state that the caller gets is summed from.  Where
-// it only serves as an operand, rounded to 8 bits, two of them (good to 2^-16) do.
-// fp32 elements are one.
+// it only serves as an operand of two parts, good to 2^-15, two of them do (off by
+// 2^-14 at most, by 2^-16 in the mean).  fp32 elements are one.
 template <typename T, int PARTS>
 struct Weighted {
     Operand<T> part[PARTS];

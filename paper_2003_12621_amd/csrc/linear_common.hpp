@@ -54,12 +54,18 @@ __device__ __forceinline__ float decay_less_one(float log2_decay, int e) {
 }
 
 // Half s of an accumulator as the operand of a product: fp32 as it is; in bf16 as the
-// sum of two operands, good to 2^-16 of each value where one is good to 2^-8.  The
-// states before the segments are handed on like this.  A state's largest terms are what
-// the keys and values have in common, and a product may cancel just these: rounded once,
-// a dq of values with a mean of 4 and gradients that add up to zero was off by 4.5e-2,
-// like this by 2e-3, as much as by other roundings (training of 4 x 3136 tokens of 8 heads of
-// 64 / 128 142 us, so 152).
+// sum of two operands, good to 2^-15 of each value where one is good to 2^-8.  What
+// later products take is held like this:
+//   the states before the segments.  A state's largest terms are what keys and values
+//   have in common, and a product may cancel just these: rounded once, a dq of values
+//   with a mean of 4 and gradients that add up to zero was off by 4.5e-2, like this by
+//   1.7e-3, which is its own rounding.  4 x 3136 training tokens of 8 heads of 64 / 128
+//   142 us, so 152; 4 x 16384 tokens of 16 heads 374, so 405;
+//   the scores with their decay: an error of 1.66e-3 of each term next to the output's
+//   own 1.66e-3.  The former 152 us, so 157; the latter 405, so 412; 8 x 784 tokens of 8
+//   heads, one segment, 27 us, so 32.
+// (The upper part is cut off, not rounded, which takes fewer registers, and no finite
+// value becomes infinite by it.)
 template <typename T>
 struct Precise {
     static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
@@ -72,8 +78,9 @@ struct Precise {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float a = c[8 * s + 2 * e], b = c[8 * s + 2 * e + 1];
-                high[e] = pack_bf16(a, b);
-                low[e] = pack_bf16(a - __uint_as_float(high[e] << 16), b - __uint_as_float(high[e] & 0xffff0000u));
+                high[e] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+                low[e] = pack_bf16(a - __uint_as_float(__float_as_uint(a) & 0xffff0000u),
+                                   b - __uint_as_float(__float_as_uint(b) & 0xffff0000u));
             }
             part[0].v = __builtin_bit_cast(bf16x8, high);
             part[1].v = __builtin_bit_cast(bf16x8, low);

@@ -291,7 +291,8 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
             const unsigned k_at = k_row + stage + j * kTile * int(sizeof(T)) * D;
             const unsigned v_at = v_column + stage + j * kTile * int(sizeof(T)) * COLUMNS;
             floatx16 s[TILES];
-            Operand<T> ring[kAhead + 1], p[2 * TILES];
+            Operand<T> ring[kAhead + 1];
+            Precise<T> p[2 * TILES];
 #pragma unroll
             for (int t = 0; t < TILES; ++t) s[t] = zero16();
             auto read = [&](int i) {
@@ -312,16 +313,18 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) {
                         weigh(s[t], t);
-                        p[2 * t] = acc_operand<T>(s[t], 0);
-                        p[2 * t + 1] = acc_operand<T>(s[t], 1);
+                        p[2 * t].set(s[t], 0);
+                        p[2 * t + 1].set(s[t], 1);
                     }
                 }
                 const Operand<T>& x = ring[i % (kAhead + 1)];
                 const int v = i - kScores;
-                if (i < kScores)
+                if (i < kScores) {
                     mma(s[i % TILES], x, q[i / TILES]);
-                else
-                    mma(out[v % kBlocks], x, p[v / kBlocks]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < Precise<T>::kParts; ++j) mma(out[v % kBlocks], x, p[v / kBlocks].part[j]);
+                }
             }
         };
         // Terms of a tile `between` tokens from the wave's own.

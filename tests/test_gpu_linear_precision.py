@@ -3,13 +3,14 @@ their outputs, also where the terms of a sum cancel.
 
 Tolerances.  A bf16 output is rounded to 2^-8 of itself at most, 1.66e-3 in the
 mean square.  Operands of later products (the state before a segment, the scores)
-are sums of two bf16 numbers, each rounded to nearest: 2^-16 of a value at most,
-2^-17.8 in the mean square.  Of a state that has a common part, which the product
-cancels, that is 2^-17.8 of the common part against the rest as the signal: here
-the state's common part is up to 4 * 150 (values' mean, terms that a memory of 300
-tokens holds) next to a sum of 150 terms that are independent, 12: 50 times as large,
-2^-17.8 * 50 = 2.2e-4 of the output in the mean square.  With the output's own that is
-1.67e-3, tested as 2e-3.
+are sums of two bf16 numbers, the first cut off and the second rounded: 2^-15 of a
+value at most, 2^-16.8 in the mean square, and as much again for the terms of a
+state, 2^-16.3 together.  Of a state that has a common part, which the product
+cancels, that is 2^-16.3 of the common part against the rest as the signal: here the
+state's common part is up to 4 * 150 (values' mean, terms that a memory of 300 tokens
+holds) next to a sum of 150 terms that are independent, 12: 50 times as large, 2^-16.3
+* 50 = 6.2e-4 of the output in the mean square.  With the output's own that is
+1.77e-3, tested as 2e-3.
 """
 import numpy as np
 import pytest
@@ -65,3 +66,25 @@ def test_states_with_a_common_part(d, dv, mean):
     assert plan.info.segments > 1
     for name in ("o", "dq", "dk", "dv"):
         assert off[name] <= 3e-3, (name, off)
+
+
+@pytest.mark.parametrize("mean", [0, 4])
+@pytest.mark.parametrize("s,state", [(300, False), (784, False), (300, True), (1000, True)])
+@pytest.mark.parametrize("d,dv", [(64, 128), (40, 24)])
+def test_only_the_outputs_are_rounded(d, dv, s, state, mean):
+    """In sequences of one segment, and of several with a state returned."""
+    plan, off = errors(*common_parts(s, 1, s, 2, 2, d, dv, mean), return_state=state)
+    for name in ("o", "dq", "dk", "dv"):
+        assert off[name] <= 2e-3, (name, off)
+
+
+@pytest.mark.parametrize("s", [9, 128, 1000])
+def test_returned_states(s):
+    """A returned state's terms are bf16 numbers times fp32 weights, as three bf16
+    operands that leave out nothing.  Their sums are fp32: in the mean square a
+    rounding of 2^-24 / sqrt(3) for each part of the 128 terms of a segment,
+    sqrt(384) of them 11 * 2^-24, and the weights (three factors and an exponent up
+    to 8) 10 * 2^-24: 15 * 2^-24 = 9e-7 together, tested as 1e-6.  (Two operands
+    would leave out 2.8e-6.)"""
+    _, off = errors(*common_parts(s, 2, s, 2, 2, 64, 64, 0), return_state=True)
+    assert off["state"] <= 1e-6, off
