@@ -161,10 +161,13 @@ class LinearAttentionBlock:
     def forward(self, x, state=None, frame=0, save=False, workspace=None):
         """(y, state behind this frame) of x [n, c, h, w] (fp32), the stream's
         `frame`-th, from the state before it (None: zero, of a first frame); with
-        save=True also what backward needs.  `workspace`: as the attention's; by
-        default each call allocates its own."""
+        save=True also what backward needs (with a copy of `state`, as step writes
+        states in place).  `workspace`: as the attention's; by default each call
+        allocates its own."""
         import torch
         p = self.params
+        if save and state is not None:
+            state = state.clone()
         tokens, mean, rstd = layer_norm(x, p["norm_weight"], p["norm_bias"], layout="first", out_layout="last",
                                         out_dtype=torch.bfloat16, return_stats=True)
         positions = self._positions(frame)
