@@ -91,7 +91,7 @@ void linear_pass_kernel(PassPair pair) {
 template <typename T, int D, int WAVES, bool WIDE, int PARTS>
 __global__ __launch_bounds__(64 * WAVES, (D <= 128 ? 2 : 1)) void linear_parts_kernel(PassPair pair) {
     constexpr int kTile = kLinearTile, DT = D / 32, kColumns = 32 * WAVES;
-    using Shape = StageShape<T, D, kColumns, WAVES>;
+    using Shape = StageShape<T, D, kColumns, WAVES, 0>;
     extern __shared__ __align__(16) char lds[];
     const bool second = int(blockIdx.x) >= pair.first_blocks;
     const LinearPass& a = pair.pass[second];
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(64 * WAVES, (D <= 128 ? 2 : 1)) void linear_parts_k
     const float log2_decay = decay_log2(linear_uniform(a.log_decay + h));
     const int end = int(min((long long)begin + a.segment_tokens, (long long)linear_length(a.lengths, a.s, b)));
 
-    KeyStream<T, D, kColumns, WAVES, WIDE> stream(a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, begin, end, 0,
-                                                  0, wave, lane);
+    KeyStream<T, D, kColumns, WAVES, 0, WIDE> stream(a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, begin, end,
+                                                     0, 0, wave, lane);
     for (int i = 0; i + 1 < Shape::kStages; ++i) stream.fetch(wave, lane);
     // a token's weight is decay to its distance from the segment's end (backwards,
     // from one before its beginning): of its place in the tile, times the tile's
@@ -314,8 +314,8 @@ long long part_blocks(const LinearPass& a, int columns) {
 // MAIN: the pass; else the parts.
 template <typename T, int D, int COLUMNS, bool MAIN>
 hipError_t launch_shaped(const LinearPass& a, const LinearPass* b, hipStream_t s, const LaunchEvents& ev) {
-    constexpr int kWaves = MAIN ? kPassWaves : COLUMNS / 32;
-    using Shape = StageShape<T, D, COLUMNS, kWaves>;
+    constexpr int kWaves = MAIN ? kPassWaves : COLUMNS / 32, kBehind = MAIN ? kDiagonalBytes : 0;
+    using Shape = StageShape<T, D, COLUMNS, kWaves, kBehind>;
     auto blocks = [](const LinearPass& p) { return MAIN ? pass_blocks(p, COLUMNS) : part_blocks(p, COLUMNS); };
     const PassPair pair{{a, b ? *b : a}, int(blocks(a))};
     void (*kernel)(PassPair);
@@ -328,7 +328,7 @@ hipError_t launch_shaped(const LinearPass& a, const LinearPass* b, hipStream_t s
         else
             kernel = a.wide ? linear_parts_kernel<T, D, kWaves, true, kSome> : linear_parts_kernel<T, D, kWaves, false, kSome>;
     }
-    constexpr int kLds = Shape::kLds + (MAIN ? kDiagonalBytes : 0);
+    constexpr int kLds = Shape::kLds + kBehind;
     if (hipError_t e = allow_dynamic_lds(kernel, kLds)) return e;
     return launch_kernel(kernel, dim3(unsigned(blocks(a) + (b ? blocks(*b) : 0))), dim3(64 * kWaves), kLds, s, ev.start, ev.stop,
                          pair);

@@ -26,6 +26,7 @@ struct GradientShape {
     static constexpr int kOccupancy =
         Rows::kPassOccupancy < Values::kPassOccupancy ? Rows::kPassOccupancy : Values::kPassOccupancy;
     static constexpr int kLds = (Rows::kLds > Values::kLds ? Rows::kLds : Values::kLds) + kDiagonalBytes;
+    static_assert(kOccupancy * kLds <= kLinearLds, "the workgroups aimed at fit");
 };
 
 template <typename T, int DIM, int DIM_V>

@@ -8,11 +8,14 @@
 
 namespace fftsplit {
 
+// LDS of a compute unit.
+constexpr int kLinearLds = 163840;
+
 // A stage: some rows of k and of v, of D and COLUMNS columns, on their way from
 // memory straight into LDS, in pieces of 1024 bytes that are dealt out to the waves
-// alike, so that every wave has the same number of copies in flight.  (What rows
-// beyond the last hold is as for RowCopy.)
-template <typename T, int D, int COLUMNS, int WAVES>
+// alike, so that every wave has the same number of copies in flight.  BEHIND: bytes
+// of LDS that the kernel needs behind the ring of stages.
+template <typename T, int D, int COLUMNS, int WAVES, int BEHIND>
 struct StageShape {
     // Whether the pass's accumulators leave room for three waves a SIMD: then stages of
     // one tile and fewer operands read ahead, which take 9 % off all kernels of 4 x 16384
@@ -22,20 +25,24 @@ struct StageShape {
     static constexpr int kPassOccupancy = kLean ? 3 : D <= 128 || sizeof(T) == 2 ? 2 : 1;
     // (as many as the registers hold)
     static constexpr int kPassAhead = kLean ? (COLUMNS > 64 ? 1 : 2) : sizeof(T) == 4 && D * COLUMNS >= 16384 ? 2 : 3;
-    // Two tiles a stage, where two workgroups' rings fit a compute unit
-    static constexpr int kRows = !kLean && 64 * (D + COLUMNS) * int(sizeof(T)) <= 40960 ? 64 : 32;
+    // Two tiles a stage, where two workgroups with rings of two stages fit a compute unit
+    // (one alone took twice the time: gradients of 4 x 3136 tokens of 8 heads of 64 / 256 in
+    // bf16 388 us, with one tile a stage 185; forward pass of 8 x 784 tokens of 256 / 64 187
+    // and 36)
+    static constexpr int kRows =
+        !kLean && 2 * 64 * (D + COLUMNS) * int(sizeof(T)) + BEHIND <= kLinearLds / 2 ? 64 : 32;
     static constexpr int kRowBytes = TileShape<T, D>::bytes(kRows);
     static constexpr int kUsedBytes = kRowBytes + TileShape<T, COLUMNS>::bytes(kRows);
     static constexpr int kPer = (kUsedBytes / 1024 + WAVES - 1) / WAVES;             // copies of a wave
     static constexpr int kStageBytes = kPer * WAVES * 1024;
     // Stages in LDS: the one worked on, and those on their way.
-    static constexpr int kStages = 3 * kStageBytes <= 81920 ? 3 : 2;
+    static constexpr int kStages = 3 * kStageBytes + BEHIND <= kLinearLds / 2 ? 3 : 2;
     static constexpr int kLds = kStages * kStageBytes;
 };
 
-template <typename T, int D, int COLUMNS, int WAVES, bool WIDE>
+template <typename T, int D, int COLUMNS, int WAVES, int BEHIND, bool WIDE>
 struct StageCopy {
-    using Shape = StageShape<T, D, COLUMNS, WAVES>;
+    using Shape = StageShape<T, D, COLUMNS, WAVES, BEHIND>;
     using Rows = TileShape<T, D>;
     using Values = TileShape<T, COLUMNS>;
     static constexpr int kRowPieces = Shape::kRowBytes / 1024, kPieces = Shape::kUsedBytes / 1024;
@@ -104,11 +111,11 @@ struct StageCopy {
 // share a state one after another: copies them into a ring.  First the tokens from
 // `first` on to `end`, then those from `other` on to `other_end` (either possibly
 // none); rows of the last stage that are not there become zero.
-template <typename T, int D, int COLUMNS, int WAVES, bool WIDE>
+template <typename T, int D, int COLUMNS, int WAVES, int BEHIND, bool WIDE>
 struct KeyStream {
-    using Shape = StageShape<T, D, COLUMNS, WAVES>;
+    using Shape = StageShape<T, D, COLUMNS, WAVES, BEHIND>;
     static constexpr int kBytes = sizeof(T);
-    const StageCopy<T, D, COLUMNS, WAVES, WIDE> copy;
+    const StageCopy<T, D, COLUMNS, WAVES, BEHIND, WIDE> copy;
     const char *k, *v;
     // to the next head; further from the last one to the next stage's first; and further
     // to the first of the other tokens
@@ -166,7 +173,7 @@ struct KeyStream {
 constexpr int kPassWaves = kLinearRows / kLinearTile;
 constexpr int kDiagonalBytes = kLinearTile * kLinearTile * 4;
 template <typename T, int D, int COLUMNS>
-using PassShape = StageShape<T, D, COLUMNS, kPassWaves>;
+using PassShape = StageShape<T, D, COLUMNS, kPassWaves, kDiagonalBytes>;
 
 inline long long pass_blocks(const LinearPass& a, int columns) {
     return (long long)a.n * a.hk * a.q_heads * ((a.dv + columns - 1) / columns) * ((a.s + kLinearRows - 1) / kLinearRows);
@@ -187,6 +194,7 @@ inline long long pass_blocks(const LinearPass& a, int columns) {
 template <typename T, int D, int COLUMNS, bool WIDE>
 __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int blocks) {
     using Shape = PassShape<T, D, COLUMNS>;
+    static_assert(Shape::kPassOccupancy * (Shape::kLds + kDiagonalBytes) <= kLinearLds, "the workgroups aimed at fit");
     constexpr int kTile = kLinearTile, kSteps = D / 16, kBlocks = COLUMNS / 32;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -216,9 +224,9 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
         // first the keys of the workgroup's own rows, then those further on (all of them
         // before its rows, backwards behind them)
         const int own_end = min(row0 + kLinearRows, end);
-        KeyStream<T, D, COLUMNS, kPassWaves, WIDE> stream(a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, row0,
-                                                          own_end, a.reverse ? own_end : begin, a.reverse ? end : row0, wave,
-                                                          lane);
+        KeyStream<T, D, COLUMNS, kPassWaves, kDiagonalBytes, WIDE> stream(
+            a, unsigned(reinterpret_cast<uintptr_t>(lds)), b, h, column0, row0, own_end, a.reverse ? own_end : begin,
+            a.reverse ? end : row0, wave, lane);
         for (int i = 0; i + 1 < Shape::kStages; ++i) stream.fetch(wave, lane);
         Operand<T> q[kSteps];
         load_row_operands<T, D, WIDE>(q, static_cast<const T*>(a.q.p) + b * a.q.b + row * a.q.t +
