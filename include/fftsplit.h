@@ -551,8 +551,12 @@ fftsplit_status_t fftsplit_head_norm_rotary_backward(const fftsplit_head_norm_t*
  *   o_t = scale S_t^T q_t                        for the query heads h of g = h / (heads_q / heads_k),
  * from the state that the caller gives, or zero.  Tokens from lengths[b] on are
  * not read; their outputs and gradients are zero, and the state is the one after
- * the last token that is there.  What the order of tokens hides from a row has to
- * be finite, as it is multiplied by zero.
+ * the last token that is there.
+ * Values are taken to be finite.  What takes an infinity or a NaN is not finite, and
+ * which of the two it is is not specified: a value's column (a key's row) of the state
+ * from its token on, and the outputs of that token, of those behind it and, in calls of
+ * more than a few tokens, of up to 31 before it, which the order of tokens hides it
+ * from but which are multiplied by zero.  Backwards likewise.
  * States, products and sums are fp32.  With bf16 tensors the scores q k^T (with
  * their decay) and the state that a segment begins with are good to 2^-14 as operands,
  * in calls of more than a few tokens, and only outputs are rounded; what a call returns
