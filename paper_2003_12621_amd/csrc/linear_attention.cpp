@@ -72,17 +72,55 @@ void choose_segments(const fftsplit_linear_attention_problem_t& p, int& tokens, 
     segments = (p.tokens + tokens - 1) / tokens;
 }
 
+// us that a wave takes for a tile of 32 rows by 32 tokens and a slice of columns.
+double tile_us(const fftsplit_linear_attention_problem_t& p, int width, int width_v) {
+    const int rows = linear_padded(width), columns = linear_columns(width_v);
+    return p.dtype == FFTSPLIT_F32 ? 0.015 * (rows + columns) : 0.25 + 0.0012 * (rows + 2 * columns);
+}
+
 // Whether a call that returns no state takes a sequence as one segment, which saves two
-// launches and the states, for pairs of all its tokens; backwards two of the three sums
-// have a key head's pairs with all the query heads that share it.  Measured, in segments
-// / as one (us): bf16 forward passes of one sequence of 8 heads of 64 / 128 and 300, 600,
-// 1000 tokens 19 / 10, 20 / 16, 20 / 23, of 8 sequences 24 / 11, 32 / 20, 37 / 33; backward
-// passes of the former 21 / 12, 23 / 17, 25 / 25, of 16 heads (4) of 64 29 / 22, 30 / 36,
-// 31 / 56, of 8 heads (4) of 128 26 / 16, 28 / 25, 31 / 36.  fp32, 160, 300, 600 tokens of 8
-// heads of 64 / 128: forward 37 / 20, 37 / 36, 38 / 64, backward 39 / 22, 40 / 38, 43 / 68.
-bool one_segment(const fftsplit_linear_attention_problem_t& p, bool backward) {
-    const long long sums = backward ? 2 * (p.heads_q / p.heads_k) + 1 : 3;
-    return p.tokens * sums <= 3 * (p.dtype == FFTSPLIT_F32 ? 320 : 900);
+// launches and the states, for pairs of all its tokens: by an estimate of both, from the
+// tiles of the longest wave and of all waves of a SIMD (which hardly overlap), the states'
+// bytes (written, read, and the same as operands; backwards for both sums) and what the
+// first two launches cost besides.  Measured, in segments / as one (us):
+//   bf16, forward, 8 heads of 64 / 128, one sequence of 300, 600, 900 tokens 21 / 12, 21 /
+//   19, 22 / 26, 32 sequences 47 / 24, 70 / 55, 97 / 105; 16 heads (4) of 64, 32 sequences 38
+//   / 29, 54 / 65, 75 / 127; 8 heads of 128 / 256, 8 sequences 46 / 17, 60 / 37, 76 / 73;
+//   backward, 8 heads of 64 / 128, one sequence 22 / 13, 25 / 20, 28 / 27, 32 sequences of 32
+//   / 32 43 / 33, 64 / 74, 91 / 158, 16 heads (4) of 64, 8 sequences 40 / 32, 47 / 65, 57 / 125;
+//   fp32, 8 heads of 64 / 128, 8 sequences of 160, 300, 600 tokens: forward 41 / 21, 45 / 38,
+//   66 / 99, backward 58 / 38, 82 / 77, 121 / 195; 6 heads (3) of 32 / 64 backward 37 / 30, 46 /
+//   55, 53 / 112.
+// The estimate's numbers are fitted to 144 such calls, of which it takes the slower way by up
+// to 12 % and by 0.3 % in the mean (a bound on the tokens alone: 74 % and 2.5 %); of 48 other
+// calls by up to 19 % and by 1 % in the mean.
+bool one_segment(const fftsplit_linear_attention_plan_s& plan, bool backward) {
+    const fftsplit_linear_attention_problem_t& p = plan.prob;
+    if (plan.segments == 1) return true;
+    const int group = p.heads_q / p.heads_k;
+    double longest = 0, all = 0;            // of a wave with one tile, and of all of them with one each
+    auto add = [&](int width, int width_v, int heads, int k_heads) {
+        const double us = tile_us(p, width, width_v) * k_heads;
+        const int columns = linear_columns(width_v);
+        if (us > longest) longest = us;
+        all += us * p.batch * heads * ((width_v + columns - 1) / columns);
+    };
+    if (backward) {
+        add(p.dim_v, p.dim, p.heads_q, 1);
+        add(p.dim_v, p.dim, p.heads_k, group);
+        add(p.dim, p.dim_v, p.heads_k, group);
+    } else {
+        add(p.dim, p.dim_v, p.heads_q, 1);
+    }
+    const double tiles = (p.tokens + kLinearTile - 1) / kLinearTile, own = plan.segment_tokens / kLinearTile;
+    constexpr double kSimds = 1024, kBytesPerUs = 4.5e6;
+    auto pairs = [&](double of) {           // rows that each see `of` tiles at most
+        const double chain = longest * of, work = all / kSimds * tiles * of / 2;
+        return chain > work ? chain : work;
+    };
+    const double states = double(state_bytes(p)) * plan.segments * (backward ? 11 : 4) / kBytesPerUs;
+    const double before = p.dtype == FFTSPLIT_F32 ? 6 : 8;
+    return pairs(tiles) <= pairs(tiles < own ? tiles : own) + 4 * longest + before + states;
 }
 
 int padded32(int width) { return (width + 31) / 32 * 32; }
@@ -321,7 +359,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_forward(fftsplit_lin
             return launched_ok(launch_linear_tokens(a, p.dtype, stream, ev), "linear attention launch");
         }
 
-        LinearPass a = pass_of(plan, in, x.wide, !state_out && one_segment(p, false));
+        LinearPass a = pass_of(plan, in, x.wide, !state_out && one_segment(*plan, false));
         a.q = x.q;
         a.k = x.k;
         a.v = x.v;
@@ -393,7 +431,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_backward(
         // The forward pass's state, of (k, v), serves dq; its gradient, of (q,
         // dout) from the last token on, dk and dv.
         const int group = p.heads_q / p.heads_k;
-        const LinearPass a = pass_of(plan, in, x.wide, !dstate && one_segment(p, true));
+        const LinearPass a = pass_of(plan, in, x.wide, !dstate && one_segment(*plan, true));
         LinearPass pq = a, pk = a, pv = a;
         pq.q = g;                       // dq: (dout, v, k)
         pq.k = x.v;
