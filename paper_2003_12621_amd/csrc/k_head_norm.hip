@@ -194,7 +194,8 @@ __global__ __launch_bounds__(kThreads, BACK ? 4 : 6) void head_norm_kernel(HeadN
         };
         // The first rows are on their way while the angles are computed, the next ones
         // while one is worked on: 150 -> 133 us of the former.  (Backwards, with twice the
-        // rows, it costs a wave: 31 -> 40 us of the latter.)
+        // rows, it costs a wave a SIMD: 28 -> 32 us of the latter with its sums, and 29 -> 32
+        // us of 5 x 4275 tokens of 6 + 3 heads of 40 in fp32.)
         Loaded<T, N> loaded[2];
         if constexpr (ONE && !BACK) {
 #pragma unroll

@@ -57,25 +57,27 @@ size_t state_bytes(const fftsplit_linear_attention_problem_t& p) {
 }
 
 // Tokens of a segment, a multiple of a workgroup's rows.  Long segments cost pairs of
-// tokens, short ones states, written and read.  Measured (us of all kernels, segments of
-// 128 / 256 / 384) where the short segments' states take up to 16 MiB: 8192 tokens of 16
-// heads (4) of 64 / 128 in bf16 47 / 51 / 56, gradients of 16384 tokens of 32 heads (4) 221
-// / 250 / 291, training of 2 x 1999 tokens of 8 heads (4) of 128 / 256 113 / 118 / 131; and
-// where they take more: 4 x 16384 tokens of 16 heads 440 / 392 / 379, training of 4 x 3136
-// tokens of 8 heads 168 / 149 / 151, of 2 x 4000 tokens of 16 heads (8) of 256 663 / 551 /
-// 544.  Products of fp32 take 16 times as long as those of bf16, so that pairs weigh more:
-// training of 6 x 301 tokens 73 / 102 / 111, of 4 x 3000 tokens of 8 heads of 64 287 / 363 /
-// 369.
+// tokens, short ones states, written and read.  Measured (us of forward + backward passes,
+// segments of 128 / 256 / 384) where the short segments' states take up to 16 MiB, bf16:
+// 8192 tokens of 16 heads (4) of 64 / 128 50 + 80 / 56 + 101 / 62 + 122, 16384 of 32 heads (4)
+// 112 + 237 / 119 + 271 / 135 + 333, 2 x 1999 tokens of 8 heads (4) of 128 / 256 42 + 79 / 49 +
+// 82 / 54 + 91; and where they take more: 4 x 16384 tokens of 16 heads 493 + 1335 / 413 + 1082 /
+// 409 + 1053, 4 x 3136 tokens of 8 heads 56 + 116 / 55 + 98 / 58 + 103, 2 x 4000 tokens of 16
+// heads (8) of 256 220 + 568 / 173 + 450 / 183 + 446.  Products of fp32 take 16 times as long
+// as those of bf16, so that pairs weigh more: 6 x 301 tokens of 6 heads (3) of 32 / 64 26 + 43 /
+// 38 + 67 / 42 + 79, 4 x 3000 tokens of 8 heads of 64 93 + 195 / 115 + 248 / 120 + 250.
 void choose_segments(const fftsplit_linear_attention_problem_t& p, int& tokens, int& segments) {
     const double states = double(state_bytes(p)) * ((p.tokens + kLinearRows - 1) / kLinearRows);
     tokens = p.dtype == FFTSPLIT_F32 || states <= 16 << 20 ? kLinearRows : 2 * kLinearRows;
     segments = (p.tokens + tokens - 1) / tokens;
 }
 
-// us that a wave takes for a tile of 32 rows by 32 tokens and a slice of columns.
-double tile_us(const fftsplit_linear_attention_problem_t& p, int width, int width_v) {
+// us that a wave takes for a tile of 32 rows by 32 tokens and a slice of columns (whose
+// elements pass through registers one by one where accesses of 16 bytes are not aligned).
+double tile_us(const fftsplit_linear_attention_problem_t& p, int width, int width_v, bool wide) {
     const int rows = linear_padded(width), columns = linear_columns(width_v);
-    return p.dtype == FFTSPLIT_F32 ? 0.015 * (rows + columns) : 0.25 + 0.0012 * (rows + 2 * columns);
+    const double products = p.dtype == FFTSPLIT_F32 ? 0.015 * (rows + columns) : 0.25 + 0.0012 * (rows + 2 * columns);
+    return products + (wide ? 0 : 0.0035 * type_bytes(p.dtype) * (rows + columns));
 }
 
 // Whether a call that returns no state takes a sequence as one segment, which saves two
@@ -94,23 +96,26 @@ double tile_us(const fftsplit_linear_attention_problem_t& p, int width, int widt
 // The estimate's numbers are fitted to 144 such calls, of which it takes the slower way by up
 // to 12 % and by 0.3 % in the mean (a bound on the tokens alone: 74 % and 2.5 %); of 48 other
 // calls by up to 19 % and by 1 % in the mean.
-bool one_segment(const fftsplit_linear_attention_plan_s& plan, bool backward) {
+// Rows that are not aligned, bf16, 8 heads of 64 / 128: forward, one sequence of 300, 600 tokens
+// 36 / 26, 37 / 46, 8 sequences of 784 62 / 82, backward (in two launches) 58 / 60, 61 / 96, 153 /
+// 209.
+bool one_segment(const fftsplit_linear_attention_plan_s& plan, bool backward, bool wide) {
     const fftsplit_linear_attention_problem_t& p = plan.prob;
     if (plan.segments == 1) return true;
     const int group = p.heads_q / p.heads_k;
     double longest = 0, all = 0;            // of a wave with one tile, and of all of them with one each
     auto add = [&](int width, int width_v, int heads, int k_heads) {
-        const double us = tile_us(p, width, width_v) * k_heads;
+        const double us = tile_us(p, width, width_v, wide) * k_heads;
         const int columns = linear_columns(width_v);
-        if (us > longest) longest = us;
         all += us * p.batch * heads * ((width_v + columns - 1) / columns);
+        return us;
     };
     if (backward) {
-        add(p.dim_v, p.dim, p.heads_q, 1);
-        add(p.dim_v, p.dim, p.heads_k, group);
-        add(p.dim, p.dim_v, p.heads_k, group);
+        const double dq = add(p.dim_v, p.dim, p.heads_q, 1), dk = add(p.dim_v, p.dim, p.heads_k, group);
+        const double dv = add(p.dim, p.dim_v, p.heads_k, group), first = dq > dk ? dq : dk;
+        longest = !wide ? first + dv : first > dv ? first : dv;
     } else {
-        add(p.dim, p.dim_v, p.heads_q, 1);
+        longest = add(p.dim, p.dim_v, p.heads_q, 1);
     }
     const double tiles = (p.tokens + kLinearTile - 1) / kLinearTile, own = plan.segment_tokens / kLinearTile;
     constexpr double kSimds = 1024, kBytesPerUs = 4.5e6;
@@ -359,7 +364,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_forward(fftsplit_lin
             return launched_ok(launch_linear_tokens(a, p.dtype, stream, ev), "linear attention launch");
         }
 
-        LinearPass a = pass_of(plan, in, x.wide, !state_out && one_segment(*plan, false));
+        LinearPass a = pass_of(plan, in, x.wide, !state_out && one_segment(*plan, false, x.wide));
         a.q = x.q;
         a.k = x.k;
         a.v = x.v;
@@ -431,7 +436,7 @@ FFTSPLIT_EXPORT fftsplit_status_t fftsplit_linear_attention_backward(
         // The forward pass's state, of (k, v), serves dq; its gradient, of (q,
         // dout) from the last token on, dk and dv.
         const int group = p.heads_q / p.heads_k;
-        const LinearPass a = pass_of(plan, in, x.wide, !dstate && one_segment(*plan, true));
+        const LinearPass a = pass_of(plan, in, x.wide, !dstate && one_segment(*plan, true, x.wide));
         LinearPass pq = a, pk = a, pv = a;
         pq.q = g;                       // dq: (dout, v, k)
         pq.k = x.v;
