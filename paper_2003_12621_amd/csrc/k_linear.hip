@@ -9,9 +9,6 @@
 //   parts  adds up what each segment adds to the state,
 //   join   makes of these the state before each segment,
 //   pass   computes the outputs of all rows at once.
-// The recurrence over tiles that this replaces has a chain of products, roundings
-// and weights per tile of 3000 cycles, in every wave; here 12 products and 55
-// vector instructions a tile depend on nothing but the keys.
 //
 // The gradients are the same sums with other roles: dq that of (dO, v, k), and
 // dk and dv those of (v, dO, q) and (k, q, dO) from the last token to the first.
@@ -178,8 +175,8 @@ struct JoinJobs {
 // time, a run of RUN of them to a wave, whose loads are in flight together; each wave
 // adds up its own run, reads the other waves' sums for the state before it, and goes
 // through its run once more.  The order is that of the segments, whatever the timing.
-// VEC: the 8 rows lie side by side in a state.  64 segments of 64 heads of 64 / 128: 201 MB
-// in 41 us, a copy's rate; of 4 heads 11 us, of waits.
+// VEC: the 8 rows lie side by side in a state.  64 segments of 64 heads of 64 / 128 in
+// bf16: 268 MB in 52 us, a copy's rate; of 4 heads 12 us, of waits.
 template <typename T, int WAVES, int RUN, bool VEC>
 __device__ __forceinline__ void linear_join(const LinearJoin& a, int block, float (&sums)[WAVES][8][64]) {
     const int items = a.rows / 8 * a.columns, per = items / 64;
@@ -347,9 +344,9 @@ hipError_t launch_typed(const LinearPass& a, const LinearPass* b, hipStream_t s,
 
 // Few waves, each with a longer run, cost less where one turn goes over all segments; for
 // more, more waves save turns.  Measured, 4 / 8 waves (us): 13 and 16 segments of the
-// three joins of a training step of 4 x 3136 tokens of 8 heads of 64 / 128 17 / 20, of 2 x
-// 1999 tokens of 8 heads (4) of 128 / 256 21 / 24; 64 segments of 4 heads 14 / 11 (of 64
-// heads 42 / 42, which is their bytes).
+// three joins of a training step of 4 x 3136 tokens of 8 heads of 64 / 128 19 / 26, of 2 x
+// 1999 tokens of 8 heads (4) of 128 / 256 24 / 31; 64 segments of 4 heads 17 / 12 (of 64
+// heads 55 / 52, which is their bytes).
 template <typename T>
 hipError_t launch_join(const JoinJobs& j, int blocks, hipStream_t s, const LaunchEvents& ev) {
     const int segments = j.job[0].segments;

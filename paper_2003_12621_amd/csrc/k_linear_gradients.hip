@@ -1,9 +1,9 @@
 // The gradients of linear attention in one launch: dq and dk are the sums of rows as
 // wide as v with values as wide as q, dv the other way round.  Side by side, the
 // workgroups of one fill what those of the other leave idle.  Measured against two
-// launches (us): training of 2 x 1999 tokens of 8 heads (4) of 128 / 256 in bf16 43 -> 32,
-// of 6 x 301 tokens of 6 heads (3) of 32 / 64 in fp32 46 -> 25, of 4 x 3136 tokens of 8
-// heads of 64 / 128 in bf16 76 -> 56.  (Aligned tensors; k_linear.hip has the rest.)
+// launches (us): training of 2 x 1999 tokens of 8 heads (4) of 128 / 256 in bf16 50 -> 40,
+// of 6 x 301 tokens of 6 heads (3) of 32 / 64 in fp32 45 -> 25, of 4 x 3136 tokens of 8
+// heads of 64 / 128 in bf16 78 -> 65.  (Aligned tensors; k_linear.hip has the rest.)
 #include "linear_pass.hpp"
 
 namespace fftsplit {

