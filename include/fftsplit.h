@@ -578,8 +578,8 @@ typedef struct {
     size_t state_bytes;            /* fp32 [batch][heads_k][dim][dim_v] */
     /* Kernel choice: 1 if the forward pass goes token by token, else 0; tokens of
      * a segment, within which pairs of tokens are taken one by one and between
-     * which a state is carried, and how many a sequence is cut into (a short one
-     * is taken as one where no state is returned). */
+     * which a state is carried, and how many a sequence is cut into (one that is not
+     * long is taken as one segment where no state is returned). */
     int recurrent, segment_tokens, segments;
 } fftsplit_linear_attention_info_t;
 

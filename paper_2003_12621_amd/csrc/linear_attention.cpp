@@ -96,7 +96,7 @@ double tile_us(const fftsplit_linear_attention_problem_t& p, int width, int widt
 //   fp32, 8 heads of 64 / 128, 8 sequences of 160, 300, 600 tokens: forward 41 / 21, 45 / 38,
 //   66 / 99, backward 58 / 38, 82 / 77, 121 / 195; 6 heads (3) of 32 / 64 backward 37 / 30, 46 /
 //   55, 53 / 112.
-// The estimate's numbers are fitted to 144 such calls, of which it takes the slower way by up
+// The estimate's numbers are fitted to 168 such calls, of which it takes the slower way by up
 // to 12 % and by 0.3 % in the mean (a bound on the tokens alone: 74 % and 2.5 %); of 48 other
 // calls by up to 19 % and by 1 % in the mean.
 // Rows that are not aligned, bf16, 8 heads of 64 / 128: forward, one sequence of 300, 600 tokens

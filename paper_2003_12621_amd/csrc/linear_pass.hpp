@@ -281,7 +281,8 @@ __device__ __forceinline__ void linear_pass(const LinearPass& a, int block, int 
                 if (j + kGroup < kAll) load(j + kGroup);
                 in_order();
 #pragma unroll
-                for (int i = j; i < j + kGroup; ++i) mma(out[i / kParts / kSteps], x[j / kGroup % 2][i - j], q[i / kParts % kSteps]);
+                for (int i = j; i < j + kGroup; ++i)
+                    mma(out[i / kParts / kSteps], x[j / kGroup % 2][i - j], q[i / kParts % kSteps]);
             }
             const float f = a.inter_scale * decay_power(log2_decay, max(a.reverse ? end - 1 - row : row - begin + 1, 0));
 #pragma unroll
